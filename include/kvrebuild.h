@@ -37,6 +37,13 @@
  * (strides in bytes, multiples of 16).  Token position p lives in block block_table[p / block_size],
  * slot p % block_size (PagedAttention, block size 16 in the paper's prototype, Section 5).
  *
+ * e4m3 pages (kv_cache_desc.elem_bytes = 1): the values are 8-bit e4m3 codes in the same [slot][kv_head][dim] order,
+ * followed by one scale byte per (kv_head, slot), laid out [kv_head][slot] and padded to a multiple of 16 bytes
+ * (kv_cache_page_bytes()).  Element = code * 2^(scale byte - 127).  The scale is a power of two, so reading a code back
+ * into bf16 or fp32 is exact.  Such caches are written by kv_op_cache_write, read by kv_op_cache_read and
+ * kv_op_paged_attention_batched, and migrate through pack / unpack (pages travel as bytes, scales included); the other
+ * entry points take bf16 pages and refuse them with KV_ERR_SHAPE.
+ *
  * Wire buffer: headerless raw pages.  Layout KV_WIRE_BLOCK_MAJOR: [block i][layer][kv][page bytes], so
  * each completed block is one contiguous self-contained message ("newly completed suffix KV-cache
  * blocks are streamed ... with their logical token positions", Section 4.3).  KV_WIRE_LAYER_MAJOR:
@@ -72,6 +79,9 @@ enum {
 
 enum { KV_WIRE_BLOCK_MAJOR = 0, KV_WIRE_LAYER_MAJOR = 1 };
 enum { KV_OP_PREFILL = 0, KV_OP_DECODE = 1 };
+enum { KV_DTYPE_BF16 = 0, KV_DTYPE_F32 = 1 };
+enum { KV_ROPE_HALF = 0, KV_ROPE_INTERLEAVED = 1 };
+enum { KV_ROPE_SCALE_NONE = 0, KV_ROPE_SCALE_LINEAR = 1, KV_ROPE_SCALE_NTK = 2, KV_ROPE_SCALE_PARTS = 3 };
 
 /* ---------------------------------------------------------------- descriptors */
 typedef struct {
@@ -97,7 +107,7 @@ typedef struct {
 typedef struct {
   void *base_dev;
   int64_t layer_stride, kv_stride, block_stride; /* bytes */
-  int32_t num_blocks, block_size, n_layers, n_kv_heads, head_dim, elem_bytes /* 2 */;
+  int32_t num_blocks, block_size, n_layers, n_kv_heads, head_dim, elem_bytes /* 2: bf16, 1: e4m3 + scale bytes */;
 } kv_cache_desc;
 
 typedef struct kv_model kv_model; /* opaque host handle */
@@ -128,6 +138,9 @@ const char *kv_last_cuda_error(void);
 
 /* Eq. (1): s_KV = 2 * L * H_KV * d_h * b bytes per token. */
 int64_t kv_bytes_per_token(int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t elem_bytes);
+
+/* Bytes of one page (one layer, K or V, one block): elem_bytes 2 = bf16 values, 1 = e4m3 codes and their scale bytes. */
+int64_t kv_cache_page_bytes(int32_t block_size, int32_t n_kv_heads, int32_t head_dim, int32_t elem_bytes);
 
 /* Synchronises `stream` and reads the device status word kept in `workspace_dev` by the last
  * prefill/decode call on it: KV_OK, or KV_ERR_DEVICE if a kernel's bounded wait ran out. */
@@ -284,6 +297,79 @@ int32_t kv_op_paged_attention(const float *q_dev, int32_t n_q_heads, const kv_ca
 int32_t kv_op_paged_attention_noalloc(const float *q_dev, int32_t n_q_heads, const kv_cache_desc *cache,
                                       int32_t layer, const int32_t *block_table_dev, int32_t n_ctx,
                                       float *out_dev, void *stream);
+
+/* ---------------------------------------------------------------- serving a batch of requests
+ * The middle of a decode step over many resident requests, and of a prefill that goes beyond rotate-half positions or
+ * bf16 pages: rotary positions, K/V rows into pages, attention of one new token per request, pages back into rows.
+ * Row arguments are [token][head][dim] with the strides given in ELEMENTS; a head's dim values are contiguous.  Row
+ * pointers are 16-byte aligned and strides are multiples of 16 bytes (kv_op_rope alone takes any element alignment), so
+ * slices of a fused QKV buffer can be passed as they are.  dtype is KV_DTYPE_BF16 or KV_DTYPE_F32.  Lists on the device
+ * (positions, slots, tables, lengths) are read by the kernels, so that a captured graph can be replayed with new ones;
+ * the library cannot refuse a call over their contents, and no entry of them makes a kernel leave its buffers. */
+
+/* Rotary position embedding.  The first rotary_dim of head_dim values are rotated in pairs, the others are copied.
+ * Pair j (0 <= j < rotary_dim / 2) holds values (j, j + rotary_dim / 2) in layout KV_ROPE_HALF and (2j, 2j + 1) in
+ * KV_ROPE_INTERLEAVED; at position p it turns by p * theta_j, and both results are multiplied by `gain`.
+ *   KV_ROPE_SCALE_NONE    theta_j = base^(-2j / rotary_dim)
+ *   KV_ROPE_SCALE_LINEAR  theta_j / factor
+ *   KV_ROPE_SCALE_NTK     base is replaced by base * factor^(rotary_dim / (rotary_dim - 2)); rotary_dim > 2
+ *   KV_ROPE_SCALE_PARTS   g_j = clamp((original_ctx * theta_j / (2 pi) - low) / (high - low), 0, 1): pairs that turn more
+ *                         than `high` times within original_ctx keep theta_j, those below `low` take theta_j / factor,
+ *                         (1 - g_j) theta_j / factor + g_j theta_j between them
+ * rotary_dim is even and at most 256; base, factor and gain are finite and positive; high > low. */
+typedef struct {
+  int32_t rotary_dim, layout, scaling;
+  double base, factor, original_ctx, low, high, gain;
+} kv_rope_desc;
+typedef struct kv_rope kv_rope; /* opaque host handle: the frequencies, formed once in fp64 */
+int32_t kv_rope_create(const kv_rope_desc *desc, kv_rope **out);
+int32_t kv_rope_destroy(kv_rope *r);
+/* theta_j into theta_host[0 .. rotary_dim / 2), n = its capacity. */
+int32_t kv_rope_frequencies(const kv_rope *r, double *theta_host, int32_t n);
+
+/* out[t][h] = rotation of x[t][h] at positions_dev[t] (int32, any sign).  backward != 0: the transpose, i.e. the gradient
+ * of x from the gradient of out (turned by -p theta_j, times gain).  The angle is reduced in fp64 (exact to 2^-24 of a
+ * turn over the whole int32 range), sine and cosine and the rotation are fp32, one rounding to dtype.  out may be x
+ * itself with the same strides; any other overlap is undefined.  n_tokens = 0 does nothing. */
+int32_t kv_op_rope(const kv_rope *rope, const void *x_dev, int64_t x_token_stride, int64_t x_head_stride, int32_t dtype,
+                   int32_t n_tokens, int32_t n_heads, int32_t head_dim, const int32_t *positions_dev, int32_t backward,
+                   void *out_dev, int64_t out_token_stride, int64_t out_head_stride, void *stream);
+
+/* K and V rows of n_tokens tokens into layer `layer` of the cache.  Token t goes to slot slots_dev[t] = block *
+ * block_size + offset; a slot outside the pool (-1 marks padding) is left out: nothing is written for that token.  The
+ * slots of one call are distinct; what a slot that is listed twice holds afterwards is undefined (other slots are not
+ * affected).  head_dim 64 or 128.
+ * bf16 pages: each value rounded to nearest even.  e4m3 pages: for every (token, KV head) of K and of V, e is the least
+ * integer with max |x| <= 448 * 2^e, kept within [-110, 119]; the codes are x * 2^-e (exact) rounded to nearest even and
+ * saturated at 448, the scale byte is e + 127.  Infinities and NaN are left out of the maximum and stored as NaN. */
+int32_t kv_op_cache_write(const kv_cache_desc *cache, int32_t layer, const void *k_dev, int64_t k_token_stride,
+                          int64_t k_head_stride, const void *v_dev, int64_t v_token_stride, int64_t v_head_stride,
+                          int32_t dtype, int32_t n_tokens, const int64_t *slots_dev, void *stream);
+
+/* The reverse: rows k_out[t], v_out[t] = the cache's values at slots_dev[t].  Rows whose slot lies outside the pool are
+ * left as they were.  Slots may repeat.  Exact: bf16 and e4m3 pages lose nothing in rows of either type. */
+int32_t kv_op_cache_read(const kv_cache_desc *cache, int32_t layer, const int64_t *slots_dev, int32_t n_tokens,
+                         void *k_out_dev, int64_t k_token_stride, int64_t k_head_stride, void *v_out_dev,
+                         int64_t v_token_stride, int64_t v_head_stride, int32_t dtype, void *stream);
+
+/* Attention of one new token per request over layer `layer` of the cache (bf16 or e4m3 pages).  Request r has query
+ * q_dev + r * q_stride ([n_q_heads][head_dim], heads contiguous, dtype), attends to positions [0, context_lens_dev[r])
+ * through block_tables_dev[r * table_stride ..] and writes out_dev + r * out_stride (same dtype).  Query head h reads KV
+ * head h / (n_q_heads / n_kv_heads):  s_n = softmax_scale * q . k_n,  out = sum_n exp(s_n) v_n / sum_n exp(s_n),
+ * lse = log sum_n exp(s_n) (fp32 [n_req][n_q_heads], natural logarithm; NULL to leave it out), so results over disjoint
+ * parts of a context can be joined.  A request of length 0 gets out = 0, lse = -inf.  Lengths are clamped to [0, max_ctx]
+ * with max_ctx <= table_stride * block_size and at most 2^26; table entries behind a request's last block are not read.  A block id
+ * outside the pool inside a context is not followed: that request's out and lse are NaN.  fp32 sums and softmax.
+ * scratch_dev: kv_paged_attention_batched_scratch_bytes() bytes, 16-byte aligned, contents need not survive between calls;
+ * calls that may overlap on the GPU need scratch of their own.  head_dim 64 or 128. */
+int64_t kv_paged_attention_batched_scratch_bytes(int32_t n_req, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                                 int32_t max_ctx);
+int32_t kv_op_paged_attention_batched(const void *q_dev, int64_t q_stride, int32_t dtype, int32_t n_req,
+                                      int32_t n_q_heads, const kv_cache_desc *cache, int32_t layer,
+                                      const int32_t *block_tables_dev, int64_t table_stride,
+                                      const int32_t *context_lens_dev, int32_t max_ctx, float softmax_scale,
+                                      void *scratch_dev, int64_t scratch_bytes, void *out_dev, int64_t out_stride,
+                                      float *lse_out_dev, void *stream);
 
 /* ---------------------------------------------------------------- window selection (host scalar code)
  * The Scheduler Engine's cost model and online selection (Section 4.1, Eqs. 3-9; Section 4.2, Algorithm 1;

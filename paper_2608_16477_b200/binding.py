@@ -21,7 +21,9 @@ EXPORTS = [
     "kv_op_attention_prefill", "kv_paged_attention_scratch_bytes", "kv_op_paged_attention", "kv_fill_pattern",
     "kv_profile_enable", "kv_profile_read", "kv_launch_count", "kv_op_paged_attention_noalloc", "kv_check_copy_status", "kv_op_gemv",
     "kv_window_evaluate", "kv_window_select", "kv_window_waste_bound", "kv_ewma", "kv_prefill_prefix_batched",
-    "kv_selftest_bounded_wait", "kv_workspace_residual",
+    "kv_selftest_bounded_wait", "kv_workspace_residual", "kv_cache_page_bytes", "kv_rope_create", "kv_rope_destroy",
+    "kv_rope_frequencies", "kv_op_rope", "kv_op_cache_write", "kv_op_cache_read",
+    "kv_paged_attention_batched_scratch_bytes", "kv_op_paged_attention_batched",
 ]
 
 PROFILE_KINDS = ("embed", "rmsnorm", "gemm_qkv", "rope_store", "attention", "gemm_o", "gemm_gate_up", "gemm_down",
@@ -59,6 +61,11 @@ class WindowEval(C.Structure):
 
     def as_dict(self):
         return {n: getattr(self, n) for n, _ in self._fields_}
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rotary_dim", "layout", "scaling")] + \
+        [(n, C.c_double) for n in ("base", "factor", "original_ctx", "low", "high", "gain")]
 
 
 class CacheDesc(C.Structure):
@@ -121,6 +128,16 @@ def load(build_if_missing: bool = True):
         "kv_profile_enable": (i32, [i32]),
         "kv_profile_read": (i32, [C.POINTER(C.c_float), C.POINTER(C.c_int64), i32]),
         "kv_launch_count": (i64, []),
+        "kv_cache_page_bytes": (i64, [i32, i32, i32, i32]),
+        "kv_rope_create": (i32, [C.POINTER(RopeDesc), C.POINTER(vp)]),
+        "kv_rope_destroy": (i32, [vp]),
+        "kv_rope_frequencies": (i32, [vp, C.POINTER(C.c_double), i32]),
+        "kv_op_rope": (i32, [vp, vp, i64, i64, i32, i32, i32, i32, vp, i32, vp, i64, i64, vp]),
+        "kv_op_cache_write": (i32, [C.POINTER(CacheDesc), i32, vp, i64, i64, vp, i64, i64, i32, i32, vp, vp]),
+        "kv_op_cache_read": (i32, [C.POINTER(CacheDesc), i32, vp, i32, vp, i64, i64, vp, i64, i64, i32, vp]),
+        "kv_paged_attention_batched_scratch_bytes": (i64, [i32, i32, i32, i32, i32]),
+        "kv_op_paged_attention_batched": (i32, [vp, i64, i32, i32, i32, C.POINTER(CacheDesc), i32, vp, i64, vp, i32,
+                                                C.c_float, vp, i64, vp, i64, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -155,17 +172,25 @@ def _ptr(t) -> int:
 
 
 class PagedCache:
-    """A paged KV cache in device memory (torch tensor of bf16 bit patterns) plus its descriptor.
+    """A paged KV cache in device memory plus its descriptor: a torch tensor of bf16 bit patterns (elem_bytes 2, int16)
+    or of e4m3 pages with their scale bytes (elem_bytes 1, uint8).
 
-    layout "layer_major": [L][2][num_blocks][page]; "block_major": [num_blocks][L][2][page].
+    layout "layer_major": [L][2][num_blocks][page]; "block_major": [num_blocks][L][2][page].  `data` gives the cache
+    memory that is there already (contiguous, of exactly the pool's size) instead of allocating it.
     """
 
-    def __init__(self, shape, num_blocks: int, layout: str = "layer_major", device="cuda", fill=None):
+    def __init__(self, shape, num_blocks: int, layout: str = "layer_major", device="cuda", fill=None,
+                 elem_bytes: int = 2, data=None):
         import torch
         self.n_layers, self.n_kv_heads, self.head_dim = shape.n_layers, shape.n_kv_heads, shape.head_dim
         self.block_size, self.num_blocks, self.layout = shape.block_size, num_blocks, layout
-        page_elems = self.block_size * self.n_kv_heads * self.head_dim
-        self.page_bytes = page_elems * 2
+        self.elem_bytes = elem_bytes
+        if elem_bytes not in (1, 2):
+            raise ValueError(f"elem_bytes {elem_bytes}: 2 (bf16) or 1 (e4m3)")
+        self.page_bytes = self.block_size * self.n_kv_heads * self.head_dim * elem_bytes
+        if elem_bytes == 1:
+            self.page_bytes += -(-self.block_size * self.n_kv_heads // 16) * 16
+        page_elems = self.page_bytes // elem_bytes
         if layout == "layer_major":
             dims = (self.n_layers, 2, num_blocks, page_elems)
             strides = (2 * num_blocks * self.page_bytes, num_blocks * self.page_bytes, self.page_bytes)
@@ -174,14 +199,20 @@ class PagedCache:
             strides = (2 * self.page_bytes, self.page_bytes, 2 * self.n_layers * self.page_bytes)
         else:
             raise ValueError(layout)
-        self.data = torch.empty(dims, dtype=torch.int16, device=device)
+        if data is None:
+            self.data = torch.empty(dims, dtype=torch.int16 if elem_bytes == 2 else torch.uint8, device=device)
+        elif not data.is_contiguous() or data.numel() * data.element_size() != int(np.prod(dims)) * elem_bytes:
+            raise ValueError("data: a contiguous tensor of the pool's size is wanted")
+        else:
+            self.data = data.view(torch.int16 if elem_bytes == 2 else torch.uint8).view(dims)
         if fill is not None:
             self.data.fill_(fill)
         self.desc = CacheDesc(self.data.data_ptr(), strides[0], strides[1], strides[2], num_blocks, self.block_size,
-                              self.n_layers, self.n_kv_heads, self.head_dim, 2)
+                              self.n_layers, self.n_kv_heads, self.head_dim, elem_bytes)
+        self._desc_ref = C.byref(self.desc)
 
     def pages(self, block_ids):
-        """int16 tensor [len(ids), L, 2, page_elems] of the given blocks (torch indexing; test helper)."""
+        """int16 (bf16) or uint8 (e4m3) tensor [len(ids), L, 2, page] of the given blocks (torch indexing; test helper)."""
         import torch
         idx = torch.as_tensor(np.asarray(block_ids, dtype=np.int64), device=self.data.device)
         if self.layout == "layer_major":
@@ -189,7 +220,9 @@ class PagedCache:
         return self.data[idx]
 
     def as_logical_numpy(self) -> np.ndarray:
-        """uint16 array [L, 2, num_blocks, Bs, Hkv, d] on the host."""
+        """uint16 array [L, 2, num_blocks, Bs, Hkv, d] of a bf16 cache on the host."""
+        if self.elem_bytes != 2:
+            raise ValueError("as_logical_numpy: bf16 caches only (kv_op_cache_read decodes e4m3 pages)")
         d = self.data if self.layout == "layer_major" else self.data.permute(1, 2, 0, 3)
         return d.contiguous().cpu().numpy().view(np.uint16).reshape(
             self.n_layers, 2, self.num_blocks, self.block_size, self.n_kv_heads, self.head_dim)
@@ -251,6 +284,13 @@ class Model:
 
 def kv_bytes_per_token(n_layers, n_kv_heads, head_dim, elem_bytes=2) -> int:
     return load().kv_bytes_per_token(n_layers, n_kv_heads, head_dim, elem_bytes)
+
+
+def kv_cache_page_bytes(block_size: int, n_kv_heads: int, head_dim: int, elem_bytes: int) -> int:
+    r = load().kv_cache_page_bytes(block_size, n_kv_heads, head_dim, elem_bytes)
+    if r < 0:
+        raise KVError(int(r), "kv_cache_page_bytes")
+    return int(r)
 
 
 def kv_workspace_bytes(model: Model, op: int, max_tokens: int) -> int:
@@ -457,3 +497,177 @@ def kv_prefill_prefix_batched(model: Model, cache: PagedCache, token_id_lists, b
                                             ptabs, _ptr(ws), ws.numel(), _ptr(logits_out), _stream(stream)),
            "kv_prefill_prefix_batched")
     return ws
+
+
+# ---- serving a batch of requests: rotary positions, rows into and out of pages, attention of one new token each
+KV_ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+KV_ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
+_DTYPES = None
+
+
+def _dtype(t, what):
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.bfloat16: 0, torch.float32: 1}
+    try:
+        return _DTYPES[t.dtype]
+    except KeyError:
+        raise ValueError(f"{what}: bfloat16 or float32 is wanted, not {t.dtype}") from None
+
+
+def _same(what, cond):
+    if not cond:
+        raise ValueError(what)
+
+
+def _inner(t):
+    """Whether the last dimension is contiguous (of an empty tensor it does not matter)."""
+    return t.numel() == 0 or t.shape[-1] == 1 or t.stride(-1) == 1
+
+
+def _stride(t, dim):
+    return t.stride(dim) if t.shape[dim] > 1 else 0
+
+
+def _run(name, stream, tensors, args):
+    """Calls `name` on the tensors' device: they all have to be on one, which need not be the current one."""
+    import torch
+    device = tensors[0].device
+    for t in tensors:
+        if t.device != device:
+            raise ValueError(f"{name}: tensors on {device} and on {t.device}")
+    if device.type != "cuda":
+        raise ValueError(f"{name}: tensors on a CUDA device are wanted, not on {device}")
+    index, current = device.index, torch.cuda.current_device()
+    if stream is None:
+        stream = torch._C._cuda_getCurrentRawStream(index)
+    else:
+        stream = getattr(stream, "cuda_stream", stream)
+    if index == current:
+        status = getattr(load(), name)(*args, stream)
+    else:
+        with torch.cuda.device(index):
+            status = getattr(load(), name)(*args, stream)
+    if status != 0:
+        raise KVError(status, name)
+
+
+class Rope:
+    """Rotary plan (kv_rope): which pairs turn, how fast, and the factor on the result.  scaling "none", "linear", "ntk"
+    or "parts" (frequencies blended between theta and theta / factor by how often a pair turns in original_ctx)."""
+
+    def __init__(self, rotary_dim: int, layout: str = "half", base: float = 1.0e6, scaling: str = "none",
+                 factor: float = 1.0, original_ctx: float = 0.0, low: float = 1.0, high: float = 32.0, gain: float = 1.0):
+        self.handle = None
+        _same(f"layout {layout!r}: one of {sorted(KV_ROPE_LAYOUTS)}", layout in KV_ROPE_LAYOUTS)
+        _same(f"scaling {scaling!r}: one of {sorted(KV_ROPE_SCALINGS)}", scaling in KV_ROPE_SCALINGS)
+        self._lib = load()
+        self.rotary_dim = rotary_dim
+        desc = RopeDesc(rotary_dim, KV_ROPE_LAYOUTS[layout], KV_ROPE_SCALINGS[scaling], base, factor, original_ctx, low,
+                        high, gain)
+        handle = C.c_void_p()
+        _check(self._lib.kv_rope_create(C.byref(desc), C.byref(handle)), "kv_rope_create")
+        self.handle = handle
+
+    def frequencies(self) -> np.ndarray:
+        """theta_j of the rotary_dim / 2 pairs (radians per position, float64)."""
+        out = np.empty(self.rotary_dim // 2, dtype=np.float64)
+        _check(self._lib.kv_rope_frequencies(self.handle, out.ctypes.data_as(C.POINTER(C.c_double)), len(out)),
+               "kv_rope_frequencies")
+        return out
+
+    def __del__(self):
+        try:
+            if self.handle:
+                self._lib.kv_rope_destroy(self.handle)
+                self.handle = None
+        except Exception:
+            pass
+
+
+def kv_op_rope(rope: Rope, x, positions, out, backward: bool = False, stream=None):
+    """out[t, h] = x[t, h] rotated at positions[t]; x and out [T, heads, head_dim] (bf16 or fp32, any strides whose last is
+    1; out may be x), positions int32 [T].  backward: the gradient of x from the gradient of out."""
+    _same("kv_op_rope: x is [tokens, heads, head_dim] with contiguous head_dim", x.dim() == 3 and _inner(x))
+    _same("kv_op_rope: out has x's shape and type, with contiguous head_dim",
+          out.shape == x.shape and out.dtype == x.dtype and _inner(out))
+    t, h, d = x.shape
+    _same("kv_op_rope: positions is a contiguous int32 vector, one per token",
+          positions.shape == (t,) and positions.element_size() == 4 and not positions.is_floating_point()
+          and (t < 2 or positions.stride(0) == 1))
+    _run("kv_op_rope", stream, (x, positions, out),
+         (rope.handle, x.data_ptr(), _stride(x, 0), _stride(x, 1), _dtype(x, "kv_op_rope"), t, h, d,
+          positions.data_ptr(), int(backward), out.data_ptr(), _stride(out, 0), _stride(out, 1)))
+
+
+def _check_rows(name, cache, k, v, slots):
+    t = slots.shape[0] if slots.dim() == 1 else -1
+    want = (t, cache.n_kv_heads, cache.head_dim)
+    _same(f"{name}: rows are [tokens, n_kv_heads, head_dim] = {want} with contiguous head_dim, of one type",
+          k.shape == want and v.shape == want and _inner(k) and _inner(v) and k.dtype == v.dtype)
+    _same(f"{name}: slots is a contiguous int64 vector, one per token",
+          slots.element_size() == 8 and not slots.is_floating_point() and (t < 2 or slots.stride(0) == 1))
+    return t
+
+
+def kv_op_cache_write(cache: PagedCache, layer: int, k, v, slots, stream=None):
+    """K and V rows [T, n_kv_heads, head_dim] (bf16 or fp32) into the cache's slots (int64 [T], block * block_size +
+    offset; -1 skips a token).  An e4m3 cache quantises them on the way."""
+    t = _check_rows("kv_op_cache_write", cache, k, v, slots)
+    _run("kv_op_cache_write", stream, (cache.data, k, v, slots),
+         (cache._desc_ref, layer, k.data_ptr(), _stride(k, 0), _stride(k, 1), v.data_ptr(), _stride(v, 0), _stride(v, 1),
+          _dtype(k, "kv_op_cache_write"), t, slots.data_ptr()))
+
+
+def kv_op_cache_read(cache: PagedCache, layer: int, slots, k_out, v_out, stream=None):
+    """The cache's rows at `slots` into k_out and v_out [T, n_kv_heads, head_dim] (bf16 or fp32); rows whose slot is
+    outside the pool stay as they were."""
+    t = _check_rows("kv_op_cache_read", cache, k_out, v_out, slots)
+    _run("kv_op_cache_read", stream, (cache.data, slots, k_out, v_out),
+         (cache._desc_ref, layer, slots.data_ptr(), t, k_out.data_ptr(), _stride(k_out, 0), _stride(k_out, 1),
+          v_out.data_ptr(), _stride(v_out, 0), _stride(v_out, 1), _dtype(k_out, "kv_op_cache_read")))
+
+
+def kv_paged_attention_batched_scratch_bytes(n_req: int, n_q_heads: int, cache: PagedCache, max_ctx: int) -> int:
+    r = load().kv_paged_attention_batched_scratch_bytes(n_req, n_q_heads, cache.n_kv_heads, cache.head_dim, max_ctx)
+    if r < 0:
+        raise KVError(int(r), "kv_paged_attention_batched_scratch_bytes")
+    return int(r)
+
+
+def kv_op_paged_attention_batched(q, cache: PagedCache, layer: int, block_tables, context_lens, max_ctx: int, out,
+                                  scratch, lse=None, softmax_scale=None, stream=None):
+    """Attention of one new token per request: q and out [R, n_q_heads, head_dim] (bf16 or fp32, heads contiguous),
+    block_tables int32 [R, B], context_lens int32 [R] (clamped to max_ctx), scratch of
+    kv_paged_attention_batched_scratch_bytes(R, ...) bytes, lse fp32 [R, n_q_heads] or None; softmax_scale defaults to
+    head_dim ** -0.5."""
+    name = "kv_op_paged_attention_batched"
+    _same(f"{name}: q is [requests, heads, head_dim] with contiguous heads",
+          q.dim() == 3 and q.shape[2] == cache.head_dim and _inner(q)
+          and (q.shape[0] == 0 or q.shape[1] < 2 or q.stride(1) == q.shape[2]))
+    r, hq, d = q.shape
+    _same(f"{name}: out has q's shape and type, with contiguous heads",
+          out.shape == q.shape and out.dtype == q.dtype and _inner(out) and (r == 0 or hq < 2 or out.stride(1) == d))
+    _same(f"{name}: block_tables is int32 [requests, blocks] with contiguous rows",
+          block_tables.dim() == 2 and block_tables.shape[0] == r and block_tables.element_size() == 4
+          and not block_tables.is_floating_point() and _inner(block_tables))
+    _same(f"{name}: context_lens is a contiguous int32 vector, one per request",
+          context_lens.shape == (r,) and context_lens.element_size() == 4 and not context_lens.is_floating_point()
+          and (r < 2 or context_lens.stride(0) == 1))
+    _same(f"{name}: lse is contiguous float32 [requests, heads]",
+          lse is None or (lse.shape == (r, hq) and lse.element_size() == 4 and lse.is_floating_point()
+                          and lse.is_contiguous()))
+    # a table of one row may have any row stride; the library takes the row's length as what it covers
+    stride = block_tables.stride(0) if r > 1 else block_tables.shape[1]
+    _same(f"{name}: rows of block_tables must not be shorter than their stride says",
+          r < 2 or stride >= block_tables.shape[1])
+    if block_tables.shape[1] * cache.block_size < max_ctx:
+        raise KVError(-8, name)
+    tensors = (cache.data, q, block_tables, context_lens, out)
+    tensors += tuple(t for t in (scratch, lse) if t is not None)
+    _run(name, stream, tensors,
+         (q.data_ptr(), _stride(q, 0), _dtype(q, name), r, hq, cache._desc_ref, layer, block_tables.data_ptr(), stride,
+          context_lens.data_ptr(), max_ctx, d ** -0.5 if softmax_scale is None else softmax_scale, _ptr(scratch),
+          0 if scratch is None else scratch.numel() * scratch.element_size(), out.data_ptr(), _stride(out, 0),
+          _ptr(lse)))

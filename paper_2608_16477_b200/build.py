@@ -11,7 +11,8 @@ LIB_PATH = os.path.join(PKG_DIR, "libkvrebuild.so")
 STAMP = os.path.join(PKG_DIR, "build", "stamp.txt")
 
 SOURCES = ["api.cu", "copy_pages.cu", "elementwise.cu", "decode.cu", "gemm_tcgen05.cu", "gemm_tcgen05_pair.cu",
-           "attention_tcgen05.cu", "paged_attention_noalloc.cu", "window.cu"]
+           "attention_tcgen05.cu", "paged_attention_noalloc.cu", "window.cu", "rope.cu", "cache_rows.cu",
+           "paged_attention_batched.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--use_fast_math", "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 

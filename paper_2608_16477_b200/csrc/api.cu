@@ -287,6 +287,8 @@ DecodeWs carve_decode(const kv_model_desc &d, void *base, int max_ctx, int /*blo
 }
 
 int check_cache(const kv_cache_desc *c) { return check_cache_desc(c); }
+// pack and unpack move whole pages as bytes: both page formats
+int check_cache_any(const kv_cache_desc *c) { return check_cache_desc(c, true); }
 
 int check_cache_vs_model(const kv_cache_desc *c, const kv_model_desc &d) {
   int rc = check_cache(c);
@@ -307,7 +309,7 @@ int check_ids(const int32_t *ids, int n, int num_blocks, bool reject_duplicates)
 }
 
 long long wire_bytes_needed(const kv_cache_desc *c, int n_blocks) {
-  return (long long)n_blocks * c->n_layers * 2 * c->block_size * c->n_kv_heads * c->head_dim * 2;
+  return (long long)n_blocks * c->n_layers * 2 * make_view(c).page_bytes();
 }
 
 // Up to 128 rows (one row tile) the one-CTA kernel runs; from there on the CTA-pair kernel was as fast or faster
@@ -417,6 +419,17 @@ const char *kv_status_string(int32_t s) {
 }
 
 const char *kv_last_cuda_error(void) { return g_cuda_error.c_str(); }
+
+int64_t kv_cache_page_bytes(int32_t block_size, int32_t n_kv_heads, int32_t head_dim, int32_t elem_bytes) {
+  if (block_size <= 0 || n_kv_heads <= 0 || head_dim <= 0) return KV_ERR_ARG;
+  if (elem_bytes != 1 && elem_bytes != 2) return KV_ERR_SHAPE;
+  CacheView v = {};
+  v.block_size = block_size;
+  v.n_kv_heads = n_kv_heads;
+  v.head_dim = head_dim;
+  v.elem_bytes = elem_bytes;
+  return v.page_bytes();
+}
 
 int64_t kv_bytes_per_token(int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t elem_bytes) {
   return 2ll * n_layers * n_kv_heads * head_dim * elem_bytes;
@@ -628,7 +641,7 @@ int32_t kv_pack_blocks(const kv_cache_desc *src, const int32_t *block_ids_host, 
                        int64_t wire_bytes, int32_t wire_layout, void *stream) {
   if (block_ids_host == nullptr || n_blocks < 0 || wire_dev == nullptr || ((uintptr_t)wire_dev & 15)) return KV_ERR_ARG;
   if (wire_layout != KV_WIRE_BLOCK_MAJOR && wire_layout != KV_WIRE_LAYER_MAJOR) return KV_ERR_ARG;
-  int rc = check_cache(src);
+  int rc = check_cache_any(src);
   if (rc != KV_OK) return rc;
   rc = check_ids(block_ids_host, n_blocks, src->num_blocks, false);
   if (rc != KV_OK) return rc;
@@ -649,7 +662,7 @@ int32_t kv_unpack_assemble(const kv_cache_desc *dst, const void *wire_dev, int64
       (n_prefix > 0 && prefix_table == nullptr) || ((uintptr_t)wire_dev & 15))
     return KV_ERR_ARG;
   if (wire_layout != KV_WIRE_BLOCK_MAJOR && wire_layout != KV_WIRE_LAYER_MAJOR) return KV_ERR_ARG;
-  int rc = check_cache(dst);
+  int rc = check_cache_any(dst);
   if (rc != KV_OK) return rc;
   const int bs = dst->block_size;
   const long long total_blocks = ((long long)n_tokens_total + bs - 1) / bs;
@@ -684,7 +697,7 @@ static int32_t batched(const kv_cache_desc *c, int32_t n_req, const int32_t *off
                        void *const *wires, int32_t layout, bool to_wire, void *stream) {
   if (n_req < 0 || offs == nullptr || ids == nullptr || wires == nullptr) return KV_ERR_ARG;
   if (layout != KV_WIRE_BLOCK_MAJOR && layout != KV_WIRE_LAYER_MAJOR) return KV_ERR_ARG;
-  int rc = check_cache(c);
+  int rc = check_cache_any(c);
   if (rc != KV_OK) return rc;
   if (n_req == 0) return KV_OK;
   if (offs[0] != 0) return KV_ERR_ARG;

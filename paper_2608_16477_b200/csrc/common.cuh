@@ -16,8 +16,12 @@ typedef __nv_bfloat16 bf16;
 struct CacheView {
   char *base;
   long long layer_stride, kv_stride, block_stride;
-  int block_size, n_kv_heads, head_dim;
-  __host__ __device__ long long page_bytes() const { return (long long)block_size * n_kv_heads * head_dim * 2; }
+  int block_size, n_kv_heads, head_dim, elem_bytes;
+  __host__ __device__ long long value_bytes() const { return (long long)block_size * n_kv_heads * head_dim * elem_bytes; }
+  // e4m3 pages (elem_bytes 1) carry one scale byte per (KV head, slot) behind the values, padded to 16 bytes
+  __host__ __device__ long long page_bytes() const {
+    return value_bytes() + (elem_bytes == 1 ? ((long long)block_size * n_kv_heads + 15) / 16 * 16 : 0);
+  }
   __device__ __forceinline__ char *page(int layer, int kv, int block) const {
     return base + layer * layer_stride + kv * kv_stride + block * block_stride;
   }
@@ -32,21 +36,36 @@ inline CacheView make_view(const kv_cache_desc *c) {
   v.block_size = c->block_size;
   v.n_kv_heads = c->n_kv_heads;
   v.head_dim = c->head_dim;
+  v.elem_bytes = c->elem_bytes;
   return v;
 }
 
-// Host-side validation of a cache descriptor, shared by every entry point that takes one.
-inline int check_cache_desc(const kv_cache_desc *c) {
+// Host-side validation of a cache descriptor, shared by every entry point that takes one.  Only the entry points that
+// know e4m3 pages pass allow_e4m3.
+inline int check_cache_desc(const kv_cache_desc *c, bool allow_e4m3 = false) {
   if (c == nullptr || c->base_dev == nullptr) return KV_ERR_ARG;
   if (c->num_blocks <= 0 || c->block_size <= 0 || c->n_layers <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0)
     return KV_ERR_ARG;
-  if (c->elem_bytes != 2) return KV_ERR_SHAPE;
-  const long long page = (long long)c->block_size * c->n_kv_heads * c->head_dim * 2;
+  if (c->elem_bytes != 2 && !(allow_e4m3 && c->elem_bytes == 1)) return KV_ERR_SHAPE;
+  if (c->elem_bytes == 1 && c->head_dim % 16 != 0) return KV_ERR_SHAPE;
+  const long long page = make_view(c).page_bytes();
   if (page % 16 != 0) return KV_ERR_SHAPE;
   if (((uintptr_t)c->base_dev & 15) || (c->layer_stride & 15) || (c->kv_stride & 15) || (c->block_stride & 15))
     return KV_ERR_ARG;
   if (c->block_stride < page || c->kv_stride <= 0 || c->layer_stride <= 0) return KV_ERR_ARG;
   return KV_OK;
+}
+
+// Whether rows [token][head] of d elements with these strides (in elements) are distinct: token-major or head-major.
+inline bool rows_disjoint(long long token_stride, long long head_stride, long long n_tokens, long long n_heads, long long d) {
+  if (token_stride < 0 || head_stride < 0) return false;
+  if (n_heads > 1 && head_stride < d) return false;
+  if (n_tokens > 1 && token_stride < d) return false;
+  if (n_heads <= 1 || n_tokens <= 1) return true;
+  const long long big = token_stride > head_stride ? token_stride : head_stride;
+  const long long small = token_stride > head_stride ? head_stride : token_stride;
+  const long long count = token_stride > head_stride ? n_heads : n_tokens;      // rows along the smaller stride
+  return small <= (big - d) / (count - 1);      // (count - 1) * small + d <= big, without overflow
 }
 
 // Layout of the device status word block at the start of every prefill/decode workspace.
