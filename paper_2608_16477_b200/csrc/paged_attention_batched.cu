@@ -34,26 +34,29 @@ namespace {
 
 constexpr int kBaWarps = 4;
 constexpr int kBaThreads = kBaWarps * 32;
-constexpr int kBaKeys = 16;          // keys of a stage
 constexpr int kBaHeads = 8;          // query heads of a pass
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kWeightBits = 12.f;  // fp16 weights are scaled to at most 2^12
 constexpr int kQueryBits = 12;       // ... and fp16 queries to less than 2^12
 
+// A stage is what a warp loads and consumes at a time: 32 keys, so that the softmax's and the loads' bookkeeping is paid
+// once for four 8-key fragments; 16 where 32 would leave the ring too few stages (bf16 rows of 128: 8 KB a stage either way).
 template <int D, int ELEM>
 struct BaCfg {
   static constexpr int row = D * ELEM;                                   // bytes of a K or V row
-  static constexpr int tile = kBaKeys * row;
-  static constexpr int stage = 2 * tile + (ELEM == 1 ? 128 : 0);         // K, V, 32 words with the scale bytes
-  static constexpr int stages = stage > 6144 ? 3 : (stage > 3072 ? 5 : 8);
+  static constexpr int keys = row > 128 ? 16 : 32;
+  static constexpr int tile = keys * row;
+  static constexpr int stage = 2 * tile + (ELEM == 1 ? 256 : 0);         // K, V, a word with the scale byte of each row
+  static constexpr int stages = stage > 6144 ? 3 : 5;
   static constexpr int ring = stages * stage;
-  static constexpr int merge = kBaWarps * kBaHeads * D * 4;              // the warps' outputs when they share a head
-  static constexpr int smem = kBaWarps * ring + merge;
+  static constexpr int merge = (kBaWarps - 1) * kBaHeads * D * 4;        // outputs of warps 1-3 when they share a head
+  static constexpr int smem(int kw) { return kBaWarps * ring + (kw > 1 ? merge : 0); }
 };
 
 struct BaParams {
   CacheView cache;
   int layer, num_blocks, block_shift;
+  int aligned16;          // block_size is a multiple of 16: 16 keys that start at a multiple of 16 share a page
   const void *q;
   void *out;
   float *lse;
@@ -140,6 +143,57 @@ __device__ __forceinline__ void split_f16(float x, float y, uint32_t &hi, uint32
       : "=f"(fx), "=f"(fy) : "r"(hi));
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(lo) : "f"(y - fy), "f"(x - fx));
 }
+template <int N>
+__device__ __forceinline__ float max_of(const float (&v)[N]) {
+  float m = fmaxf(v[0], v[1]);
+#pragma unroll
+  for (int i = 2; i < N; i += 2) m = fmaxf(m, fmaxf(v[i], v[i + 1]));
+  return m;
+}
+__device__ __forceinline__ float2 load2(const float *q) { return *reinterpret_cast<const float2 *>(q); }
+__device__ __forceinline__ float2 load2(const bf16 *q) {
+  return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(q));
+}
+__device__ __forceinline__ void load8(const float *q, float *x) {
+  const float4 a = reinterpret_cast<const float4 *>(q)[0], b = reinterpret_cast<const float4 *>(q)[1];
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void load8(const bf16 *q, float *x) {
+  const uint4 r = *reinterpret_cast<const uint4 *>(q);
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void store4(float *p, float a, float b, float c, float d) {
+  *reinterpret_cast<float4 *>(p) = make_float4(a, b, c, d);
+}
+__device__ __forceinline__ void store4(bf16 *p, float a, float b, float c, float d) {
+  const __nv_bfloat162 x = __floats2bfloat162_rn(a, b), y = __floats2bfloat162_rn(c, d);
+  *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const uint32_t *>(&x), *reinterpret_cast<const uint32_t *>(&y));
+}
+__device__ __forceinline__ void store2(float *p, float a, float b) { *reinterpret_cast<float2 *>(p) = make_float2(a, b); }
+__device__ __forceinline__ void store2(bf16 *p, float a, float b) {
+  *reinterpret_cast<__nv_bfloat162 *>(p) = __floats2bfloat162_rn(a, b);
+}
+// The lane's share of a head's D values (times f): ELEM 2: dims nt * 8 + cq + {0, 1}; ELEM 1: dims (cq + {0, 1}) * NT + nt,
+// which are 2 NT consecutive ones.
+template <int D, int ELEM, typename P>
+__device__ __forceinline__ void store_head(P *row, const float (&ov)[D / 8][2], int cq, float f) {
+  constexpr int NT = D / 8;
+  if (ELEM == 2) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) store2(row + nt * 8 + cq, ov[nt][0] * f, ov[nt][1] * f);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int nt = 0; nt < NT; nt += 4)
+        store4(row + (cq + i) * NT + nt, ov[nt][i] * f, ov[nt + 1][i] * f, ov[nt + 2][i] * f, ov[nt + 3][i] * f);
+  }
+}
 __device__ __forceinline__ float quad_max(float v) {
   v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
   return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
@@ -185,7 +239,9 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
   constexpr int NT = D / 8;                  // n-tiles of O = P V
   constexpr int CH = C::row / 16;            // 16-byte chunks of a row
   constexpr int RPI = 32 / CH;               // rows per copy instruction
-  constexpr int TILE = KW * kBaKeys;         // keys of a tile of the split
+  constexpr int KEYS = C::keys;
+  constexpr int NK = KEYS / 8;               // n-tiles of S
+  constexpr int TILE = KW * KEYS;            // keys of a tile of the split
   extern __shared__ __align__(128) unsigned char ba_smem[];
   __shared__ float2 ml_s[2][kBaWarps][kBaHeads];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -250,13 +306,15 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
     cons.tile = (int)(first_tile - before);
   }
 
-  // ---- loads.  Lane l looks up the page of row l % 16 of the stage to come, one stage ahead of its copies.
+  asm volatile("griddepcontrol.launch_dependents;");      // the joining kernel may be put in place
+
+  // ---- loads.  Lane l looks up the page of row l % KEYS of the stage to come, one stage ahead of its copies.
   Cursor prod = cons;
   long long to_load = todo;
   int blk = -1, off = 0;                     // row of the stage that `prod` stands at: block (-1: none), slot
-  const int my_row = lane & 15;
+  const int my_row = lane % KEYS;
   auto look_up = [&]() {
-    const int pos = (prod.tile * KW + kg) * kBaKeys + my_row;
+    const int pos = (prod.tile * KW + kg) * KEYS + my_row;
     blk = -1;
     if (to_load > 0 && pos < prod.n) {
       const int b = p.block_shift >= 0 ? pos >> p.block_shift : pos / p.cache.block_size;
@@ -265,6 +323,10 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
       if ((unsigned)blk >= (unsigned)p.num_blocks) blk = -2;      // not in the pool: never followed
     }
   };
+  const long long row_stride = (long long)p.cache.n_kv_heads * C::row;
+  // the lane's chunk of row lane / CH, and the scale bytes, in block 0 of K
+  const char *base0 = p.cache.page(p.layer, 0, 0) + (long long)kvh * C::row + (lane / CH) * row_stride + (lane % CH) * 16;
+  const char *scale0 = p.cache.page(p.layer, 0, 0) + p.cache.value_bytes();
   unsigned poison = 0;                       // bit s: the stage in ring slot s has a row outside the pool
   int put = 0;                               // ring slot to fill next
   auto issue = [&]() {
@@ -274,22 +336,40 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
     if (any) {
       const uint32_t k_s = ring + put * C::stage, v_s = k_s + C::tile;
       const int sub = lane / CH, c = lane % CH;
+      const unsigned live = __ballot_sync(0xffffffffu, blk >= 0);
+      if (p.aligned16) {      // one address per 16 rows
 #pragma unroll
-      for (int i = 0; i < kBaKeys / RPI; ++i) {
-        const int row = i * RPI + sub;
-        const int b = __shfl_sync(0xffffffffu, blk, row), o = __shfl_sync(0xffffffffu, off, row);
-        const bool ok = b >= 0;
-        const char *src = p.cache.page(p.layer, 0, ok ? b : 0) +
-                          ((long long)(ok ? o : 0) * p.cache.n_kv_heads + kvh) * C::row + c * 16;
-        const uint32_t dst = chunk_at<D, ELEM>(row, c);
-        cp16(k_s + dst, src, ok);                                 // rows that are not there are zeros
-        cp16(v_s + dst, src + p.cache.kv_stride, ok);
+        for (int half = 0; half < KEYS / 16; ++half) {
+          const int b = __shfl_sync(0xffffffffu, blk, half * 16), o = __shfl_sync(0xffffffffu, off, half * 16);
+          const char *src = base0 + (b >= 0 ? b * p.cache.block_stride + o * row_stride : 0);
+#pragma unroll
+          for (int i = 0; i < 16 / RPI; ++i) {
+            const int row = half * 16 + i * RPI + sub;
+            const bool ok = (live >> row) & 1u;
+            const uint32_t dst = chunk_at<D, ELEM>(row, c);
+            cp16(k_s + dst, src, ok);                             // rows that are not there are zeros
+            cp16(v_s + dst, src + p.cache.kv_stride, ok);
+            src += RPI * row_stride;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < KEYS / RPI; ++i) {
+          const int row = i * RPI + sub;
+          const int b = __shfl_sync(0xffffffffu, blk, row), o = __shfl_sync(0xffffffffu, off, row);
+          const bool ok = b >= 0;
+          const char *src = base0 + (ok ? b * p.cache.block_stride + (o - sub) * row_stride : 0);
+          const uint32_t dst = chunk_at<D, ELEM>(row, c);
+          cp16(k_s + dst, src, ok);
+          cp16(v_s + dst, src + p.cache.kv_stride, ok);
+        }
       }
-      if (ELEM == 1) {   // the word that holds the scale byte of row l % 16 of K (lanes 0-15) or V
+      if (ELEM == 1) {   // the words that hold the scale bytes of row l of K and of V
         const bool ok = blk >= 0;
         const int at = kvh * p.cache.block_size + (ok ? off : 0);
-        const char *src = p.cache.page(p.layer, lane >> 4, ok ? blk : 0) + p.cache.value_bytes() + (at & ~3);
+        const char *src = scale0 + (ok ? blk * p.cache.block_stride : 0) + (at & ~3);
         cp4(k_s + 2 * C::tile + lane * 4, src, ok);
+        cp4(k_s + 2 * C::tile + 128 + lane * 4, src + p.cache.kv_stride, ok);
       }
     }
     cp_commit();
@@ -320,17 +400,19 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
         const float f = on * p.scale;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          const int d0 = ks * 16 + cq;
-          split_bf16((float)q[d0] * f, (float)q[d0 + 1] * f, qf[ks][0], qf[ks][1]);
-          split_bf16((float)q[d0 + 8] * f, (float)q[d0 + 9] * f, qf[ks][2], qf[ks][3]);
+          const float2 a = load2(q + ks * 16 + cq), b = load2(q + ks * 16 + cq + 8);
+          split_bf16(a.x * f, a.y * f, qf[ks][0], qf[ks][1]);
+          split_bf16(b.x * f, b.y * f, qf[ks][2], qf[ks][3]);
         }
       } else {
         // the lane's dims: 4 KS consecutive ones, so that a key's codes are read as 16-byte vectors
         const T *ql = q + (lane & 3) * (4 * KS);
         float x[4 * KS], most = 0.f;
 #pragma unroll
+        for (int i = 0; i < KS / 2; ++i) load8(ql + 8 * i, x + 8 * i);
+#pragma unroll
         for (int i = 0; i < 4 * KS; ++i) {
-          x[i] = (float)ql[i] * on;
+          x[i] *= on;
           most = fmaxf(most, fabsf(x[i]));
         }
         most = quad_max(most);
@@ -356,12 +438,12 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
       __syncwarp();
       issue();                                        // into the slot that the previous step has left
       const uint32_t k_s = ring + get * C::stage, v_s = k_s + C::tile;
-      const int key0 = (cons.tile * KW + kg) * kBaKeys;
+      const int key0 = (cons.tile * KW + kg) * KEYS;
       if (key0 < n) {
-        // ---- S = Q K^T: two n-tiles of 8 keys; the lane ends with keys cq, cq + 1, cq + 8, cq + 9 of head r0
-        float sc[2][4];
+        // ---- S = Q K^T: n-tiles of 8 keys; the lane ends with keys cq, cq + 1 of each for head r0
+        float sc[NK][4];
 #pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
+        for (int nt = 0; nt < NK; ++nt) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) sc[nt][i] = 0.f;
           if (ELEM == 2) {
@@ -384,48 +466,51 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
             }
           }
         }
-        float t[4] = {sc[0][0] + sc[0][2], sc[0][1] + sc[0][3], sc[1][0] + sc[1][2], sc[1][1] + sc[1][3]};
-        float ev[4];
+        float t[2 * NK], ev[2 * NK];                  // value i: key (i / 2) * 8 + cq + i % 2
+#pragma unroll
+        for (int i = 0; i < 2 * NK; ++i) t[i] = sc[i >> 1][i & 1] + sc[i >> 1][2 + (i & 1)];
         if (ELEM == 1) {
-          // lane l has the scale byte of K row l (l < 16) or V row l - 16
+          // lane l has the scale bytes of row l: K's goes to the exponent field of a float, V's to the low bits
           const int pos = min(key0 + my_row, n - 1);
           const int o = p.block_shift >= 0 ? pos & (p.cache.block_size - 1) : pos % p.cache.block_size;
-          const int byte = (kvh * p.cache.block_size + o) & 3;
-          const int e = (int)((lds4(k_s + 2 * C::tile + lane * 4) >> (8 * byte)) & 255u);
-          const int both = e | (__shfl_down_sync(0xffffffffu, e, 16) << 8);
+          const int shift = 8 * ((kvh * p.cache.block_size + o) & 3);
+          const uint32_t ek = (lds4(k_s + 2 * C::tile + lane * 4) >> shift) & 255u;
+          const uint32_t both = ek << 23 | ((lds4(k_s + 2 * C::tile + 128 + lane * 4) >> shift) & 255u);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int b = __shfl_sync(0xffffffffu, both, cq + (i & 1) + (i >> 1) * 8);
-            t[i] = (t[i] * q_scale) * __uint_as_float((uint32_t)(b & 255) << 23);
-            ev[i] = (float)((b >> 8) - 127);
+          for (int i = 0; i < 2 * NK; ++i) {
+            const uint32_t b = __shfl_sync(0xffffffffu, both, (i >> 1) * 8 + cq + (i & 1));
+            t[i] = (t[i] * q_scale) * __uint_as_float(b & 0x7f800000u);
+            ev[i] = __uint_as_float(0x4b000000u | (b & 255u)) - 8388735.f;      // 2^23 + byte, less 2^23 + 127
           }
         }
+        if (key0 + KEYS > n) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (key0 + cq + (i & 1) + (i >> 1) * 8 >= n) t[i] = -INFINITY;
-        const float m_new = fmaxf(m, quad_max(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]))));
+          for (int i = 0; i < 2 * NK; ++i)
+            if (key0 + (i >> 1) * 8 + cq + (i & 1) >= n) t[i] = -INFINITY;
+        }
+        const float m_new = fmaxf(m, quad_max(max_of(t)));
         const float m_use = m_new == -INFINITY ? 0.f : m_new;      // no score yet: nothing to subtract
-        float w[4], corr;
+        float w[2 * NK], corr;
         if (ELEM == 2) {
           corr = ex2(m - m_use);
           l *= corr;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < 2 * NK; ++i) {
             w[i] = ex2(t[i] - m_use);
             l += w[i];
           }
         } else {
           l *= ex2(m - m_use);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < 2 * NK; ++i) {
             l += ex2(t[i] - m_use);
             t[i] += ev[i];
           }
-          const float w_new = fmaxf(mw, quad_max(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]))));
+          const float w_new = fmaxf(mw, quad_max(max_of(t)));
           const float w_use = w_new == -INFINITY ? 0.f : w_new;
           corr = ex2(mw - w_use);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = ex2(t[i] - w_use + kWeightBits);
+          for (int i = 0; i < 2 * NK; ++i) w[i] = ex2(t[i] - (w_use - kWeightBits));
           mw = w_new;
         }
         m = m_new;
@@ -437,42 +522,45 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
         }
         if ((poison >> get) & 1u) l = __uint_as_float(0x7fc00000u);      // a row outside the pool: the request is NaN
         // ---- O += P V: the high parts are row r0, the low parts row r0 + 8
-        uint32_t pf[4];
-        if (ELEM == 2) {
-          split_bf16(w[0], w[1], pf[0], pf[1]);
-          split_bf16(w[2], w[3], pf[2], pf[3]);
-          const int row = ((lane >> 3) & 1) * 8 + (lane & 7);
 #pragma unroll
-          for (int nt = 0; nt < NT; nt += 2) {
-            uint32_t b[4];
-            ldsm4_trans(v_s + chunk_at<D, ELEM>(row, nt + (lane >> 4)), b);
-            mma_bf16(oc[nt], pf, b[0], b[1]);
-            mma_bf16(oc[nt + 1], pf, b[2], b[3]);
-          }
-        } else {
-          split_f16(w[0], w[1], pf[0], pf[1]);
-          split_f16(w[2], w[3], pf[2], pf[3]);
-          // column r0 of n-tile nt is dim r0 * NT + nt: the lane reads NT consecutive codes of its four keys
-          uint32_t v[4][NT / 4];
+        for (int kk = 0; kk < KEYS / 16; ++kk) {
+          uint32_t pf[4];
+          if (ELEM == 2) {
+            split_bf16(w[4 * kk], w[4 * kk + 1], pf[0], pf[1]);
+            split_bf16(w[4 * kk + 2], w[4 * kk + 3], pf[2], pf[3]);
+            const int row = kk * 16 + ((lane >> 3) & 1) * 8 + (lane & 7);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int row = cq + (i & 1) + (i >> 1) * 8;
-            if (NT == 16) {
-              const uint4 x = lds16(v_s + chunk_at<D, ELEM>(row, r0));
-              v[i][0] = x.x; v[i][1] = x.y; v[i][NT / 4 - 2] = x.z; v[i][NT / 4 - 1] = x.w;
-            } else {
-              const uint2 x = lds8(v_s + chunk_at<D, ELEM>(row, r0 >> 1) + (r0 & 1) * 8);
-              v[i][0] = x.x; v[i][1] = x.y;
+            for (int nt = 0; nt < NT; nt += 2) {
+              uint32_t b[4];
+              ldsm4_trans(v_s + chunk_at<D, ELEM>(row, nt + (lane >> 4)), b);
+              mma_bf16(oc[nt], pf, b[0], b[1]);
+              mma_bf16(oc[nt + 1], pf, b[2], b[3]);
             }
-          }
+          } else {
+            split_f16(w[4 * kk], w[4 * kk + 1], pf[0], pf[1]);
+            split_f16(w[4 * kk + 2], w[4 * kk + 3], pf[2], pf[3]);
+            // column r0 of n-tile nt is dim r0 * NT + nt: the lane reads NT consecutive codes of its four keys
+            uint32_t v[4][NT / 4];
 #pragma unroll
-          for (int j = 0; j < NT / 4; ++j) {
-            const uint32_t a0 = __byte_perm(v[0][j], v[1][j], 0x5140), a1 = __byte_perm(v[0][j], v[1][j], 0x7362);
-            const uint32_t b0 = __byte_perm(v[2][j], v[3][j], 0x5140), b1 = __byte_perm(v[2][j], v[3][j], 0x7362);
-            mma_f16(oc[4 * j], pf, half2_of_e4m3(a0), half2_of_e4m3(b0));
-            mma_f16(oc[4 * j + 1], pf, half2_of_e4m3(a0 >> 16), half2_of_e4m3(b0 >> 16));
-            mma_f16(oc[4 * j + 2], pf, half2_of_e4m3(a1), half2_of_e4m3(b1));
-            mma_f16(oc[4 * j + 3], pf, half2_of_e4m3(a1 >> 16), half2_of_e4m3(b1 >> 16));
+            for (int i = 0; i < 4; ++i) {
+              const int row = kk * 16 + cq + (i & 1) + (i >> 1) * 8;
+              if (NT == 16) {
+                const uint4 x = lds16(v_s + chunk_at<D, ELEM>(row, r0));
+                v[i][0] = x.x; v[i][1] = x.y; v[i][NT / 4 - 2] = x.z; v[i][NT / 4 - 1] = x.w;
+              } else {
+                const uint2 x = lds8(v_s + chunk_at<D, ELEM>(row, r0 >> 1) + (r0 & 1) * 8);
+                v[i][0] = x.x; v[i][1] = x.y;
+              }
+            }
+#pragma unroll
+            for (int j = 0; j < NT / 4; ++j) {
+              const uint32_t a0 = __byte_perm(v[0][j], v[1][j], 0x5140), a1 = __byte_perm(v[0][j], v[1][j], 0x7362);
+              const uint32_t b0 = __byte_perm(v[2][j], v[3][j], 0x5140), b1 = __byte_perm(v[2][j], v[3][j], 0x7362);
+              mma_f16(oc[4 * j], pf, half2_of_e4m3(a0), half2_of_e4m3(b0));
+              mma_f16(oc[4 * j + 1], pf, half2_of_e4m3(a0 >> 16), half2_of_e4m3(b0 >> 16));
+              mma_f16(oc[4 * j + 2], pf, half2_of_e4m3(a1), half2_of_e4m3(b1));
+              mma_f16(oc[4 * j + 3], pf, half2_of_e4m3(a1 >> 16), half2_of_e4m3(b1 >> 16));
+            }
           }
         }
       }
@@ -494,73 +582,59 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
     const bool whole = s_tile == 0 && steps == max(1, (n + TILE - 1) / TILE);
     const long long rec_slot = s_tile == 0 ? 1 : 0;      // a range can begin and end inside a request: two records
 
-    if (KW == 1) {
-      if (r0 < nh) {
-        const int h = head0 + r0;
-        float *rec_o = nullptr;
-        T *out = nullptr;
-        float inv = 1.f;
-        if (whole) {
-          out = static_cast<T *>(p.out) + req * p.out_stride + (long long)h * D;
-          inv = n == 0 ? 0.f : 1.f / l;
-          if (p.lse != nullptr && (lane & 3) == 0)
-            p.lse[(long long)req * p.n_q_heads + h] = n == 0 ? -INFINITY : (m + log2f(l)) * (1.f / kLog2e);
-        } else {
-          const long long rec = ((long long)h * p.parts + part) * 2 + rec_slot;
-          rec_o = p.o + rec * D;
-          if ((lane & 3) == 0) p.ml[rec] = make_float2(m, l);
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int d = ELEM == 2 ? nt * 8 + cq + i : (cq + i) * NT + nt;
-            if (whole)
-              out[d] = (T)(ov[nt][i] * inv);
-            else
-              rec_o[d] = ov[nt][i];
-          }
-        }
+    auto finish = [&]() {
+      if (r0 >= nh) return;
+      const int h = head0 + r0;
+      if (whole) {
+        store_head<D, ELEM>(static_cast<T *>(p.out) + req * p.out_stride + (long long)h * D, ov, cq, n == 0 ? 0.f : 1.f / l);
+        if (p.lse != nullptr && (lane & 3) == 0)
+          p.lse[(long long)req * p.n_q_heads + h] = n == 0 ? -INFINITY : (m + log2f(l)) * (1.f / kLog2e);
+      } else {
+        const long long rec = ((long long)h * p.parts + part) * 2 + rec_slot;
+        store_head<D, ELEM>(p.o + rec * D, ov, cq, 1.f);
+        if ((lane & 3) == 0) p.ml[rec] = make_float2(m, l);
       }
+    };
+    if (KW == 1) {
+      finish();
     } else {
-      // the CTA's four warps share the head: common maximum, outputs added in shared memory
-      float *buf = reinterpret_cast<float *>(ba_smem + kBaWarps * C::ring);
-      const int par = seg & 1;
-      if ((lane & 3) == 0) ml_s[par][warp][r0] = make_float2(m, l);
+      // the CTA's four warps share the head: brought to the common maximum, warps 1-3 hand theirs to warp 0, lane by lane.
+      // (ml_s takes turns: warp 0 may still read it while the others write the next request's.)
+      float4 *buf = reinterpret_cast<float4 *>(ba_smem + kBaWarps * C::ring);
+      float2(*ml)[kBaHeads] = ml_s[seg & 1];
+      if ((lane & 3) == 0) ml[warp][r0] = make_float2(m, l);
       __syncthreads();
       float all = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < kBaWarps; ++w) all = fmaxf(all, ml_s[par][w][r0].x);
+      for (int w = 0; w < kBaWarps; ++w) all = fmaxf(all, ml[w][r0].x);
       const float f = m == -INFINITY ? 0.f : ex2(m - all);
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int nt = 0; nt < NT; ++nt) {
+        ov[nt][0] *= f;
+        ov[nt][1] *= f;
+      }
+      if (warp > 0) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int d = ELEM == 2 ? nt * 8 + cq + i : (cq + i) * NT + nt;
-          buf[(warp * kBaHeads + r0) * D + d] = m == -INFINITY && ov[nt][i] == 0.f ? 0.f : ov[nt][i] * f;
-        }
+        for (int k = 0; k < NT / 2; ++k)
+          buf[((warp - 1) * (NT / 2) + k) * 32 + lane] = make_float4(ov[2 * k][0], ov[2 * k][1], ov[2 * k + 1][0], ov[2 * k + 1][1]);
+      }
       __syncthreads();
-      for (int e = threadIdx.x; e < nh * D; e += kBaThreads) {
-        const int row = e / D, d = e % D, h = head0 + row;
-        float o = 0.f, mm = -INFINITY, ll = 0.f;
+      if (warp == 0) {
 #pragma unroll
-        for (int w = 0; w < kBaWarps; ++w) mm = fmaxf(mm, ml_s[par][w][row].x);
+        for (int w = 0; w < kBaWarps - 1; ++w)
+#pragma unroll
+          for (int k = 0; k < NT / 2; ++k) {
+            const float4 x = buf[(w * (NT / 2) + k) * 32 + lane];
+            ov[2 * k][0] += x.x; ov[2 * k][1] += x.y; ov[2 * k + 1][0] += x.z; ov[2 * k + 1][1] += x.w;
+          }
+        l = 0.f;
 #pragma unroll
         for (int w = 0; w < kBaWarps; ++w) {
-          const float2 x = ml_s[par][w][row];
-          o += buf[(w * kBaHeads + row) * D + d];
-          ll += x.x == -INFINITY ? x.y : x.y * ex2(x.x - mm);
+          const float2 x = ml[w][r0];
+          l += x.x == -INFINITY ? x.y : x.y * ex2(x.x - all);
         }
-        if (whole) {
-          T *out = static_cast<T *>(p.out) + req * p.out_stride + (long long)h * D;
-          out[d] = (T)(n == 0 ? 0.f : o / ll);
-          if (p.lse != nullptr && d == 0)
-            p.lse[(long long)req * p.n_q_heads + h] = n == 0 ? -INFINITY : (mm + log2f(ll)) * (1.f / kLog2e);
-        } else {
-          const long long rec = ((long long)h * p.parts + part) * 2 + rec_slot;
-          p.o[rec * D + d] = o;
-          if (d == 0) p.ml[rec] = make_float2(mm, ll);
-        }
+        m = all;
+        finish();
       }
       ++seg;
     }
@@ -568,27 +642,63 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
   cp_wait_group<0>();
 }
 
-// Joins the records of one (request, query head): the parts that hold its tiles follow from the starts.
+// Joins the records of one (request, query head) per warp: the parts that hold its tiles follow from the starts.  Placed
+// while the first kernel still runs (programmatic launch); everything that kernel wrote is read behind the wait, past L1.
+constexpr int kJoinWarps = 8;
 template <int D, typename T>
-__global__ void __launch_bounds__(D) paged_attention_join_kernel(const __grid_constant__ BaParams p) {
-  const int req = blockIdx.x, h = blockIdx.y, d = threadIdx.x;
+__global__ void __launch_bounds__(kJoinWarps * 32) paged_attention_join_kernel(const __grid_constant__ BaParams p) {
+  constexpr int V = D / 128 > 0 ? 4 : 2;           // values of a lane
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int lane = threadIdx.x & 31, req = blockIdx.x, h = blockIdx.y * kJoinWarps + (threadIdx.x >> 5);
+  if (h >= p.n_q_heads) return;
   const long long total = __ldcg(p.tile_start + p.n_req);
   const long long t0 = __ldcg(p.tile_start + req), t1 = __ldcg(p.tile_start + req + 1);
   const long long ranges = min((long long)p.parts, total);
-  const int first = (int)(((t0 + 1) * ranges - 1) / total), last = (int)((t1 * ranges - 1) / total);
-  if (first == last) return;                       // one part held it all and wrote the output
-  float m = -INFINITY;
-  for (int q = first; q <= last; ++q) m = fmaxf(m, __ldcg(p.ml + ((long long)h * p.parts + q) * 2 + (q == first)).x);
-  float l = 0.f, o = 0.f;
-  for (int q = first; q <= last; ++q) {
-    const long long rec = ((long long)h * p.parts + q) * 2 + (q == first);
-    const float2 x = __ldcg(p.ml + rec);
-    const float f = x.x == -INFINITY ? 0.f : ex2(x.x - m);
-    l += x.x == -INFINITY ? x.y : x.y * f;
-    o += f * __ldcg(p.o + rec * D + d);
+  int first, last;
+  if (total * ranges <= 0xffffffffll) {
+    first = (int)((uint32_t)((t0 + 1) * ranges - 1) / (uint32_t)total);
+    last = (int)((uint32_t)(t1 * ranges - 1) / (uint32_t)total);
+  } else {
+    first = (int)(((t0 + 1) * ranges - 1) / total);
+    last = (int)((t1 * ranges - 1) / total);
   }
-  static_cast<T *>(p.out)[req * p.out_stride + (long long)h * D + d] = (T)(o / l);
-  if (p.lse != nullptr && d == 0) p.lse[(long long)req * p.n_q_heads + h] = (m + log2f(l)) * (1.f / kLog2e);
+  if (first == last) return;                       // one part held it all and wrote the output
+  const long long rec0 = (long long)h * p.parts * 2;
+  float m = -INFINITY;
+  for (int q = first + lane; q <= last; q += 32) m = fmaxf(m, __ldcg(p.ml + rec0 + 2 * q + (q == first)).x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float l = 0.f, acc[V] = {};
+  for (int q0 = first; q0 <= last; q0 += 32) {
+    const int q = q0 + lane, count = min(32, last - q0 + 1);
+    float f = 0.f;
+    if (q <= last) {
+      const float2 x = __ldcg(p.ml + rec0 + 2 * q + (q == first));
+      f = x.x == -INFINITY ? 0.f : ex2(x.x - m);
+      l += x.x == -INFINITY ? x.y : x.y * f;
+    }
+#pragma unroll 8
+    for (int j = 0; j < count; ++j) {
+      const float fj = __shfl_sync(0xffffffffu, f, j);
+      const float *src = p.o + (rec0 + 2 * (q0 + j) + (q0 + j == first)) * D + lane * V;
+      if (V == 4) {
+        const float4 v = __ldcg(reinterpret_cast<const float4 *>(src));
+        acc[0] += fj * v.x; acc[1] += fj * v.y; acc[V - 2] += fj * v.z; acc[V - 1] += fj * v.w;
+      } else {
+        const float2 v = __ldcg(reinterpret_cast<const float2 *>(src));
+        acc[0] += fj * v.x; acc[1] += fj * v.y;
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  T *out = static_cast<T *>(p.out) + req * p.out_stride + (long long)h * D + lane * V;
+  const float inv = 1.f / l;
+  if (V == 4)
+    store4(out, acc[0] * inv, acc[1] * inv, acc[V - 2] * inv, acc[V - 1] * inv);
+  else
+    store2(out, acc[0] * inv, acc[1] * inv);
+  if (p.lse != nullptr && lane == 0) p.lse[(long long)req * p.n_q_heads + h] = (m + log2f(l)) * (1.f / kLog2e);
 }
 
 // Contexts of at most this many tokens are not split: one launch, a CTA per (request, KV head).
@@ -600,7 +710,7 @@ struct BaPlan {
   int kw, parts, columns;   // warps per KV head, ranges (0: a CTA per request), CTAs over the KV heads
 };
 
-BaPlan ba_plan(int n_req, int vheads, int max_ctx, int sms) {
+BaPlan ba_plan(int n_req, int vheads, int max_ctx, int sms, int keys) {
   BaPlan b;
   // A warp per KV head once the batch has a tile for every warp of the machine; four warps per head below that.
   b.kw = (long long)n_req * vheads >= 4ll * sms ? 1 : kBaWarps;
@@ -610,7 +720,7 @@ BaPlan ba_plan(int n_req, int vheads, int max_ctx, int sms) {
     b.parts = 0;
     return b;
   }
-  const long long tiles = (long long)n_req * ((max_ctx + b.kw * kBaKeys - 1) / (b.kw * kBaKeys));
+  const long long tiles = (long long)n_req * ((max_ctx + b.kw * keys - 1) / (b.kw * keys));
   long long parts = 2ll * sms / b.columns;         // two CTAs per SM
   parts = parts < 1 ? 1 : parts;
   b.parts = (int)(parts < tiles ? parts : tiles);
@@ -637,17 +747,25 @@ int ba_launch(const BaParams &p, const BaPlan &b, int device, cudaStream_t st) {
   static bool attr_set[kMaxDevices] = {};
   auto kernel = paged_attention_batched_kernel<D, ELEM, T, KW>;
   if (!attr_set[device]) {
-    KV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BaCfg<D, ELEM>::smem));
+    KV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BaCfg<D, ELEM>::smem(KW)));
     attr_set[device] = true;
   }
   const dim3 grid(b.parts == 0 ? p.n_req : b.parts, b.columns);
-  kernel<<<grid, kBaThreads, BaCfg<D, ELEM>::smem, st>>>(p);
+  kernel<<<grid, kBaThreads, BaCfg<D, ELEM>::smem(KW), st>>>(p);
   KV_COUNT_LAUNCH();
   KV_CUDA(cudaGetLastError());
   if (b.parts == 0) return KV_OK;
-  paged_attention_join_kernel<D, T><<<dim3(p.n_req, p.n_q_heads), D, 0, st>>>(p);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(p.n_req, (p.n_q_heads + kJoinWarps - 1) / kJoinWarps);
+  cfg.blockDim = dim3(kJoinWarps * 32);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  KV_CUDA(cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<D, T>, p));
   KV_COUNT_LAUNCH();
-  KV_CUDA(cudaGetLastError());
   return KV_OK;
 }
 
@@ -673,7 +791,7 @@ int64_t kv_paged_attention_batched_scratch_bytes(int32_t n_req, int32_t n_q_head
   if (max_ctx > kBaMaxCtx) return KV_ERR_SHAPE;
   if (n_q_heads % n_kv_heads != 0 || (head_dim != 64 && head_dim != 128)) return KV_ERR_SHAPE;
   const int vheads = n_kv_heads * ba_passes(n_q_heads / n_kv_heads);
-  const BaPlan b = ba_plan(n_req > 0 ? n_req : 1, vheads, max_ctx, sm_count(current_device()));
+  const BaPlan b = ba_plan(n_req > 0 ? n_req : 1, vheads, max_ctx, sm_count(current_device()), 16);
   return b.parts == 0 ? 256 : ba_scratch(n_req, n_q_heads, head_dim, b.parts).bytes;
 }
 
@@ -708,7 +826,7 @@ int32_t kv_op_paged_attention_batched(const void *q_dev, int64_t q_stride, int32
   p.passes = ba_passes(p.group);
   const long long vheads = (long long)cache->n_kv_heads * p.passes;
   if (vheads > 65535 || n_q_heads > 65535) return KV_ERR_SHAPE;      // second dimension of the grids
-  const BaPlan b = ba_plan(n_req, (int)vheads, max_ctx, sm_count(device));
+  const BaPlan b = ba_plan(n_req, (int)vheads, max_ctx, sm_count(device), 16);
   const BaScratch s = ba_scratch(n_req, n_q_heads, cache->head_dim, b.parts);
   if (b.parts > 0) {
     if (scratch_dev == nullptr || ((uintptr_t)scratch_dev & 15) || scratch_bytes < s.bytes) return KV_ERR_WORKSPACE;
@@ -720,6 +838,7 @@ int32_t kv_op_paged_attention_batched(const void *q_dev, int64_t q_stride, int32
   p.block_shift = -1;
   for (int i = 0; i < 31; ++i)
     if ((1 << i) == cache->block_size) p.block_shift = i;
+  p.aligned16 = cache->block_size % 16 == 0;
   p.q = q_dev;
   p.out = out_dev;
   p.lse = lse_out_dev;
