@@ -17,13 +17,18 @@
 // rows are neighbouring memory), or every fourth stage of one KV head (few requests: four times fewer records; their
 // results meet in shared memory).
 //
-// The products run on mma.sync m16n8k16 with the query heads as rows: a KV group has 8 heads or fewer, and the tile's 16
-// rows hold each head twice, the high and the low half of an operand that is split in two: q (rows 0-7: high, 8-15: low)
-// against K, p against V.  The two rows are added afterwards, which gives fp32-level accuracy at the price of one pass.
-// (A 128-row tcgen05 tile would be fifteen sixteenths padding.)  Groups of more than 8 heads are taken 8 at a time.
+// The products run on mma.sync m16n8k16 with the keys (S^T = K Q^T) and the head's dims (O^T = V^T P^T) as the 16 rows and
+// the query heads as the 8 columns: a KV group has 8 heads or fewer, so nothing is padding.  (A 128-row tcgen05 tile would
+// hold 8 useful columns of at least 16 as well, but wants its operands through shared-memory descriptors, and e4m3 rows
+// would have to be converted and written back there first.)  Groups of more than 8 heads are taken 8 at a time.
+// fp32 operands are split into two halves, hi + lo, that are multiplied one after the other: q for fp32 queries, and the
+// weights p, but for bf16 results over e4m3 pages: there p is one fp16, off by 2^-12, a sixteenth of the result's rounding.
+//
+// The running maximum is lazy: m is replaced only when a score passes it by more than 2^8, so most stages need no
+// reduction over the lanes and no rescaling; sums and weights have the head room for it.
 //
 // e4m3 pages: codes go to fp16 fragments (exact) and the power-of-two scales stay outside: K's multiplies the score,
-// V's goes into the weight, w = 2^(t + e_v - M), with its own running maximum M of t + e_v, so that fp16 keeps 22 bits
+// V's goes into the weight, w = 2^(t + e_v - M), with its own running maximum M of t + e_v, so that fp16 keeps the bits
 // of every weight that matters next to the largest CONTRIBUTION, however the rows' scales differ.
 #include <float.h>
 
@@ -36,7 +41,8 @@ constexpr int kBaWarps = 4;
 constexpr int kBaThreads = kBaWarps * 32;
 constexpr int kBaHeads = 8;          // query heads of a pass
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kWeightBits = 12.f;  // fp16 weights are scaled to at most 2^12
+constexpr float kLazy = 8.f;         // a running maximum may be passed by 2^8 before it is replaced
+constexpr float kWeightBits = 7.f;   // fp16 weights: 2^7 at the running maximum, so at most 2^15
 constexpr int kQueryBits = 12;       // ... and fp16 queries to less than 2^12
 
 // A stage is what a warp loads and consumes at a time: 32 keys, so that the softmax's and the loads' bookkeeping is paid
@@ -143,12 +149,11 @@ __device__ __forceinline__ void split_f16(float x, float y, uint32_t &hi, uint32
       : "=f"(fx), "=f"(fy) : "r"(hi));
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(lo) : "f"(y - fy), "f"(x - fx));
 }
-template <int N>
-__device__ __forceinline__ float max_of(const float (&v)[N]) {
-  float m = fmaxf(v[0], v[1]);
-#pragma unroll
-  for (int i = 2; i < N; i += 2) m = fmaxf(m, fmaxf(v[i], v[i + 1]));
-  return m;
+// 8x8 16-bit values, two of a row to a lane -> the same of the transposed block
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
 }
 __device__ __forceinline__ float2 load2(const float *q) { return *reinterpret_cast<const float2 *>(q); }
 __device__ __forceinline__ float2 load2(const bf16 *q) {
@@ -178,21 +183,26 @@ __device__ __forceinline__ void store2(float *p, float a, float b) { *reinterpre
 __device__ __forceinline__ void store2(bf16 *p, float a, float b) {
   *reinterpret_cast<__nv_bfloat162 *>(p) = __floats2bfloat162_rn(a, b);
 }
-// The lane's share of a head's D values (times f): ELEM 2: dims nt * 8 + cq + {0, 1}; ELEM 1: dims (cq + {0, 1}) * NT + nt,
-// which are 2 NT consecutive ones.
+// The lane's share of the D values (times f) of head cq + i.  ELEM 2: dims 16 mt + lane / 4 + {0, 8}; ELEM 1: D / 8
+// consecutive ones.
 template <int D, int ELEM, typename P>
-__device__ __forceinline__ void store_head(P *row, const float (&ov)[D / 8][2], int cq, float f) {
-  constexpr int NT = D / 8;
+__device__ __forceinline__ void store_head(P *row, const float (&oc)[D / 16][4], int i, int g, float f) {
   if (ELEM == 2) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) store2(row + nt * 8 + cq, ov[nt][0] * f, ov[nt][1] * f);
+    for (int mt = 0; mt < D / 16; ++mt) {
+      row[mt * 16 + g] = (P)(oc[mt][i] * f);
+      row[mt * 16 + g + 8] = (P)(oc[mt][2 + i] * f);
+    }
   } else {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int nt = 0; nt < NT; nt += 4)
-        store4(row + (cq + i) * NT + nt, ov[nt][i] * f, ov[nt + 1][i] * f, ov[nt + 2][i] * f, ov[nt + 3][i] * f);
+    for (int mt = 0; mt < D / 16; mt += 2)
+      store4(row + g * (D / 8) + 2 * mt, oc[mt][i] * f, oc[mt][2 + i] * f, oc[mt + 1][i] * f, oc[mt + 1][2 + i] * f);
   }
+}
+__device__ __forceinline__ float column_max(float v) {      // over the eight lanes that share lane % 4
+  v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+  v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+  return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
 }
 __device__ __forceinline__ float quad_max(float v) {
   v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
@@ -235,12 +245,15 @@ struct Cursor {
 template <int D, int ELEM, typename T, int KW>      // KW: warps that share a KV head
 __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(const __grid_constant__ BaParams p) {
   typedef BaCfg<D, ELEM> C;
-  constexpr int KS = D / 16;                 // k-steps of S = Q K^T
-  constexpr int NT = D / 8;                  // n-tiles of O = P V
+  constexpr int KS = D / 16;                 // k-steps of S^T = K Q^T
+  constexpr int NT = D / 8;                  // dims of a lane's V fragments (ELEM 1)
+  constexpr int MO = D / 16;                 // 16-dim tiles of O^T
+  constexpr int QP = sizeof(T) == 4 ? 2 : 1;                    // parts of a query
+  constexpr int PP = ELEM == 1 && sizeof(T) == 2 ? 1 : 2;       // parts of a weight
   constexpr int CH = C::row / 16;            // 16-byte chunks of a row
   constexpr int RPI = 32 / CH;               // rows per copy instruction
   constexpr int KEYS = C::keys;
-  constexpr int NK = KEYS / 8;               // n-tiles of S
+  constexpr int MK = KEYS / 16;              // 16-key tiles of S^T
   constexpr int TILE = KW * KEYS;            // keys of a tile of the split
   extern __shared__ __align__(128) unsigned char ba_smem[];
   __shared__ float2 ml_s[2][kBaWarps][kBaHeads];
@@ -385,31 +398,32 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
   for (int i = 0; i < C::stages - 1; ++i) issue();
 
   // ---- per request of the range
-  const int r0 = lane >> 2, cq = (lane & 3) * 2;      // query head (row) and first column of the lane's fragments
+  const int g = lane >> 2, c = lane & 3, cq = c * 2;   // the lane's query fragments are of head g, its results of cq, cq + 1
   int get = 0, seg = 0;
   while (todo > 0) {
     const int req = cons.r, n = cons.n, s_tile = cons.tile;
     const int steps = (int)min((long long)(cons.n_tiles - s_tile), todo);
-    // Q fragments: row r0 high parts, row r0 + 8 low parts of head head0 + r0
-    uint32_t qf[KS][4];
-    float q_scale = 1.f;
+    uint32_t qf[QP][KS][2];
+    float q_scale[2] = {p.scale, p.scale};
     {
-      const T *q = static_cast<const T *>(p.q) + req * p.q_stride + (long long)(head0 + min(r0, nh - 1)) * D;
-      const float on = r0 < nh ? 1.f : 0.f;
+      const T *q = static_cast<const T *>(p.q) + req * p.q_stride + (long long)(head0 + min(g, nh - 1)) * D;
+      const float on = g < nh ? 1.f : 0.f;
       if (ELEM == 2) {
-        const float f = on * p.scale;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          const float2 a = load2(q + ks * 16 + cq), b = load2(q + ks * 16 + cq + 8);
-          split_bf16(a.x * f, a.y * f, qf[ks][0], qf[ks][1]);
-          split_bf16(b.x * f, b.y * f, qf[ks][2], qf[ks][3]);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const float2 a = load2(q + ks * 16 + cq + 8 * j);
+            uint32_t lo;
+            split_bf16(a.x * on, a.y * on, qf[0][ks][j], lo);      // a bf16 query is its own first half
+            if (QP == 2) qf[QP - 1][ks][j] = lo;
+          }
         }
       } else {
         // the lane's dims: 4 KS consecutive ones, so that a key's codes are read as 16-byte vectors
-        const T *ql = q + (lane & 3) * (4 * KS);
         float x[4 * KS], most = 0.f;
 #pragma unroll
-        for (int i = 0; i < KS / 2; ++i) load8(ql + 8 * i, x + 8 * i);
+        for (int i = 0; i < KS / 2; ++i) load8(q + c * (4 * KS) + 8 * i, x + 8 * i);
 #pragma unroll
         for (int i = 0; i < 4 * KS; ++i) {
           x[i] *= on;
@@ -418,20 +432,28 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
         most = quad_max(most);
         const int e = min(max((int)(__float_as_uint(most) >> 23) - 126, -100), 127);       // most < 2^e
         const float up = __uint_as_float((uint32_t)(127 + kQueryBits - e) << 23);
-        q_scale = p.scale * __uint_as_float((uint32_t)(127 - kQueryBits + e) << 23);
+        const float down = p.scale * __uint_as_float((uint32_t)(127 - kQueryBits + e) << 23);
+        q_scale[0] = __shfl_sync(0xffffffffu, down, cq * 4);
+        q_scale[1] = __shfl_sync(0xffffffffu, down, cq * 4 + 4);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          split_f16(x[4 * ks] * up, x[4 * ks + 1] * up, qf[ks][0], qf[ks][1]);
-          split_f16(x[4 * ks + 2] * up, x[4 * ks + 3] * up, qf[ks][2], qf[ks][3]);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            uint32_t lo;
+            split_f16(x[4 * ks + 2 * j] * up, x[4 * ks + 2 * j + 1] * up, qf[0][ks][j], lo);      // bf16: exact in one
+            if (QP == 2) qf[QP - 1][ks][j] = lo;
+          }
         }
       }
     }
-    float m = -INFINITY, mw = -INFINITY, l = 0.f;     // running maxima of t and of t + e_v (ELEM 1), the lane's sum
-    float oc[NT][4];
+    // per head cq + i: running maxima of t and of t + e_v (ELEM 1; -inf: none yet, then 0 is subtracted), the lane's sum
+    float m[2] = {-INFINITY, -INFINITY}, mw[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    float m_sub[2] = {0.f, 0.f}, w_sub[2] = {0.f, 0.f};
+    float oc[MO][4];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int mt = 0; mt < MO; ++mt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) oc[nt][i] = 0.f;
+      for (int i = 0; i < 4; ++i) oc[mt][i] = 0.f;
 
     for (int s = 0; s < steps; ++s) {
       cp_wait_group<C::stages - 2>();
@@ -440,35 +462,39 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
       const uint32_t k_s = ring + get * C::stage, v_s = k_s + C::tile;
       const int key0 = (cons.tile * KW + kg) * KEYS;
       if (key0 < n) {
-        // ---- S = Q K^T: n-tiles of 8 keys; the lane ends with keys cq, cq + 1 of each for head r0
-        float sc[NK][4];
+        // ---- S^T = K Q^T: the lane ends with keys g + 8 j of heads cq, cq + 1
+        float t[2 * MK][2];
 #pragma unroll
-        for (int nt = 0; nt < NK; ++nt) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sc[nt][i] = 0.f;
+        for (int mt = 0; mt < MK; ++mt) {
+          float sc[2][4] = {};                        // two chains: even and odd k-steps
           if (ELEM == 2) {
-            const int row = nt * 8 + (lane & 7);
+            const int row = mt * 16 + (lane & 15);
 #pragma unroll
-            for (int ks = 0; ks < KS; ks += 2) {
-              uint32_t b[4];
-              ldsm4(k_s + chunk_at<D, ELEM>(row, ks * 2 + (lane >> 3)), b);
-              mma_bf16(sc[nt], qf[ks], b[0], b[1]);
-              mma_bf16(sc[nt], qf[ks + 1], b[2], b[3]);
+            for (int ks = 0; ks < KS; ++ks) {
+              uint32_t a[4];
+              ldsm4(k_s + chunk_at<D, ELEM>(row, ks * 2 + (lane >> 4)), a);
+#pragma unroll
+              for (int h = 0; h < QP; ++h) mma_bf16(sc[ks & 1], a, qf[h][ks][0], qf[h][ks][1]);
             }
           } else {
-            const int row = nt * 8 + r0;
 #pragma unroll
-            for (int c = 0; c < KS / 4; ++c) {
-              const uint4 v = lds16(k_s + chunk_at<D, ELEM>(row, (lane & 3) * (KS / 4) + c));
-              const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            for (int j = 0; j < KS / 4; ++j) {
+              const uint4 x = lds16(k_s + chunk_at<D, ELEM>(mt * 16 + g, c * (KS / 4) + j));
+              const uint4 y = lds16(k_s + chunk_at<D, ELEM>(mt * 16 + g + 8, c * (KS / 4) + j));
+              const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-              for (int i = 0; i < 4; ++i) mma_f16(sc[nt], qf[4 * c + i], half2_of_e4m3(w[i]), half2_of_e4m3(w[i] >> 16));
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t a[4] = {half2_of_e4m3(xs[i]), half2_of_e4m3(ys[i]), half2_of_e4m3(xs[i] >> 16),
+                                       half2_of_e4m3(ys[i] >> 16)};
+#pragma unroll
+                for (int h = 0; h < QP; ++h) mma_f16(sc[i & 1], a, qf[h][4 * j + i][0], qf[h][4 * j + i][1]);
+              }
             }
           }
-        }
-        float t[2 * NK], ev[2 * NK];                  // value i: key (i / 2) * 8 + cq + i % 2
 #pragma unroll
-        for (int i = 0; i < 2 * NK; ++i) t[i] = sc[i >> 1][i & 1] + sc[i >> 1][2 + (i & 1)];
+          for (int i = 0; i < 4; ++i) t[2 * mt + (i >> 1)][i & 1] = (sc[0][i] + sc[1][i]) * q_scale[i & 1];
+        }
+        float ev[2 * MK];
         if (ELEM == 1) {
           // lane l has the scale bytes of row l: K's goes to the exponent field of a float, V's to the low bits
           const int pos = min(key0 + my_row, n - 1);
@@ -477,89 +503,109 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
           const uint32_t ek = (lds4(k_s + 2 * C::tile + lane * 4) >> shift) & 255u;
           const uint32_t both = ek << 23 | ((lds4(k_s + 2 * C::tile + 128 + lane * 4) >> shift) & 255u);
 #pragma unroll
-          for (int i = 0; i < 2 * NK; ++i) {
-            const uint32_t b = __shfl_sync(0xffffffffu, both, (i >> 1) * 8 + cq + (i & 1));
-            t[i] = (t[i] * q_scale) * __uint_as_float(b & 0x7f800000u);
-            ev[i] = __uint_as_float(0x4b000000u | (b & 255u)) - 8388735.f;      // 2^23 + byte, less 2^23 + 127
+          for (int j = 0; j < 2 * MK; ++j) {
+            const uint32_t b = __shfl_sync(0xffffffffu, both, 8 * j + g);
+            t[j][0] *= __uint_as_float(b & 0x7f800000u);
+            t[j][1] *= __uint_as_float(b & 0x7f800000u);
+            ev[j] = __uint_as_float(0x4b000000u | (b & 255u)) - 8388735.f;      // 2^23 + byte, less 2^23 + 127
           }
         }
         if (key0 + KEYS > n) {
 #pragma unroll
-          for (int i = 0; i < 2 * NK; ++i)
-            if (key0 + (i >> 1) * 8 + cq + (i & 1) >= n) t[i] = -INFINITY;
+          for (int j = 0; j < 2 * MK; ++j)
+            if (key0 + 8 * j + g >= n) t[j][0] = t[j][1] = -INFINITY;
         }
-        const float m_new = fmaxf(m, quad_max(max_of(t)));
-        const float m_use = m_new == -INFINITY ? 0.f : m_new;      // no score yet: nothing to subtract
-        float w[2 * NK], corr;
-        if (ELEM == 2) {
-          corr = ex2(m - m_use);
-          l *= corr;
+        // ---- running maxima
+        float top[2], wtop[2];
+        bool raise = false;
 #pragma unroll
-          for (int i = 0; i < 2 * NK; ++i) {
-            w[i] = ex2(t[i] - m_use);
-            l += w[i];
+        for (int i = 0; i < 2; ++i) {
+          top[i] = t[0][i];
+          wtop[i] = ELEM == 1 ? t[0][i] + ev[0] : 0.f;
+#pragma unroll
+          for (int j = 1; j < 2 * MK; ++j) {
+            top[i] = fmaxf(top[i], t[j][i]);
+            if (ELEM == 1) wtop[i] = fmaxf(wtop[i], t[j][i] + ev[j]);
           }
-        } else {
-          l *= ex2(m - m_use);
+          raise |= top[i] > m[i] + kLazy || (ELEM == 1 && wtop[i] > mw[i] + kLazy);
+        }
+        if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
-          for (int i = 0; i < 2 * NK; ++i) {
-            l += ex2(t[i] - m_use);
-            t[i] += ev[i];
+          for (int i = 0; i < 2; ++i) {
+            const float m_new = fmaxf(m[i], column_max(top[i]));
+            const float sub = m_new == -INFINITY ? 0.f : m_new;
+            l[i] *= ex2(m[i] - sub);
+            float corr = ex2(m[i] - sub);
+            m[i] = m_new;
+            m_sub[i] = sub;
+            if (ELEM == 1) {
+              const float w_new = fmaxf(mw[i], column_max(wtop[i]));
+              const float wsub = w_new == -INFINITY ? 0.f : w_new;
+              corr = ex2(mw[i] - wsub);
+              mw[i] = w_new;
+              w_sub[i] = wsub - kWeightBits;
+            }
+#pragma unroll
+            for (int mt = 0; mt < MO; ++mt) {
+              oc[mt][i] *= corr;
+              oc[mt][2 + i] *= corr;
+            }
           }
-          const float w_new = fmaxf(mw, quad_max(max_of(t)));
-          const float w_use = w_new == -INFINITY ? 0.f : w_new;
-          corr = ex2(mw - w_use);
-#pragma unroll
-          for (int i = 0; i < 2 * NK; ++i) w[i] = ex2(t[i] - (w_use - kWeightBits));
-          mw = w_new;
         }
-        m = m_new;
-        if (__any_sync(0xffffffffu, corr != 1.f)) {
+        // ---- weights, as B fragments of P^T (head g, two keys to a register)
+        uint32_t pf[PP][2 * MK];
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) oc[nt][i] *= corr;
+        for (int j = 0; j < 2 * MK; ++j) {
+          const float p0 = ex2(t[j][0] - m_sub[0]), p1 = ex2(t[j][1] - m_sub[1]);
+          l[0] += p0;
+          l[1] += p1;
+          uint32_t hi, lo;
+          if (ELEM == 2)
+            split_bf16(p0, p1, hi, lo);
+          else
+            split_f16(ex2(t[j][0] + ev[j] - w_sub[0]), ex2(t[j][1] + ev[j] - w_sub[1]), hi, lo);
+          pf[0][j] = transpose8(hi);
+          if (PP == 2) pf[PP - 1][j] = transpose8(lo);
         }
-        if ((poison >> get) & 1u) l = __uint_as_float(0x7fc00000u);      // a row outside the pool: the request is NaN
-        // ---- O += P V: the high parts are row r0, the low parts row r0 + 8
+        if ((poison >> get) & 1u) l[0] = l[1] = __uint_as_float(0x7fc00000u);   // a row outside the pool: the request is NaN
+        // ---- O^T += V^T P^T
 #pragma unroll
-        for (int kk = 0; kk < KEYS / 16; ++kk) {
-          uint32_t pf[4];
+        for (int kk = 0; kk < MK; ++kk) {
           if (ELEM == 2) {
-            split_bf16(w[4 * kk], w[4 * kk + 1], pf[0], pf[1]);
-            split_bf16(w[4 * kk + 2], w[4 * kk + 3], pf[2], pf[3]);
-            const int row = kk * 16 + ((lane >> 3) & 1) * 8 + (lane & 7);
+            const int row = kk * 16 + (lane & 7) + (lane >> 4) * 8;
 #pragma unroll
-            for (int nt = 0; nt < NT; nt += 2) {
-              uint32_t b[4];
-              ldsm4_trans(v_s + chunk_at<D, ELEM>(row, nt + (lane >> 4)), b);
-              mma_bf16(oc[nt], pf, b[0], b[1]);
-              mma_bf16(oc[nt + 1], pf, b[2], b[3]);
+            for (int mt = 0; mt < MO; ++mt) {
+              uint32_t a[4];
+              ldsm4_trans(v_s + chunk_at<D, ELEM>(row, mt * 2 + ((lane >> 3) & 1)), a);
+#pragma unroll
+              for (int h = 0; h < PP; ++h) mma_bf16(oc[mt], a, pf[h][2 * kk], pf[h][2 * kk + 1]);
             }
           } else {
-            split_f16(w[4 * kk], w[4 * kk + 1], pf[0], pf[1]);
-            split_f16(w[4 * kk + 2], w[4 * kk + 3], pf[2], pf[3]);
-            // column r0 of n-tile nt is dim r0 * NT + nt: the lane reads NT consecutive codes of its four keys
+            // rows g and g + 8 of tile mt are dims g NT + 2 mt and + 1: the lane reads NT consecutive codes of four keys
             uint32_t v[4][NT / 4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int row = kk * 16 + cq + (i & 1) + (i >> 1) * 8;
               if (NT == 16) {
-                const uint4 x = lds16(v_s + chunk_at<D, ELEM>(row, r0));
+                const uint4 x = lds16(v_s + chunk_at<D, ELEM>(row, g));
                 v[i][0] = x.x; v[i][1] = x.y; v[i][NT / 4 - 2] = x.z; v[i][NT / 4 - 1] = x.w;
               } else {
-                const uint2 x = lds8(v_s + chunk_at<D, ELEM>(row, r0 >> 1) + (r0 & 1) * 8);
+                const uint2 x = lds8(v_s + chunk_at<D, ELEM>(row, g >> 1) + (g & 1) * 8);
                 v[i][0] = x.x; v[i][1] = x.y;
               }
             }
 #pragma unroll
             for (int j = 0; j < NT / 4; ++j) {
+              // bytes (key, key + 1) of dims 4 j, 4 j + 1 and of 4 j + 2, 4 j + 3
               const uint32_t a0 = __byte_perm(v[0][j], v[1][j], 0x5140), a1 = __byte_perm(v[0][j], v[1][j], 0x7362);
               const uint32_t b0 = __byte_perm(v[2][j], v[3][j], 0x5140), b1 = __byte_perm(v[2][j], v[3][j], 0x7362);
-              mma_f16(oc[4 * j], pf, half2_of_e4m3(a0), half2_of_e4m3(b0));
-              mma_f16(oc[4 * j + 1], pf, half2_of_e4m3(a0 >> 16), half2_of_e4m3(b0 >> 16));
-              mma_f16(oc[4 * j + 2], pf, half2_of_e4m3(a1), half2_of_e4m3(b1));
-              mma_f16(oc[4 * j + 3], pf, half2_of_e4m3(a1 >> 16), half2_of_e4m3(b1 >> 16));
+              const uint32_t x[4] = {half2_of_e4m3(a0), half2_of_e4m3(a0 >> 16), half2_of_e4m3(b0), half2_of_e4m3(b0 >> 16)};
+              const uint32_t y[4] = {half2_of_e4m3(a1), half2_of_e4m3(a1 >> 16), half2_of_e4m3(b1), half2_of_e4m3(b1 >> 16)};
+#pragma unroll
+              for (int h = 0; h < PP; ++h) {
+                mma_f16(oc[2 * j], x, pf[h][2 * kk], pf[h][2 * kk + 1]);
+                mma_f16(oc[2 * j + 1], y, pf[h][2 * kk], pf[h][2 * kk + 1]);
+              }
             }
           }
         }
@@ -569,30 +615,31 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
     }
     todo -= steps;
 
-    // ---- the request's share: row sums over the quad, high and low rows together, fp16 weights back to 2^(t - m)
-    l += __shfl_xor_sync(0xffffffffu, l, 1);
-    l += __shfl_xor_sync(0xffffffffu, l, 2);
-    const float back = ELEM == 1 && mw != -INFINITY ? ex2(mw - m - kWeightBits) : 1.f;
-    float ov[NT][2];
+    // ---- the request's share: sums over the lanes of a column, fp16 weights back to 2^(t - m)
+    float f[2];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      ov[nt][0] = (oc[nt][0] + oc[nt][2]) * back;
-      ov[nt][1] = (oc[nt][1] + oc[nt][3]) * back;
+    for (int i = 0; i < 2; ++i) {
+      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 4);
+      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 8);
+      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 16);
+      f[i] = ELEM == 1 && mw[i] != -INFINITY ? ex2(mw[i] - m[i] - kWeightBits) : 1.f;
     }
     const bool whole = s_tile == 0 && steps == max(1, (n + TILE - 1) / TILE);
     const long long rec_slot = s_tile == 0 ? 1 : 0;      // a range can begin and end inside a request: two records
-
     auto finish = [&]() {
-      if (r0 >= nh) return;
-      const int h = head0 + r0;
-      if (whole) {
-        store_head<D, ELEM>(static_cast<T *>(p.out) + req * p.out_stride + (long long)h * D, ov, cq, n == 0 ? 0.f : 1.f / l);
-        if (p.lse != nullptr && (lane & 3) == 0)
-          p.lse[(long long)req * p.n_q_heads + h] = n == 0 ? -INFINITY : (m + log2f(l)) * (1.f / kLog2e);
-      } else {
-        const long long rec = ((long long)h * p.parts + part) * 2 + rec_slot;
-        store_head<D, ELEM>(p.o + rec * D, ov, cq, 1.f);
-        if ((lane & 3) == 0) p.ml[rec] = make_float2(m, l);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (cq + i >= nh) break;
+        const int h = head0 + cq + i;
+        if (whole) {
+          store_head<D, ELEM>(static_cast<T *>(p.out) + req * p.out_stride + (long long)h * D, oc, i, g, n == 0 ? 0.f : f[i] / l[i]);
+          if (p.lse != nullptr && g == 0)
+            p.lse[(long long)req * p.n_q_heads + h] = n == 0 ? -INFINITY : (m[i] + log2f(l[i])) * (1.f / kLog2e);
+        } else {
+          const long long rec = ((long long)h * p.parts + part) * 2 + rec_slot;
+          store_head<D, ELEM>(p.o + rec * D, oc, i, g, f[i]);
+          if (g == 0) p.ml[rec] = make_float2(m[i], l[i]);
+        }
       }
     };
     if (KW == 1) {
@@ -602,38 +649,45 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
       // (ml_s takes turns: warp 0 may still read it while the others write the next request's.)
       float4 *buf = reinterpret_cast<float4 *>(ba_smem + kBaWarps * C::ring);
       float2(*ml)[kBaHeads] = ml_s[seg & 1];
-      if ((lane & 3) == 0) ml[warp][r0] = make_float2(m, l);
+      if (g == 0) {
+        ml[warp][cq] = make_float2(m[0], l[0]);
+        ml[warp][cq + 1] = make_float2(m[1], l[1]);
+      }
       __syncthreads();
-      float all = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < kBaWarps; ++w) all = fmaxf(all, ml[w][r0].x);
-      const float f = m == -INFINITY ? 0.f : ex2(m - all);
+      for (int i = 0; i < 2; ++i) {
+        float all = -INFINITY;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        ov[nt][0] *= f;
-        ov[nt][1] *= f;
+        for (int w = 0; w < kBaWarps; ++w) all = fmaxf(all, ml[w][cq + i].x);
+        f[i] = m[i] == -INFINITY ? 0.f : f[i] * ex2(m[i] - all);
+        l[i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kBaWarps; ++w) {
+          const float2 x = ml[w][cq + i];
+          l[i] += x.x == -INFINITY ? x.y : x.y * ex2(x.x - all);
+        }
+        m[i] = all;
+#pragma unroll
+        for (int mt = 0; mt < MO; ++mt) {
+          oc[mt][i] *= f[i];
+          oc[mt][2 + i] *= f[i];
+        }
+        f[i] = 1.f;
       }
       if (warp > 0) {
 #pragma unroll
-        for (int k = 0; k < NT / 2; ++k)
-          buf[((warp - 1) * (NT / 2) + k) * 32 + lane] = make_float4(ov[2 * k][0], ov[2 * k][1], ov[2 * k + 1][0], ov[2 * k + 1][1]);
+        for (int mt = 0; mt < MO; ++mt)
+          buf[((warp - 1) * MO + mt) * 32 + lane] = make_float4(oc[mt][0], oc[mt][1], oc[mt][2], oc[mt][3]);
       }
       __syncthreads();
       if (warp == 0) {
 #pragma unroll
         for (int w = 0; w < kBaWarps - 1; ++w)
 #pragma unroll
-          for (int k = 0; k < NT / 2; ++k) {
-            const float4 x = buf[(w * (NT / 2) + k) * 32 + lane];
-            ov[2 * k][0] += x.x; ov[2 * k][1] += x.y; ov[2 * k + 1][0] += x.z; ov[2 * k + 1][1] += x.w;
+          for (int mt = 0; mt < MO; ++mt) {
+            const float4 x = buf[(w * MO + mt) * 32 + lane];
+            oc[mt][0] += x.x; oc[mt][1] += x.y; oc[mt][2] += x.z; oc[mt][3] += x.w;
           }
-        l = 0.f;
-#pragma unroll
-        for (int w = 0; w < kBaWarps; ++w) {
-          const float2 x = ml[w][r0];
-          l += x.x == -INFINITY ? x.y : x.y * ex2(x.x - all);
-        }
-        m = all;
         finish();
       }
       ++seg;
