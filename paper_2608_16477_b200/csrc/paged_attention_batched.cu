@@ -41,6 +41,8 @@ constexpr int kBaWarps = 4;
 constexpr int kBaThreads = kBaWarps * 32;
 constexpr int kBaHeads = 8;          // query heads of a pass
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kLookAhead = 3;        // stages between looking a page up and copying its rows
+constexpr int kNoRow = (int)0x80000000;
 constexpr float kLazy = 8.f;         // a running maximum may be passed by 2^8 before it is replaced
 constexpr float kWeightBits = 7.f;   // fp16 weights: 2^7 at the running maximum, so at most 2^15
 constexpr int kQueryBits = 12;       // ... and fp16 queries to less than 2^12
@@ -155,23 +157,37 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
   return r;
 }
-__device__ __forceinline__ float2 load2(const float *q) { return *reinterpret_cast<const float2 *>(q); }
-__device__ __forceinline__ float2 load2(const bf16 *q) {
-  return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(q));
-}
-__device__ __forceinline__ void load8(const float *q, float *x) {
-  const float4 a = reinterpret_cast<const float4 *>(q)[0], b = reinterpret_cast<const float4 *>(q)[1];
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
-__device__ __forceinline__ void load8(const bf16 *q, float *x) {
-  const uint4 r = *reinterpret_cast<const uint4 *>(q);
-  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+// The D / 4 values of a query head that a lane (c = lane % 4) turns into fragments, as they were loaded.  Pair i of
+// ELEM 2 is dims 8 i + 2 c, + 1; of ELEM 1 dims c D / 4 + 2 i, + 1.
+template <int D, int ELEM, typename T>
+struct RawQuery {
+  static constexpr int W = sizeof(T) / 2;            // 32-bit words of a pair
+  uint32_t w[D / 8 * W];
+  __device__ __forceinline__ void load(const T *q, int c) {
+    if (ELEM == 1) {
+      const uint4 *src = reinterpret_cast<const uint4 *>(q + c * (D / 4));
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      for (int i = 0; i < D / 8 * W / 4; ++i) {
+        const uint4 x = src[i];
+        w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) {
+        if (W == 1) {
+          w[i] = *reinterpret_cast<const uint32_t *>(q + 8 * i + 2 * c);
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2 *>(q + 8 * i + 2 * c);
+          w[W * i] = x.x; w[W * i + W - 1] = x.y;
+        }
+      }
+    }
   }
-}
+  __device__ __forceinline__ float2 pair(int i) const {
+    if (W == 1) return make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+    return make_float2(__uint_as_float(w[W * i]), __uint_as_float(w[W * i + W - 1]));
+  }
+};
 __device__ __forceinline__ void store4(float *p, float a, float b, float c, float d) {
   *reinterpret_cast<float4 *>(p) = make_float4(a, b, c, d);
 }
@@ -321,19 +337,27 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
 
   asm volatile("griddepcontrol.launch_dependents;");      // the joining kernel may be put in place
 
-  // ---- loads.  Lane l looks up the page of row l % KEYS of the stage to come, one stage ahead of its copies.
+  // ---- loads.  Lane l looks up the page of row l % KEYS of a stage, kLookAhead stages before its copies are issued: a
+  // table entry can be a microsecond away.
   Cursor prod = cons;
-  long long to_load = todo;
-  int blk = -1, off = 0;                     // row of the stage that `prod` stands at: block (-1: none), slot
+  long long to_look = todo;
+  int blks[kLookAhead], offs[kLookAhead];    // of the next stages to be copied: block of the lane's row (-1: none), slot
   const int my_row = lane % KEYS;
-  auto look_up = [&]() {
+  auto look_up = [&](int &blk, int &off) {
     const int pos = (prod.tile * KW + kg) * KEYS + my_row;
     blk = -1;
-    if (to_load > 0 && pos < prod.n) {
-      const int b = p.block_shift >= 0 ? pos >> p.block_shift : pos / p.cache.block_size;
-      off = pos - b * p.cache.block_size;
-      blk = __ldg(p.tables + prod.r * p.table_stride + b);
-      if ((unsigned)blk >= (unsigned)p.num_blocks) blk = -2;      // not in the pool: never followed
+    off = 0;
+    if (to_look > 0) {
+      if (pos < prod.n) {
+        const int b = p.block_shift >= 0 ? pos >> p.block_shift : pos / p.cache.block_size;
+        off = pos - b * p.cache.block_size;
+        blk = __ldg(p.tables + prod.r * p.table_stride + b);
+      }
+      off |= pos < prod.n ? 0 : kNoRow;
+      --to_look;
+      prod.step(p, TILE);
+    } else {
+      off = kNoRow;
     }
   };
   const long long row_stride = (long long)p.cache.n_kv_heads * C::row;
@@ -343,8 +367,11 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
   unsigned poison = 0;                       // bit s: the stage in ring slot s has a row outside the pool
   int put = 0;                               // ring slot to fill next
   auto issue = [&]() {
-    const bool any = __any_sync(0xffffffffu, blk != -1);
-    const bool bad = __any_sync(0xffffffffu, blk == -2);
+    const bool row_is = offs[0] >= 0;                                            // the lane's row is one of the context
+    const int blk = row_is && (unsigned)blks[0] < (unsigned)p.num_blocks ? blks[0] : -1;      // -1: never followed
+    const int off = row_is ? offs[0] : 0;
+    const bool any = __any_sync(0xffffffffu, row_is);
+    const bool bad = __any_sync(0xffffffffu, row_is && blk < 0);
     poison = (poison & ~(1u << put)) | ((unsigned)bad << put);
     if (any) {
       const uint32_t k_s = ring + put * C::stage, v_s = k_s + C::tile;
@@ -387,18 +414,25 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
     }
     cp_commit();
     put = put + 1 == C::stages ? 0 : put + 1;
-    if (to_load > 0) {
-      --to_load;
-      prod.step(p, TILE);
+#pragma unroll
+    for (int i = 0; i + 1 < kLookAhead; ++i) {
+      blks[i] = blks[i + 1];
+      offs[i] = offs[i + 1];
     }
-    look_up();
+    look_up(blks[kLookAhead - 1], offs[kLookAhead - 1]);
   };
-  look_up();
+#pragma unroll
+  for (int i = 0; i < kLookAhead; ++i) look_up(blks[i], offs[i]);
+  const int g = lane >> 2, c = lane & 3, cq = c * 2;   // the lane's query fragments are of head g, its results of cq, cq + 1
+  RawQuery<D, ELEM, T> raw;
+  auto load_query = [&](int req) {
+    raw.load(static_cast<const T *>(p.q) + req * p.q_stride + (long long)(head0 + min(g, nh - 1)) * D, c);
+  };
+  load_query(cons.r);
 #pragma unroll
   for (int i = 0; i < C::stages - 1; ++i) issue();
 
   // ---- per request of the range
-  const int g = lane >> 2, c = lane & 3, cq = c * 2;   // the lane's query fragments are of head g, its results of cq, cq + 1
   int get = 0, seg = 0;
   while (todo > 0) {
     const int req = cons.r, n = cons.n, s_tile = cons.tile;
@@ -406,14 +440,13 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
     uint32_t qf[QP][KS][2];
     float q_scale[2] = {p.scale, p.scale};
     {
-      const T *q = static_cast<const T *>(p.q) + req * p.q_stride + (long long)(head0 + min(g, nh - 1)) * D;
       const float on = g < nh ? 1.f : 0.f;
       if (ELEM == 2) {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const float2 a = load2(q + ks * 16 + cq + 8 * j);
+            const float2 a = raw.pair(2 * ks + j);
             uint32_t lo;
             split_bf16(a.x * on, a.y * on, qf[0][ks][j], lo);      // a bf16 query is its own first half
             if (QP == 2) qf[QP - 1][ks][j] = lo;
@@ -423,11 +456,11 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
         // the lane's dims: 4 KS consecutive ones, so that a key's codes are read as 16-byte vectors
         float x[4 * KS], most = 0.f;
 #pragma unroll
-        for (int i = 0; i < KS / 2; ++i) load8(q + c * (4 * KS) + 8 * i, x + 8 * i);
-#pragma unroll
-        for (int i = 0; i < 4 * KS; ++i) {
-          x[i] *= on;
-          most = fmaxf(most, fabsf(x[i]));
+        for (int i = 0; i < 2 * KS; ++i) {
+          const float2 a = raw.pair(i);
+          x[2 * i] = a.x * on;
+          x[2 * i + 1] = a.y * on;
+          most = fmaxf(most, fmaxf(fabsf(x[2 * i]), fabsf(x[2 * i + 1])));
         }
         most = quad_max(most);
         const int e = min(max((int)(__float_as_uint(most) >> 23) - 126, -100), 127);       // most < 2^e
@@ -614,6 +647,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
       cons.step(p, TILE);
     }
     todo -= steps;
+    if (todo > 0) load_query(cons.r);        // on its way while this one is finished
 
     // ---- the request's share: sums over the lanes of a column, fp16 weights back to 2^(t - m)
     float f[2];
@@ -696,15 +730,29 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
   cp_wait_group<0>();
 }
 
-// Joins the records of one (request, query head) per warp: the parts that hold its tiles follow from the starts.  Placed
-// while the first kernel still runs (programmatic launch); everything that kernel wrote is read behind the wait, past L1.
-constexpr int kJoinWarps = 8;
-template <int D, typename T>
-__global__ void __launch_bounds__(kJoinWarps * 32) paged_attention_join_kernel(const __grid_constant__ BaParams p) {
-  constexpr int V = D / 128 > 0 ? 4 : 2;           // values of a lane
+// Joins the records of a (request, query head): the parts that hold its tiles follow from the starts.  Placed while the
+// first kernel still runs (programmatic launch); everything that kernel wrote is read behind the wait, past L1.
+// A chain of loads from L2 is all this costs, so a warp has the (m, l) and the outputs of kJoinBatch records in flight at
+// once, and where there are few requests (with many records each) four warps share a head.
+constexpr int kJoinThreads = 128;
+constexpr int kJoinBatch = 10;
+__device__ __forceinline__ void load_past_l1(const float *p, float (&v)[4]) {
+  const float4 x = __ldcg(reinterpret_cast<const float4 *>(p));
+  v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+}
+__device__ __forceinline__ void load_past_l1(const float *p, float (&v)[2]) {
+  const float2 x = __ldcg(reinterpret_cast<const float2 *>(p));
+  v[0] = x.x; v[1] = x.y;
+}
+template <int D, typename T, int WPH>      // WPH: warps per head
+__global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(const __grid_constant__ BaParams p) {
+  constexpr int V = D / 32;                // values of a lane
+  constexpr int HEADS = kJoinThreads / 32 / WPH;
+  __shared__ float m_s[WPH], l_s[WPH], o_s[WPH][WPH > 1 ? D : 1];
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int lane = threadIdx.x & 31, req = blockIdx.x, h = blockIdx.y * kJoinWarps + (threadIdx.x >> 5);
-  if (h >= p.n_q_heads) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part_of = warp % WPH;
+  const int req = blockIdx.x, h = blockIdx.y * HEADS + warp / WPH;
+  if (h >= p.n_q_heads) return;            // WPH > 1: one head per block, so the block leaves together
   const long long total = __ldcg(p.tile_start + p.n_req);
   const long long t0 = __ldcg(p.tile_start + req), t1 = __ldcg(p.tile_start + req + 1);
   const long long ranges = min((long long)p.parts, total);
@@ -716,36 +764,64 @@ __global__ void __launch_bounds__(kJoinWarps * 32) paged_attention_join_kernel(c
     first = (int)(((t0 + 1) * ranges - 1) / total);
     last = (int)((t1 * ranges - 1) / total);
   }
-  if (first == last) return;                       // one part held it all and wrote the output
+  if (first == last) return;               // one part held it all and wrote the output
   const long long rec0 = (long long)h * p.parts * 2;
-  float m = -INFINITY;
-  for (int q = first + lane; q <= last; q += 32) m = fmaxf(m, __ldcg(p.ml + rec0 + 2 * q + (q == first)).x);
+  float m = -INFINITY, l = 0.f, acc[V] = {};
+  for (int q0 = first + part_of; q0 <= last; q0 += kJoinBatch * WPH) {
+    float2 ml[kJoinBatch];
+    float v[kJoinBatch][V];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  float l = 0.f, acc[V] = {};
-  for (int q0 = first; q0 <= last; q0 += 32) {
-    const int q = q0 + lane, count = min(32, last - q0 + 1);
-    float f = 0.f;
-    if (q <= last) {
-      const float2 x = __ldcg(p.ml + rec0 + 2 * q + (q == first));
-      f = x.x == -INFINITY ? 0.f : ex2(x.x - m);
-      l += x.x == -INFINITY ? x.y : x.y * f;
-    }
-#pragma unroll 8
-    for (int j = 0; j < count; ++j) {
-      const float fj = __shfl_sync(0xffffffffu, f, j);
-      const float *src = p.o + (rec0 + 2 * (q0 + j) + (q0 + j == first)) * D + lane * V;
-      if (V == 4) {
-        const float4 v = __ldcg(reinterpret_cast<const float4 *>(src));
-        acc[0] += fj * v.x; acc[1] += fj * v.y; acc[V - 2] += fj * v.z; acc[V - 1] += fj * v.w;
+    for (int b = 0; b < kJoinBatch; ++b) {
+      const int q = q0 + b * WPH;
+      if (q <= last) {
+        ml[b] = __ldcg(p.ml + rec0 + 2 * q + (q == first));
+        load_past_l1(p.o + (rec0 + 2 * q + (q == first)) * D + lane * V, v[b]);
       } else {
-        const float2 v = __ldcg(reinterpret_cast<const float2 *>(src));
-        acc[0] += fj * v.x; acc[1] += fj * v.y;
+        ml[b] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[b][i] = 0.f;
       }
     }
-  }
+    float top = m;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    for (int b = 0; b < kJoinBatch; ++b) top = fmaxf(top, ml[b].x);
+    const float old = m == -INFINITY ? 0.f : ex2(m - top);
+    l *= m == -INFINITY ? 1.f : old;       // without a maximum l is 0, or NaN to keep
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] *= old;
+#pragma unroll
+    for (int b = 0; b < kJoinBatch; ++b) {
+      const float f = ml[b].x == -INFINITY ? 0.f : ex2(ml[b].x - top);
+      l += ml[b].x == -INFINITY ? ml[b].y : ml[b].y * f;
+#pragma unroll
+      for (int i = 0; i < V; ++i) acc[i] += f * v[b][i];
+    }
+    m = top;
+  }
+  if (WPH > 1) {
+    if (lane == 0) {
+      m_s[part_of] = m;
+      l_s[part_of] = l;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) o_s[part_of][lane * V + i] = acc[i];
+    __syncthreads();
+    if (part_of > 0) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < WPH; ++w) top = fmaxf(top, m_s[w]);
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] = 0.f;
+#pragma unroll
+    for (int w = 0; w < WPH; ++w) {
+      const float f = m_s[w] == -INFINITY ? 0.f : ex2(m_s[w] - top);
+      l += m_s[w] == -INFINITY ? l_s[w] : l_s[w] * f;
+#pragma unroll
+      for (int i = 0; i < V; ++i) acc[i] += f * o_s[w][lane * V + i];
+    }
+    m = top;
+  }
   T *out = static_cast<T *>(p.out) + req * p.out_stride + (long long)h * D + lane * V;
   const float inv = 1.f / l;
   if (V == 4)
@@ -809,16 +885,19 @@ int ba_launch(const BaParams &p, const BaPlan &b, int device, cudaStream_t st) {
   KV_COUNT_LAUNCH();
   KV_CUDA(cudaGetLastError());
   if (b.parts == 0) return KV_OK;
+  // four warps per head while every block of such a grid can be resident at once
+  const int wph = (long long)p.n_req * p.n_q_heads <= 8ll * sm_count(device) ? 4 : 1, heads = kJoinThreads / 32 / wph;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.n_req, (p.n_q_heads + kJoinWarps - 1) / kJoinWarps);
-  cfg.blockDim = dim3(kJoinWarps * 32);
+  cfg.gridDim = dim3(p.n_req, (p.n_q_heads + heads - 1) / heads);
+  cfg.blockDim = dim3(kJoinThreads);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  KV_CUDA(cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<D, T>, p));
+  KV_CUDA(wph == 4 ? cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<D, T, 4>, p)
+                   : cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<D, T, 1>, p));
   KV_COUNT_LAUNCH();
   return KV_OK;
 }
