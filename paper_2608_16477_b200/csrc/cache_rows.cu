@@ -7,8 +7,8 @@
 // is exact.
 //
 // HBM-bound: every value is read once and written once.  head_dim / 8 lanes own a row (8 values each), the row maximum
-// is a shuffle over them; consecutive lanes move consecutive 16-byte (bf16) or 8-byte (codes) pieces.  A thread walks
-// rows that are a whole grid apart, two at a time, so that both rows' loads are in flight together.
+// is a shuffle over them; consecutive lanes move consecutive 16-byte (bf16) or 8-byte (codes) pieces.  Once there are rows
+// enough, a thread takes four of them and has their slots, then all their loads, in flight together.
 #include <float.h>
 
 #include "common.cuh"
@@ -23,7 +23,7 @@ constexpr long long kSlots32 = 0x7fffffffll;
 
 struct RowsParams {
   CacheView cache;
-  int layer, n_tokens, num_blocks, block_shift;   // block_shift: log2(block_size), -1 if it is no power of two
+  int layer, block_shift, token_shift;            // log2 of block_size and of 2 * n_kv_heads, -1 if no power of two
   long long n_slots;
   const long long *slots;
   char *k, *v;                                    // rows
@@ -31,37 +31,42 @@ struct RowsParams {
   long long n_rows;                               // n_tokens * 2 * n_kv_heads
 };
 
+// Row r of the call: token, K or V, KV head; its strided side; and, from the token's slot, its page.
 struct RowAt {
-  char *row;          // the strided side
-  char *page;         // the cache side; nullptr: the slot is outside the pool
-  int head, offset;   // KV head, slot inside the page
-};
-
-__device__ __forceinline__ RowAt locate(const RowsParams &p, long long r) {
-  const int per = 2 * p.cache.n_kv_heads;
-  const int t = p.n_rows <= 0xffffffffll ? (int)((uint32_t)r / (uint32_t)per) : (int)(r / per);
-  const int rem = (int)(r - (long long)t * per);
-  const int kv = rem >= p.cache.n_kv_heads, h = rem - kv * p.cache.n_kv_heads;
-  const long long slot = __ldg(p.slots + t);
-  RowAt a;
-  a.row = kv ? p.v + t * p.v_ts + h * p.v_hs : p.k + t * p.k_ts + h * p.k_hs;
-  a.head = h;
-  if (slot < 0 || slot >= p.n_slots) {
-    a.page = nullptr;
-    a.offset = 0;
-    return a;
+  char *row, *page;
+  int token, kv, head, offset;   // offset: slot inside the page
+  bool live;                     // the slot lies inside the pool
+  __device__ __forceinline__ void find(const RowsParams &p, long long r) {
+    const int per = 2 * p.cache.n_kv_heads;
+    if (p.token_shift >= 0)
+      token = (int)(r >> p.token_shift);
+    else
+      token = p.n_rows <= 0xffffffffll ? (int)((uint32_t)r / (uint32_t)per) : (int)(r / per);
+    const int rem = (int)(r - (long long)token * per);
+    kv = rem >= p.cache.n_kv_heads;
+    head = rem - kv * p.cache.n_kv_heads;
+    row = kv ? p.v + token * p.v_ts + head * p.v_hs : p.k + token * p.k_ts + head * p.k_hs;
   }
-  long long block;
-  if (p.block_shift >= 0)
-    block = slot >> p.block_shift;
-  else if (p.n_slots <= kSlots32)
-    block = (uint32_t)slot / (uint32_t)p.cache.block_size;
-  else
-    block = slot / p.cache.block_size;
-  a.offset = (int)(slot - block * p.cache.block_size);
-  a.page = p.cache.page(p.layer, kv, (int)block);
-  return a;
-}
+  __device__ __forceinline__ void place(const RowsParams &p, long long slot) {
+    live = slot >= 0 && slot < p.n_slots;
+    if (!live) slot = 0;
+    long long block;
+    if (p.block_shift >= 0)
+      block = slot >> p.block_shift;
+    else if (p.n_slots <= kSlots32)
+      block = (uint32_t)slot / (uint32_t)p.cache.block_size;
+    else
+      block = slot / p.cache.block_size;
+    offset = (int)(slot - block * p.cache.block_size);
+    page = p.cache.page(p.layer, kv, (int)block);
+  }
+  __device__ __forceinline__ char *values(const RowsParams &p, int bytes) const {
+    return page + ((long long)offset * p.cache.n_kv_heads + head) * bytes;
+  }
+  __device__ __forceinline__ char *scale(const RowsParams &p) const {
+    return page + p.cache.value_bytes() + head * p.cache.block_size + offset;
+  }
+};
 
 // 8 values of a row as floats; the raw registers are loaded first and unpacked later
 template <typename T>
@@ -120,137 +125,127 @@ __device__ __forceinline__ float2 from_e4m3x2(uint16_t c) {
   return f;
 }
 
-template <typename T, int D, bool E4M3>
-__global__ void __launch_bounds__(kRowThreads) cache_write_kernel(const RowsParams p) {
+template <typename T, int D, bool E4M3, int U>      // U: rows of a thread
+__global__ void __launch_bounds__(kRowThreads) cache_write_kernel(const __grid_constant__ RowsParams p) {
   constexpr int LPR = D / 8;                 // lanes of a row
-  constexpr int RPC = kRowThreads / LPR;     // rows of a CTA
+  constexpr int RPC = kRowThreads / LPR;     // rows of a CTA at a time
   const int sub = threadIdx.x % LPR;
-  const long long stride = (long long)gridDim.x * RPC;
-  // every lane of a warp stays in the loop while one of its rows is left: the maximum is a full-warp shuffle
-  const long long first = (long long)blockIdx.x * RPC + threadIdx.x / LPR;
-  const long long warp_first = (long long)blockIdx.x * RPC + (threadIdx.x & ~31) / LPR;
-  for (long long base = 0; warp_first + base < p.n_rows; base += 2 * stride) {
-    RowAt at[2];
-    Raw8<T> raw[2];
-    bool live[2];
+  const long long r0 = (long long)blockIdx.x * RPC * U + threadIdx.x / LPR;
+  RowAt at[U];
+  Raw8<T> raw[U];
+  long long slot[U];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const long long r = first + base + i * stride;
-      live[i] = r < p.n_rows;
-      if (live[i]) {
-        at[i] = locate(p, r);
-        live[i] = at[i].page != nullptr;
+  for (int i = 0; i < U; ++i) {
+    const long long r = r0 + i * RPC;
+    at[i].find(p, r < p.n_rows ? r : p.n_rows - 1);           // every lane stays for the shuffles
+    slot[i] = r < p.n_rows ? __ldg(p.slots + at[i].token) : -1;
+    raw[i].load(at[i].row + sub * 8 * (int)sizeof(T));
+  }
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    float f[8];
+    raw[i].unpack(f);
+    at[i].place(p, slot[i]);
+    if (E4M3) {
+      float most = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float a = fabsf(f[j]);
+        most = fmaxf(most, a <= FLT_MAX ? a : 0.f);           // infinities and NaN do not set the scale
       }
-      if (live[i]) raw[i].load(at[i].row + sub * 8 * (int)sizeof(T));
-    }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      float f[8];
-      if (live[i])
-        raw[i].unpack(f);
-      else
+      for (int o = LPR / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+      // most = m * 2^x with 1 <= m < 2; 448 = 1.75 * 2^8, so e = x - 8, one more if m > 1.75
+      const uint32_t bits = __float_as_uint(most);
+      int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u);
+      e = min(max(e, kMinExp), kMaxExp);
+      const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = 0.f;
-      if (E4M3) {
-        float most = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float a = fabsf(f[j]);
-          most = fmaxf(most, a <= FLT_MAX ? a : 0.f);      // infinities and NaN do not set the scale
-        }
-#pragma unroll
-        for (int o = LPR / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-        // most = m * 2^x with 1 <= m < 2; 448 = 1.75 * 2^8, so e = x - 8, one more if m > 1.75
-        const uint32_t bits = __float_as_uint(most);
-        int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u);
-        e = min(max(e, kMinExp), kMaxExp);
-        const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = fabsf(f[j]) <= FLT_MAX ? f[j] * inv : __uint_as_float(0x7fc00000u);
-        if (live[i]) {
-          uint2 c;
-          c.x = e4m3x2(f[0], f[1]) | (e4m3x2(f[2], f[3]) << 16);
-          c.y = e4m3x2(f[4], f[5]) | (e4m3x2(f[6], f[7]) << 16);
-          char *row = at[i].page + ((long long)at[i].offset * p.cache.n_kv_heads + at[i].head) * D;
-          *reinterpret_cast<uint2 *>(row + sub * 8) = c;
-          if (sub == 0)
-            at[i].page[p.cache.value_bytes() + at[i].head * p.cache.block_size + at[i].offset] = (char)(e + 127);
-        }
-      } else if (live[i]) {
-        char *row = at[i].page + ((long long)at[i].offset * p.cache.n_kv_heads + at[i].head) * D * 2;
-        *reinterpret_cast<uint4 *>(row + sub * 16) = pack_bf16(f);
+      for (int j = 0; j < 8; ++j) f[j] = fabsf(f[j]) <= FLT_MAX ? f[j] * inv : __uint_as_float(0x7fc00000u);
+      if (at[i].live) {
+        uint2 c;
+        c.x = e4m3x2(f[0], f[1]) | (e4m3x2(f[2], f[3]) << 16);
+        c.y = e4m3x2(f[4], f[5]) | (e4m3x2(f[6], f[7]) << 16);
+        *reinterpret_cast<uint2 *>(at[i].values(p, D) + sub * 8) = c;
+        if (sub == 0) *at[i].scale(p) = (char)(e + 127);
       }
+    } else if (at[i].live) {
+      *reinterpret_cast<uint4 *>(at[i].values(p, 2 * D) + sub * 16) = pack_bf16(f);
     }
   }
 }
 
-template <typename T, int D, bool E4M3>
-__global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const RowsParams p) {
+template <typename T, int D, bool E4M3, int U>
+__global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_constant__ RowsParams p) {
   constexpr int LPR = D / 8, RPC = kRowThreads / LPR;
   const int sub = threadIdx.x % LPR;
-  const long long stride = (long long)gridDim.x * RPC;
-  for (long long r0 = (long long)blockIdx.x * RPC + threadIdx.x / LPR; r0 < p.n_rows; r0 += 2 * stride) {
-    RowAt at[2];
-    uint4 raw[2];
-    uint32_t scale[2];
-    bool live[2];
+  const long long r0 = (long long)blockIdx.x * RPC * U + threadIdx.x / LPR;
+  RowAt at[U];
+  uint4 raw[U];
+  uint32_t scale[U];
+  long long slot[U];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const long long r = r0 + i * stride;
-      live[i] = r < p.n_rows;
-      if (live[i]) {
-        at[i] = locate(p, r);
-        live[i] = at[i].page != nullptr;
-      }
-      if (!live[i]) continue;
-      const long long row = (long long)at[i].offset * p.cache.n_kv_heads + at[i].head;
-      if (E4M3) {
-        const uint2 c = *reinterpret_cast<const uint2 *>(at[i].page + row * D + sub * 8);
-        raw[i].x = c.x;
-        raw[i].y = c.y;
-        scale[i] = *reinterpret_cast<const uint8_t *>(at[i].page + p.cache.value_bytes() +
-                                                      at[i].head * p.cache.block_size + at[i].offset);
-      } else {
-        raw[i] = *reinterpret_cast<const uint4 *>(at[i].page + row * D * 2 + sub * 16);
-      }
+  for (int i = 0; i < U; ++i) {
+    const long long r = r0 + i * RPC;
+    at[i].find(p, r < p.n_rows ? r : p.n_rows - 1);
+    slot[i] = r < p.n_rows ? __ldg(p.slots + at[i].token) : -1;
+  }
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    at[i].place(p, slot[i]);
+    if (E4M3) {
+      const uint2 c = *reinterpret_cast<const uint2 *>(at[i].values(p, D) + sub * 8);      // slot 0 if it is not live
+      raw[i] = make_uint4(c.x, c.y, 0, 0);
+      scale[i] = *reinterpret_cast<const uint8_t *>(at[i].scale(p));
+    } else {
+      raw[i] = *reinterpret_cast<const uint4 *>(at[i].values(p, 2 * D) + sub * 16);
     }
+  }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (!live[i]) continue;
-      float f[8];
-      if (E4M3) {
-        const float s = __uint_as_float(scale[i] << 23);
-        const uint32_t w[2] = {raw[i].x, raw[i].y};
+  for (int i = 0; i < U; ++i) {
+    if (!at[i].live) continue;
+    float f[8];
+    if (E4M3) {
+      const float s = __uint_as_float(scale[i] << 23);
+      const uint32_t w[2] = {raw[i].x, raw[i].y};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2 c = from_e4m3x2((uint16_t)(w[j >> 1] >> ((j & 1) * 16)));
-          f[2 * j] = c.x * s;
-          f[2 * j + 1] = c.y * s;
-        }
-      } else {
-        Raw8<bf16> b;
-        b.a = raw[i];
-        b.unpack(f);
+      for (int j = 0; j < 4; ++j) {
+        const float2 c = from_e4m3x2((uint16_t)(w[j >> 1] >> ((j & 1) * 16)));
+        f[2 * j] = c.x * s;
+        f[2 * j + 1] = c.y * s;
       }
-      store8(at[i].row + sub * 8 * (int)sizeof(T), f, T());
+    } else {
+      Raw8<bf16> b;
+      b.a = raw[i];
+      b.unpack(f);
     }
+    store8(at[i].row + sub * 8 * (int)sizeof(T), f, T());
   }
 }
 
-template <typename T, int D, bool E4M3>
-int launch_rows(const RowsParams &p, bool write, cudaStream_t st) {
-  constexpr int RPC = kRowThreads / (D / 8);
-  const int device = current_device();
-  if (device < 0) return KV_ERR_CUDA;
-  const long long want = (p.n_rows + RPC - 1) / RPC, most = 8ll * sm_count(device);
-  const int grid = (int)(want < most ? want : most);
+template <typename T, int D, bool E4M3, int U>
+int launch_rows_u(const RowsParams &p, bool write, cudaStream_t st) {
+  constexpr long long rows = (long long)kRowThreads / (D / 8) * U;
+  const long long grid = (p.n_rows + rows - 1) / rows;
+  if (grid > 0x7fffffffll) return KV_ERR_SHAPE;
   if (write)
-    cache_write_kernel<T, D, E4M3><<<grid, kRowThreads, 0, st>>>(p);
+    cache_write_kernel<T, D, E4M3, U><<<(unsigned)grid, kRowThreads, 0, st>>>(p);
   else
-    cache_read_kernel<T, D, E4M3><<<grid, kRowThreads, 0, st>>>(p);
+    cache_read_kernel<T, D, E4M3, U><<<(unsigned)grid, kRowThreads, 0, st>>>(p);
   KV_COUNT_LAUNCH();
   KV_CUDA(cudaGetLastError());
   return KV_OK;
+}
+
+// Four rows to a thread once that still gives every SM four CTAs, one below that (few rows: the chain slot -> row -> store
+// is all there is, and more CTAs share it).
+template <typename T, int D, bool E4M3>
+int launch_rows(const RowsParams &p, bool write, cudaStream_t st) {
+  const int device = current_device();
+  if (device < 0) return KV_ERR_CUDA;
+  const long long rows = kRowThreads / (D / 8);
+  return p.n_rows >= 16 * rows * sm_count(device) ? launch_rows_u<T, D, E4M3, 4>(p, write, st)
+                                                  : launch_rows_u<T, D, E4M3, 1>(p, write, st);
 }
 
 // strides are in elements of dtype
@@ -276,12 +271,12 @@ int rows_call(const kv_cache_desc *cache, int layer, const void *k, int64_t k_ts
   RowsParams p;
   p.cache = make_view(cache);
   p.layer = layer;
-  p.n_tokens = n_tokens;
-  p.num_blocks = cache->num_blocks;
   p.n_slots = (long long)cache->num_blocks * cache->block_size;
-  p.block_shift = -1;
-  for (int b = 0; b < 31; ++b)
+  p.block_shift = p.token_shift = -1;
+  for (int b = 0; b < 31; ++b) {
     if ((1 << b) == cache->block_size) p.block_shift = b;
+    if ((1ll << b) == 2ll * cache->n_kv_heads) p.token_shift = b;
+  }
   p.slots = reinterpret_cast<const long long *>(slots);
   p.k = (char *)const_cast<void *>(k);
   p.v = (char *)const_cast<void *>(v);
