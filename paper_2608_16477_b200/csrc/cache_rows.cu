@@ -6,9 +6,12 @@
 // costs only values below 2^-15 of the row's maximum), the two directions need no division, and reading back into bf16
 // is exact.
 //
-// HBM-bound: every value is read once and written once.  head_dim / 8 lanes own a row (8 values each), the row maximum
-// is a shuffle over them; consecutive lanes move consecutive 16-byte (bf16) or 8-byte (codes) pieces.  Once there are rows
-// enough, a thread takes four of them and has their slots, then all their loads, in flight together.
+// HBM-bound: every value is read once and written once; instructions are what has to be saved beside that.  head_dim / 8
+// lanes own a row (8 values each), the row maximum is a shuffle over them; consecutive lanes move consecutive 16-byte (bf16)
+// or 8-byte (codes) pieces.  A thread keeps its place in the token (K or V, head, piece) for all its tokens, so that only
+// the slot's page has to be worked out for each; once there are tokens enough it takes four, with their slots, then all
+// their loads, in flight together.  The maximum runs over the raw bits (an infinity or NaN shows in it, and only then the
+// row is gone through value by value).
 #include <float.h>
 
 #include "common.cuh"
@@ -23,50 +26,53 @@ constexpr long long kSlots32 = 0x7fffffffll;
 
 struct RowsParams {
   CacheView cache;
-  int layer, block_shift, token_shift;            // log2 of block_size and of 2 * n_kv_heads, -1 if no power of two
+  int layer, block_shift;                         // block_shift: log2(block_size), -1 if it is no power of two
+  int n_tokens, heads;                            // heads of K, and of V, that a CTA takes
   long long n_slots;
   const long long *slots;
   char *k, *v;                                    // rows
   long long k_ts, k_hs, v_ts, v_hs;               // strides, bytes
-  long long n_rows;                               // n_tokens * 2 * n_kv_heads
 };
 
-// Row r of the call: token, K or V, KV head; its strided side; and, from the token's slot, its page.
-struct RowAt {
-  char *row, *page;
-  int token, kv, head, offset;   // offset: slot inside the page
-  bool live;                     // the slot lies inside the pool
-  __device__ __forceinline__ void find(const RowsParams &p, long long r) {
-    const int per = 2 * p.cache.n_kv_heads;
-    if (p.token_shift >= 0)
-      token = (int)(r >> p.token_shift);
-    else
-      token = p.n_rows <= 0xffffffffll ? (int)((uint32_t)r / (uint32_t)per) : (int)(r / per);
-    const int rem = (int)(r - (long long)token * per);
-    kv = rem >= p.cache.n_kv_heads;
-    head = rem - kv * p.cache.n_kv_heads;
-    row = kv ? p.v + token * p.v_ts + head * p.v_hs : p.k + token * p.k_ts + head * p.k_hs;
-  }
-  __device__ __forceinline__ void place(const RowsParams &p, long long slot) {
-    live = slot >= 0 && slot < p.n_slots;
-    if (!live) slot = 0;
-    long long block;
-    if (p.block_shift >= 0)
-      block = slot >> p.block_shift;
-    else if (p.n_slots <= kSlots32)
-      block = (uint32_t)slot / (uint32_t)p.cache.block_size;
-    else
-      block = slot / p.cache.block_size;
-    offset = (int)(slot - block * p.cache.block_size);
-    page = p.cache.page(p.layer, kv, (int)block);
-  }
-  __device__ __forceinline__ char *values(const RowsParams &p, int bytes) const {
-    return page + ((long long)offset * p.cache.n_kv_heads + head) * bytes;
-  }
-  __device__ __forceinline__ char *scale(const RowsParams &p) const {
-    return page + p.cache.value_bytes() + head * p.cache.block_size + offset;
+// A thread's place: the piece `sub` of head `head` of K or V, for tokens first, first + step, ...
+template <int D>
+struct Place {
+  static constexpr int LPR = D / 8;               // lanes of a row
+  int sub, first, step;
+  bool idle;
+  unsigned group;                                 // the row's lanes
+  char *row, *values, *scale;                     // of token 0; of slot 0 of block 0
+  long long row_step, slot_bytes;
+  __device__ __forceinline__ Place(const RowsParams &p, int elem, int u, int bytes) {      // bytes: of the piece
+    const int per = 2 * p.heads * LPR, tokens = kRowThreads / per;      // threads of a token, tokens of a CTA at a time
+    const int at = threadIdx.x / per, in = threadIdx.x - at * per;
+    const int line = in / LPR, kv = line >= p.heads, head = blockIdx.y * p.heads + line - kv * p.heads;
+    sub = in % LPR;
+    idle = at >= tokens || head >= p.cache.n_kv_heads;
+    step = tokens;
+    first = blockIdx.x * tokens * u + at;
+    group = (LPR == 32 ? 0xffffffffu : ((1u << LPR) - 1u)) << (threadIdx.x & 31 & ~(LPR - 1));
+    row = (kv ? p.v + head * p.v_hs : p.k + head * p.k_hs) + sub * bytes;
+    row_step = kv ? p.v_ts : p.k_ts;
+    slot_bytes = (long long)p.cache.n_kv_heads * D * elem;
+    char *page = p.cache.page(p.layer, kv, 0);
+    values = page + head * D * elem + sub * 8 * elem;
+    scale = page + p.cache.value_bytes() + head * p.cache.block_size;
   }
 };
+// Block and offset of a slot; false if it lies outside the pool.
+__device__ __forceinline__ bool split_slot(const RowsParams &p, long long slot, int &block, int &offset) {
+  block = offset = 0;
+  if (slot < 0 || slot >= p.n_slots) return false;
+  if (p.block_shift >= 0)
+    block = (int)(slot >> p.block_shift);
+  else if (p.n_slots <= kSlots32)
+    block = (int)((uint32_t)slot / (uint32_t)p.cache.block_size);
+  else
+    block = (int)(slot / p.cache.block_size);
+  offset = (int)(slot - (long long)block * p.cache.block_size);
+  return true;
+}
 
 // 8 values of a row as floats; the raw registers are loaded first and unpacked later
 template <typename T>
@@ -74,6 +80,17 @@ struct Raw8;
 template <>
 struct Raw8<bf16> {
   uint4 a;
+  // The largest |x| over the row's lanes, as an fp32 pattern: above 0x7f7fffff if one is no finite number.
+  __device__ __forceinline__ uint32_t top(unsigned group, int lanes) const {
+    uint32_t m = max2(max2(a.x & 0x7fff7fffu, a.y & 0x7fff7fffu), max2(a.z & 0x7fff7fffu, a.w & 0x7fff7fffu));
+    for (int o = lanes / 2; o > 0; o >>= 1) m = max2(m, __shfl_xor_sync(group, m, o));
+    return max(m & 0xffff0000u, m << 16);
+  }
+  static __device__ __forceinline__ uint32_t max2(uint32_t x, uint32_t y) {
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
+  }
   __device__ __forceinline__ void load(const char *p) { a = *reinterpret_cast<const uint4 *>(p); }
   __device__ __forceinline__ void unpack(float (&f)[8]) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
@@ -87,6 +104,16 @@ struct Raw8<bf16> {
 template <>
 struct Raw8<float> {
   float4 a, b;
+  __device__ __forceinline__ uint32_t top(unsigned group, int lanes) const {
+    float m = larger(larger(larger(a.x, a.y), larger(a.z, a.w)), larger(larger(b.x, b.y), larger(b.z, b.w)));
+    for (int o = lanes / 2; o > 0; o >>= 1) m = larger(m, __shfl_xor_sync(group, m, o));
+    return __float_as_uint(m) & 0x7fffffffu;
+  }
+  static __device__ __forceinline__ float larger(float x, float y) {      // of the magnitudes, NaN if one is NaN
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(x)), "f"(fabsf(y)));
+    return r;
+  }
   __device__ __forceinline__ void load(const char *p) {
     a = reinterpret_cast<const float4 *>(p)[0];
     b = reinterpret_cast<const float4 *>(p)[1];
@@ -125,85 +152,87 @@ __device__ __forceinline__ float2 from_e4m3x2(uint16_t c) {
   return f;
 }
 
-template <typename T, int D, bool E4M3, int U>      // U: rows of a thread
+template <typename T, int D, bool E4M3, int U>      // U: tokens of a thread
 __global__ void __launch_bounds__(kRowThreads) cache_write_kernel(const __grid_constant__ RowsParams p) {
-  constexpr int LPR = D / 8;                 // lanes of a row
-  constexpr int RPC = kRowThreads / LPR;     // rows of a CTA at a time
-  const int sub = threadIdx.x % LPR;
-  const long long r0 = (long long)blockIdx.x * RPC * U + threadIdx.x / LPR;
-  RowAt at[U];
+  const Place<D> me(p, E4M3 ? 1 : 2, U, 8 * (int)sizeof(T));
+  if (me.idle) return;                                        // whole rows at a time: the shuffles are the row's own
   Raw8<T> raw[U];
   long long slot[U];
 #pragma unroll
   for (int i = 0; i < U; ++i) {
-    const long long r = r0 + i * RPC;
-    at[i].find(p, r < p.n_rows ? r : p.n_rows - 1);           // every lane stays for the shuffles
-    slot[i] = r < p.n_rows ? __ldg(p.slots + at[i].token) : -1;
-    raw[i].load(at[i].row + sub * 8 * (int)sizeof(T));
+    const int t = me.first + i * me.step;
+    const bool is = t < p.n_tokens;
+    slot[i] = is ? __ldg(p.slots + t) : -1;
+    raw[i].load(me.row + (is ? t : 0) * me.row_step);
   }
 #pragma unroll
   for (int i = 0; i < U; ++i) {
+    int block, offset;
+    const bool live = split_slot(p, slot[i], block, offset);
+    char *values = me.values + block * p.cache.block_stride + offset * me.slot_bytes;
     float f[8];
     raw[i].unpack(f);
-    at[i].place(p, slot[i]);
-    if (E4M3) {
+    if (!E4M3) {
+      if (live) *reinterpret_cast<uint4 *>(values) = pack_bf16(f);
+      continue;
+    }
+    uint32_t bits = raw[i].top(me.group, D / 8);
+    if (bits > 0x7f7fffffu) {                                 // infinities and NaN do not set the scale and become NaN
       float most = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float a = fabsf(f[j]);
-        most = fmaxf(most, a <= FLT_MAX ? a : 0.f);           // infinities and NaN do not set the scale
+        if (!(fabsf(f[j]) <= FLT_MAX)) f[j] = __uint_as_float(0x7fc00000u);
+        most = fmaxf(most, fabsf(f[j]));                      // ignores NaN
       }
 #pragma unroll
-      for (int o = LPR / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-      // most = m * 2^x with 1 <= m < 2; 448 = 1.75 * 2^8, so e = x - 8, one more if m > 1.75
-      const uint32_t bits = __float_as_uint(most);
-      int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u);
-      e = min(max(e, kMinExp), kMaxExp);
-      const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+      for (int o = D / 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(me.group, most, o));
+      bits = __float_as_uint(most);
+    }
+    // |x| <= m * 2^x with 1 <= m < 2; 448 = 1.75 * 2^8, so e = x - 8, one more if m > 1.75
+    int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u);
+    e = min(max(e, kMinExp), kMaxExp);
+    const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = fabsf(f[j]) <= FLT_MAX ? f[j] * inv : __uint_as_float(0x7fc00000u);
-      if (at[i].live) {
-        uint2 c;
-        c.x = e4m3x2(f[0], f[1]) | (e4m3x2(f[2], f[3]) << 16);
-        c.y = e4m3x2(f[4], f[5]) | (e4m3x2(f[6], f[7]) << 16);
-        *reinterpret_cast<uint2 *>(at[i].values(p, D) + sub * 8) = c;
-        if (sub == 0) *at[i].scale(p) = (char)(e + 127);
-      }
-    } else if (at[i].live) {
-      *reinterpret_cast<uint4 *>(at[i].values(p, 2 * D) + sub * 16) = pack_bf16(f);
+    for (int j = 0; j < 8; ++j) f[j] *= inv;
+    if (live) {
+      uint2 c;
+      c.x = e4m3x2(f[0], f[1]) | (e4m3x2(f[2], f[3]) << 16);
+      c.y = e4m3x2(f[4], f[5]) | (e4m3x2(f[6], f[7]) << 16);
+      *reinterpret_cast<uint2 *>(values) = c;
+      if (me.sub == 0) me.scale[block * p.cache.block_stride + offset] = (char)(e + 127);
     }
   }
 }
 
 template <typename T, int D, bool E4M3, int U>
 __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_constant__ RowsParams p) {
-  constexpr int LPR = D / 8, RPC = kRowThreads / LPR;
-  const int sub = threadIdx.x % LPR;
-  const long long r0 = (long long)blockIdx.x * RPC * U + threadIdx.x / LPR;
-  RowAt at[U];
+  const Place<D> me(p, E4M3 ? 1 : 2, U, 8 * (int)sizeof(T));
+  if (me.idle) return;
   uint4 raw[U];
   uint32_t scale[U];
   long long slot[U];
+  bool live[U];
 #pragma unroll
   for (int i = 0; i < U; ++i) {
-    const long long r = r0 + i * RPC;
-    at[i].find(p, r < p.n_rows ? r : p.n_rows - 1);
-    slot[i] = r < p.n_rows ? __ldg(p.slots + at[i].token) : -1;
+    const int t = me.first + i * me.step;
+    slot[i] = t < p.n_tokens ? __ldg(p.slots + t) : -1;
   }
 #pragma unroll
   for (int i = 0; i < U; ++i) {
-    at[i].place(p, slot[i]);
+    int block, offset;
+    live[i] = split_slot(p, slot[i], block, offset);          // block 0, offset 0 if not: read, but not written anywhere
+    const char *values = me.values + block * p.cache.block_stride + offset * me.slot_bytes;
     if (E4M3) {
-      const uint2 c = *reinterpret_cast<const uint2 *>(at[i].values(p, D) + sub * 8);      // slot 0 if it is not live
+      const uint2 c = *reinterpret_cast<const uint2 *>(values);
       raw[i] = make_uint4(c.x, c.y, 0, 0);
-      scale[i] = *reinterpret_cast<const uint8_t *>(at[i].scale(p));
+      scale[i] = *reinterpret_cast<const uint8_t *>(me.scale + block * p.cache.block_stride + offset);
     } else {
-      raw[i] = *reinterpret_cast<const uint4 *>(at[i].values(p, 2 * D) + sub * 16);
+      raw[i] = *reinterpret_cast<const uint4 *>(values);
     }
   }
 #pragma unroll
   for (int i = 0; i < U; ++i) {
-    if (!at[i].live) continue;
+    if (!live[i]) continue;
     float f[8];
     if (E4M3) {
       const float s = __uint_as_float(scale[i] << 23);
@@ -219,33 +248,35 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
       b.a = raw[i];
       b.unpack(f);
     }
-    store8(at[i].row + sub * 8 * (int)sizeof(T), f, T());
+    store8(me.row + (me.first + i * me.step) * me.row_step, f, T());
   }
 }
 
 template <typename T, int D, bool E4M3, int U>
 int launch_rows_u(const RowsParams &p, bool write, cudaStream_t st) {
-  constexpr long long rows = (long long)kRowThreads / (D / 8) * U;
-  const long long grid = (p.n_rows + rows - 1) / rows;
-  if (grid > 0x7fffffffll) return KV_ERR_SHAPE;
+  const int tokens = kRowThreads / (2 * p.heads * (D / 8)) * U;
+  const dim3 grid((p.n_tokens + tokens - 1) / tokens, (p.cache.n_kv_heads + p.heads - 1) / p.heads);
+  if (grid.y > 65535) return KV_ERR_SHAPE;
   if (write)
-    cache_write_kernel<T, D, E4M3, U><<<(unsigned)grid, kRowThreads, 0, st>>>(p);
+    cache_write_kernel<T, D, E4M3, U><<<grid, kRowThreads, 0, st>>>(p);
   else
-    cache_read_kernel<T, D, E4M3, U><<<(unsigned)grid, kRowThreads, 0, st>>>(p);
+    cache_read_kernel<T, D, E4M3, U><<<grid, kRowThreads, 0, st>>>(p);
   KV_COUNT_LAUNCH();
   KV_CUDA(cudaGetLastError());
   return KV_OK;
 }
 
-// Four rows to a thread once that still gives every SM four CTAs, one below that (few rows: the chain slot -> row -> store
-// is all there is, and more CTAs share it).
+// Four tokens to a thread once that still gives every SM four CTAs, one below that (few rows: the chain slot -> row ->
+// store is all there is, and more CTAs share it).
 template <typename T, int D, bool E4M3>
-int launch_rows(const RowsParams &p, bool write, cudaStream_t st) {
+int launch_rows(RowsParams &p, bool write, cudaStream_t st) {
   const int device = current_device();
   if (device < 0) return KV_ERR_CUDA;
-  const long long rows = kRowThreads / (D / 8);
-  return p.n_rows >= 16 * rows * sm_count(device) ? launch_rows_u<T, D, E4M3, 4>(p, write, st)
-                                                  : launch_rows_u<T, D, E4M3, 1>(p, write, st);
+  const int most = kRowThreads / (2 * (D / 8));               // heads that fit a CTA with their K and V
+  p.heads = p.cache.n_kv_heads < most ? p.cache.n_kv_heads : most;
+  const long long threads = (long long)p.n_tokens * 2 * p.cache.n_kv_heads * (D / 8);
+  return threads >= 16ll * kRowThreads * sm_count(device) ? launch_rows_u<T, D, E4M3, 4>(p, write, st)
+                                                          : launch_rows_u<T, D, E4M3, 1>(p, write, st);
 }
 
 // strides are in elements of dtype
@@ -272,11 +303,10 @@ int rows_call(const kv_cache_desc *cache, int layer, const void *k, int64_t k_ts
   p.cache = make_view(cache);
   p.layer = layer;
   p.n_slots = (long long)cache->num_blocks * cache->block_size;
-  p.block_shift = p.token_shift = -1;
-  for (int b = 0; b < 31; ++b) {
+  p.block_shift = -1;
+  for (int b = 0; b < 31; ++b)
     if ((1 << b) == cache->block_size) p.block_shift = b;
-    if ((1ll << b) == 2ll * cache->n_kv_heads) p.token_shift = b;
-  }
+  p.n_tokens = n_tokens;
   p.slots = reinterpret_cast<const long long *>(slots);
   p.k = (char *)const_cast<void *>(k);
   p.v = (char *)const_cast<void *>(v);
@@ -284,7 +314,6 @@ int rows_call(const kv_cache_desc *cache, int layer, const void *k, int64_t k_ts
   p.k_hs = k_hs * size;
   p.v_ts = v_ts * size;
   p.v_hs = v_hs * size;
-  p.n_rows = (long long)n_tokens * 2 * cache->n_kv_heads;
   cudaStream_t st = (cudaStream_t)stream;
   const bool e4m3 = cache->elem_bytes == 1, f32 = dtype == KV_DTYPE_F32;
   if (d == 128) {
