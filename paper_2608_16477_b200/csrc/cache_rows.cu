@@ -6,9 +6,9 @@
 // costs only values below 2^-15 of the row's maximum), the two directions need no division, and reading back into bf16
 // is exact.
 //
-// HBM-bound: every value is read once and written once; instructions are what has to be saved beside that.  head_dim / 8
-// lanes own a row (8 values each), the row maximum is a shuffle over them; consecutive lanes move consecutive 16-byte (bf16)
-// or 8-byte (codes) pieces.  A thread keeps its place in the token (K or V, head, piece) for all its tokens, so that only
+// HBM-bound: every value is read once and written once; instructions are what has to be saved beside that.  head_dim / 16
+// lanes own a row, the row maximum is a shuffle over them; a lane has two pieces of 8 values, half a row apart, so that
+// consecutive lanes move consecutive 16-byte (bf16) or 8-byte (codes) pieces.  A thread keeps its place in the token (K or V, head, piece) for all its tokens, so that only
 // the slot's page has to be worked out for each; once there are tokens enough it takes four, with their slots, then all
 // their loads, in flight together.  The maximum runs over the raw bits (an infinity or NaN shows in it, and only then the
 // row is gone through value by value).
@@ -20,6 +20,7 @@ namespace kvr {
 namespace {
 
 constexpr int kRowThreads = 256;
+constexpr int kMaxTokens = 1 << 30;   // tokens are counted in 32 bits, a CTA's ahead
 constexpr int kMinExp = -110, kMaxExp = 119;
 // largest page pool for which slots fit 32 bits: the division by the block size is then a 32-bit one
 constexpr long long kSlots32 = 0x7fffffffll;
@@ -37,15 +38,15 @@ struct RowsParams {
 // A thread's place: the piece `sub` of head `head` of K or V, for tokens first, first + step, ...
 template <int D>
 struct Place {
-  static constexpr int LPR = D / 8;               // lanes of a row
+  static constexpr int LPR = D / 16;              // lanes of a row
   int sub, first, step;
   bool idle;
   unsigned group;                                 // the row's lanes
   char *row, *values, *scale;                     // of token 0; of slot 0 of block 0
   long long row_step, slot_bytes;
-  __device__ __forceinline__ Place(const RowsParams &p, int elem, int u, int bytes) {      // bytes: of the piece
+  __device__ __forceinline__ Place(const RowsParams &p, int elem, int u, int bytes) {      // bytes: of a piece of the row
     const int per = 2 * p.heads * LPR, tokens = kRowThreads / per;      // threads of a token, tokens of a CTA at a time
-    const int at = threadIdx.x / per, in = threadIdx.x - at * per;
+    const int at = (int)threadIdx.x / per, in = (int)threadIdx.x - at * per;
     const int line = in / LPR, kv = line >= p.heads, head = blockIdx.y * p.heads + line - kv * p.heads;
     sub = in % LPR;
     idle = at >= tokens || head >= p.cache.n_kv_heads;
@@ -63,7 +64,7 @@ struct Place {
 // Block and offset of a slot; false if it lies outside the pool.
 __device__ __forceinline__ bool split_slot(const RowsParams &p, long long slot, int &block, int &offset) {
   block = offset = 0;
-  if (slot < 0 || slot >= p.n_slots) return false;
+  if ((unsigned long long)slot >= (unsigned long long)p.n_slots) return false;
   if (p.block_shift >= 0)
     block = (int)(slot >> p.block_shift);
   else if (p.n_slots <= kSlots32)
@@ -74,52 +75,69 @@ __device__ __forceinline__ bool split_slot(const RowsParams &p, long long slot, 
   return true;
 }
 
-// 8 values of a row as floats; the raw registers are loaded first and unpacked later
+// Two pieces of 8 values of a row: the raw registers are loaded first and unpacked later.
 template <typename T>
-struct Raw8;
+struct Raw;
 template <>
-struct Raw8<bf16> {
-  uint4 a;
-  // The largest |x| over the row's lanes, as an fp32 pattern: above 0x7f7fffff if one is no finite number.
-  __device__ __forceinline__ uint32_t top(unsigned group, int lanes) const {
-    uint32_t m = max2(max2(a.x & 0x7fff7fffu, a.y & 0x7fff7fffu), max2(a.z & 0x7fff7fffu, a.w & 0x7fff7fffu));
-    for (int o = lanes / 2; o > 0; o >>= 1) m = max2(m, __shfl_xor_sync(group, m, o));
-    return max(m & 0xffff0000u, m << 16);
+struct Raw<bf16> {
+  uint4 a[2];
+  __device__ __forceinline__ void load(const char *p, int apart) {
+    a[0] = *reinterpret_cast<const uint4 *>(p);
+    a[1] = *reinterpret_cast<const uint4 *>(p + apart);
   }
-  static __device__ __forceinline__ uint32_t max2(uint32_t x, uint32_t y) {
-    uint32_t r;
-    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
-    return r;
-  }
-  __device__ __forceinline__ void load(const char *p) { a = *reinterpret_cast<const uint4 *>(p); }
-  __device__ __forceinline__ void unpack(float (&f)[8]) const {
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+  __device__ __forceinline__ void unpack(int h, float (&f)[8]) const {
+    const uint32_t w[4] = {a[h].x, a[h].y, a[h].z, a[h].w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       f[2 * i] = __uint_as_float(w[i] << 16);
       f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
   }
+  static __device__ __forceinline__ uint32_t max2(uint32_t x, uint32_t y) {
+    uint32_t r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
+  }
+  // The largest |x| over the row's lanes, as an fp32 pattern: above 0x7f7fffff if one is no finite number.
+  template <int LANES>
+  __device__ __forceinline__ uint32_t top(unsigned group) const {
+    const uint32_t s = 0x7fff7fffu;
+    uint32_t m = max2(max2(max2(a[0].x & s, a[0].y & s), max2(a[0].z & s, a[0].w & s)),
+                      max2(max2(a[1].x & s, a[1].y & s), max2(a[1].z & s, a[1].w & s)));
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) m = max2(m, __shfl_xor_sync(group, m, o));
+    return max(m & 0xffff0000u, m << 16);
+  }
 };
 template <>
-struct Raw8<float> {
-  float4 a, b;
-  __device__ __forceinline__ uint32_t top(unsigned group, int lanes) const {
-    float m = larger(larger(larger(a.x, a.y), larger(a.z, a.w)), larger(larger(b.x, b.y), larger(b.z, b.w)));
-    for (int o = lanes / 2; o > 0; o >>= 1) m = larger(m, __shfl_xor_sync(group, m, o));
-    return __float_as_uint(m) & 0x7fffffffu;
+struct Raw<float> {
+  float4 a[2][2];
+  __device__ __forceinline__ void load(const char *p, int apart) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      a[h][0] = reinterpret_cast<const float4 *>(p + h * apart)[0];
+      a[h][1] = reinterpret_cast<const float4 *>(p + h * apart)[1];
+    }
+  }
+  __device__ __forceinline__ void unpack(int h, float (&f)[8]) const {
+    f[0] = a[h][0].x; f[1] = a[h][0].y; f[2] = a[h][0].z; f[3] = a[h][0].w;
+    f[4] = a[h][1].x; f[5] = a[h][1].y; f[6] = a[h][1].z; f[7] = a[h][1].w;
   }
   static __device__ __forceinline__ float larger(float x, float y) {      // of the magnitudes, NaN if one is NaN
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(x)), "f"(fabsf(y)));
     return r;
   }
-  __device__ __forceinline__ void load(const char *p) {
-    a = reinterpret_cast<const float4 *>(p)[0];
-    b = reinterpret_cast<const float4 *>(p)[1];
-  }
-  __device__ __forceinline__ void unpack(float (&f)[8]) const {
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  template <int LANES>
+  __device__ __forceinline__ uint32_t top(unsigned group) const {
+    float m = 0.f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) m = larger(m, larger(larger(a[h][i].x, a[h][i].y), larger(a[h][i].z, a[h][i].w)));
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) m = larger(m, __shfl_xor_sync(group, m, o));
+    return __float_as_uint(m) & 0x7fffffffu;
   }
 };
 
@@ -156,49 +174,57 @@ template <typename T, int D, bool E4M3, int U>      // U: tokens of a thread
 __global__ void __launch_bounds__(kRowThreads) cache_write_kernel(const __grid_constant__ RowsParams p) {
   const Place<D> me(p, E4M3 ? 1 : 2, U, 8 * (int)sizeof(T));
   if (me.idle) return;                                        // whole rows at a time: the shuffles are the row's own
-  Raw8<T> raw[U];
+  Raw<T> raw[U];
   long long slot[U];
 #pragma unroll
   for (int i = 0; i < U; ++i) {
     const int t = me.first + i * me.step;
     const bool is = t < p.n_tokens;
     slot[i] = is ? __ldg(p.slots + t) : -1;
-    raw[i].load(me.row + (is ? t : 0) * me.row_step);
+    raw[i].load(me.row + (is ? t : 0) * me.row_step, D / 2 * (int)sizeof(T));
   }
 #pragma unroll
   for (int i = 0; i < U; ++i) {
     int block, offset;
     const bool live = split_slot(p, slot[i], block, offset);
     char *values = me.values + block * p.cache.block_stride + offset * me.slot_bytes;
-    float f[8];
-    raw[i].unpack(f);
+    float f[2][8];
+    raw[i].unpack(0, f[0]);
+    raw[i].unpack(1, f[1]);
     if (!E4M3) {
-      if (live) *reinterpret_cast<uint4 *>(values) = pack_bf16(f);
+      if (live) {
+        *reinterpret_cast<uint4 *>(values) = pack_bf16(f[0]);
+        *reinterpret_cast<uint4 *>(values + D) = pack_bf16(f[1]);
+      }
       continue;
     }
-    uint32_t bits = raw[i].top(me.group, D / 8);
+    uint32_t bits = raw[i].template top<Place<D>::LPR>(me.group);
     if (bits > 0x7f7fffffu) {                                 // infinities and NaN do not set the scale and become NaN
       float most = 0.f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (!(fabsf(f[j]) <= FLT_MAX)) f[j] = __uint_as_float(0x7fc00000u);
-        most = fmaxf(most, fabsf(f[j]));                      // ignores NaN
-      }
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int o = D / 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(me.group, most, o));
+        for (int j = 0; j < 8; ++j) {
+          if (!(fabsf(f[h][j]) <= FLT_MAX)) f[h][j] = __uint_as_float(0x7fc00000u);
+          most = fmaxf(most, fabsf(f[h][j]));                 // ignores NaN
+        }
+#pragma unroll
+      for (int o = Place<D>::LPR / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(me.group, most, o));
       bits = __float_as_uint(most);
     }
     // |x| <= m * 2^x with 1 <= m < 2; 448 = 1.75 * 2^8, so e = x - 8, one more if m > 1.75
     int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u);
     e = min(max(e, kMinExp), kMaxExp);
     const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+    uint2 c[2];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] *= inv;
+    for (int h = 0; h < 2; ++h) {
+      c[h].x = e4m3x2(f[h][0] * inv, f[h][1] * inv) | (e4m3x2(f[h][2] * inv, f[h][3] * inv) << 16);
+      c[h].y = e4m3x2(f[h][4] * inv, f[h][5] * inv) | (e4m3x2(f[h][6] * inv, f[h][7] * inv) << 16);
+    }
     if (live) {
-      uint2 c;
-      c.x = e4m3x2(f[0], f[1]) | (e4m3x2(f[2], f[3]) << 16);
-      c.y = e4m3x2(f[4], f[5]) | (e4m3x2(f[6], f[7]) << 16);
-      *reinterpret_cast<uint2 *>(values) = c;
+      *reinterpret_cast<uint2 *>(values) = c[0];
+      *reinterpret_cast<uint2 *>(values + D / 2) = c[1];
       if (me.sub == 0) me.scale[block * p.cache.block_stride + offset] = (char)(e + 127);
     }
   }
@@ -208,7 +234,7 @@ template <typename T, int D, bool E4M3, int U>
 __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_constant__ RowsParams p) {
   const Place<D> me(p, E4M3 ? 1 : 2, U, 8 * (int)sizeof(T));
   if (me.idle) return;
-  uint4 raw[U];
+  uint4 raw[U][E4M3 ? 1 : 2];                                 // e4m3: both pieces in one
   uint32_t scale[U];
   long long slot[U];
   bool live[U];
@@ -223,38 +249,43 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
     live[i] = split_slot(p, slot[i], block, offset);          // block 0, offset 0 if not: read, but not written anywhere
     const char *values = me.values + block * p.cache.block_stride + offset * me.slot_bytes;
     if (E4M3) {
-      const uint2 c = *reinterpret_cast<const uint2 *>(values);
-      raw[i] = make_uint4(c.x, c.y, 0, 0);
+      const uint2 a = *reinterpret_cast<const uint2 *>(values), b = *reinterpret_cast<const uint2 *>(values + D / 2);
+      raw[i][0] = make_uint4(a.x, a.y, b.x, b.y);
       scale[i] = *reinterpret_cast<const uint8_t *>(me.scale + block * p.cache.block_stride + offset);
     } else {
-      raw[i] = *reinterpret_cast<const uint4 *>(values);
+      raw[i][0] = *reinterpret_cast<const uint4 *>(values);
+      raw[i][E4M3 ? 0 : 1] = *reinterpret_cast<const uint4 *>(values + D);
     }
   }
 #pragma unroll
   for (int i = 0; i < U; ++i) {
     if (!live[i]) continue;
-    float f[8];
+    char *row = me.row + (me.first + i * me.step) * me.row_step;
+    float f[2][8];
     if (E4M3) {
       const float s = __uint_as_float(scale[i] << 23);
-      const uint32_t w[2] = {raw[i].x, raw[i].y};
+      const uint32_t w[4] = {raw[i][0].x, raw[i][0].y, raw[i][0].z, raw[i][0].w};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < 8; ++j) {
         const float2 c = from_e4m3x2((uint16_t)(w[j >> 1] >> ((j & 1) * 16)));
-        f[2 * j] = c.x * s;
-        f[2 * j + 1] = c.y * s;
+        f[j >> 2][(2 * j) & 7] = c.x * s;
+        f[j >> 2][(2 * j + 1) & 7] = c.y * s;
       }
     } else {
-      Raw8<bf16> b;
-      b.a = raw[i];
-      b.unpack(f);
+      Raw<bf16> b;
+      b.a[0] = raw[i][0];
+      b.a[1] = raw[i][E4M3 ? 0 : 1];
+      b.unpack(0, f[0]);
+      b.unpack(1, f[1]);
     }
-    store8(me.row + (me.first + i * me.step) * me.row_step, f, T());
+    store8(row, f[0], T());
+    store8(row + D / 2 * (int)sizeof(T), f[1], T());
   }
 }
 
 template <typename T, int D, bool E4M3, int U>
 int launch_rows_u(const RowsParams &p, bool write, cudaStream_t st) {
-  const int tokens = kRowThreads / (2 * p.heads * (D / 8)) * U;
+  const int tokens = kRowThreads / (2 * p.heads * Place<D>::LPR) * U;
   const dim3 grid((p.n_tokens + tokens - 1) / tokens, (p.cache.n_kv_heads + p.heads - 1) / p.heads);
   if (grid.y > 65535) return KV_ERR_SHAPE;
   if (write)
@@ -266,16 +297,16 @@ int launch_rows_u(const RowsParams &p, bool write, cudaStream_t st) {
   return KV_OK;
 }
 
-// Four tokens to a thread once that still gives every SM four CTAs, one below that (few rows: the chain slot -> row ->
+// Two tokens to a thread once that still gives every SM eight CTAs, one below that (few rows: the chain slot -> row ->
 // store is all there is, and more CTAs share it).
 template <typename T, int D, bool E4M3>
 int launch_rows(RowsParams &p, bool write, cudaStream_t st) {
   const int device = current_device();
   if (device < 0) return KV_ERR_CUDA;
-  const int most = kRowThreads / (2 * (D / 8));               // heads that fit a CTA with their K and V
+  const int most = kRowThreads / (2 * Place<D>::LPR);          // heads that fit a CTA with their K and V
   p.heads = p.cache.n_kv_heads < most ? p.cache.n_kv_heads : most;
-  const long long threads = (long long)p.n_tokens * 2 * p.cache.n_kv_heads * (D / 8);
-  return threads >= 16ll * kRowThreads * sm_count(device) ? launch_rows_u<T, D, E4M3, 4>(p, write, st)
+  const long long threads = (long long)p.n_tokens * 2 * p.cache.n_kv_heads * Place<D>::LPR;
+  return threads >= 16ll * kRowThreads * sm_count(device) ? launch_rows_u<T, D, E4M3, 2>(p, write, st)
                                                           : launch_rows_u<T, D, E4M3, 1>(p, write, st);
 }
 
@@ -286,7 +317,7 @@ int rows_call(const kv_cache_desc *cache, int layer, const void *k, int64_t k_ts
   int rc = check_cache_desc(cache, true);
   if (rc != KV_OK) return rc;
   if (cache->head_dim != 64 && cache->head_dim != 128) return KV_ERR_SHAPE;
-  if (layer < 0 || layer >= cache->n_layers) return KV_ERR_SHAPE;
+  if (layer < 0 || layer >= cache->n_layers || n_tokens > kMaxTokens) return KV_ERR_SHAPE;
   if (n_tokens == 0) return KV_OK;
   if (k == nullptr || v == nullptr || slots == nullptr) return KV_ERR_ARG;
   const int size = dtype == KV_DTYPE_BF16 ? 2 : 4, d = cache->head_dim;
