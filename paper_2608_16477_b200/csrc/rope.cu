@@ -26,6 +26,7 @@ namespace {
 constexpr int kRopeThreads = 256;
 constexpr int kRopeMaxPairs = 128;
 constexpr int kRopeMaxTokens = 4;   // tokens of a CTA
+constexpr int kRopeAhead = 3;       // heads of a thread whose loads are in flight together
 
 struct RopeParams {
   const void *x;
@@ -108,25 +109,25 @@ __global__ void __launch_bounds__(kRopeThreads) rope_vec_kernel(const __grid_con
   const bool copies = u >= turned;
   const int items = idle || (copies && in_place) ? 0 : nt * nh;
 
-  uint4 a, b = make_uint4(0, 0, 0, 0);
-  auto load = [&](int it) {
-    const int t = it / nh, h = it - t * nh;
-    const T *row = x + (t0 + t) * p.x_ts + (h0 + h) * p.x_hs;
-    a = *reinterpret_cast<const uint4 *>(row + e0);
-    if (two) b = *reinterpret_cast<const uint4 *>(row + e1);
+  uint4 a[kRopeAhead], b[kRopeAhead];
+  auto load = [&](int first) {
+#pragma unroll
+    for (int i = 0; i < kRopeAhead; ++i) {
+      const int it = first + i * lanes;
+      if (it >= items) break;
+      const int t = it / nh, h = it - t * nh;
+      const T *row = x + (t0 + t) * p.x_ts + (h0 + h) * p.x_hs;
+      a[i] = *reinterpret_cast<const uint4 *>(row + e0);
+      if (two) b[i] = *reinterpret_cast<const uint4 *>(row + e1);
+    }
   };
-  if (slot < items) load(slot);      // under the trigonometry
-  rope_table_of(p, t0, nt, cs);
-  __syncthreads();
-  for (int it = slot; it < items; it += lanes) {
-    const uint4 ca = a, cb = b;
-    if (it + lanes < items) load(it + lanes);
+  auto turn = [&](int it, const uint4 &ca, const uint4 &cb) {
     const int t = it / nh, h = it - t * nh;
     T *row = out + (t0 + t) * p.o_ts + (h0 + h) * p.o_hs;
     if (copies) {
       *reinterpret_cast<uint4 *>(row + e0) = ca;
       if (two) *reinterpret_cast<uint4 *>(row + e1) = cb;
-      continue;
+      return;
     }
     float fa[VE], fb[VE];
     Vec<T>::unpack(ca, fa);
@@ -153,6 +154,15 @@ __global__ void __launch_bounds__(kRopeThreads) rope_vec_kernel(const __grid_con
     }
     *reinterpret_cast<uint4 *>(row + e0) = Vec<T>::pack(fa);
     *reinterpret_cast<uint4 *>(row + e1) = Vec<T>::pack(fb);
+  };
+  load(slot);      // under the trigonometry
+  rope_table_of(p, t0, nt, cs);
+  __syncthreads();
+  for (int first = slot; first < items; first += kRopeAhead * lanes) {
+    if (first > slot) load(first);
+#pragma unroll
+    for (int i = 0; i < kRopeAhead; ++i)
+      if (first + i * lanes < items) turn(first + i * lanes, a[i], b[i]);
   }
 }
 
