@@ -499,56 +499,53 @@ def kv_prefill_prefix_batched(model: Model, cache: PagedCache, token_id_lists, b
     return ws
 
 
-# ---- serving a batch of requests: rotary positions, rows into and out of pages, attention of one new token each
+# ---- serving a batch of requests: rotary positions, rows into and out of pages, attention of one new token each.
+# A decode step makes these calls for every layer, so their checks are written out instead of shared.
 KV_ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 KV_ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
-_DTYPES = None
+_TORCH = None
 
 
-def _dtype(t, what):
-    global _DTYPES
-    if _DTYPES is None:
+def _torch():
+    global _TORCH
+    if _TORCH is None:
         import torch
-        _DTYPES = {torch.bfloat16: 0, torch.float32: 1}
-    try:
-        return _DTYPES[t.dtype]
-    except KeyError:
-        raise ValueError(f"{what}: bfloat16 or float32 is wanted, not {t.dtype}") from None
+        _TORCH = torch
+    return _TORCH
 
 
-def _same(what, cond):
-    if not cond:
-        raise ValueError(what)
+def _dtype(name, dtype):
+    torch = _torch()
+    if dtype is torch.bfloat16:
+        return 0
+    if dtype is torch.float32:
+        return 1
+    raise ValueError(f"{name}: bfloat16 or float32 is wanted, not {dtype}")
 
 
-def _inner(t):
-    """Whether the last dimension is contiguous (of an empty tensor it does not matter)."""
-    return t.numel() == 0 or t.shape[-1] == 1 or t.stride(-1) == 1
+def _refuse(name, what):
+    raise ValueError(f"{name}: {what}")
 
 
-def _stride(t, dim):
-    return t.stride(dim) if t.shape[dim] > 1 else 0
-
-
-def _run(name, stream, tensors, args):
-    """Calls `name` on the tensors' device: they all have to be on one, which need not be the current one."""
-    import torch
-    device = tensors[0].device
+def _on_device(name, stream, tensors):
+    """(device index, raw stream) of a call on `tensors`, which all have to be on one CUDA device."""
+    index = tensors[0].get_device() if tensors[0].is_cuda else -1
     for t in tensors:
-        if t.device != device:
-            raise ValueError(f"{name}: tensors on {device} and on {t.device}")
-    if device.type != "cuda":
-        raise ValueError(f"{name}: tensors on a CUDA device are wanted, not on {device}")
-    index, current = device.index, torch.cuda.current_device()
+        if not t.is_cuda or t.get_device() != index:
+            _refuse(name, f"tensors on one CUDA device are wanted, not on {[str(t.device) for t in tensors]}")
     if stream is None:
-        stream = torch._C._cuda_getCurrentRawStream(index)
-    else:
-        stream = getattr(stream, "cuda_stream", stream)
-    if index == current:
-        status = getattr(load(), name)(*args, stream)
+        return index, _torch()._C._cuda_getCurrentRawStream(index)
+    return index, getattr(stream, "cuda_stream", stream)
+
+
+def _launch(name, index, args):
+    """Calls the library with `index` as the current device (it need not be that of the caller)."""
+    torch, call = _torch(), getattr(_LIB or load(), name)
+    if index == torch._C._cuda_getDevice():
+        status = call(*args)
     else:
         with torch.cuda.device(index):
-            status = getattr(load(), name)(*args, stream)
+            status = call(*args)
     if status != 0:
         raise KVError(status, name)
 
@@ -560,8 +557,10 @@ class Rope:
     def __init__(self, rotary_dim: int, layout: str = "half", base: float = 1.0e6, scaling: str = "none",
                  factor: float = 1.0, original_ctx: float = 0.0, low: float = 1.0, high: float = 32.0, gain: float = 1.0):
         self.handle = None
-        _same(f"layout {layout!r}: one of {sorted(KV_ROPE_LAYOUTS)}", layout in KV_ROPE_LAYOUTS)
-        _same(f"scaling {scaling!r}: one of {sorted(KV_ROPE_SCALINGS)}", scaling in KV_ROPE_SCALINGS)
+        if layout not in KV_ROPE_LAYOUTS:
+            _refuse("Rope", f"layout {layout!r}: one of {sorted(KV_ROPE_LAYOUTS)}")
+        if scaling not in KV_ROPE_SCALINGS:
+            _refuse("Rope", f"scaling {scaling!r}: one of {sorted(KV_ROPE_SCALINGS)}")
         self._lib = load()
         self.rotary_dim = rotary_dim
         desc = RopeDesc(rotary_dim, KV_ROPE_LAYOUTS[layout], KV_ROPE_SCALINGS[scaling], base, factor, original_ctx, low,
@@ -589,44 +588,57 @@ class Rope:
 def kv_op_rope(rope: Rope, x, positions, out, backward: bool = False, stream=None):
     """out[t, h] = x[t, h] rotated at positions[t]; x and out [T, heads, head_dim] (bf16 or fp32, any strides whose last is
     1; out may be x), positions int32 [T].  backward: the gradient of x from the gradient of out."""
-    _same("kv_op_rope: x is [tokens, heads, head_dim] with contiguous head_dim", x.dim() == 3 and _inner(x))
-    _same("kv_op_rope: out has x's shape and type, with contiguous head_dim",
-          out.shape == x.shape and out.dtype == x.dtype and _inner(out))
-    t, h, d = x.shape
-    _same("kv_op_rope: positions is a contiguous int32 vector, one per token",
-          positions.shape == (t,) and positions.element_size() == 4 and not positions.is_floating_point()
-          and (t < 2 or positions.stride(0) == 1))
-    _run("kv_op_rope", stream, (x, positions, out),
-         (rope.handle, x.data_ptr(), _stride(x, 0), _stride(x, 1), _dtype(x, "kv_op_rope"), t, h, d,
-          positions.data_ptr(), int(backward), out.data_ptr(), _stride(out, 0), _stride(out, 1)))
+    name, shape = "kv_op_rope", x.shape
+    if len(shape) != 3 or out.shape != shape or out.dtype is not x.dtype:
+        _refuse(name, "x and out are [tokens, heads, head_dim] of one type")
+    t, h, d = shape
+    (xt, xh, xd), (ot, oh, od) = x.stride(), out.stride()
+    if t * h * d and d > 1 and (xd != 1 or od != 1):
+        _refuse(name, "head_dim has to be contiguous")
+    if positions.shape != (t,) or positions.dtype is not _torch().int32 or not positions.is_contiguous():
+        _refuse(name, "positions is a contiguous int32 vector, one per token")
+    dtype = _dtype(name, x.dtype)
+    index, stream = _on_device(name, stream, (x, positions, out))
+    _launch(name, index, (rope.handle, x.data_ptr(), xt if t > 1 else 0, xh if h > 1 else 0, dtype, t, h, d,
+                          positions.data_ptr(), 1 if backward else 0, out.data_ptr(), ot if t > 1 else 0,
+                          oh if h > 1 else 0, stream))
 
 
-def _check_rows(name, cache, k, v, slots):
-    t = slots.shape[0] if slots.dim() == 1 else -1
-    want = (t, cache.n_kv_heads, cache.head_dim)
-    _same(f"{name}: rows are [tokens, n_kv_heads, head_dim] = {want} with contiguous head_dim, of one type",
-          k.shape == want and v.shape == want and _inner(k) and _inner(v) and k.dtype == v.dtype)
-    _same(f"{name}: slots is a contiguous int64 vector, one per token",
-          slots.element_size() == 8 and not slots.is_floating_point() and (t < 2 or slots.stride(0) == 1))
-    return t
+def _rows(name, cache, k, v, slots):
+    """(tokens, dtype, strides of K, strides of V) of rows [tokens, n_kv_heads, head_dim]."""
+    if slots.dim() != 1 or slots.dtype is not _torch().int64 or not slots.is_contiguous():
+        _refuse(name, "slots is a contiguous int64 vector, one per token")
+    t, h, d = slots.shape[0], cache.n_kv_heads, cache.head_dim
+    if k.shape != (t, h, d) or v.shape != (t, h, d) or k.dtype is not v.dtype:
+        _refuse(name, f"rows are [tokens, n_kv_heads, head_dim] = {(t, h, d)} of one type")
+    (kt, kh, kd), (vt, vh, vd) = k.stride(), v.stride()
+    if t and (kd != 1 or vd != 1):
+        _refuse(name, "head_dim has to be contiguous")
+    if t < 2:
+        kt = vt = 0
+    if h < 2:
+        kh = vh = 0
+    return t, _dtype(name, k.dtype), kt, kh, vt, vh
 
 
 def kv_op_cache_write(cache: PagedCache, layer: int, k, v, slots, stream=None):
     """K and V rows [T, n_kv_heads, head_dim] (bf16 or fp32) into the cache's slots (int64 [T], block * block_size +
     offset; -1 skips a token).  An e4m3 cache quantises them on the way."""
-    t = _check_rows("kv_op_cache_write", cache, k, v, slots)
-    _run("kv_op_cache_write", stream, (cache.data, k, v, slots),
-         (cache._desc_ref, layer, k.data_ptr(), _stride(k, 0), _stride(k, 1), v.data_ptr(), _stride(v, 0), _stride(v, 1),
-          _dtype(k, "kv_op_cache_write"), t, slots.data_ptr()))
+    name = "kv_op_cache_write"
+    t, dtype, kt, kh, vt, vh = _rows(name, cache, k, v, slots)
+    index, stream = _on_device(name, stream, (cache.data, k, v, slots))
+    _launch(name, index, (cache._desc_ref, layer, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, dtype, t, slots.data_ptr(),
+                          stream))
 
 
 def kv_op_cache_read(cache: PagedCache, layer: int, slots, k_out, v_out, stream=None):
     """The cache's rows at `slots` into k_out and v_out [T, n_kv_heads, head_dim] (bf16 or fp32); rows whose slot is
     outside the pool stay as they were."""
-    t = _check_rows("kv_op_cache_read", cache, k_out, v_out, slots)
-    _run("kv_op_cache_read", stream, (cache.data, slots, k_out, v_out),
-         (cache._desc_ref, layer, slots.data_ptr(), t, k_out.data_ptr(), _stride(k_out, 0), _stride(k_out, 1),
-          v_out.data_ptr(), _stride(v_out, 0), _stride(v_out, 1), _dtype(k_out, "kv_op_cache_read")))
+    name = "kv_op_cache_read"
+    t, dtype, kt, kh, vt, vh = _rows(name, cache, k_out, v_out, slots)
+    index, stream = _on_device(name, stream, (cache.data, slots, k_out, v_out))
+    _launch(name, index, (cache._desc_ref, layer, slots.data_ptr(), t, k_out.data_ptr(), kt, kh, v_out.data_ptr(), vt, vh,
+                          dtype, stream))
 
 
 def kv_paged_attention_batched_scratch_bytes(n_req: int, n_q_heads: int, cache: PagedCache, max_ctx: int) -> int:
@@ -642,32 +654,38 @@ def kv_op_paged_attention_batched(q, cache: PagedCache, layer: int, block_tables
     block_tables int32 [R, B], context_lens int32 [R] (clamped to max_ctx), scratch of
     kv_paged_attention_batched_scratch_bytes(R, ...) bytes, lse fp32 [R, n_q_heads] or None; softmax_scale defaults to
     head_dim ** -0.5."""
-    name = "kv_op_paged_attention_batched"
-    _same(f"{name}: q is [requests, heads, head_dim] with contiguous heads",
-          q.dim() == 3 and q.shape[2] == cache.head_dim and _inner(q)
-          and (q.shape[0] == 0 or q.shape[1] < 2 or q.stride(1) == q.shape[2]))
-    r, hq, d = q.shape
-    _same(f"{name}: out has q's shape and type, with contiguous heads",
-          out.shape == q.shape and out.dtype == q.dtype and _inner(out) and (r == 0 or hq < 2 or out.stride(1) == d))
-    _same(f"{name}: block_tables is int32 [requests, blocks] with contiguous rows",
-          block_tables.dim() == 2 and block_tables.shape[0] == r and block_tables.element_size() == 4
-          and not block_tables.is_floating_point() and _inner(block_tables))
-    _same(f"{name}: context_lens is a contiguous int32 vector, one per request",
-          context_lens.shape == (r,) and context_lens.element_size() == 4 and not context_lens.is_floating_point()
-          and (r < 2 or context_lens.stride(0) == 1))
-    _same(f"{name}: lse is contiguous float32 [requests, heads]",
-          lse is None or (lse.shape == (r, hq) and lse.element_size() == 4 and lse.is_floating_point()
-                          and lse.is_contiguous()))
-    # a table of one row may have any row stride; the library takes the row's length as what it covers
-    stride = block_tables.stride(0) if r > 1 else block_tables.shape[1]
-    _same(f"{name}: rows of block_tables must not be shorter than their stride says",
-          r < 2 or stride >= block_tables.shape[1])
-    if block_tables.shape[1] * cache.block_size < max_ctx:
+    name, torch, shape = "kv_op_paged_attention_batched", _torch(), q.shape
+    if len(shape) != 3 or shape[2] != cache.head_dim or out.shape != shape or out.dtype is not q.dtype:
+        _refuse(name, "q and out are [requests, heads, head_dim] of one type")
+    r, hq, d = shape
+    (qr, qh, qd), (outr, outh, outd) = q.stride(), out.stride()
+    if r and (qd != 1 or outd != 1 or (hq > 1 and (qh != d or outh != d))):
+        _refuse(name, "a request's heads have to be contiguous")
+    columns = block_tables.shape[1] if block_tables.dim() == 2 else -1
+    if columns < 0 or block_tables.shape[0] != r or block_tables.dtype is not torch.int32:
+        _refuse(name, "block_tables is int32 [requests, blocks]")
+    # one row may have any row stride: what counts is its length
+    row, step = (block_tables.stride() if r > 1 else (columns, block_tables.stride(1)))
+    if (r and columns > 1 and step != 1) or (r > 1 and row < columns):
+        _refuse(name, "rows of block_tables have to be contiguous, and not to overlap")
+    if context_lens.shape != (r,) or context_lens.dtype is not torch.int32 or not context_lens.is_contiguous():
+        _refuse(name, "context_lens is a contiguous int32 vector, one per request")
+    if columns * cache.block_size < max_ctx:
         raise KVError(-8, name)
-    tensors = (cache.data, q, block_tables, context_lens, out)
-    tensors += tuple(t for t in (scratch, lse) if t is not None)
-    _run(name, stream, tensors,
-         (q.data_ptr(), _stride(q, 0), _dtype(q, name), r, hq, cache._desc_ref, layer, block_tables.data_ptr(), stride,
-          context_lens.data_ptr(), max_ctx, d ** -0.5 if softmax_scale is None else softmax_scale, _ptr(scratch),
-          0 if scratch is None else scratch.numel() * scratch.element_size(), out.data_ptr(), _stride(out, 0),
-          _ptr(lse)))
+    tensors = [cache.data, q, block_tables, context_lens, out]
+    lse_ptr = scratch_ptr = scratch_bytes = 0
+    if lse is not None:
+        if lse.shape != (r, hq) or lse.dtype is not torch.float32 or not lse.is_contiguous():
+            _refuse(name, "lse is contiguous float32 [requests, heads]")
+        tensors.append(lse)
+        lse_ptr = lse.data_ptr()
+    if scratch is not None:
+        if not scratch.is_contiguous():
+            _refuse(name, "scratch has to be contiguous")
+        tensors.append(scratch)
+        scratch_ptr, scratch_bytes = scratch.data_ptr(), scratch.numel() * scratch.element_size()
+    dtype = _dtype(name, q.dtype)
+    index, stream = _on_device(name, stream, tensors)
+    _launch(name, index, (q.data_ptr(), qr if r > 1 else 0, dtype, r, hq, cache._desc_ref, layer, block_tables.data_ptr(),
+                          row, context_lens.data_ptr(), max_ctx, d ** -0.5 if softmax_scale is None else softmax_scale,
+                          scratch_ptr, scratch_bytes, out.data_ptr(), outr if r > 1 else 0, lse_ptr, stream))
