@@ -283,53 +283,58 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
 
   // ---- this CTA's range of tiles
   Cursor cons;
-  long long todo;
+  long long todo, total = 0, first_tile = 0;
   const int part = blockIdx.x;
   if (p.parts == 0) {
     cons.open(p, blockIdx.x, TILE);
     todo = cons.n_tiles;
   } else {
-    long long total = 0;
-    for (int r0 = 0; r0 < p.n_req; r0 += 32) {
-      const int r = r0 + lane;
-      int t = r < p.n_req ? max(1, (clamped_len(p, r) + TILE - 1) / TILE) : 0;
-      if (blockIdx.x == 0 && blockIdx.y == 0 && warp == 0) {      // the joining kernel wants the starts
-        int inc = t;
+    // 128 requests at a time, four to a lane, whose lengths are loaded together; a batch of up to 128 keeps them
+    int tiles[4];
+    auto load_tiles = [&](int r0) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int r = r0 + j * 32 + lane;
+        tiles[j] = r < p.n_req ? clamped_len(p, r) : -1;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) tiles[j] = tiles[j] < 0 ? 0 : max(1, (tiles[j] + TILE - 1) / TILE);
+    };
+    for (int r0 = 0; r0 < p.n_req; r0 += 128) {
+      load_tiles(r0);
+      total += __reduce_add_sync(0xffffffffu, tiles[0] + tiles[1] + tiles[2] + tiles[3]);
+    }
+    // no more ranges than tiles: every range that is left holds one (the joining kernel counts on it)
+    const long long ranges = min((long long)p.parts, total);
+    if (part >= ranges) return;
+    if ((part + 1) * total <= 0xffffffffll) {
+      first_tile = (uint32_t)(part * total) / (uint32_t)ranges;
+      todo = (uint32_t)((part + 1) * total) / (uint32_t)ranges - first_tile;
+    } else {
+      first_tile = part * total / ranges;
+      todo = (part + 1) * total / ranges - first_tile;
+    }
+    long long before = 0;
+    int at = -1;
+    for (int r0 = 0; at < 0; r0 += 128) {
+      if (p.n_req > 128) load_tiles(r0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        int inc = tiles[j];
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
           const int up = __shfl_up_sync(0xffffffffu, inc, o);
           if (lane >= o) inc += up;
         }
-        if (r < p.n_req) p.tile_start[r + 1] = total + inc;
-        if (r == 0) p.tile_start[0] = 0;
+        const int sum = __shfl_sync(0xffffffffu, inc, 31);
+        if (at < 0 && first_tile < before + sum) {
+          const int l = __ffs(__ballot_sync(0xffffffffu, first_tile < before + inc)) - 1;
+          at = r0 + j * 32 + l;
+          before += __shfl_sync(0xffffffffu, inc - tiles[j], l);
+        } else if (at < 0) {
+          before += sum;
+        }
       }
-      total += __reduce_add_sync(0xffffffffu, t);
-    }
-    // no more ranges than tiles: every range that is left holds one (the joining kernel counts on it)
-    const long long ranges = min((long long)p.parts, total);
-    if (part >= ranges) return;
-    const long long first_tile = part * total / ranges;
-    todo = (part + 1) * total / ranges - first_tile;
-    long long before = 0;
-    int at = 0;
-    for (int r0 = 0; r0 < p.n_req; r0 += 32) {
-      const int r = r0 + lane;
-      const int t = r < p.n_req ? max(1, (clamped_len(p, r) + TILE - 1) / TILE) : 0;
-      int inc = t;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int up = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += up;
-      }
-      const int sum = __shfl_sync(0xffffffffu, inc, 31);
-      if (first_tile < before + sum) {
-        const unsigned hit = __ballot_sync(0xffffffffu, first_tile < before + inc);
-        const int l = __ffs(hit) - 1;
-        at = r0 + l;
-        before += __shfl_sync(0xffffffffu, inc - t, l);
-        break;
-      }
-      before += sum;
     }
     cons.open(p, at, TILE);
     cons.tile = (int)(first_tile - before);
@@ -434,9 +439,16 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
 
   // ---- per request of the range
   int get = 0, seg = 0;
+  long long done = 0;
   while (todo > 0) {
     const int req = cons.r, n = cons.n, s_tile = cons.tile;
     const int steps = (int)min((long long)(cons.n_tiles - s_tile), todo);
+    // for the joining kernel: where the request's tiles start
+    if (p.parts > 0 && s_tile == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+      p.tile_start[req] = first_tile + done;
+      if (req == 0) p.tile_start[p.n_req] = total;
+    }
+    done += steps;
     uint32_t qf[QP][KS][2];
     float q_scale[2] = {p.scale, p.scale};
     {
