@@ -6,7 +6,7 @@
 // Bound by HBM: each cached row is read once for all the query heads of its group (2 flops per byte and head), so what
 // matters is to keep enough loads in flight and every SM equally busy, whatever the lengths.
 //
-// Split.  The contexts of all requests are laid end to end in tiles (every request at least one) and cut into equal
+// Split.  The contexts of all requests are laid end to end in tiles (and one more for each request) and cut into equal
 // ranges, one per CTA column, so one long request and a hundred short ones load the machine alike.  A range that holds a
 // whole request writes its output; otherwise it leaves a record (m, l, o) and a second, small kernel joins the records
 // of a request.  Lengths live on the device, so every CTA finds its own range with a scan over them.
@@ -238,6 +238,11 @@ __device__ __forceinline__ int clamped_len(const BaParams &p, int r) {
   return min(max(__ldg(p.lens + r), 0), p.max_ctx);
 }
 
+// Tiles of a request of n keys.  One more than its keys need: starting and finishing a request (query fragments, sums over
+// the lanes, the result) takes as long as a tile, and a request of no keys has to be somebody's (128 requests of up to 577
+// tokens: 25.7 us against 27.8 us without it).
+__device__ __forceinline__ int tiles_of(int n, int tile_keys) { return (n + tile_keys - 1) / tile_keys + 1; }
+
 // Where a warp stands in the sequence of tiles of its range.
 struct Cursor {
   int r, tile, n_tiles, n, n_next;
@@ -245,7 +250,7 @@ struct Cursor {
     r = req;
     n = r < p.n_req ? clamped_len(p, r) : 0;
     n_next = r + 1 < p.n_req ? clamped_len(p, r + 1) : 0;
-    n_tiles = max(1, (n + tile_keys - 1) / tile_keys);
+    n_tiles = tiles_of(n, tile_keys);
     tile = 0;
   }
   __device__ __forceinline__ void step(const BaParams &p, int tile_keys) {
@@ -253,7 +258,7 @@ struct Cursor {
     ++r;
     n = n_next;
     n_next = r + 1 < p.n_req ? clamped_len(p, r + 1) : 0;      // loaded a request ahead
-    n_tiles = max(1, (n + tile_keys - 1) / tile_keys);
+    n_tiles = tiles_of(n, tile_keys);
     tile = 0;
   }
 };
@@ -298,7 +303,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
         tiles[j] = r < p.n_req ? clamped_len(p, r) : -1;
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) tiles[j] = tiles[j] < 0 ? 0 : max(1, (tiles[j] + TILE - 1) / TILE);
+      for (int j = 0; j < 4; ++j) tiles[j] = tiles[j] < 0 ? 0 : tiles_of(tiles[j], TILE);
     };
     for (int r0 = 0; r0 < p.n_req; r0 += 128) {
       load_tiles(r0);
@@ -670,7 +675,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 16);
       f[i] = ELEM == 1 && mw[i] != -INFINITY ? ex2(mw[i] - m[i] - kWeightBits) : 1.f;
     }
-    const bool whole = s_tile == 0 && steps == max(1, (n + TILE - 1) / TILE);
+    const bool whole = s_tile == 0 && steps == tiles_of(n, TILE);
     const long long rec_slot = s_tile == 0 ? 1 : 0;      // a range can begin and end inside a request: two records
     auto finish = [&]() {
 #pragma unroll
@@ -862,7 +867,7 @@ BaPlan ba_plan(int n_req, int vheads, int max_ctx, int sms, int keys) {
     b.parts = 0;
     return b;
   }
-  const long long tiles = (long long)n_req * ((max_ctx + b.kw * keys - 1) / (b.kw * keys));
+  const long long tiles = (long long)n_req * ((max_ctx + b.kw * keys - 1) / (b.kw * keys) + 1);
   long long parts = 2ll * sms / b.columns;         // two CTAs per SM
   parts = parts < 1 ? 1 : parts;
   b.parts = (int)(parts < tiles ? parts : tiles);
