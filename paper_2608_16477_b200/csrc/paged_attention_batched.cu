@@ -848,8 +848,16 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(cons
   if (p.lse != nullptr && lane == 0) p.lse[(long long)req * p.n_q_heads + h] = (m + log2f(l)) * (1.f / kLog2e);
 }
 
-// Contexts of at most this many tokens are not split: one launch, a CTA per (request, KV head).
-constexpr int kBaWholeCtx = 512;
+// Short contexts are not split: one launch, a CTA per request and KV head or four.  Splitting costs a second kernel and the
+// search for the range (3 to 5 us), not splitting leaves the longest request to one CTA.  Measured (8 KV heads of 128, 64
+// query heads, uniform lengths; split against whole): one request of 400 tokens 7.6 / 7.3 us (8-bit), 7.6 / 8.2 (bf16), of
+// 1,000 7.8 / 10.7; 8 of up to 577 10.3 / 8.3 and 11.5 / 10.0, of 1,000 10.7 / 10.8 and 12.0 / 13.7; 32 of up to 577 13.1 /
+// 9.7, of 1,000 15.7 / 13.8; with a warp per KV head 128 of up to 400 23.7 / 20.7 and of up to 577 27.0 / 25.9 (fp32
+// queries: 25.7 / 30.0).
+int ba_whole_ctx(int n_req, int kw, int elem_bytes) {
+  if (kw == 1) return 512;
+  return n_req >= 8 ? 768 : (elem_bytes == 1 ? 512 : 384);
+}
 // Positions and the tiles of 32 requests are counted in 32 bits.
 constexpr int kBaMaxCtx = 1 << 26;
 
@@ -857,17 +865,18 @@ struct BaPlan {
   int kw, parts, columns;   // warps per KV head, ranges (0: a CTA per request), CTAs over the KV heads
 };
 
-BaPlan ba_plan(int n_req, int vheads, int max_ctx, int sms, int keys) {
+BaPlan ba_plan(int n_req, int vheads, int max_ctx, int sms, int elem_bytes) {
   BaPlan b;
   // A warp per KV head once the batch has a tile for every warp of the machine; four warps per head below that.
   b.kw = (long long)n_req * vheads >= 4ll * sms ? 1 : kBaWarps;
   const int per_cta = kBaWarps / b.kw;
   b.columns = (vheads + per_cta - 1) / per_cta;
-  if (max_ctx <= kBaWholeCtx) {
+  if (max_ctx <= ba_whole_ctx(n_req, b.kw, elem_bytes)) {
     b.parts = 0;
     return b;
   }
-  const long long tiles = (long long)n_req * ((max_ctx + b.kw * keys - 1) / (b.kw * keys) + 1);
+  // no more parts than 16-key tiles (the shortest there are) could give work to
+  const long long tiles = (long long)n_req * ((max_ctx + b.kw * 16 - 1) / (b.kw * 16) + 1);
   long long parts = 2ll * sms / b.columns;         // two CTAs per SM
   parts = parts < 1 ? 1 : parts;
   b.parts = (int)(parts < tiles ? parts : tiles);
@@ -941,7 +950,8 @@ int64_t kv_paged_attention_batched_scratch_bytes(int32_t n_req, int32_t n_q_head
   if (max_ctx > kBaMaxCtx) return KV_ERR_SHAPE;
   if (n_q_heads % n_kv_heads != 0 || (head_dim != 64 && head_dim != 128)) return KV_ERR_SHAPE;
   const int vheads = n_kv_heads * ba_passes(n_q_heads / n_kv_heads);
-  const BaPlan b = ba_plan(n_req > 0 ? n_req : 1, vheads, max_ctx, sm_count(current_device()), 16);
+  // bf16 pages are split first: what is enough for them is enough for either
+  const BaPlan b = ba_plan(n_req > 0 ? n_req : 1, vheads, max_ctx, sm_count(current_device()), 2);
   return b.parts == 0 ? 256 : ba_scratch(n_req, n_q_heads, head_dim, b.parts).bytes;
 }
 
@@ -976,7 +986,7 @@ int32_t kv_op_paged_attention_batched(const void *q_dev, int64_t q_stride, int32
   p.passes = ba_passes(p.group);
   const long long vheads = (long long)cache->n_kv_heads * p.passes;
   if (vheads > 65535 || n_q_heads > 65535) return KV_ERR_SHAPE;      // second dimension of the grids
-  const BaPlan b = ba_plan(n_req, (int)vheads, max_ctx, sm_count(device), 16);
+  const BaPlan b = ba_plan(n_req, (int)vheads, max_ctx, sm_count(device), cache->elem_bytes);
   const BaScratch s = ba_scratch(n_req, n_q_heads, cache->head_dim, b.parts);
   if (b.parts > 0) {
     if (scratch_dev == nullptr || ((uintptr_t)scratch_dev & 15) || scratch_bytes < s.bytes) return KV_ERR_WORKSPACE;
