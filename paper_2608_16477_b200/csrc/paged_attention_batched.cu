@@ -21,8 +21,9 @@
 // the query heads as the 8 columns: a KV group has 8 heads or fewer, so nothing is padding.  (A 128-row tcgen05 tile would
 // hold 8 useful columns of at least 16 as well, but wants its operands through shared-memory descriptors, and e4m3 rows
 // would have to be converted and written back there first.)  Groups of more than 8 heads are taken 8 at a time.
-// fp32 operands are split into two halves, hi + lo, that are multiplied one after the other: q for fp32 queries, and the
-// weights p, but for bf16 results over e4m3 pages: there p is one fp16, off by 2^-12, a sixteenth of the result's rounding.
+// fp32 operands go in as sums of 16-bit parts that are multiplied one after the other.  fp32 calls: q and the weights p in
+// three bf16 (bf16 pages) or two fp16 (e4m3 pages), 2^-23 or better.  bf16 calls: q is one part and exact; p is two bf16
+// (2^-16), or one fp16 over e4m3 pages (2^-12), a sixteenth of the rounding of the result.
 //
 // The running maximum is lazy: m is replaced only when a score passes it by more than 2^8, so most stages need no
 // reduction over the lanes and no rescaling; sums and weights have the head room for it.
@@ -136,20 +137,29 @@ __device__ __forceinline__ uint32_t half2_of_e4m3(uint32_t two) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
   return h;
 }
-// x = hi + lo: two bf16 with 16 significant bits together, two fp16 with 22
-__device__ __forceinline__ void split_bf16(float x, float y, uint32_t &hi, uint32_t &lo) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-  const float2 f = __bfloat1622float2(h);
-  const __nv_bfloat162 l = __floats2bfloat162_rn(x - f.x, y - f.y);
-  hi = *reinterpret_cast<const uint32_t *>(&h);
-  lo = *reinterpret_cast<const uint32_t *>(&l);
+// x and y as the sum of N bf16 each (8 significant bits a part) or of N fp16 (11): what a part leaves goes to the next.
+template <int N>
+__device__ __forceinline__ void split_bf16(float x, float y, uint32_t (&parts)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+    const float2 f = __bfloat1622float2(h);
+    parts[i] = *reinterpret_cast<const uint32_t *>(&h);
+    x -= f.x;
+    y -= f.y;
+  }
 }
-__device__ __forceinline__ void split_f16(float x, float y, uint32_t &hi, uint32_t &lo) {
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(y), "f"(x));
-  float fx, fy;
-  asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, u;\n\t}"
-      : "=f"(fx), "=f"(fy) : "r"(hi));
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(lo) : "f"(y - fy), "f"(x - fx));
+template <int N>
+__device__ __forceinline__ void split_f16(float x, float y, uint32_t (&parts)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(parts[i]) : "f"(y), "f"(x));
+    float fx, fy;
+    asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, u;\n\t}"
+        : "=f"(fx), "=f"(fy) : "r"(parts[i]));
+    x -= fx;
+    y -= fy;
+  }
 }
 // 8x8 16-bit values, two of a row to a lane -> the same of the transposed block
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
@@ -269,8 +279,8 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
   constexpr int KS = D / 16;                 // k-steps of S^T = K Q^T
   constexpr int NT = D / 8;                  // dims of a lane's V fragments (ELEM 1)
   constexpr int MO = D / 16;                 // 16-dim tiles of O^T
-  constexpr int QP = sizeof(T) == 4 ? 2 : 1;                    // parts of a query
-  constexpr int PP = ELEM == 1 && sizeof(T) == 2 ? 1 : 2;       // parts of a weight
+  constexpr int QP = sizeof(T) == 2 ? 1 : (ELEM == 1 ? 2 : 3);          // parts of a query
+  constexpr int PP = sizeof(T) == 2 ? (ELEM == 1 ? 1 : 2) : (ELEM == 1 ? 2 : 3);      // parts of a weight
   constexpr int CH = C::row / 16;            // 16-byte chunks of a row
   constexpr int RPI = 32 / CH;               // rows per copy instruction
   constexpr int KEYS = C::keys;
@@ -464,9 +474,10 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
             const float2 a = raw.pair(2 * ks + j);
-            uint32_t lo;
-            split_bf16(a.x * on, a.y * on, qf[0][ks][j], lo);      // a bf16 query is its own first half
-            if (QP == 2) qf[QP - 1][ks][j] = lo;
+            uint32_t parts[QP];
+            split_bf16(a.x * on, a.y * on, parts);      // a bf16 query is its own one part
+#pragma unroll
+            for (int h = 0; h < QP; ++h) qf[h][ks][j] = parts[h];
           }
         }
       } else {
@@ -489,9 +500,10 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
         for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            uint32_t lo;
-            split_f16(x[4 * ks + 2 * j] * up, x[4 * ks + 2 * j + 1] * up, qf[0][ks][j], lo);      // bf16: exact in one
-            if (QP == 2) qf[QP - 1][ks][j] = lo;
+            uint32_t parts[QP];
+            split_f16(x[4 * ks + 2 * j] * up, x[4 * ks + 2 * j + 1] * up, parts);      // bf16: exact in one
+#pragma unroll
+            for (int h = 0; h < QP; ++h) qf[h][ks][j] = parts[h];
           }
         }
       }
@@ -609,13 +621,13 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
           const float p0 = ex2(t[j][0] - m_sub[0]), p1 = ex2(t[j][1] - m_sub[1]);
           l[0] += p0;
           l[1] += p1;
-          uint32_t hi, lo;
+          uint32_t parts[PP];
           if (ELEM == 2)
-            split_bf16(p0, p1, hi, lo);
+            split_bf16(p0, p1, parts);
           else
-            split_f16(ex2(t[j][0] + ev[j] - w_sub[0]), ex2(t[j][1] + ev[j] - w_sub[1]), hi, lo);
-          pf[0][j] = transpose8(hi);
-          if (PP == 2) pf[PP - 1][j] = transpose8(lo);
+            split_f16(ex2(t[j][0] + ev[j] - w_sub[0]), ex2(t[j][1] + ev[j] - w_sub[1]), parts);
+#pragma unroll
+          for (int h = 0; h < PP; ++h) pf[h][j] = transpose8(parts[h]);
         }
         if ((poison >> get) & 1u) l[0] = l[1] = __uint_as_float(0x7fc00000u);   // a row outside the pool: the request is NaN
         // ---- O^T += V^T P^T
