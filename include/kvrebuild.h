@@ -136,7 +136,8 @@ const char *kv_status_string(int32_t status);
 /* Text of the last CUDA error seen by this thread's calls ("" if none). */
 const char *kv_last_cuda_error(void);
 
-/* Eq. (1): s_KV = 2 * L * H_KV * d_h * b bytes per token. */
+/* Eq. (1): s_KV = 2 * L * H_KV * d_h * b bytes per token (the values; e4m3 pages add one scale byte per layer, K or V and
+ * KV head: kv_cache_page_bytes()). */
 int64_t kv_bytes_per_token(int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t elem_bytes);
 
 /* Bytes of one page (one layer, K or V, one block): elem_bytes 2 = bf16 values, 1 = e4m3 codes and their scale bytes. */
@@ -316,7 +317,8 @@ int32_t kv_op_paged_attention_noalloc(const float *q_dev, int32_t n_q_heads, con
  *   KV_ROPE_SCALE_PARTS   g_j = clamp((original_ctx * theta_j / (2 pi) - low) / (high - low), 0, 1): pairs that turn more
  *                         than `high` times within original_ctx keep theta_j, those below `low` take theta_j / factor,
  *                         (1 - g_j) theta_j / factor + g_j theta_j between them
- * rotary_dim is even and at most 256; base, factor and gain are finite and positive; high > low. */
+ * rotary_dim is even and at most 256; base, factor and gain are finite and positive; high > low; no pair may turn by more
+ * than one radian per position (a base below 1, or a factor that speeds positions up, is refused with KV_ERR_ARG). */
 typedef struct {
   int32_t rotary_dim, layout, scaling;
   double base, factor, original_ctx, low, high, gain;

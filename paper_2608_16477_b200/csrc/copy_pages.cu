@@ -6,8 +6,8 @@
 // compiled: up to 896 ids / 8 requests (under 4 KiB, the single-request calls of the migration path) and up
 // to 7,680 ids / 64 requests (under the 32 KiB limit of the launch interface, the batched calls); longer
 // lists are split over several launches.
-// A page (block_size * n_kv_heads * head_dim bf16) is contiguous on both sides; it moves as 16 KiB
-// bulk copies (cp.async.bulk) through a shared-memory ring.  HBM-bound: 2 * page bytes of traffic
+// A page (block_size * n_kv_heads * head_dim bf16, or as many e4m3 codes and their scale bytes) is contiguous on both sides;
+// it moves as bulk copies (cp.async.bulk) of 16 KiB, a little more for e4m3 pages, through a shared-memory ring.  HBM-bound: 2 * page bytes of traffic
 // per page, nothing is re-read.
 #include <vector>
 
@@ -16,6 +16,9 @@
 namespace kvr {
 
 constexpr int kPieceBytes = 16384;    // bytes per bulk copy
+// An e4m3 page is a power of two of codes and a few scale bytes: cut at 16 KiB it would leave a scrap that takes a slot of
+// the ring of its own, so its pieces are equal parts of at most this.
+constexpr int kPieceBytesE4m3 = 18432;
 constexpr int kBufs = 8;              // shared-memory ring: 128 KiB per CTA, one CTA per SM (measured best: ~128 KiB in flight per SM)
 constexpr int kLag = 4;               // stores left in flight before a slot is refilled (kBufs - kLag loads in flight)
 constexpr int kCopyThreads = 32;
@@ -36,7 +39,8 @@ struct PageCopyParams {
   int n_segs;
   int layout;                // KV_WIRE_BLOCK_MAJOR / KV_WIRE_LAYER_MAJOR
   int page_bytes;
-  int pieces_per_page;       // ceil(page_bytes / kPieceBytes)
+  int piece_bytes;           // multiple of 128
+  int pieces_per_page;       // ceil(page_bytes / piece_bytes)
   CopySegment segs[MAX_SEGS];
   int ids[MAX_IDS];
 };
@@ -103,13 +107,13 @@ __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_c
       wire_page = ((long long)w * p.n_layers + layer) * 2 + kv;
     else
       wire_page = ((long long)layer * 2 + kv) * sg.wire_total + w;
-    const long long off = (long long)piece * kPieceBytes;
+    const long long off = (long long)piece * p.piece_bytes;
     char *c = p.cache.page(layer, kv, p.ids[i]) + off;
     char *wp = sg.wire + wire_page * p.page_bytes + off;
     src = TO_WIRE ? c : wp;
     dst = TO_WIRE ? wp : c;
     const long long left = p.page_bytes - off;
-    bytes = (uint32_t)(left < kPieceBytes ? left : kPieceBytes);
+    bytes = (uint32_t)(left < p.piece_bytes ? left : p.piece_bytes);
   };
   int load_seg = 0, store_seg = 0;
   auto load = [&](long long k) {
@@ -119,7 +123,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_c
     const uint32_t bar = cp_smem(&full[slot]);
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(cp_smem(ring + slot * kPieceBytes)), "l"(src), "r"(bytes), "r"(bar) : "memory");
+                 ::"r"(cp_smem(ring + slot * p.piece_bytes)), "l"(src), "r"(bytes), "r"(bar) : "memory");
   };
 
   const long long prologue = mine < kBufs ? mine : kBufs;
@@ -130,7 +134,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const __grid_c
     const char *src; char *dst; uint32_t bytes;
     locate(k, store_seg, src, dst, bytes);
     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
-                 ::"l"(dst), "r"(cp_smem(ring + slot * kPieceBytes)), "r"(bytes) : "memory");
+                 ::"l"(dst), "r"(cp_smem(ring + slot * p.piece_bytes)), "r"(bytes) : "memory");
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     // refill the slot of item k - kLag once its store has read it: up to kLag younger stores stay pending, so
     // the issuing thread never waits on the store it has just issued
@@ -149,9 +153,9 @@ int launch_copy(const Params &p, bool to_wire, int sms, cudaStream_t st) {
   const long long items = (long long)p.n_blocks * p.n_layers * 2 * p.pieces_per_page;
   const int grid = (int)(items < sms ? items : sms);
   if (to_wire)
-    copy_pages_kernel<true, Params><<<grid, kCopyThreads, kBufs * kPieceBytes, st>>>(p);
+    copy_pages_kernel<true, Params><<<grid, kCopyThreads, kBufs * p.piece_bytes, st>>>(p);
   else
-    copy_pages_kernel<false, Params><<<grid, kCopyThreads, kBufs * kPieceBytes, st>>>(p);
+    copy_pages_kernel<false, Params><<<grid, kCopyThreads, kBufs * p.piece_bytes, st>>>(p);
   KV_COUNT_LAUNCH();
   KV_CUDA(cudaGetLastError());
   return KV_OK;
@@ -168,7 +172,12 @@ int copy_requests(const CacheView &cache, int n_layers, const CopyRequest *reqs,
     p.n_layers = n_layers;
     p.layout = wire_layout;
     p.page_bytes = (int)cache.page_bytes();
-    p.pieces_per_page = (p.page_bytes + kPieceBytes - 1) / kPieceBytes;
+    p.piece_bytes = kPieceBytes;
+    if (cache.elem_bytes == 1) {
+      const int pieces = (p.page_bytes + kPieceBytesE4m3 - 1) / kPieceBytesE4m3;
+      p.piece_bytes = ((p.page_bytes + pieces - 1) / pieces + 127) / 128 * 128;
+    }
+    p.pieces_per_page = (p.page_bytes + p.piece_bytes - 1) / p.piece_bytes;
     p.n_blocks = 0;
     p.n_segs = 0;
   };
@@ -206,13 +215,13 @@ int copy_pages(CacheView cache, int n_layers, const CopyRequest *reqs, int n_req
   if (device < 0) return KV_ERR_CUDA;
   if (!attr_set[device]) {
     KV_CUDA(cudaFuncSetAttribute(copy_pages_kernel<true, SmallCopyParams>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kBufs * kPieceBytes));
+                                 kBufs * kPieceBytesE4m3));
     KV_CUDA(cudaFuncSetAttribute(copy_pages_kernel<false, SmallCopyParams>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kBufs * kPieceBytes));
+                                 kBufs * kPieceBytesE4m3));
     KV_CUDA(cudaFuncSetAttribute(copy_pages_kernel<true, LargeCopyParams>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kBufs * kPieceBytes));
+                                 kBufs * kPieceBytesE4m3));
     KV_CUDA(cudaFuncSetAttribute(copy_pages_kernel<false, LargeCopyParams>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kBufs * kPieceBytes));
+                                 kBufs * kPieceBytesE4m3));
     attr_set[device] = true;
   }
   const int sms = sm_count(device);

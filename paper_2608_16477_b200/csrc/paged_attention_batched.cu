@@ -975,7 +975,7 @@ int32_t kv_op_paged_attention_batched(const void *q_dev, int64_t q_stride, int32
                                       float *lse_out_dev, void *stream) {
   using namespace kvr;
   if (n_req < 0 || n_q_heads <= 0 || max_ctx <= 0 || (dtype != KV_DTYPE_BF16 && dtype != KV_DTYPE_F32)) return KV_ERR_ARG;
-  if (!(softmax_scale > 0.f) || softmax_scale > FLT_MAX) return KV_ERR_ARG;
+  if (!(softmax_scale > 0.f) || softmax_scale > FLT_MAX / 2.f) return KV_ERR_ARG;      // times log2(e) it stays finite
   if (max_ctx > kBaMaxCtx) return KV_ERR_SHAPE;
   int rc = check_cache_desc(cache, true);
   if (rc != KV_OK) return rc;

@@ -3,7 +3,8 @@
 //
 // (y_a, y_b) = gain * (a cos - b sin, b cos + a sin) with the angle p * theta_j.  The angle is formed in TURNS,
 // p * (theta_j / 2 pi), in fp64 and reduced to [-1/2, 1/2] there; the remainder goes to fp32 sincospi.  That costs three
-// fp64 operations instead of an fp64 sine and cosine and is exact to 2^-24 of a turn for every int32 position.
+// fp64 operations instead of an fp64 sine and cosine and, with theta_j <= 1, is exact to 2^-24 of a turn for every int32
+// position (2^31 / 2 pi turns are less than 2^29, where fp64 has steps of 2^-24).
 //
 // HBM-bound: 2 * rows * head_dim elements move (3 fma per element).  A token's cosines and sines are needed by all its
 // heads, so a CTA takes 1 to 4 whole tokens, its threads form each (token, pair) once into shared memory, and the heads
@@ -262,7 +263,7 @@ int32_t kv_rope_create(const kv_rope_desc *desc, kv_rope **out) {
       g = g < 0.0 ? 0.0 : (g > 1.0 ? 1.0 : g);
       theta = (1.0 - g) * theta / d.factor + g * theta;
     }
-    if (!std::isfinite(theta)) {
+    if (!(theta <= 1.0)) {      // what the reduction of the angle in turns counts on
       delete r;
       return KV_ERR_ARG;
     }

@@ -590,3 +590,40 @@ def test_a_batch_migrates_and_decodes(kv, torch, elem, wire_layout):
             share = most * 2.0 ** -13 + 2.0 ** -14 + (n / 16 + 64) * 2.0 ** -22
             assert (np.abs(_np(out)[r] - o) <= size * share + 2.0 ** -8 * np.abs(o) * 1.01).all()
             assert (np.abs(_np(lse)[r] - ls) <= share + 2.0 ** -23 * np.abs(ls)).all()
+
+
+def test_two_calls_at_once(kv, torch):
+    """Two batches on two streams at the same time, each with scratch of its own, over and over."""
+    a = Batch(kv, torch, [3000, 90, 700], 8, 8, 128, 16, 1, torch.bfloat16)
+    b = Batch(kv, torch, [2500, 1, 0, 1800], 8, 4, 128, 16, 2, torch.float32, seed=2)
+    a.run(kv); b.run(kv)
+    torch.cuda.synchronize()
+    want = a.out.clone(), b.out.clone()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(30):
+        a.run(kv, stream=streams[0])
+        b.run(kv, stream=streams[1])
+    torch.cuda.synchronize()
+    assert torch.equal(a.out, want[0]) and torch.equal(b.out, want[1])
+
+
+@pytest.mark.parametrize("case", [(8, 128, 16), (3, 64, 7), (8, 128, 64), (2, 64, 16), (1, 64, 4)], ids=str)
+def test_e4m3_pages_travel_whole(kv, torch, case):
+    """Pack and unpack of e4m3 pages (one piece, several equal ones, a short one), scale bytes and padding included."""
+    hkv, d, block = case
+    shape = _shape(hkv, d, block, layers=2)
+    for layout in ("layer_major", "block_major"):
+        src, dst = (kv.PagedCache(shape, 13, layout=layout, elem_bytes=1) for _ in range(2))
+        src.data.copy_(torch.randint(0, 256, src.data.shape, device="cuda", dtype=torch.uint8))
+        dst.data.fill_(0xA5)
+        ids, to = [7, 0, 12, 3, 5], [1, 11, 4, 2, 9]
+        wire = torch.full((5 * 4 * src.page_bytes + 64,), 0x3C, dtype=torch.uint8, device="cuda")
+        kv.kv_pack_blocks_batched(src, [0, 3, 5], ids, [wire, wire[3 * 4 * src.page_bytes:]])
+        kv.kv_unpack_blocks_batched(dst, [0, 3, 5], to, [wire, wire[3 * 4 * src.page_bytes:]])
+        kv.kv_check_copy_status()
+        a, b = _pages_numpy(src), _pages_numpy(dst)
+        assert np.array_equal(a[:, :, ids], b[:, :, to]) and (wire[-64:] == 0x3C).all()
+        assert (b[:, :, np.setdiff1d(np.arange(13), to)] == 0xA5).all()
+        assert np.array_equal(wire[:src.page_bytes].cpu().numpy(), a[0, 0, 7])

@@ -129,10 +129,10 @@ def test_rope_plan_refusals(kv):
         return e.value.status
     for rotary in (0, -2, 7, 258):
         assert status(rotary) == O.ERR_SHAPE
-    for base in (0.0, -1.0, math.inf, math.nan):
+    for base in (0.0, -1.0, math.inf, math.nan, 0.5):         # 0.5: pairs that turn by more than a radian a position
         assert status(64, base=base) == O.ERR_ARG
     assert status(64, gain=0.0) == O.ERR_ARG
-    assert status(64, scaling="linear", factor=0.0) == O.ERR_ARG
+    assert status(64, scaling="linear", factor=0.0) == status(64, scaling="linear", factor=0.5) == O.ERR_ARG
     assert status(2, scaling="ntk", factor=2.0) == O.ERR_SHAPE
     assert status(64, scaling="parts", factor=2.0, original_ctx=0.0) == O.ERR_ARG
     assert status(64, scaling="parts", factor=2.0, original_ctx=10.0, low=4.0, high=4.0) == O.ERR_ARG
@@ -220,7 +220,7 @@ def test_batched_attention_refusals(kv, elem):
     assert call(r=-1) == call(hq=0) == call(ctx=0) == call(dtype=2) == O.ERR_ARG
     for p in ("q", "tab", "lens", "out"):
         assert call(**{p: None}) == O.ERR_ARG
-    for s in (0.0, -1.0, math.inf, math.nan):
+    for s in (0.0, -1.0, math.inf, math.nan, 3e38):
         assert call(scale=s) == O.ERR_ARG
     assert call(q=q + 8) == call(out=out + 8) == call(tab=tab + 2) == call(lens=lens + 1) == call(lse=lse + 2) == O.ERR_ARG
     assert call(qs=1020) == call(os=1020) == call(os=1016) == call(qs=-1024) == call(ts=-1) == O.ERR_ARG
