@@ -361,7 +361,9 @@ int32_t kv_op_cache_read(const kv_cache_desc *cache, int32_t layer, const int64_
  * lse = log sum_n exp(s_n) (fp32 [n_req][n_q_heads], natural logarithm; NULL to leave it out), so results over disjoint
  * parts of a context can be joined.  A request of length 0 gets out = 0, lse = -inf.  Lengths are clamped to [0, max_ctx]
  * with max_ctx <= table_stride * block_size and at most 2^26; table entries behind a request's last block are not read.  A block id
- * outside the pool inside a context is not followed: that request's out and lse are NaN.  fp32 sums and softmax.
+ * outside the pool inside a context is not followed: that request's out and lse are NaN.  Infinities and NaN in a query, or
+ * among the cached values inside its context, make the results they reach NaN; what lies behind a context enters no result.
+ * fp32 sums and softmax.  out may be q itself with the same strides.
  * scratch_dev: kv_paged_attention_batched_scratch_bytes() bytes, 16-byte aligned, contents need not survive between calls;
  * calls that may overlap on the GPU need scratch of their own.  head_dim 64 or 128. */
 int64_t kv_paged_attention_batched_scratch_bytes(int32_t n_req, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,

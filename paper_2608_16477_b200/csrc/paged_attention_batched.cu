@@ -11,7 +11,7 @@
 // whole request writes its output; otherwise it leaves a record (m, l, o) and a second, small kernel joins the records
 // of a request.  Lengths live on the device, so every CTA finds its own range with a scan over them.
 //
-// A warp works alone: it copies 16 keys of one KV head (K and V rows, 16 bytes per cp.async, whole rows per instruction)
+// A warp works alone: it copies 16 or 32 keys of one KV head (K and V rows, 16 bytes per cp.async, whole rows per instruction)
 // into a ring of its own and consumes them stage by stage with no barrier but the warp's, so loads never wait for other
 // warps and run on across the end of a request.  Four warps of a CTA take four KV heads (batches: neighbouring heads'
 // rows are neighbouring memory), or every fourth stage of one KV head (few requests: four times fewer records; their
@@ -21,9 +21,10 @@
 // the query heads as the 8 columns: a KV group has 8 heads or fewer, so nothing is padding.  (A 128-row tcgen05 tile would
 // hold 8 useful columns of at least 16 as well, but wants its operands through shared-memory descriptors, and e4m3 rows
 // would have to be converted and written back there first.)  Groups of more than 8 heads are taken 8 at a time.
-// fp32 operands go in as sums of 16-bit parts that are multiplied one after the other.  fp32 calls: q and the weights p in
-// three bf16 (bf16 pages) or two fp16 (e4m3 pages), 2^-23 or better.  bf16 calls: q is one part and exact; p is two bf16
-// (2^-16), or one fp16 over e4m3 pages (2^-12), a sixteenth of the rounding of the result.
+// fp32 operands go in as sums of 16-bit parts that are multiplied one after the other.  Over e4m3 pages q and the weights p
+// are two fp16 (2^-22; a bf16 query is one, and exact); over bf16 pages they are three bf16 in fp32 calls (2^-24), in bf16
+// calls q is one part and p two (2^-16, a 256th of the rounding of the result).  The second part of the weights costs bf16
+// calls over e4m3 pages 0.5 % (128 requests of up to 577 tokens: 1.6 %): the loads are what bounds them.
 //
 // The running maximum is lazy: m is replaced only when a score passes it by more than 2^8, so most stages need no
 // reduction over the lanes and no rescaling; sums and weights have the head room for it.
@@ -296,7 +297,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
   constexpr int NT = D / 8;                  // dims of a lane's V fragments (ELEM 1)
   constexpr int MO = D / 16;                 // 16-dim tiles of O^T
   constexpr int QP = sizeof(T) == 2 ? 1 : (ELEM == 1 ? 2 : 3);          // parts of a query
-  constexpr int PP = sizeof(T) == 2 ? (ELEM == 1 ? 1 : 2) : (ELEM == 1 ? 2 : 3);      // parts of a weight
+  constexpr int PP = sizeof(T) == 4 && ELEM == 2 ? 3 : 2;                // parts of a weight
   constexpr int CH = C::row / 16;            // 16-byte chunks of a row
   constexpr int RPI = 32 / CH;               // rows per copy instruction
   constexpr int KEYS = C::keys;
@@ -372,7 +373,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
   // table entry can be a microsecond away.
   Cursor prod = cons;
   long long to_look = todo;
-  int blks[kLookAhead], offs[kLookAhead];    // of the next stages to be copied: block of the lane's row (-1: none), slot
+  int blks[kLookAhead], offs[kLookAhead];    // of the next stages to be copied: block and slot of the lane's row (kNoRow: none)
   const int my_row = lane % KEYS;
   auto look_up = [&](int &blk, int &off) {
     const int pos = (prod.tile * KW + kg) * KEYS + my_row;

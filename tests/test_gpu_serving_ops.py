@@ -592,6 +592,16 @@ def test_a_batch_migrates_and_decodes(kv, torch, elem, wire_layout):
             assert (np.abs(_np(lse)[r] - ls) <= share + 2.0 ** -23 * np.abs(ls)).all()
 
 
+@pytest.mark.parametrize("lens", [[300, 20], [3000, 0, 900], [40] * 150])
+def test_attention_in_place_of_its_queries(kv, torch, lens):
+    b = Batch(kv, torch, lens, 4, 12, 64, 16, 1, torch.bfloat16)
+    b.run(kv)
+    want = b.out.clone()
+    b.out = b.q
+    b.run(kv)
+    assert torch.equal(b.out, want)
+
+
 def test_two_calls_at_once(kv, torch):
     """Two batches on two streams at the same time, each with scratch of its own, over and over."""
     a = Batch(kv, torch, [3000, 90, 700], 8, 8, 128, 16, 1, torch.bfloat16)
