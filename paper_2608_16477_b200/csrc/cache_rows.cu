@@ -2,16 +2,17 @@
 //
 // e4m3 pages: one scale 2^e per (token, KV head) of K and of V, e the least integer with max |x| <= 448 * 2^e.  A power
 // of two instead of max / 448: x * 2^-e and code * 2^e are exact, so a stored value is x rounded once to four significant
-// bits (the e4m3 format itself has 2^-9 .. 448 to spread over, so the up to one binade that the power of two gives away
-// costs only values below 2^-15 of the row's maximum), the two directions need no division, and reading back into bf16
-// is exact.
+// bits, the two directions need no division, and reading back into bf16 is exact.  The price is up to one binade of the
+// range: codes keep their four bits down to 2^-6, which is 2^-13.8 of the row's maximum at the worst and 2^-14.8 at best.
 //
 // HBM-bound: every value is read once and written once; instructions are what has to be saved beside that.  head_dim / 16
 // lanes own a row, the row maximum is a shuffle over them; a lane has two pieces of 8 values, half a row apart, so that
-// consecutive lanes move consecutive 16-byte (bf16) or 8-byte (codes) pieces.  A thread keeps its place in the token (K or V, head, piece) for all its tokens, so that only
-// the slot's page has to be worked out for each; once there are tokens enough it takes four, with their slots, then all
-// their loads, in flight together.  The maximum runs over the raw bits (an infinity or NaN shows in it, and only then the
-// row is gone through value by value).
+// consecutive lanes move consecutive 16-byte (bf16) or 8-byte (codes) pieces.  A thread keeps its place in the token (K or
+// V, head, piece) for all its tokens, so that only the slot's page has to be worked out for each; once there are tokens
+// enough it takes two at a time, with their slots, then all their loads, in flight together.  The maximum runs over the raw
+// bits (an infinity or NaN shows in it, and only then the row is gone through value by value).  Measured: 16,384 tokens of
+// 8 heads of 128, bf16 to e4m3 and back, 101 MB each way: 18.8 us (5.4 TB/s, 82 % of a copy's rate with the launch in it);
+// 64 tokens 2.0 us.  A piece of 8 to a lane and index arithmetic for every row: 161 instructions a warp and row, 27 us.
 #include <float.h>
 
 #include "common.cuh"

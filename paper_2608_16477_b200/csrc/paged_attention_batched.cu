@@ -4,7 +4,10 @@
 //   s_n = scale * q . k_n      o = sum_n 2^(t_n - m) v_n / sum_n 2^(t_n - m)      t = s * log2(e), m = max t
 //
 // Bound by HBM: each cached row is read once for all the query heads of its group (2 flops per byte and head), so what
-// matters is to keep enough loads in flight and every SM equally busy, whatever the lengths.
+// matters is to keep enough loads in flight (135 KB an SM) and every SM equally busy, whatever the lengths.  Measured, 64
+// query and 8 KV heads of 128: 32 requests of up to 18,433 tokens over e4m3 pages (512 MB) 89 to 95 us, 5.4 to 5.8 TB/s; 16 of
+// up to 8,192 over bf16 pages (305 MB) 54 us, 5.6 TB/s; one of 18,433 (38 MB) 16 us, of which 9 us are the fixed cost of a
+// split call.
 //
 // Split.  The contexts of all requests are laid end to end in tiles (and one more for each request) and cut into equal
 // ranges, one per CTA column, so one long request and a hundred short ones load the machine alike.  A range that holds a
