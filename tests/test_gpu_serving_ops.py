@@ -65,6 +65,13 @@ ROPE = [  # tokens, heads, head_dim, rotary, layout, scaling, dtype, arrangement
     (700, 2, 256, 256, "half", dict(), "bfloat16", "plain"),
     (2500, 3, 64, 64, "interleaved", dict(), "bfloat16", "plain"),   # several tokens to a CTA, the last one short
     (4, 40, 64, 2, "half", dict(), "float32", "plain"),
+    (19, 21, 128, 102, "half", dict(), "bfloat16", "qkv"),           # halves that start on different places of a vector
+    (19, 9, 128, 102, "interleaved", dict(), "bfloat16", "qkv"),     # ... and pairs that end inside one
+    (700, 3, 1024, 250, "half", dict(), "float32", "heads"),
+    (6, 5, 72, 70, "interleaved", dict(), "bfloat16", "plain"),
+    (6, 5, 72, 72, "interleaved", dict(), "float32", "plain"),
+    (3, 19, 1024, 6, "half", dict(), "bfloat16", "plain"),
+    (2, 3, 68, 66, "half", dict(), "float32", "heads"),
 ]
 
 
