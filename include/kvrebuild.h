@@ -340,7 +340,7 @@ int32_t kv_op_rope(const kv_rope *rope, const void *x_dev, int64_t x_token_strid
 /* K and V rows of n_tokens tokens into layer `layer` of the cache.  Token t goes to slot slots_dev[t] = block *
  * block_size + offset; a slot outside the pool (-1 marks padding) is left out: nothing is written for that token.  The
  * slots of one call are distinct; what a slot that is listed twice holds afterwards is undefined (other slots are not
- * affected).  head_dim 64 or 128.
+ * affected).  head_dim 64 or 128, n_tokens at most 2^30.
  * bf16 pages: each value rounded to nearest even.  e4m3 pages: for every (token, KV head) of K and of V, e is the least
  * integer with max |x| <= 448 * 2^e, kept within [-110, 119]; the codes are x * 2^-e (exact) rounded to nearest even and
  * saturated at 448, the scale byte is e + 127.  Infinities and NaN are left out of the maximum and stored as NaN. */
@@ -364,8 +364,9 @@ int32_t kv_op_cache_read(const kv_cache_desc *cache, int32_t layer, const int64_
  * outside the pool inside a context is not followed: that request's out and lse are NaN.  Infinities and NaN in a query, or
  * among the cached values inside its context, make the results they reach NaN; what lies behind a context enters no result.
  * fp32 sums and softmax.  out may be q itself with the same strides.
- * scratch_dev: kv_paged_attention_batched_scratch_bytes() bytes, 16-byte aligned, contents need not survive between calls;
- * calls that may overlap on the GPU need scratch of their own.  head_dim 64 or 128. */
+ * scratch_dev: kv_paged_attention_batched_scratch_bytes() bytes (what is enough for n_req and max_ctx is enough for fewer
+ * requests and a smaller max_ctx), 16-byte aligned, contents need not survive between calls; calls that may overlap on the
+ * GPU need scratch of their own.  head_dim 64 or 128. */
 int64_t kv_paged_attention_batched_scratch_bytes(int32_t n_req, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                                  int32_t max_ctx);
 int32_t kv_op_paged_attention_batched(const void *q_dev, int64_t q_stride, int32_t dtype, int32_t n_req,

@@ -896,27 +896,26 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(cons
 // 1,000 7.8 / 10.7; 8 of up to 577 10.3 / 8.3 and 11.5 / 10.0, of 1,000 10.7 / 10.8 and 12.0 / 13.7; 32 of up to 577 13.1 /
 // 9.7, of 1,000 15.7 / 13.8; with a warp per KV head 128 of up to 400 23.7 / 20.7 and of up to 577 27.0 / 25.9 (fp32
 // queries: 25.7 / 30.0).
+constexpr int kBaNeverSplit = 384;   // the least that this can be
 int ba_whole_ctx(int n_req, int kw, int elem_bytes) {
   if (kw == 1) return 512;
-  return n_req >= 8 ? 768 : (elem_bytes == 1 ? 512 : 384);
+  return n_req >= 8 ? 768 : (elem_bytes == 1 ? 512 : kBaNeverSplit);
 }
 // Positions and the tiles of 32 requests are counted in 32 bits.
 constexpr int kBaMaxCtx = 1 << 26;
 
 struct BaPlan {
-  int kw, parts, columns;   // warps per KV head, ranges (0: a CTA per request), CTAs over the KV heads
+  int kw, parts, columns;   // warps per KV head, ranges if contexts are split, CTAs over the KV heads
+  bool whole;               // they are not: a CTA per request
 };
 
-BaPlan ba_plan(int n_req, int vheads, int max_ctx, int sms, int elem_bytes) {
+BaPlan ba_plan(int n_req, int vheads, int max_ctx, int elem_bytes, int sms) {
   BaPlan b;
   // A warp per KV head once the batch has a tile for every warp of the machine; four warps per head below that.
   b.kw = (long long)n_req * vheads >= 4ll * sms ? 1 : kBaWarps;
   const int per_cta = kBaWarps / b.kw;
   b.columns = (vheads + per_cta - 1) / per_cta;
-  if (max_ctx <= ba_whole_ctx(n_req, b.kw, elem_bytes)) {
-    b.parts = 0;
-    return b;
-  }
+  b.whole = max_ctx <= ba_whole_ctx(n_req, b.kw, elem_bytes);
   // no more parts than 16-key tiles (the shortest there are) could give work to
   const long long tiles = (long long)n_req * ((max_ctx + b.kw * 16 - 1) / (b.kw * 16) + 1);
   long long parts = 2ll * sms / b.columns;         // two CTAs per SM
@@ -948,11 +947,11 @@ int ba_launch(const BaParams &p, const BaPlan &b, int device, cudaStream_t st) {
     KV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BaCfg<D, ELEM>::smem(KW)));
     attr_set[device] = true;
   }
-  const dim3 grid(b.parts == 0 ? p.n_req : b.parts, b.columns);
+  const dim3 grid(b.whole ? p.n_req : b.parts, b.columns);
   kernel<<<grid, kBaThreads, BaCfg<D, ELEM>::smem(KW), st>>>(p);
   KV_COUNT_LAUNCH();
   KV_CUDA(cudaGetLastError());
-  if (b.parts == 0) return KV_OK;
+  if (b.whole) return KV_OK;
   // four warps per head while every block of such a grid can be resident at once
   const int wph = (long long)p.n_req * p.n_q_heads <= 8ll * sm_count(device) ? 4 : 1, heads = kJoinThreads / 32 / wph;
   cudaLaunchConfig_t cfg = {};
@@ -992,9 +991,10 @@ int64_t kv_paged_attention_batched_scratch_bytes(int32_t n_req, int32_t n_q_head
   if (max_ctx > kBaMaxCtx) return KV_ERR_SHAPE;
   if (n_q_heads % n_kv_heads != 0 || (head_dim != 64 && head_dim != 128)) return KV_ERR_SHAPE;
   const int vheads = n_kv_heads * ba_passes(n_q_heads / n_kv_heads);
-  // bf16 pages are split first: what is enough for them is enough for either
-  const BaPlan b = ba_plan(n_req > 0 ? n_req : 1, vheads, max_ctx, sm_count(current_device()), 2);
-  return b.parts == 0 ? 256 : ba_scratch(n_req, n_q_heads, head_dim, b.parts).bytes;
+  // As if contexts were split wherever any batch's are: more requests and longer contexts never need less (a warp per KV head
+  // makes more ranges than four do), so that scratch for the largest batch serves every smaller one.
+  if (max_ctx <= kBaNeverSplit || n_req == 0) return 256;
+  return ba_scratch(n_req, n_q_heads, head_dim, ba_plan(n_req, vheads, max_ctx, 2, sm_count(current_device())).parts).bytes;
 }
 
 int32_t kv_op_paged_attention_batched(const void *q_dev, int64_t q_stride, int32_t dtype, int32_t n_req,
@@ -1028,9 +1028,9 @@ int32_t kv_op_paged_attention_batched(const void *q_dev, int64_t q_stride, int32
   p.passes = ba_passes(p.group);
   const long long vheads = (long long)cache->n_kv_heads * p.passes;
   if (vheads > 65535 || n_q_heads > 65535) return KV_ERR_SHAPE;      // second dimension of the grids
-  const BaPlan b = ba_plan(n_req, (int)vheads, max_ctx, sm_count(device), cache->elem_bytes);
+  const BaPlan b = ba_plan(n_req, (int)vheads, max_ctx, cache->elem_bytes, sm_count(device));
   const BaScratch s = ba_scratch(n_req, n_q_heads, cache->head_dim, b.parts);
-  if (b.parts > 0) {
+  if (!b.whole) {
     if (scratch_dev == nullptr || ((uintptr_t)scratch_dev & 15) || scratch_bytes < s.bytes) return KV_ERR_WORKSPACE;
   }
   if (device < 0) return KV_ERR_CUDA;
@@ -1052,7 +1052,7 @@ int32_t kv_op_paged_attention_batched(const void *q_dev, int64_t q_stride, int32
   p.n_req = n_req;
   p.n_q_heads = n_q_heads;
   p.max_ctx = max_ctx;
-  p.parts = b.parts;
+  p.parts = b.whole ? 0 : b.parts;
   p.scale = softmax_scale * kLog2e;
   char *base = static_cast<char *>(scratch_dev);
   p.tile_start = reinterpret_cast<long long *>(base);

@@ -644,3 +644,42 @@ def test_e4m3_pages_travel_whole(kv, torch, case):
         assert np.array_equal(a[:, :, ids], b[:, :, to]) and (wire[-64:] == 0x3C).all()
         assert (b[:, :, np.setdiff1d(np.arange(13), to)] == 0xA5).all()
         assert np.array_equal(wire[:src.page_bytes].cpu().numpy(), a[0, 0, 7])
+
+
+def test_e4m3_suffix_streams_to_the_target(kv, torch):
+    """Suffix streaming of an 8-bit cache: blocks are packed as they complete, the target's pages equal the source's."""
+    from paper_2608_16477_b200 import streaming
+    shape = _shape(2, 64, 16, layers=2)
+    src, tgt = (kv.PagedCache(shape, 20, elem_bytes=1, fill=0) for _ in range(2))
+    perm, fresh = np.random.default_rng(3).permutation(20), np.random.default_rng(4).permutation(20)
+    k, n = 32, 32 + 53
+    table = perm[:-(-n // 16)]
+    rx = streaming.SuffixReceiver(tgt, request_id=1, expected_epoch=2, k_split=k, max_suffix_blocks=6, fresh_block_ids=fresh[2:10])
+    tx = streaming.SuffixStreamer(src, table, k, request_id=1, epoch=2, transport=streaming.LoopbackTransport(rx))
+    for pos in range(n):
+        rows = torch.randn(2, 1, 2, 64, device="cuda")
+        slots = torch.tensor([int(table[pos // 16]) * 16 + pos % 16], device="cuda")
+        for layer in range(2):
+            kv.kv_op_cache_write(src, layer, rows[0], rows[1] + layer, slots)
+        if pos >= k:
+            tx.on_token(pos)
+            if pos % 20 == 0:
+                tx.pump(max_blocks=1)
+    tx.final_sync(n)
+    merged = rx.assemble(fresh[:2], n, epoch=2)
+    torch.cuda.synchronize()
+    a, b = _pages_numpy(src), _pages_numpy(tgt)
+    assert np.array_equal(a[:, :, table[2:]], b[:, :, merged[2:]]) and a[:, :, table[2:]].any()
+
+
+def test_one_scratch_for_batches_of_every_size(kv, torch):
+    """Scratch for the largest batch serves smaller ones, whatever path they take."""
+    need, cases = 0, [([600] * 3, 1), ([700] * 9, 2), ([400], 2), ([800, 5] * 60, 1), ([30] * 120, 2)]
+    batches = [Batch(kv, torch, lens, 8, 2, 64, 16, elem, torch.float32, ctx=800) for lens, elem in cases]
+    need = kv.kv_paged_attention_batched_scratch_bytes(120, 16, batches[0].cache, 800)
+    scratch = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    for b in batches:
+        for ctx in (800, max(b.lens)):
+            b.scratch, b.ctx = scratch, ctx
+            b.run(kv)
+            b.check(torch)

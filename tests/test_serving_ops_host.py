@@ -234,6 +234,33 @@ def test_batched_attention_refusals(kv, elem):
     assert lib.kv_paged_attention_batched_scratch_bytes(3, 8, 2, 128, 0) == O.ERR_ARG
 
 
+@pytest.mark.parametrize("heads", [(64, 8), (8, 1), (4, 2), (40, 5), (256, 4)])
+def test_scratch_for_a_batch_serves_every_smaller_one(kv, heads):
+    """The size grows with the requests and the context; a smaller call on a larger call's scratch is not refused (the fake
+    addresses get as far as the missing device)."""
+    lib = kv.load()
+    hq, hkv = heads
+    for d in (64, 128):
+        for ctx in (1, 384, 385, 500, 512, 513, 768, 769, 5000):
+            sizes = [lib.kv_paged_attention_batched_scratch_bytes(r, hq, hkv, d, ctx) for r in (0, 1, 2, 7, 8, 9, 40, 100, 700)]
+            assert sizes == sorted(sizes) and sizes[0] > 0
+        for r in (1, 7, 8, 100):
+            sizes = [lib.kv_paged_attention_batched_scratch_bytes(r, hq, hkv, d, c) for c in (1, 384, 385, 512, 768, 769, 9000)]
+            assert sizes == sorted(sizes)
+    import torch
+    if torch.cuda.is_available():
+        return
+    need = lib.kv_paged_attention_batched_scratch_bytes(100, hq, hkv, 128, 4096)
+    q, tab, lens, scr, out = (FAKE + i * 0x1000000 for i in range(1, 6))
+    for elem in (1, 2):
+        desc = _desc(elem_bytes=elem, n_kv_heads=hkv)
+        for r in (1, 5, 8, 60, 100):
+            for ctx in (100, 390, 600, 800, 4096):
+                got = lib.kv_op_paged_attention_batched(q, hq * 128, 0, r, hq, C.byref(desc), 0, tab, 256, lens, ctx, 0.1,
+                                                        scr, need, out, hq * 128, None, 0)
+                assert got == -13, (r, ctx, got)
+
+
 def test_entry_points_for_bf16_pages_refuse_e4m3_pages(kv):
     lib, d = kv.load(), _desc()
     tab, q, out, scr = FAKE + 0x1000000, FAKE + 0x2000000, FAKE + 0x3000000, FAKE + 0x4000000
