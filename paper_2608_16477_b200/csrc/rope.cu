@@ -7,9 +7,9 @@
 // position (2^31 / 2 pi turns are less than 2^29, where fp64 has steps of 2^-24).
 //
 // HBM-bound: 2 * rows * head_dim elements move (3 fma per element).  A token's cosines and sines are needed by all its
-// heads, so a CTA takes 1 to 4 whole tokens, its threads form each (token, pair) once into shared memory, and the heads
+// heads, so a CTA takes one or two whole tokens, its threads form each (token, pair) once into shared memory, and the heads
 // are then streamed: one thread owns 2 x 16 bytes of a head (both members of its pairs), neighbouring threads
-// neighbouring vectors.  Measured: 16,384 tokens of 72 heads of 128, bf16, 604 MB: 101 us, 6.0 TB/s (91 % of a copy's rate);
+// neighbouring vectors.  Measured: 16,384 tokens of 72 heads of 128, bf16, 604 MB: 98 us, 6.2 TB/s (94 % of a copy's rate);
 // 1,003 tokens of 40 heads, fp32, 41 MB: 9.1 us; one token 2.5 us.
 #include <cmath>
 #include <new>
@@ -27,7 +27,7 @@ namespace {
 
 constexpr int kRopeThreads = 128;
 constexpr int kRopeMaxPairs = 128;
-constexpr int kRopeMaxTokens = 4;   // tokens of a CTA
+constexpr int kRopeMaxTokens = 2;   // tokens of a CTA (16,384 tokens of 72 heads: 97.7 us with two, 102 us with four)
 constexpr int kRopeAhead = 3;       // heads of a thread whose loads are in flight together
 
 struct RopeParams {
@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_vec_kernel(const __grid_con
 
 // Halves whose members do not start on the same place of a vector (rotary / 2 no multiple of its length), in rows that can
 // be read as vectors all the same: a warp takes up to eight heads of a token through shared memory, vectors in and out, pairs
-// in between (8,000 tokens of 72 heads of 128, 102 rotated: 74 us, against 255 us with a thread per pair straight from
+// in between (8,000 tokens of 72 heads of 128, 102 rotated: 70 us, against 255 us with a thread per pair straight from
 // global memory).
 constexpr int kRopeRowBytes = 4096;      // of a warp
 template <typename T>
