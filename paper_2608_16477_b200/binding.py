@@ -529,9 +529,9 @@ def _refuse(name, what):
 
 def _on_device(name, stream, tensors):
     """(device index, raw stream) of a call on `tensors`, which all have to be on one CUDA device."""
-    index = tensors[0].get_device() if tensors[0].is_cuda else -1
+    index = tensors[0].get_device()                 # -1 on the host
     for t in tensors:
-        if not t.is_cuda or t.get_device() != index:
+        if t.get_device() != index or index < 0:
             _refuse(name, f"tensors on one CUDA device are wanted, not on {[str(t.device) for t in tensors]}")
     if stream is None:
         return index, _torch()._C._cuda_getCurrentRawStream(index)
