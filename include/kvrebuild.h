@@ -332,7 +332,7 @@ int32_t kv_rope_frequencies(const kv_rope *r, double *theta_host, int32_t n);
 /* out[t][h] = rotation of x[t][h] at positions_dev[t] (int32, any sign).  backward != 0: the transpose, i.e. the gradient
  * of x from the gradient of out (turned by -p theta_j, times gain).  The angle is reduced in fp64 (exact to 2^-24 of a
  * turn over the whole int32 range), sine and cosine and the rotation are fp32, one rounding to dtype.  out may be x
- * itself with the same strides; any other overlap is undefined.  n_tokens = 0 does nothing. */
+ * itself with the same strides; any other overlap is undefined.  head_dim is at most 1024; n_tokens = 0 does nothing. */
 int32_t kv_op_rope(const kv_rope *rope, const void *x_dev, int64_t x_token_stride, int64_t x_head_stride, int32_t dtype,
                    int32_t n_tokens, int32_t n_heads, int32_t head_dim, const int32_t *positions_dev, int32_t backward,
                    void *out_dev, int64_t out_token_stride, int64_t out_head_stride, void *stream);
@@ -360,10 +360,10 @@ int32_t kv_op_cache_read(const kv_cache_desc *cache, int32_t layer, const int64_
  * head h / (n_q_heads / n_kv_heads):  s_n = softmax_scale * q . k_n,  out = sum_n exp(s_n) v_n / sum_n exp(s_n),
  * lse = log sum_n exp(s_n) (fp32 [n_req][n_q_heads], natural logarithm; NULL to leave it out), so results over disjoint
  * parts of a context can be joined.  A request of length 0 gets out = 0, lse = -inf.  Lengths are clamped to [0, max_ctx]
- * with max_ctx <= table_stride * block_size and at most 2^26; table entries behind a request's last block are not read.  A block id
- * outside the pool inside a context is not followed: that request's out and lse are NaN.  Infinities and NaN in a query, or
- * among the cached values inside its context, make the results they reach NaN; what lies behind a context enters no result.
- * fp32 sums and softmax.  out may be q itself with the same strides.
+ * with max_ctx <= table_stride * block_size and at most 2^26; table entries behind a request's last block are not read.
+ * A block id outside the pool inside a context is not followed: that request's out and lse are NaN.  Infinities and NaN in a
+ * query, or among the cached values inside its context, make the results they reach NaN; what lies behind a context enters
+ * no result.  fp32 sums and softmax.  out may be q itself with the same strides.
  * scratch_dev: kv_paged_attention_batched_scratch_bytes() bytes (what is enough for n_req and max_ctx is enough for fewer
  * requests and a smaller max_ctx), 16-byte aligned, contents need not survive between calls; calls that may overlap on the
  * GPU need scratch of their own.  head_dim 64 or 128. */

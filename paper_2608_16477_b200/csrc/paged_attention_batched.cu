@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
   // table entry can be a microsecond away.
   Cursor prod = cons;
   long long to_look = todo;
-  int blks[kLookAhead], offs[kLookAhead];    // of the next stages to be copied: block and slot of the lane's row (kNoRow: none)
+  int blks[kLookAhead] = {}, offs[kLookAhead] = {};   // of the next stages to be copied: block and slot of the lane's row (kNoRow: none)
   const int my_row = lane % KEYS;
   auto look_up = [&](int &blk, int &off) {
     const int pos = (prod.tile * KW + kg) * KEYS + my_row;
