@@ -361,9 +361,12 @@ int32_t kv_op_cache_read(const kv_cache_desc *cache, int32_t layer, const int64_
  * lse = log sum_n exp(s_n) (fp32 [n_req][n_q_heads], natural logarithm; NULL to leave it out), so results over disjoint
  * parts of a context can be joined.  A request of length 0 gets out = 0, lse = -inf.  Lengths are clamped to [0, max_ctx]
  * with max_ctx <= table_stride * block_size and at most 2^26; table entries behind a request's last block are not read.
- * A block id outside the pool inside a context is not followed: that request's out and lse are NaN.  Infinities and NaN in a
- * query, or among the cached values inside its context, make the results they reach NaN; what lies behind a context enters
- * no result.  fp32 sums and softmax.  out may be q itself with the same strides.
+ * A block id outside the pool inside a context is not followed: that request's out and lse are NaN.  Infinities and NaN turn
+ * into NaN what they enter, and nothing else: in a query, its head's out and lse; in a cached key inside a context, the out and
+ * lse of that request's heads that read its KV head; in a cached value, its dim of those outs.  What lies behind a context
+ * enters no result.  Where finite numbers leave fp32: a score below its range weighs nothing, a score or a weighted sum of
+ * values beyond it gives NaN, and a context whose scores are all below it gives NaN in out and lse.
+ * fp32 sums and softmax.  out may be q itself with the same strides.
  * scratch_dev: kv_paged_attention_batched_scratch_bytes() bytes (what is enough for n_req and max_ctx is enough for fewer
  * requests and a smaller max_ctx), 16-byte aligned, contents need not survive between calls; calls that may overlap on the
  * GPU need scratch of their own.  head_dim 64 or 128. */

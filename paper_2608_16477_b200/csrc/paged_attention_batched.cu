@@ -208,6 +208,9 @@ struct RawQuery {
     return make_float2(__uint_as_float(w[W * i]), __uint_as_float(w[W * i + W - 1]));
   }
 };
+// x, or NaN for an infinity: results say that something infinite entered them in one way, however it met the parts of a
+// weight or of a query (infinity times a positive part, a negative one or zero).
+__device__ __forceinline__ float nan_of_inf(float x) { return fmaf(x, 0.f, x); }
 __device__ __forceinline__ void store4(float *p, float a, float b, float c, float d) {
   *reinterpret_cast<float4 *>(p) = make_float4(a, b, c, d);
 }
@@ -226,13 +229,14 @@ __device__ __forceinline__ void store_head(P *row, const float (&oc)[D / 16][4],
   if (ELEM == 2) {
 #pragma unroll
     for (int mt = 0; mt < D / 16; ++mt) {
-      row[mt * 16 + g] = (P)(oc[mt][i] * f);
-      row[mt * 16 + g + 8] = (P)(oc[mt][2 + i] * f);
+      row[mt * 16 + g] = (P)nan_of_inf(oc[mt][i] * f);
+      row[mt * 16 + g + 8] = (P)nan_of_inf(oc[mt][2 + i] * f);
     }
   } else {
 #pragma unroll
     for (int mt = 0; mt < D / 16; mt += 2)
-      store4(row + g * (D / 8) + 2 * mt, oc[mt][i] * f, oc[mt][2 + i] * f, oc[mt + 1][i] * f, oc[mt + 1][2 + i] * f);
+      store4(row + g * (D / 8) + 2 * mt, nan_of_inf(oc[mt][i] * f), nan_of_inf(oc[mt][2 + i] * f), nan_of_inf(oc[mt + 1][i] * f),
+             nan_of_inf(oc[mt + 1][2 + i] * f));
   }
 }
 __device__ __forceinline__ float column_max(float v) {      // over the eight lanes that share lane % 4
@@ -490,7 +494,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
           for (int j = 0; j < 2; ++j) {
             const float2 a = raw.pair(2 * ks + j);
             uint32_t parts[QP];
-            split_bf16(a.x * on, a.y * on, parts);      // a bf16 query is its own one part
+            split_bf16(nan_of_inf(a.x) * on, nan_of_inf(a.y) * on, parts);      // a bf16 query is its own one part
 #pragma unroll
             for (int h = 0; h < QP; ++h) qf[h][ks][j] = parts[h];
           }
@@ -501,8 +505,8 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
 #pragma unroll
         for (int i = 0; i < 2 * KS; ++i) {
           const float2 a = raw.pair(i);
-          x[2 * i] = a.x * on;
-          x[2 * i + 1] = a.y * on;
+          x[2 * i] = nan_of_inf(a.x) * on;
+          x[2 * i + 1] = nan_of_inf(a.y) * on;
           most = fmaxf(most, fmaxf(fabsf(x[2 * i]), fabsf(x[2 * i + 1])));
         }
         most = quad_max(most);
@@ -571,6 +575,12 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
 #pragma unroll
           for (int i = 0; i < 4; ++i) t[2 * mt + (i >> 1)][i & 1] = (sc[0][i] + sc[1][i]) * q_scale[i & 1];
         }
+        // 0, or NaN if a score is no finite number (bf16 pages: e4m3 has no infinities, and NaN runs through)
+        float odd = 0.f;
+        if (ELEM == 2) {
+#pragma unroll
+          for (int j = 0; j < 2 * MK; ++j) odd = fmaf(t[j][1], 0.f, fmaf(t[j][0], 0.f, odd));
+        }
         float ev[2 * MK];
         if (ELEM == 1) {
           // lane l has the scale bytes of row l: K's goes to the exponent field of a float, V's to the low bits
@@ -606,26 +616,44 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
           }
           raise |= top[i] > m[i] + kLazy || (ELEM == 1 && wtop[i] > mw[i] + kLazy);
         }
-        if (__any_sync(0xffffffffu, raise)) {
+        if (__any_sync(0xffffffffu, raise || !(odd == 0.f))) {
+          if (ELEM == 2 && __any_sync(0xffffffffu, !(odd == 0.f))) {
+            // A score of -inf is a finite one below fp32's range, which weighs nothing, or comes of an infinity in the key. The
+            // keys times zero tell: the rows that hold no number but infinity or NaN give NaN.
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float m_new = fmaxf(m[i], column_max(top[i]));
-            const float sub = m_new == -INFINITY ? 0.f : m_new;
-            l[i] *= ex2(m[i] - sub);
-            float corr = ex2(m[i] - sub);
-            m[i] = m_new;
-            m_sub[i] = sub;
-            if (ELEM == 1) {
-              const float w_new = fmaxf(mw[i], column_max(wtop[i]));
-              const float wsub = w_new == -INFINITY ? 0.f : w_new;
-              corr = ex2(mw[i] - wsub);
-              mw[i] = w_new;
-              w_sub[i] = wsub - kWeightBits;
+            for (int mt = 0; mt < MK; ++mt) {
+              float z[4] = {};
+#pragma unroll 1
+              for (int ks = 0; ks < KS; ++ks) {
+                uint32_t a[4];
+                ldsm4(k_s + chunk_at<D, ELEM>(mt * 16 + (lane & 15), ks * 2 + (lane >> 4)), a);
+                mma_bf16(z, a, 0u, 0u);
+              }
+#pragma unroll
+              for (int i = 0; i < 4; ++i) t[2 * mt + (i >> 1)][i & 1] += z[i];
             }
+          }
+          if (__any_sync(0xffffffffu, raise)) {      // of the maxima alone: they do not depend on another head's NaN
 #pragma unroll
-            for (int mt = 0; mt < MO; ++mt) {
-              oc[mt][i] *= corr;
-              oc[mt][2 + i] *= corr;
+            for (int i = 0; i < 2; ++i) {
+              const float m_new = fmaxf(m[i], column_max(top[i]));
+              const float sub = m_new == -INFINITY ? 0.f : m_new;
+              l[i] *= ex2(m[i] - sub);
+              float corr = ex2(m[i] - sub);
+              m[i] = m_new;
+              m_sub[i] = sub;
+              if (ELEM == 1) {
+                const float w_new = fmaxf(mw[i], column_max(wtop[i]));
+                const float wsub = w_new == -INFINITY ? 0.f : w_new;
+                corr = ex2(mw[i] - wsub);
+                mw[i] = w_new;
+                w_sub[i] = wsub - kWeightBits;
+              }
+#pragma unroll
+              for (int mt = 0; mt < MO; ++mt) {
+                oc[mt][i] *= corr;
+                oc[mt][2 + i] *= corr;
+              }
             }
           }
         }
@@ -712,7 +740,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
         if (whole) {
           store_head<D, ELEM>(static_cast<T *>(p.out) + req * p.out_stride + (long long)h * D, oc, i, g, n == 0 ? 0.f : f[i] / l[i]);
           if (p.lse != nullptr && g == 0)
-            p.lse[(long long)req * p.n_q_heads + h] = n == 0 ? -INFINITY : (m[i] + log2f(l[i])) * (1.f / kLog2e);
+            p.lse[(long long)req * p.n_q_heads + h] = n == 0 ? -INFINITY : nan_of_inf((m[i] + log2f(l[i])) * (1.f / kLog2e));
         } else {
           const long long rec = ((long long)h * p.parts + part) * 2 + rec_slot;
           store_head<D, ELEM>(p.o + rec * D, oc, i, g, f[i]);
@@ -883,11 +911,14 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(cons
   }
   T *out = static_cast<T *>(p.out) + req * p.out_stride + (long long)h * D + lane * V;
   const float inv = 1.f / l;
+#pragma unroll
+  for (int i = 0; i < V; ++i) acc[i] = nan_of_inf(acc[i] * inv);
   if (V == 4)
-    store4(out, acc[0] * inv, acc[1] * inv, acc[V - 2] * inv, acc[V - 1] * inv);
+    store4(out, acc[0], acc[1], acc[V - 2], acc[V - 1]);
   else
-    store2(out, acc[0] * inv, acc[1] * inv);
-  if (p.lse != nullptr && lane == 0) p.lse[(long long)req * p.n_q_heads + h] = (m + log2f(l)) * (1.f / kLog2e);
+    store2(out, acc[0], acc[1]);
+  if (p.lse != nullptr && lane == 0)
+    p.lse[(long long)req * p.n_q_heads + h] = nan_of_inf((m + log2f(l)) * (1.f / kLog2e));
 }
 
 // Short contexts are not split: one launch, a CTA per request and KV head or four.  Splitting costs a second kernel and the
