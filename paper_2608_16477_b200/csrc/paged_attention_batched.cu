@@ -505,13 +505,14 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
 #pragma unroll
         for (int i = 0; i < 2 * KS; ++i) {
           const float2 a = raw.pair(i);
-          x[2 * i] = nan_of_inf(a.x) * on;
-          x[2 * i + 1] = nan_of_inf(a.y) * on;
+          x[2 * i] = a.x * on;
+          x[2 * i + 1] = a.y * on;
           most = fmaxf(most, fmaxf(fabsf(x[2 * i]), fabsf(x[2 * i + 1])));
         }
         most = quad_max(most);
         const int e = min(max((int)(__float_as_uint(most) >> 23) - 126, -100), 127);       // most < 2^e
-        const float up = __uint_as_float((uint32_t)(127 + kQueryBits - e) << 23);
+        // NaN times everything where the largest is infinite
+        const float up = __uint_as_float(most <= FLT_MAX ? (uint32_t)(127 + kQueryBits - e) << 23 : 0x7fc00000u);
         const float down = p.scale * __uint_as_float((uint32_t)(127 - kQueryBits + e) << 23);
         q_scale[0] = __shfl_sync(0xffffffffu, down, cq * 4);
         q_scale[1] = __shfl_sync(0xffffffffu, down, cq * 4 + 4);
@@ -530,6 +531,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
     // per head cq + i: running maxima of t and of t + e_v (ELEM 1; -inf: none yet, then 0 is subtracted), the lane's sum
     float m[2] = {-INFINITY, -INFINITY}, mw[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
     float m_sub[2] = {0.f, 0.f}, w_sub[2] = {0.f, 0.f};
+    float low = INFINITY;      // ELEM 2: the lowest score
     float oc[MO][4];
 #pragma unroll
     for (int mt = 0; mt < MO; ++mt)
@@ -575,11 +577,9 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
 #pragma unroll
           for (int i = 0; i < 4; ++i) t[2 * mt + (i >> 1)][i & 1] = (sc[0][i] + sc[1][i]) * q_scale[i & 1];
         }
-        // 0, or NaN if a score is no finite number (bf16 pages: e4m3 has no infinities, and NaN runs through)
-        float odd = 0.f;
         if (ELEM == 2) {
 #pragma unroll
-          for (int j = 0; j < 2 * MK; ++j) odd = fmaf(t[j][1], 0.f, fmaf(t[j][0], 0.f, odd));
+          for (int j = 0; j < 2 * MK; ++j) low = fminf(low, fminf(t[j][0], t[j][1]));
         }
         float ev[2 * MK];
         if (ELEM == 1) {
@@ -616,44 +616,26 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
           }
           raise |= top[i] > m[i] + kLazy || (ELEM == 1 && wtop[i] > mw[i] + kLazy);
         }
-        if (__any_sync(0xffffffffu, raise || !(odd == 0.f))) {
-          if (ELEM == 2 && __any_sync(0xffffffffu, !(odd == 0.f))) {
-            // A score of -inf is a finite one below fp32's range, which weighs nothing, or comes of an infinity in the key. The
-            // keys times zero tell: the rows that hold no number but infinity or NaN give NaN.
+        if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
-            for (int mt = 0; mt < MK; ++mt) {
-              float z[4] = {};
-#pragma unroll 1
-              for (int ks = 0; ks < KS; ++ks) {
-                uint32_t a[4];
-                ldsm4(k_s + chunk_at<D, ELEM>(mt * 16 + (lane & 15), ks * 2 + (lane >> 4)), a);
-                mma_bf16(z, a, 0u, 0u);
-              }
-#pragma unroll
-              for (int i = 0; i < 4; ++i) t[2 * mt + (i >> 1)][i & 1] += z[i];
+          for (int i = 0; i < 2; ++i) {
+            const float m_new = fmaxf(m[i], column_max(top[i]));
+            const float sub = m_new == -INFINITY ? 0.f : m_new;
+            l[i] *= ex2(m[i] - sub);
+            float corr = ex2(m[i] - sub);
+            m[i] = m_new;
+            m_sub[i] = sub;
+            if (ELEM == 1) {
+              const float w_new = fmaxf(mw[i], column_max(wtop[i]));
+              const float wsub = w_new == -INFINITY ? 0.f : w_new;
+              corr = ex2(mw[i] - wsub);
+              mw[i] = w_new;
+              w_sub[i] = wsub - kWeightBits;
             }
-          }
-          if (__any_sync(0xffffffffu, raise)) {      // of the maxima alone: they do not depend on another head's NaN
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const float m_new = fmaxf(m[i], column_max(top[i]));
-              const float sub = m_new == -INFINITY ? 0.f : m_new;
-              l[i] *= ex2(m[i] - sub);
-              float corr = ex2(m[i] - sub);
-              m[i] = m_new;
-              m_sub[i] = sub;
-              if (ELEM == 1) {
-                const float w_new = fmaxf(mw[i], column_max(wtop[i]));
-                const float wsub = w_new == -INFINITY ? 0.f : w_new;
-                corr = ex2(mw[i] - wsub);
-                mw[i] = w_new;
-                w_sub[i] = wsub - kWeightBits;
-              }
-#pragma unroll
-              for (int mt = 0; mt < MO; ++mt) {
-                oc[mt][i] *= corr;
-                oc[mt][2 + i] *= corr;
-              }
+            for (int mt = 0; mt < MO; ++mt) {
+              oc[mt][i] *= corr;
+              oc[mt][2 + i] *= corr;
             }
           }
         }
@@ -720,6 +702,28 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
     }
     todo -= steps;
     if (todo > 0) load_query(cons.r);        // on its way while this one is finished
+
+    // A score of -inf is a finite one below fp32's range, which weighs nothing, or comes of an infinity in the key and has to
+    // show: the keys are looked through once more.  (bf16 pages: e4m3 has no infinities.  Scores of +inf and NaN show by themselves.)
+    if (ELEM == 2 && __builtin_expect(__any_sync(0xffffffffu, low == -INFINITY), 0)) {
+      bool inf = false;
+#pragma unroll 1
+      for (int s = 0; s < steps; ++s) {
+        const int pos = ((s_tile + s) * KW + kg) * KEYS + my_row;
+        if (pos >= n) continue;
+        const int b = pos / p.cache.block_size, blk = __ldg(p.tables + req * p.table_stride + b);
+        if ((unsigned)blk >= (unsigned)p.num_blocks) continue;
+        const char *row = p.cache.page(p.layer, 0, blk) + (pos - b * p.cache.block_size) * row_stride + (long long)kvh * C::row;
+#pragma unroll 1
+        for (int i = lane / KEYS * 16; i < C::row; i += 32 / KEYS * 16) {
+          const uint4 x = *reinterpret_cast<const uint4 *>(row + i);
+          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) inf |= (w[j] & 0x7f80u) == 0x7f80u || (w[j] & 0x7f800000u) == 0x7f800000u;
+        }
+      }
+      if (__any_sync(0xffffffffu, inf)) l[0] = l[1] = __uint_as_float(0x7fc00000u);
+    }
 
     // ---- the request's share: sums over the lanes of a column, fp16 weights back to 2^(t - m)
     float f[2];
