@@ -932,10 +932,12 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(cons
 // 9.7, of 1,000 15.7 / 13.8; with a warp per KV head 128 of up to 400 23.7 / 20.7 and of up to 577 27.0 / 25.9 (fp32
 // queries: 25.7 / 30.0).
 constexpr int kBaNeverSplit = 384;   // the least that this can be
+constexpr int kBaWholeWarp = 512;    // with a warp per KV head
 int ba_whole_ctx(int n_req, int kw, int elem_bytes) {
-  if (kw == 1) return 512;
+  if (kw == 1) return kBaWholeWarp;
   return n_req >= 8 ? 768 : (elem_bytes == 1 ? 512 : kBaNeverSplit);
 }
+constexpr int kBaShort = 1024;       // ... although up to half of the warps have no head
 // Positions and the tiles of 32 requests are counted in 32 bits.
 constexpr int kBaMaxCtx = 1 << 26;
 
@@ -949,7 +951,18 @@ BaPlan ba_plan(int n_req, int vheads, int max_ctx, int elem_bytes, int sms) {
   // A warp per KV head once the batch has a (request, head) for every other warp of the machine; four warps per head below
   // that.  Measured, a warp / four warps: 128 requests of up to 577 tokens 28.8 / 34.2 us, 256 of up to 500 39.4 / 48.3,
   // 64 of up to 4,608 71.3 / 72.4; 4 of up to 4,608 15.1 / 11.2, one of 18,433 20.8 / 16.2.
-  b.kw = (long long)n_req * vheads >= 4ll * sms ? 1 : kBaWarps;
+  // A warp without a head leaves, and its share of the loads in flight with it.  Where that is less than one warp in eight, it does
+  // not matter; where it is half of them or more, heads keep four warps each (700 requests of up to 500 tokens over 1, 2 KV heads, 8
+  // bits, a warp / four: 35 / 22, 43 / 37 us; of up to 4,096 157 / 78, 223 / 136).  Between the two it is the contexts: short ones are
+  // better off without bringing four warps together (700 of up to 700 over 3, 5, 6 heads 55 / 76, 97 / 122, 96 / 138 us), long ones
+  // with every warp at work (of up to 4,096 251 / 210, 493 / 348, 523 / 390), and so are whole ones up to six heads an SM (120 of
+  // up to 500 over 5, 6 heads 25.5 / 20.0, 25.3 / 22.8; 300 over 3, 5, 6 heads 26 / 28, 40 / 40, 44 / 45).
+  const long long heads = (long long)n_req * vheads;
+  const int slots = (vheads + kBaWarps - 1) / kBaWarps * kBaWarps;
+  bool single = heads >= 4ll * sms;
+  if (8 * vheads < 7 * slots)
+    single = 2 * vheads > slots && max_ctx <= kBaShort && heads >= (max_ctx <= kBaWholeWarp ? 6ll : 4ll) * sms;
+  b.kw = single ? 1 : kBaWarps;
   const int per_cta = kBaWarps / b.kw;
   b.columns = (vheads + per_cta - 1) / per_cta;
   b.whole = max_ctx <= ba_whole_ctx(n_req, b.kw, elem_bytes);
@@ -1030,10 +1043,17 @@ int64_t kv_paged_attention_batched_scratch_bytes(int32_t n_req, int32_t n_q_head
   if (max_ctx > kBaMaxCtx) return KV_ERR_SHAPE;
   if (n_q_heads % n_kv_heads != 0 || (head_dim != 64 && head_dim != 128)) return KV_ERR_SHAPE;
   const int vheads = n_kv_heads * ba_passes(n_q_heads / n_kv_heads);
-  // As if contexts were split wherever any batch's are: more requests and longer contexts never need less (a warp per KV head
-  // makes more ranges than four do), so that scratch for the largest batch serves every smaller one.
+  // As if contexts were split wherever any batch's are: more requests and longer contexts never need less, so that scratch for
+  // the largest batch serves every smaller one.  A warp per KV head makes more ranges than four do: more requests can only
+  // change to it, longer contexts also from it.
   if (max_ctx <= kBaNeverSplit || n_req == 0) return 256;
-  return ba_scratch(n_req, n_q_heads, head_dim, ba_plan(n_req, vheads, max_ctx, 2, sm_count(current_device())).parts).bytes;
+  const int sms = sm_count(current_device());
+  int parts = ba_plan(n_req, vheads, max_ctx, 2, sms).parts;
+  if (max_ctx > kBaShort) {
+    const int short_parts = ba_plan(n_req, vheads, kBaShort, 2, sms).parts;
+    parts = parts > short_parts ? parts : short_parts;
+  }
+  return ba_scratch(n_req, n_q_heads, head_dim, parts).bytes;
 }
 
 int32_t kv_op_paged_attention_batched(const void *q_dev, int64_t q_stride, int32_t dtype, int32_t n_req,

@@ -1,0 +1,61 @@
+"""How the batched attention cuts its work, as far as the scratch size shows it (no GPU needed; 148 SMs without one)."""
+import pytest
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import paper_2608_16477_b200 as kv
+    return kv.load()
+
+
+def _records(lib, n_req, kv_heads, ctx, group=8, dim=128):
+    """Bytes of the scratch that hold records: what the starts of the requests leave."""
+    whole = lib.kv_paged_attention_batched_scratch_bytes(n_req, group * kv_heads, kv_heads, dim, ctx)
+    return whole - -(-(n_req + 1) * 8 // 256) * 256
+
+
+@pytest.mark.parametrize("kv_heads,group", [(2, 8), (1, 16), (2, 1)])
+def test_heads_that_leave_half_of_a_cta_idle_keep_four_warps_each(lib, kv_heads, group):
+    """A warp per KV head makes more ranges, hence records, than four do.  One or two heads (or passes over one) are not given a
+    warp each, however many requests there are: the CTA's other warps would have nothing to load."""
+    for ctx in (600, 4096):
+        few = _records(lib, 8, kv_heads, ctx, group)
+        assert [_records(lib, n, kv_heads, ctx, group) for n in (100, 700, 5000)] == [few] * 3
+
+
+@pytest.mark.parametrize("kv_heads", [4, 8, 16])
+def test_heads_that_fill_the_ctas_take_a_warp_each_in_large_batches(lib, kv_heads):
+    assert _records(lib, 8, kv_heads, 4096) < _records(lib, 700, kv_heads, 4096)
+
+
+@pytest.mark.parametrize("kv_heads", [1, 2, 3, 5, 6, 8])
+@pytest.mark.parametrize("n_req", [8, 100, 300, 700])
+def test_scratch_grows_with_the_context(lib, kv_heads, n_req):
+    sizes = [lib.kv_paged_attention_batched_scratch_bytes(n_req, 8 * kv_heads, kv_heads, 128, c)
+             for c in (1, 384, 385, 511, 512, 513, 768, 769, 1024, 1025, 4096, 100000)]
+    assert sizes == sorted(sizes)
+
+
+FAKE = 0x7000000000
+
+
+@pytest.mark.parametrize("kv_heads", [1, 2, 3, 5, 6, 7, 8])
+def test_scratch_serves_fewer_requests_and_shorter_contexts(lib, kv_heads):
+    """No call on a larger call's scratch is refused (the fake addresses get as far as the missing device)."""
+    torch = pytest.importorskip("torch")
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are not real")
+    import ctypes as C
+    from paper_2608_16477_b200.binding import CacheDesc
+    page = 16 * kv_heads * 64 * 2
+    desc = CacheDesc(FAKE, 2 * 16 * page, 16 * page, page, 16, 16, 1, kv_heads, 64, 2)
+    q, tab, lens, scr, out = (FAKE + i * 0x1000000 for i in range(1, 6))
+    ctxs, reqs = (300, 400, 512, 513, 800, 1024, 1025, 4096), (1, 7, 8, 119, 120, 198, 300, 592, 700)
+    for n in reqs:
+        for ctx in ctxs:
+            need = lib.kv_paged_attention_batched_scratch_bytes(n, 8 * kv_heads, kv_heads, 64, ctx)
+            for m in reqs[:reqs.index(n) + 1]:
+                for c in ctxs[:ctxs.index(ctx) + 1]:
+                    got = lib.kv_op_paged_attention_batched(q, 512 * kv_heads, 0, m, 8 * kv_heads, C.byref(desc), 0, tab, 256, lens,
+                                                            c, 0.1, scr, need, out, 512 * kv_heads, None, 0)
+                    assert got == -13, (n, ctx, m, c, got)
