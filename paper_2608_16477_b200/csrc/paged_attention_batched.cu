@@ -25,12 +25,14 @@
 // hold 8 useful columns of at least 16 as well, but wants its operands through shared-memory descriptors, and e4m3 rows
 // would have to be converted and written back there first.)  Groups of more than 8 heads are taken 8 at a time.
 // fp32 operands go in as sums of 16-bit parts that are multiplied one after the other.  Over e4m3 pages q and the weights p
-// are two fp16 (2^-22; a bf16 query is one, and exact); over bf16 pages they are three bf16 in fp32 calls (2^-24), in bf16
-// calls q is one part and p two (2^-16, a 256th of the rounding of the result).  The second part of the weights costs bf16
+// are two fp16: 2^-22 of a value, but no less than fp16's smallest step, which is 2^-36 of the query's largest value (a bf16
+// query is one part: exact down to 2^-28 of its largest) and half of which is 2^-36 of the request's largest contribution so far.
+// Over bf16 pages they are three bf16 in fp32 calls (2^-24); in bf16 calls q is one part, exact, and p two (2^-16, a 256th of
+// the rounding of the result; the sum of the weights, and lse, take them whole).  The second part of the weights costs bf16
 // calls over e4m3 pages 0.5 % (128 requests of up to 577 tokens: 1.6 %): the loads are what bounds them.
 //
-// The running maximum is lazy: m is replaced only when a score passes it by more than 2^8, so most stages need no
-// reduction over the lanes and no rescaling; sums and weights have the head room for it.
+// The running maximum is lazy: m is replaced only when a score passes it by more than 2^8 (e4m3 pages: 2^4, for the head room
+// goes to small fp16 weights), so most stages need no reduction over the lanes and no rescaling.
 //
 // e4m3 pages: codes go to fp16 fragments (exact) and the power-of-two scales stay outside: K's multiplies the score,
 // V's goes into the weight, w = 2^(t + e_v - M), with its own running maximum M of t + e_v, so that fp16 keeps the bits
@@ -48,8 +50,9 @@ constexpr int kBaHeads = 8;          // query heads of a pass
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kLookAhead = 3;        // stages between looking a page up and copying its rows
 constexpr int kNoRow = (int)0x80000000;
-constexpr float kLazy = 8.f;         // a running maximum may be passed by 2^8 before it is replaced
-constexpr float kWeightBits = 7.f;   // fp16 weights: 2^7 at the running maximum, so at most 2^15
+template <int ELEM>
+constexpr float kLazy = ELEM == 1 ? 4.f : 8.f;      // a running maximum may be passed by 2^4 (2^8) before it is replaced
+constexpr float kWeightBits = 11.f;  // fp16 weights: 2^11 at the running maximum, so at most 2^15
 constexpr int kQueryBits = 12;       // ... and fp16 queries to less than 2^12
 
 // A stage is what a warp loads and consumes at a time: 32 keys, so that the softmax's and the loads' bookkeeping is paid
@@ -614,7 +617,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
             top[i] = fmaxf(top[i], t[j][i]);
             if (ELEM == 1) wtop[i] = fmaxf(wtop[i], t[j][i] + ev[j]);
           }
-          raise |= top[i] > m[i] + kLazy || (ELEM == 1 && wtop[i] > mw[i] + kLazy);
+          raise |= top[i] > m[i] + kLazy<ELEM> || (ELEM == 1 && wtop[i] > mw[i] + kLazy<ELEM>);
         }
         if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll

@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 
 from oracle import serving_oracle as S
-from tests.test_gpu_serving_ops import Batch, _np
+from tests.test_gpu_serving_ops import Batch, _np, _shape
 
 pytestmark = pytest.mark.gpu
 
@@ -121,3 +121,32 @@ def test_attention_of_no_score_that_is_a_number(kv, torch, n, dtype):
     b.run(kv)
     assert torch.isnan(b.out[0]).all() and torch.isnan(b.lse[0]).all()
     b.check(torch, only=[1])
+
+
+# ------------------------------------------------------------------ small weights beside a large one
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_attention_many_small_weights_beside_a_large_one(kv, torch, dtype):
+    """e4m3 pages: one key with e^23 times the weight of each of the others, whose values lie in a dim where its own is 0.  There are
+    so many KV heads that one part holds the context.  A weight may be off by 2^-36 of the largest contribution (1 here) and
+    2^-22 of itself, sums and the factors that join them by (n / 16 + 64) 2^-22 of what they hold."""
+    n, one, heads = 16384, 777, 300
+    cache = kv.PagedCache(_shape(heads, 64, 16), n // 16, elem_bytes=1)
+    k, v = torch.zeros(n, 1, 64, device="cuda"), torch.zeros(n, 1, 64, device="cuda")
+    k[one, :, 0], v[one, :, 0] = 1.0, 1.0
+    v[:, :, 1] = 1.0
+    v[one, :, 1] = 0.0
+    kv.kv_op_cache_write(cache, 0, k.expand(n, heads, 64), v.expand(n, heads, 64), torch.arange(n, device="cuda"))
+    q = torch.zeros(1, heads, 64, dtype=getattr(torch, dtype), device="cuda")
+    q[:, :, 0] = 23.0
+    out, table = torch.empty_like(q), torch.arange(n // 16, dtype=torch.int32, device="cuda")[None]
+    scratch = torch.empty(kv.kv_paged_attention_batched_scratch_bytes(1, heads, cache, n), dtype=torch.uint8, device="cuda")
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    kv.kv_op_paged_attention_batched(q, cache, 0, table, lens, n, out, scratch, softmax_scale=1.0)
+    small = (n - 1) * math.exp(-23.0)
+    want0, want1 = 1 / (1 + small), small / (1 + small)
+    got = _np(out)[0]
+    # 23 is exact in both types, so are the scores; the exponent of a weight is rounded to 2^-24 of 23 log2(e) = 33: 2^-19
+    share = 2.0 ** -18 + 2.0 ** -21 + (n / 16 + 64) * 2.0 ** -22 + torch.finfo(q.dtype).eps
+    assert (np.abs(got[:, 1] - want1) <= n * 2.0 ** -36 + want1 * share).all(), (got[:, 1], want1)
+    assert (np.abs(got[:, 0] - want0) <= want0 * share).all(), (got[:, 0], want0)
+    assert (got[:, 2:] == 0).all()
