@@ -317,8 +317,9 @@ int32_t kv_op_paged_attention_noalloc(const float *q_dev, int32_t n_q_heads, con
  *   KV_ROPE_SCALE_PARTS   g_j = clamp((original_ctx * theta_j / (2 pi) - low) / (high - low), 0, 1): pairs that turn more
  *                         than `high` times within original_ctx keep theta_j, those below `low` take theta_j / factor,
  *                         (1 - g_j) theta_j / factor + g_j theta_j between them
- * rotary_dim is even and at most 256; base, factor and gain are finite and positive; high > low; no pair may turn by more
- * than one radian per position (a base below 1, or a factor that speeds positions up, is refused with KV_ERR_ARG). */
+ * rotary_dim is even and at most 256; base (NTK: the replaced one too) and factor are finite and positive, gain is in fp32's normal
+ * range; high > low; no pair may turn by more than one radian per position (a base below 1, or a factor that speeds
+ * positions up, is refused with KV_ERR_ARG). */
 typedef struct {
   int32_t rotary_dim, layout, scaling;
   double base, factor, original_ctx, low, high, gain;

@@ -59,3 +59,17 @@ def test_scratch_serves_fewer_requests_and_shorter_contexts(lib, kv_heads):
                     got = lib.kv_op_paged_attention_batched(q, 512 * kv_heads, 0, m, 8 * kv_heads, C.byref(desc), 0, tab, 256, lens,
                                                             c, 0.1, scr, need, out, 512 * kv_heads, None, 0)
                     assert got == -13, (n, ctx, m, c, got)
+
+
+# ------------------------------------------------------------------ refusals
+def test_rope_plans_that_leave_the_kernels_range_are_refused():
+    """The gain is applied in fp32: one that is infinite or zero there would make every result so.  A base that overflows when it is
+    scaled would turn the first pair alone."""
+    import paper_2608_16477_b200 as kv
+    for bad in (dict(gain=1e39), dict(gain=1e-46), dict(gain=1e-39), dict(gain=float("inf")), dict(gain=float("nan")), dict(gain=-1.0),
+                dict(base=1e300, scaling="ntk", factor=1e200)):
+        with pytest.raises(kv.KVError) as e:
+            kv.Rope(64, **bad)
+        assert e.value.status == -1, bad
+    for good in (dict(gain=3e38), dict(gain=1.2e-38), dict(base=1e300, scaling="ntk", factor=2.0)):
+        kv.Rope(64, **good)
