@@ -19,7 +19,7 @@ def test_heads_that_leave_half_of_a_cta_idle_keep_four_warps_each(lib, kv_heads,
     """A warp per KV head makes more ranges, hence records, than four do.  One or two heads (or passes over one) are not given a
     warp each, however many requests there are: the CTA's other warps would have nothing to load."""
     for ctx in (600, 4096):
-        few = _records(lib, 8, kv_heads, ctx, group)
+        few = _records(lib, 50, kv_heads, ctx, group)      # enough keys for every range, too few requests for a warp each
         assert [_records(lib, n, kv_heads, ctx, group) for n in (100, 700, 5000)] == [few] * 3
 
 
