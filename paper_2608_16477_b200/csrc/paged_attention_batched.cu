@@ -1082,6 +1082,7 @@ int32_t kv_op_paged_attention_batched(const void *q_dev, int64_t q_stride, int32
     return KV_ERR_ARG;
   if (((uintptr_t)block_tables_dev & 3) || ((uintptr_t)context_lens_dev & 3) || ((uintptr_t)lse_out_dev & 3)) return KV_ERR_ARG;
   if (q_stride < 0 || table_stride < 0 || (n_req > 1 && out_stride < width)) return KV_ERR_ARG;
+  if (q_dev == out_dev && n_req > 1 && q_stride != out_stride) return KV_ERR_ARG;      // one request's out would be another's query
   const long long blocks = ((long long)max_ctx + cache->block_size - 1) / cache->block_size;
   if (table_stride < blocks) return KV_ERR_TABLE_SHORT;
   const int device = current_device();

@@ -73,3 +73,21 @@ def test_rope_plans_that_leave_the_kernels_range_are_refused():
         assert e.value.status == -1, bad
     for good in (dict(gain=3e38), dict(gain=1.2e-38), dict(base=1e300, scaling="ntk", factor=2.0)):
         kv.Rope(64, **good)
+
+
+@pytest.mark.parametrize("elem", [1, 2])
+def test_attention_in_place_with_other_strides_is_refused(lib, elem):
+    """out may be q itself with the same strides.  With others, one request's result would overwrite another's query."""
+    import ctypes as C
+    from paper_2608_16477_b200.binding import CacheDesc
+    page = 16 * 2 * 64 * elem + (32 if elem == 1 else 0)
+    desc = CacheDesc(FAKE, 2 * 16 * page, 16 * page, page, 16, 16, 1, 2, 64, elem)
+    tab, lens, scr, x, other = (FAKE + i * 0x1000000 for i in range(1, 6))
+
+    def call(n_req, out, q_stride, out_stride):
+        return lib.kv_op_paged_attention_batched(x, q_stride, 0, n_req, 4, C.byref(desc), 0, tab, 256, lens, 100, 0.1, scr, 1 << 30, out,
+                                                 out_stride, None, 0)
+    assert call(3, x, 256, 512) == call(3, x, 512, 256) == call(2, x, 0, 256) == -1
+    import torch
+    if not torch.cuda.is_available():      # these go on, as far as the missing device
+        assert call(3, x, 256, 256) == call(1, x, 0, 256) == call(3, other, 512, 256) == -13
