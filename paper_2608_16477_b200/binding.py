@@ -527,6 +527,16 @@ def _refuse(name, what):
     raise ValueError(f"{name}: {what}")
 
 
+_INT32 = (1 << 31) - 1
+
+
+def _int32(name, *values):
+    """The library counts in 32 bits, and ctypes passes what is left of a larger number."""
+    for v in values:
+        if not -_INT32 <= v <= _INT32:
+            _refuse(name, f"{v} is past the library's 32-bit counts")
+
+
 def _on_device(name, stream, tensors):
     """(device index, raw stream) of a call on `tensors`, which all have to be on one CUDA device."""
     index = tensors[0].get_device()                 # -1 on the host
@@ -561,6 +571,7 @@ class Rope:
             _refuse("Rope", f"layout {layout!r}: one of {sorted(KV_ROPE_LAYOUTS)}")
         if scaling not in KV_ROPE_SCALINGS:
             _refuse("Rope", f"scaling {scaling!r}: one of {sorted(KV_ROPE_SCALINGS)}")
+        _int32("Rope", rotary_dim)
         self._lib = load()
         self.rotary_dim = rotary_dim
         desc = RopeDesc(rotary_dim, KV_ROPE_LAYOUTS[layout], KV_ROPE_SCALINGS[scaling], base, factor, original_ctx, low,
@@ -598,13 +609,15 @@ def kv_op_rope(rope: Rope, x, positions, out, backward: bool = False, stream=Non
     if positions.shape != (t,) or positions.dtype is not _torch().int32 or not positions.is_contiguous():
         _refuse(name, "positions is a contiguous int32 vector, one per token")
     dtype = _dtype(name, x.dtype)
+    if t > _INT32 or h > _INT32 or d > _INT32:
+        _int32(name, t, h, d)
     index, stream = _on_device(name, stream, (x, positions, out))
     _launch(name, index, (rope.handle, x.data_ptr(), xt if t > 1 else 0, xh if h > 1 else 0, dtype, t, h, d,
                           positions.data_ptr(), 1 if backward else 0, out.data_ptr(), ot if t > 1 else 0,
                           oh if h > 1 else 0, stream))
 
 
-def _rows(name, cache, k, v, slots):
+def _rows(name, cache, layer, k, v, slots):
     """(tokens, dtype, strides of K, strides of V) of rows [tokens, n_kv_heads, head_dim]."""
     if slots.dim() != 1 or slots.dtype is not _torch().int64 or not slots.is_contiguous():
         _refuse(name, "slots is a contiguous int64 vector, one per token")
@@ -614,6 +627,8 @@ def _rows(name, cache, k, v, slots):
     (kt, kh, kd), (vt, vh, vd) = k.stride(), v.stride()
     if t and (kd != 1 or vd != 1):
         _refuse(name, "head_dim has to be contiguous")
+    if t > _INT32 or layer > _INT32 or layer < 0:
+        _int32(name, t, layer)
     if t < 2:
         kt = vt = 0
     if h < 2:
@@ -625,7 +640,7 @@ def kv_op_cache_write(cache: PagedCache, layer: int, k, v, slots, stream=None):
     """K and V rows [T, n_kv_heads, head_dim] (bf16 or fp32) into the cache's slots (int64 [T], block * block_size +
     offset; -1 skips a token).  An e4m3 cache quantises them on the way."""
     name = "kv_op_cache_write"
-    t, dtype, kt, kh, vt, vh = _rows(name, cache, k, v, slots)
+    t, dtype, kt, kh, vt, vh = _rows(name, cache, layer, k, v, slots)
     index, stream = _on_device(name, stream, (cache.data, k, v, slots))
     _launch(name, index, (cache._desc_ref, layer, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, dtype, t, slots.data_ptr(),
                           stream))
@@ -635,13 +650,14 @@ def kv_op_cache_read(cache: PagedCache, layer: int, slots, k_out, v_out, stream=
     """The cache's rows at `slots` into k_out and v_out [T, n_kv_heads, head_dim] (bf16 or fp32); rows whose slot is
     outside the pool stay as they were."""
     name = "kv_op_cache_read"
-    t, dtype, kt, kh, vt, vh = _rows(name, cache, k_out, v_out, slots)
+    t, dtype, kt, kh, vt, vh = _rows(name, cache, layer, k_out, v_out, slots)
     index, stream = _on_device(name, stream, (cache.data, slots, k_out, v_out))
     _launch(name, index, (cache._desc_ref, layer, slots.data_ptr(), t, k_out.data_ptr(), kt, kh, v_out.data_ptr(), vt, vh,
                           dtype, stream))
 
 
 def kv_paged_attention_batched_scratch_bytes(n_req: int, n_q_heads: int, cache: PagedCache, max_ctx: int) -> int:
+    _int32("kv_paged_attention_batched_scratch_bytes", n_req, n_q_heads, max_ctx)
     r = load().kv_paged_attention_batched_scratch_bytes(n_req, n_q_heads, cache.n_kv_heads, cache.head_dim, max_ctx)
     if r < 0:
         raise KVError(int(r), "kv_paged_attention_batched_scratch_bytes")
@@ -685,6 +701,8 @@ def kv_op_paged_attention_batched(q, cache: PagedCache, layer: int, block_tables
         tensors.append(scratch)
         scratch_ptr, scratch_bytes = scratch.data_ptr(), scratch.numel() * scratch.element_size()
     dtype = _dtype(name, q.dtype)
+    if r > _INT32 or hq > _INT32 or max_ctx > _INT32 or layer > _INT32 or max_ctx < 0 or layer < 0:
+        _int32(name, r, hq, max_ctx, layer)
     index, stream = _on_device(name, stream, tensors)
     _launch(name, index, (q.data_ptr(), qr if r > 1 else 0, dtype, r, hq, cache._desc_ref, layer, block_tables.data_ptr(),
                           row, context_lens.data_ptr(), max_ctx, d ** -0.5 if softmax_scale is None else softmax_scale,

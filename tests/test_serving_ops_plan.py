@@ -91,3 +91,30 @@ def test_attention_in_place_with_other_strides_is_refused(lib, elem):
     import torch
     if not torch.cuda.is_available():      # these go on, as far as the missing device
         assert call(3, x, 256, 256) == call(1, x, 0, 256) == call(3, other, 512, 256) == -13
+
+
+def test_numbers_past_32_bits_are_refused_not_cut():
+    """2^32 + 5 tokens are not 5, layer 2^32 is not layer 0 (tensors without memory: nothing of them is read)."""
+    torch = pytest.importorskip("torch")
+    import paper_2608_16477_b200 as kv
+    import synth
+    cache, big = kv.PagedCache(synth.SHAPES["tiny"], 4, device="cpu"), (1 << 32) + 5
+    rope = kv.Rope(64)
+    x = torch.empty(big, 2, 64, device="meta")
+    rows, slots = torch.empty(3, 2, 64, device="meta"), torch.empty(3, dtype=torch.int64, device="meta")
+    q, lens = torch.empty(1, 4, 64, device="meta"), torch.empty(1, dtype=torch.int32, device="meta")
+    table = torch.empty(1, big, dtype=torch.int32, device="meta")
+    calls = [lambda: kv.kv_op_rope(rope, x, torch.empty(big, dtype=torch.int32, device="meta"), x),
+             lambda: kv.kv_op_cache_write(cache, 0, x, x, torch.empty(big, dtype=torch.int64, device="meta")),
+             lambda: kv.kv_op_cache_read(cache, 0, torch.empty(big, dtype=torch.int64, device="meta"), x, x),
+             lambda: kv.kv_op_cache_write(cache, 1 << 32, rows, rows, slots),
+             lambda: kv.kv_op_cache_read(cache, -(1 << 32), slots, rows, rows),
+             lambda: kv.kv_op_paged_attention_batched(q, cache, 1 << 32, table, lens, 16, q, None),
+             lambda: kv.kv_op_paged_attention_batched(q, cache, 0, table, lens, big, q, None),
+             lambda: kv.kv_paged_attention_batched_scratch_bytes(big, 4, cache, 16),
+             lambda: kv.kv_paged_attention_batched_scratch_bytes(1, 4, cache, big),
+             lambda: kv.Rope((1 << 32) + 64)]
+    for i, call in enumerate(calls):
+        with pytest.raises(ValueError, match="32-bit"):
+            call()
+            pytest.fail(f"call {i} was taken")
