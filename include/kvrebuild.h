@@ -39,8 +39,8 @@
  *
  * e4m3 pages (kv_cache_desc.elem_bytes = 1): the values are 8-bit e4m3 codes in the same [slot][kv_head][dim] order,
  * followed by one scale byte per (kv_head, slot), laid out [kv_head][slot] and padded to a multiple of 16 bytes
- * (kv_cache_page_bytes()).  Element = code * 2^(scale byte - 127).  The scale is a power of two, so reading a code back
- * into bf16 or fp32 is exact.  Such caches are written by kv_op_cache_write, read by kv_op_cache_read and
+ * (kv_cache_page_bytes()).  Element = code * 2^(scale byte - 127), scale byte 17 to 246.  The scale is a power of two, so reading
+ * a code back into bf16 or fp32 is exact.  Such caches are written by kv_op_cache_write, read by kv_op_cache_read and
  * kv_op_paged_attention_batched, and migrate through pack / unpack (pages travel as bytes, scales included); the other
  * entry points take bf16 pages and refuse them with KV_ERR_SHAPE.
  *
@@ -316,7 +316,9 @@ int32_t kv_op_paged_attention_noalloc(const float *q_dev, int32_t n_q_heads, con
  *   KV_ROPE_SCALE_NTK     base is replaced by base * factor^(rotary_dim / (rotary_dim - 2)); rotary_dim > 2
  *   KV_ROPE_SCALE_PARTS   g_j = clamp((original_ctx * theta_j / (2 pi) - low) / (high - low), 0, 1): pairs that turn more
  *                         than `high` times within original_ctx keep theta_j, those below `low` take theta_j / factor,
- *                         (1 - g_j) theta_j / factor + g_j theta_j between them
+ *                         (1 - g_j) theta_j / factor + g_j theta_j between them.  The blend is linear in the number of TURNS.  Another
+ *                         convention is linear in the pair's index between the same two borders: its frequencies differ in the
+ *                         middle, so a cache that was rotated by it does not fit a query that is rotated here
  * rotary_dim is even and at most 256; base (NTK: the replaced one too) and factor are finite and positive, gain is in fp32's normal
  * range; high > low; no pair may turn by more than one radian per position (a base below 1, or a factor that speeds
  * positions up, is refused with KV_ERR_ARG). */
@@ -367,7 +369,10 @@ int32_t kv_op_cache_read(const kv_cache_desc *cache, int32_t layer, const int64_
  * lse of that request's heads that read its KV head; in a cached value, its dim of those outs.  What lies behind a context
  * enters no result.  Where finite numbers leave fp32: a score below its range weighs nothing, a score or a weighted sum of
  * values beyond it gives NaN, and a context whose scores are all below it gives NaN in out and lse.
- * fp32 sums and softmax.  out may be q itself with the same strides.
+ * Sums, softmax and accumulators are fp32.  The operands of the matrix instructions are sums of 16-bit parts: in fp32 calls queries
+ * and weights to 2^-24 over bf16 pages and to 2^-22 over e4m3 pages, in bf16 calls queries as they are and weights to 2^-16 (2^-22);
+ * over e4m3 pages nothing finer than 2^-36 of a query's largest value or of a request's largest contribution.
+ * out may be q itself with the same strides (KV_ERR_ARG with others).
  * scratch_dev: kv_paged_attention_batched_scratch_bytes() bytes (what is enough for n_req and max_ctx is enough for fewer
  * requests and a smaller max_ctx), 16-byte aligned, contents need not survive between calls; calls that may overlap on the
  * GPU need scratch of their own.  head_dim 64 or 128. */

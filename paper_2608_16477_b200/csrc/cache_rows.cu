@@ -10,9 +10,11 @@
 // consecutive lanes move consecutive 16-byte (bf16) or 8-byte (codes) pieces.  A thread keeps its place in the token (K or
 // V, head, piece) for all its tokens, so that only the slot's page has to be worked out for each; once there are tokens
 // enough it takes two at a time, with their slots, then all their loads, in flight together.  The maximum runs over the raw
-// bits (an infinity or NaN shows in it, and only then the row is gone through value by value).  Measured: 16,384 tokens of
-// 8 heads of 128, bf16 to e4m3 and back, 101 MB each way: 18.8 us (5.4 TB/s, 82 % of a copy's rate with the launch in it);
-// 64 tokens 2.0 us.  A piece of 8 to a lane and index arithmetic for every row: 161 instructions a warp and row, 27 us.
+// bits (an infinity or NaN shows in it, and only then the row is gone through value by value).  Measured in a graph / call after
+// call, 16,384 tokens of 8 heads of 128: bf16 to e4m3 and back, 101 MB each way, 18.4 / 20.5 and 18.8 / 20.5 us (5.4 / 4.9 TB/s,
+// 82 / 75 % of a copy's rate with the launch in it); bf16 to bf16 pages and back, 134 MB, 24.3 / 26.6 and 23.0 / 24.9 us (5.5 and 5.8
+// TB/s), fp32, 201 MB, 33.9 / 36.1 and 38.3 / 40.7 us.  64 tokens 1.9 to 2.5 us.  A piece of 8 to a lane and index arithmetic for
+// every row: 161 instructions a warp and row, 27 us.
 #include <float.h>
 
 #include "common.cuh"

@@ -4,10 +4,10 @@
 //   s_n = scale * q . k_n      o = sum_n 2^(t_n - m) v_n / sum_n 2^(t_n - m)      t = s * log2(e), m = max t
 //
 // Bound by HBM: each cached row is read once for all the query heads of its group (2 flops per byte and head), so what
-// matters is to keep enough loads in flight (135 KB an SM) and every SM equally busy, whatever the lengths.  Measured, 64
-// query and 8 KV heads of 128: 32 requests of up to 18,433 tokens over e4m3 pages (512 MB) 89 to 95 us, 5.4 to 5.8 TB/s; 16 of
-// up to 8,192 over bf16 pages (305 MB) 54 us, 5.6 TB/s; one of 18,433 (38 MB) 16 us, of which 9 us are the fixed cost of a
-// split call.
+// matters is to keep enough loads in flight (135 KB an SM) and every SM equally busy, whatever the lengths.  Measured in a graph /
+// call after call in a stream, 64 query and 8 KV heads of 128: 32 requests of up to 18,433 tokens over e4m3 pages (512 MB) 89 / 92 us,
+// 5.7 / 5.6 TB/s (102 us after seconds of it, when the power cap has the clock at 1.64 of 1.97 GHz); 16 of up to 8,192 over bf16
+// pages (305 MB) 55 / 57 us, 5.6 / 5.3 TB/s; one of 18,433 (38 MB) 16 / 18.5 us, of which 9 us are the fixed cost of a split call.
 //
 // Split.  The contexts of all requests are laid end to end in tiles (and one more for each request) and cut into equal
 // ranges, one per CTA column, so one long request and a hundred short ones load the machine alike.  A range that holds a
@@ -23,10 +23,11 @@
 // The products run on mma.sync m16n8k16 with the keys (S^T = K Q^T) and the head's dims (O^T = V^T P^T) as the 16 rows and
 // the query heads as the 8 columns: a KV group has 8 heads or fewer, so nothing is padding.  (A 128-row tcgen05 tile would
 // hold 8 useful columns of at least 16 as well, but wants its operands through shared-memory descriptors, and e4m3 rows
-// would have to be converted and written back there first.)  Groups of more than 8 heads are taken 8 at a time.
+// would have to be converted and written back there first.)  Groups of more than 8 heads are taken 8 at a time, each time with
+// a copy of K and V from L2 (16 requests of up to 8,192, 64 / 128 / 256 query heads: 36 / 55 / 99 us, over bf16 pages 56 / 67 / 115).
 // fp32 operands go in as sums of 16-bit parts that are multiplied one after the other.  Over e4m3 pages q and the weights p
-// are two fp16: 2^-22 of a value, but no less than fp16's smallest step, which is 2^-36 of the query's largest value (a bf16
-// query is one part: exact down to 2^-28 of its largest) and half of which is 2^-36 of the request's largest contribution so far.
+// are two fp16: off by 2^-22 of themselves, and by up to 2^-36 of the query's largest value or of the request's largest contribution
+// so far, where fp16 ends (a bf16 query is one part: exact down to 2^-28 of its largest value).
 // Over bf16 pages they are three bf16 in fp32 calls (2^-24); in bf16 calls q is one part, exact, and p two (2^-16, a 256th of
 // the rounding of the result; the sum of the weights, and lse, take them whole).  The second part of the weights costs bf16
 // calls over e4m3 pages 0.5 % (128 requests of up to 577 tokens: 1.6 %): the loads are what bounds them.
@@ -816,8 +817,9 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
   cp_wait_group<0>();
 }
 
-// Joins the records of a (request, query head): the parts that hold its tiles follow from the starts.  Placed while the
-// first kernel still runs (programmatic launch); everything that kernel wrote is read behind the wait, past L1.
+// Joins the records of a (request, query head): the parts that hold its tiles follow from the starts.  Its blocks are placed as
+// CTAs of the first kernel leave (programmatic launch; two of those for 128 dims fill an SM's registers); everything that kernel wrote is
+// read behind the wait, past L1.
 // A chain of loads from L2 is all this costs, so a warp has the (m, l) and the outputs of kJoinBatch records in flight at
 // once, and where there are few requests (with many records each) four warps share a head.
 constexpr int kJoinThreads = 128;
@@ -1012,9 +1014,9 @@ int ba_launch(const BaParams &p, const BaPlan &b, int device, cudaStream_t st) {
   KV_COUNT_LAUNCH();
   KV_CUDA(cudaGetLastError());
   if (b.whole) return KV_OK;
-  // Four warps per head while every block of such a grid can be resident at once, one beyond that.  Measured, the whole call,
-  // four / one: one request of 18,433 tokens 16.0 / 21.2 us, 4 of up to 4,608 10.7 / 12.8, 16 23.8 / 24.0, 32 39.8 / 38.1, 128
-  // of up to 577 48.6 / 28.4 (nearly every block has nothing, or two records, to join).
+  // Four warps per head up to eight heads an SM, one beyond that.  Measured, the whole call, four / one, 64 heads: one request of
+  // 18,433 tokens 16.0 / 21.2 us, 4 of up to 4,608 10.7 / 12.8, 16 23.8 / 24.0, 32 39.8 / 38.1, 128 of up to 577 48.6 / 28.4 (nearly
+  // every block has nothing, or two records, to join).
   const int wph = (long long)p.n_req * p.n_q_heads <= 8ll * sm_count(device) ? 4 : 1, heads = kJoinThreads / 32 / wph;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(p.n_req, (p.n_q_heads + heads - 1) / heads);

@@ -9,8 +9,9 @@
 // HBM-bound: 2 * rows * head_dim elements move (3 fma per element).  A token's cosines and sines are needed by all its
 // heads, so a CTA takes one or two whole tokens, its threads form each (token, pair) once into shared memory, and the heads
 // are then streamed: one thread owns 2 x 16 bytes of a head (both members of its pairs), neighbouring threads
-// neighbouring vectors.  Measured: 16,384 tokens of 72 heads of 128, bf16, 604 MB: 98 us, 6.2 TB/s (94 % of a copy's rate);
-// 1,003 tokens of 40 heads, fp32, 41 MB: 9.1 us; one token 2.5 us.
+// neighbouring vectors.  Measured in a graph / call after call in a stream: 16,384 tokens of 72 heads of 128, bf16, 604 MB: 98 / 100 us,
+// 6.2 / 6.0 TB/s (94 / 92 % of a copy's rate; 108 us after seconds of it, when the power cap has the clock at 1.79 of 1.97 GHz);
+// 1,003 tokens of 40 heads, fp32, 41 MB: 8.6 / 10.2 us; one token 2.5 / 6.7 us.
 #include <float.h>
 
 #include <cmath>
@@ -77,7 +78,8 @@ struct Vec<bf16> {
   }
 };
 
-// cosines and sines (times gain) of the CTA's tokens: cs[token][pair]
+// cosines and sines (times gain) of the CTA's tokens: cs[token][pair].  The product with gain is a rounding of its own, 2^-24
+// beside sincospi's ulp, and none where gain is 1: fp64 for it would be an operation more for each pair of every token.
 __device__ __forceinline__ void rope_table_of(const RopeParams &p, int t0, int nt, float2 (*cs)[kRopeMaxPairs]) {
   const int half = p.rotary >> 1;
   for (int i = threadIdx.x; i < nt * half; i += kRopeThreads) {
@@ -178,7 +180,8 @@ __global__ void __launch_bounds__(kRopeThreads) rope_vec_kernel(const __grid_con
 // Halves whose members do not start on the same place of a vector (rotary / 2 no multiple of its length), in rows that can
 // be read as vectors all the same: a warp takes up to eight heads of a token through shared memory, vectors in and out, pairs
 // in between (8,000 tokens of 72 heads of 128, 102 rotated: 70 us, against 255 us with a thread per pair straight from
-// global memory).
+// global memory; 45 us of bytes, 53 us where all 128 are rotated: a warp's loads, turns and stores follow one another with
+// nothing in flight meanwhile, and its pairs are read from shared memory two bytes at a time).
 constexpr int kRopeRowBytes = 4096;      // of a warp
 template <typename T>
 __global__ void __launch_bounds__(kRopeThreads) rope_row_kernel(const __grid_constant__ RopeParams p) {
