@@ -5,9 +5,10 @@
 //
 // Bound by HBM: each cached row is read once for all the query heads of its group (2 flops per byte and head), so what
 // matters is to keep enough loads in flight (135 KB an SM) and every SM equally busy, whatever the lengths.  Measured in a graph /
-// call after call in a stream, 64 query and 8 KV heads of 128: 32 requests of up to 18,433 tokens over e4m3 pages (512 MB) 89 / 92 us,
-// 5.7 / 5.6 TB/s (102 us after seconds of it, when the power cap has the clock at 1.64 of 1.97 GHz); 16 of up to 8,192 over bf16
-// pages (305 MB) 55 / 57 us, 5.6 / 5.3 TB/s; one of 18,433 (38 MB) 16 / 18.5 us, of which 9 us are the fixed cost of a split call.
+// call after call in a stream, 64 query and 8 KV heads of 128: 32 requests of up to 18,433 tokens over e4m3 pages (512 MB)
+// 89 / 92 us, 5.7 / 5.6 TB/s (97 to 102 us after seconds of it, when the power cap has taken the clock from 1.97 to 1.64 GHz);
+// 16 of up to 8,192 over bf16 pages (305 MB) 55 / 57 us, 5.6 / 5.3 TB/s; one of 18,433 (38 MB) 16 / 18.5 us, of which 9 us are
+// the fixed cost of a split call.
 //
 // Split.  The contexts of all requests are laid end to end in tiles (and one more for each request) and cut into equal
 // ranges, one per CTA column, so one long request and a hundred short ones load the machine alike.  A range that holds a

@@ -9,9 +9,9 @@
 // HBM-bound: 2 * rows * head_dim elements move (3 fma per element).  A token's cosines and sines are needed by all its
 // heads, so a CTA takes one or two whole tokens, its threads form each (token, pair) once into shared memory, and the heads
 // are then streamed: one thread owns 2 x 16 bytes of a head (both members of its pairs), neighbouring threads
-// neighbouring vectors.  Measured in a graph / call after call in a stream: 16,384 tokens of 72 heads of 128, bf16, 604 MB: 98 / 100 us,
-// 6.2 / 6.0 TB/s (94 / 92 % of a copy's rate; 108 us after seconds of it, when the power cap has the clock at 1.79 of 1.97 GHz);
-// 1,003 tokens of 40 heads, fp32, 41 MB: 8.6 / 10.2 us; one token 2.5 / 6.7 us.
+// neighbouring vectors.  Measured in a graph / call after call in a stream: 16,384 tokens of 72 heads of 128, bf16, 604 MB:
+// 98 / 100 us, 6.2 / 6.0 TB/s (94 / 92 % of a copy's rate; 102 to 108 us after seconds of it, when the power cap has taken the
+// clock from 1.97 to 1.8 GHz); 1,003 tokens of 40 heads, fp32, 41 MB: 8.6 / 10.2 us; one token 2.5 / 6.7 us.
 #include <float.h>
 
 #include <cmath>
