@@ -141,9 +141,9 @@ def _quantised4(x):
     max |x| <= 6 * 448 * 2^e, a group's the least e4m3 number with max |x| <= 6 * s * 2^e; halves between two codes go up."""
     fine = torch.isfinite(x)
     size = torch.where(fine, x.abs(), torch.zeros_like(x))
-    power = _power(size.amax(-1), 0.65625, 12)                                                      # 2688
+    power = _power(size.amax(-1), 0.65625, 12).clamp_max(116)                 # 2688; what is stored stays in fp32's range
     size = (size * torch.exp2(-power.float()).unsqueeze(-1)).unflatten(-1, (-1, 16))
-    scale = 1 + torch.searchsorted(6.0 * E4M3.to(x.device), size.amax(-1).contiguous())
+    scale = (1 + torch.searchsorted(6.0 * E4M3.to(x.device), size.amax(-1).contiguous())).clamp_max(126)
     border = E4M3.to(x.device)[scale - 1].unsqueeze(-1)
     mids = MIDS.to(x.device)
     codes = (size >= mids[0] * border).int()
