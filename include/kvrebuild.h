@@ -40,9 +40,16 @@
  * e4m3 pages (kv_cache_desc.elem_bytes = 1): the values are 8-bit e4m3 codes in the same [slot][kv_head][dim] order,
  * followed by one scale byte per (kv_head, slot), laid out [kv_head][slot] and padded to a multiple of 16 bytes
  * (kv_cache_page_bytes()).  Element = code * 2^(scale byte - 127), scale byte 17 to 246.  The scale is a power of two, so reading
- * a code back into bf16 or fp32 is exact.  Such caches are written by kv_op_cache_write, read by kv_op_cache_read and
- * kv_op_paged_attention_batched, and migrate through pack / unpack (pages travel as bytes, scales included); the other
- * entry points take bf16 pages and refuse them with KV_ERR_SHAPE.
+ * a code back into bf16 or fp32 is exact.
+ *
+ * e2m1 pages (kv_cache_desc.elem_bytes = KV_ELEM_E2M1): for every KV head a record, padded to a multiple of 16 bytes, of 4-bit e2m1
+ * codes [slot][head_dim / 2] (two to a byte, the even dim in the low half), e4m3 scales of 16 consecutive dims [slot][head_dim / 16]
+ * and scale bytes [slot].  Element = code * e4m3 scale * 2^(scale byte - 127): six significant bits, exact in bf16 and fp32.  A row
+ * of 128 takes 73 bytes (e4m3: 129, bf16: 256).
+ *
+ * e4m3 and e2m1 caches are written by kv_op_cache_write and kv_op_cache_append, read by kv_op_cache_read, kv_op_block_bounds and the
+ * batched attention, and migrate through pack / unpack (pages travel as bytes, scales included); the other entry points take bf16
+ * pages and refuse them with KV_ERR_SHAPE.
  *
  * Wire buffer: headerless raw pages.  Layout KV_WIRE_BLOCK_MAJOR: [block i][layer][kv][page bytes], so
  * each completed block is one contiguous self-contained message ("newly completed suffix KV-cache
@@ -80,6 +87,7 @@ enum {
 enum { KV_WIRE_BLOCK_MAJOR = 0, KV_WIRE_LAYER_MAJOR = 1 };
 enum { KV_OP_PREFILL = 0, KV_OP_DECODE = 1 };
 enum { KV_DTYPE_BF16 = 0, KV_DTYPE_F32 = 1 };
+enum { KV_ELEM_E2M1 = -2 }; /* kv_cache_desc.elem_bytes: two elements to a byte */
 enum { KV_ROPE_HALF = 0, KV_ROPE_INTERLEAVED = 1 };
 enum { KV_ROPE_SCALE_NONE = 0, KV_ROPE_SCALE_LINEAR = 1, KV_ROPE_SCALE_NTK = 2, KV_ROPE_SCALE_PARTS = 3 };
 
@@ -107,7 +115,8 @@ typedef struct {
 typedef struct {
   void *base_dev;
   int64_t layer_stride, kv_stride, block_stride; /* bytes */
-  int32_t num_blocks, block_size, n_layers, n_kv_heads, head_dim, elem_bytes /* 2: bf16, 1: e4m3 + scale bytes */;
+  int32_t num_blocks, block_size, n_layers, n_kv_heads, head_dim;
+  int32_t elem_bytes; /* 2: bf16, 1: e4m3 + scale bytes, KV_ELEM_E2M1: e2m1 + scales */
 } kv_cache_desc;
 
 typedef struct kv_model kv_model; /* opaque host handle */
@@ -136,11 +145,12 @@ const char *kv_status_string(int32_t status);
 /* Text of the last CUDA error seen by this thread's calls ("" if none). */
 const char *kv_last_cuda_error(void);
 
-/* Eq. (1): s_KV = 2 * L * H_KV * d_h * b bytes per token (the values; e4m3 pages add one scale byte per layer, K or V and
- * KV head: kv_cache_page_bytes()). */
+/* Eq. (1): s_KV = 2 * L * H_KV * d_h * b bytes per token (the values; e4m3 and e2m1 pages add their scales:
+ * kv_cache_page_bytes()).  elem_bytes KV_ELEM_E2M1: b = 1/2. */
 int64_t kv_bytes_per_token(int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t elem_bytes);
 
-/* Bytes of one page (one layer, K or V, one block): elem_bytes 2 = bf16 values, 1 = e4m3 codes and their scale bytes. */
+/* Bytes of one page (one layer, K or V, one block): elem_bytes 2 = bf16 values, 1 = e4m3 codes and their scale bytes,
+ * KV_ELEM_E2M1 = e2m1 codes and their scales (head_dim a multiple of 16). */
 int64_t kv_cache_page_bytes(int32_t block_size, int32_t n_kv_heads, int32_t head_dim, int32_t elem_bytes);
 
 /* Synchronises `stream` and reads the device status word kept in `workspace_dev` by the last
@@ -346,18 +356,33 @@ int32_t kv_op_rope(const kv_rope *rope, const void *x_dev, int64_t x_token_strid
  * affected).  head_dim 64 or 128, n_tokens at most 2^30.
  * bf16 pages: each value rounded to nearest even.  e4m3 pages: for every (token, KV head) of K and of V, e is the least
  * integer with max |x| <= 448 * 2^e, kept within [-110, 119]; the codes are x * 2^-e (exact) rounded to nearest even and
- * saturated at 448, the scale byte is e + 127.  Infinities and NaN are left out of the maximum and stored as NaN. */
+ * saturated at 448, the scale byte is e + 127.  Infinities and NaN are left out of the maximum and stored as NaN.
+ * e2m1 pages: for every row e is the least integer with max |x| <= 6 * 448 * 2^e, kept within [-110, 116]; for every 16 dims s is
+ * the least positive e4m3 number with max |x| <= 6 * s * 2^e (448 beyond it); the codes are the e2m1 numbers nearest to x / (s * 2^e),
+ * of two the one away from zero.  Infinities and NaN are left out of the maxima; the 16 dims that one stands among are stored as NaN. */
 int32_t kv_op_cache_write(const kv_cache_desc *cache, int32_t layer, const void *k_dev, int64_t k_token_stride,
                           int64_t k_head_stride, const void *v_dev, int64_t v_token_stride, int64_t v_head_stride,
                           int32_t dtype, int32_t n_tokens, const int64_t *slots_dev, void *stream);
 
 /* The reverse: rows k_out[t], v_out[t] = the cache's values at slots_dev[t].  Rows whose slot lies outside the pool are
- * left as they were.  Slots may repeat.  Exact: bf16 and e4m3 pages lose nothing in rows of either type. */
+ * left as they were.  Slots may repeat.  Exact: pages of every format lose nothing in rows of either type. */
 int32_t kv_op_cache_read(const kv_cache_desc *cache, int32_t layer, const int64_t *slots_dev, int32_t n_tokens,
                          void *k_out_dev, int64_t k_token_stride, int64_t k_head_stride, void *v_out_dev,
                          int64_t v_token_stride, int64_t v_head_stride, int32_t dtype, void *stream);
 
-/* Attention of one new token per request over layer `layer` of the cache (bf16 or e4m3 pages).  Request r has query
+/* K and V rows of n_tokens tokens into the cache as kv_op_cache_write puts them there, K turned on the way as kv_op_rope turns it at
+ * positions_dev[t] (and rounded to dtype before it is quantised), and n_q_heads query heads of the same tokens turned from q_dev into
+ * q_out_dev: the same bits as kv_op_rope on both and kv_op_cache_write of the result, in one launch.  k_dev and v_dev are left as they
+ * were.  n_q_heads may be 0 (then q_dev and q_out_dev are not looked at); q_out may be q itself with the same strides; any other
+ * overlap of q_out with what is read is undefined.  A token whose slot lies outside the pool has its queries turned all the same.
+ * head_dim 64 or 128, rotary_dim at most head_dim, n_tokens at most 2^30. */
+int32_t kv_op_cache_append(const kv_rope *rope, const kv_cache_desc *cache, int32_t layer, const void *q_dev, int64_t q_token_stride,
+                           int64_t q_head_stride, int32_t n_q_heads, void *q_out_dev, int64_t q_out_token_stride,
+                           int64_t q_out_head_stride, const void *k_dev, int64_t k_token_stride, int64_t k_head_stride,
+                           const void *v_dev, int64_t v_token_stride, int64_t v_head_stride, int32_t dtype, int32_t n_tokens,
+                           const int32_t *positions_dev, const int64_t *slots_dev, void *stream);
+
+/* Attention of one new token per request over layer `layer` of the cache (bf16, e4m3 or e2m1 pages).  Request r has query
  * q_dev + r * q_stride ([n_q_heads][head_dim], heads contiguous, dtype), attends to positions [0, context_lens_dev[r])
  * through block_tables_dev[r * table_stride ..] and writes out_dev + r * out_stride (same dtype).  Query head h reads KV
  * head h / (n_q_heads / n_kv_heads):  s_n = softmax_scale * q . k_n,  out = sum_n exp(s_n) v_n / sum_n exp(s_n),
@@ -366,12 +391,13 @@ int32_t kv_op_cache_read(const kv_cache_desc *cache, int32_t layer, const int64_
  * with max_ctx <= table_stride * block_size and at most 2^26; table entries behind a request's last block are not read.
  * A block id outside the pool inside a context is not followed: that request's out and lse are NaN.  Infinities and NaN turn
  * into NaN what they enter, and nothing else: in a query, its head's out and lse; in a cached key inside a context, the out and
- * lse of that request's heads that read its KV head; in a cached value, its dim of those outs.  What lies behind a context
+ * lse of that request's heads that read its KV head; in a cached value, its dim (e2m1: the 16 dims of its scale) of those outs.  What
+ * lies behind a context
  * enters no result.  Where finite numbers leave fp32: a score below its range weighs nothing, a score or a weighted sum of
  * values beyond it gives NaN, and a context whose scores are all below it gives NaN in out and lse.
  * Sums, softmax and accumulators are fp32.  The operands of the matrix instructions are sums of 16-bit parts: in fp32 calls queries
- * and weights to 2^-24 over bf16 pages and to 2^-22 over e4m3 pages, in bf16 calls queries as they are and weights to 2^-16 (2^-22);
- * over e4m3 pages nothing finer than 2^-36 of a query's largest value or of a request's largest contribution.
+ * and weights to 2^-24 over bf16 pages and to 2^-22 over e4m3 and e2m1 pages, in bf16 calls queries as they are and weights to 2^-16
+ * (2^-22); over e4m3 and e2m1 pages nothing finer than 2^-36 of a query's largest value or of a request's largest contribution.
  * out may be q itself with the same strides (KV_ERR_ARG with others).
  * scratch_dev: kv_paged_attention_batched_scratch_bytes() bytes (what is enough for n_req and max_ctx is enough for fewer
  * requests and a smaller max_ctx), 16-byte aligned, contents need not survive between calls; calls that may overlap on the
@@ -384,6 +410,48 @@ int32_t kv_op_paged_attention_batched(const void *q_dev, int64_t q_stride, int32
                                       const int32_t *context_lens_dev, int32_t max_ctx, float softmax_scale,
                                       void *scratch_dev, int64_t scratch_bytes, void *out_dev, int64_t out_stride,
                                       float *lse_out_dev, void *stream);
+
+/* ---- attention over the blocks that promise most.  A long context is mostly blocks of small weight.  kv_op_block_bounds notes what
+ * every block's keys span, kv_op_select_blocks ranks a request's blocks by it for each KV head, kv_op_paged_attention_selected
+ * attends to the chosen ones.  A decode step: append, bounds of the blocks appended to, select, attend. */
+
+/* Bounds of blocks blocks_dev[0..n) of layer `layer`, from the keys in their slots [0, counts_dev[i]) (clamped to block_size).  For every
+ * KV head, e is the least integer with max |k| <= 127 * 2^e, at least -60; bounds_dev[block][head][0][dim] (int8, [num_blocks][n_kv_heads]
+ * [2][head_dim], 16-byte aligned) is the largest key value of the dim in units of 2^e rounded up, [1] the smallest rounded down, and
+ * bound_scales_dev[block][head] = e + 127.  Keys that are not finite or larger than 127 * 2^60 make codes of 0 and the scale byte 255:
+ * such a block is always chosen.  A block outside the pool, or a count below 1, is left out: nothing is written.  A block that is
+ * listed twice with different counts gets one of the two. */
+int32_t kv_op_block_bounds(const kv_cache_desc *cache, int32_t layer, const int32_t *blocks_dev, const int32_t *counts_dev, int32_t n,
+                           int8_t *bounds_dev, uint8_t *bound_scales_dev, void *stream);
+
+/* The blocks that each request's KV heads attend to: kept_dev[r][head][0..keep) (int32 block ids, contiguous) in the order of their
+ * positions, -1 behind them, and the length of the context that they make, kept_lens_dev[r].  A context of no more than `keep` blocks
+ * keeps them all.  Of a longer one the first `first` and the last `last` >= 1 blocks are always kept (the last may be partly filled,
+ * and is the only one that counts in part), and of the others the keep - first - last of the highest score, among equals the one at the
+ * lowest position.  Score of a block for a KV head: with u+ (u-) the sums over the group's query heads of the positive (negative)
+ * parts of their queries, in units of the least 2^e (at least 2^-100) that leaves them within 32767 and rounded to whole
+ * numbers (halves to even), score = sum_d (u+_d bounds[0][d] + u-_d bounds[1][d]) rounded to fp32, times 2^(scale byte - 127): the
+ * sum over the heads of a bound on q . k over the block's keys, up to that rounding.  It is exact but for its last rounding, so equal
+ * inputs choose equal blocks.  Infinities and NaN in a query count as 0.  A block outside the pool is always chosen, like one of scale byte 255; if
+ * there are more of those than places, the lowest positions are.  Query rows, tables and lengths as in kv_op_paged_attention_batched; bounds
+ * as kv_op_block_bounds writes them.  first + last <= keep, keep * block_size at most 2^26, n_req at most 65535.
+ * scratch_dev: kv_select_blocks_scratch_bytes() bytes, 16-byte aligned, contents need not survive; what is enough for n_req and max_ctx
+ * is enough for less.  Calls that may overlap on the GPU need scratch of their own. */
+int64_t kv_select_blocks_scratch_bytes(int32_t n_req, int32_t n_kv_heads, int32_t block_size, int32_t max_ctx);
+int32_t kv_op_select_blocks(const void *q_dev, int64_t q_stride, int32_t dtype, int32_t n_req, int32_t n_q_heads, int32_t n_kv_heads,
+                            int32_t head_dim, const int8_t *bounds_dev, const uint8_t *bound_scales_dev, int32_t num_blocks,
+                            int32_t block_size, const int32_t *block_tables_dev, int64_t table_stride, const int32_t *context_lens_dev,
+                            int32_t max_ctx, int32_t first, int32_t last, int32_t keep, void *scratch_dev, int64_t scratch_bytes,
+                            int32_t *kept_dev, int32_t *kept_lens_dev, void *stream);
+
+/* kv_op_paged_attention_batched with a block table for every KV head: KV head h of request r reads kept_dev[r * kept_stride + h *
+ * kept_head_stride ..] (strides in elements, at least the blocks of max_len).  Everything else, the scratch included, is as there, with
+ * max_len in the place of max_ctx and the one length kept_lens_dev[r] for all heads of a request. */
+int32_t kv_op_paged_attention_selected(const void *q_dev, int64_t q_stride, int32_t dtype, int32_t n_req, int32_t n_q_heads,
+                                       const kv_cache_desc *cache, int32_t layer, const int32_t *kept_dev, int64_t kept_stride,
+                                       int64_t kept_head_stride, const int32_t *kept_lens_dev, int32_t max_len, float softmax_scale,
+                                       void *scratch_dev, int64_t scratch_bytes, void *out_dev, int64_t out_stride, float *lse_out_dev,
+                                       void *stream);
 
 /* ---------------------------------------------------------------- window selection (host scalar code)
  * The Scheduler Engine's cost model and online selection (Section 4.1, Eqs. 3-9; Section 4.2, Algorithm 1;

@@ -23,7 +23,8 @@ EXPORTS = [
     "kv_window_evaluate", "kv_window_select", "kv_window_waste_bound", "kv_ewma", "kv_prefill_prefix_batched",
     "kv_selftest_bounded_wait", "kv_workspace_residual", "kv_cache_page_bytes", "kv_rope_create", "kv_rope_destroy",
     "kv_rope_frequencies", "kv_op_rope", "kv_op_cache_write", "kv_op_cache_read",
-    "kv_paged_attention_batched_scratch_bytes", "kv_op_paged_attention_batched",
+    "kv_paged_attention_batched_scratch_bytes", "kv_op_paged_attention_batched", "kv_op_cache_append", "kv_op_block_bounds",
+    "kv_select_blocks_scratch_bytes", "kv_op_select_blocks", "kv_op_paged_attention_selected",
 ]
 
 PROFILE_KINDS = ("embed", "rmsnorm", "gemm_qkv", "rope_store", "attention", "gemm_o", "gemm_gate_up", "gemm_down",
@@ -138,6 +139,14 @@ def load(build_if_missing: bool = True):
         "kv_paged_attention_batched_scratch_bytes": (i64, [i32, i32, i32, i32, i32]),
         "kv_op_paged_attention_batched": (i32, [vp, i64, i32, i32, i32, C.POINTER(CacheDesc), i32, vp, i64, vp, i32,
                                                 C.c_float, vp, i64, vp, i64, vp, vp]),
+        "kv_op_cache_append": (i32, [vp, C.POINTER(CacheDesc), i32, vp, i64, i64, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64,
+                                     i32, i32, vp, vp, vp]),
+        "kv_op_block_bounds": (i32, [C.POINTER(CacheDesc), i32, vp, vp, i32, vp, vp, vp]),
+        "kv_select_blocks_scratch_bytes": (i64, [i32, i32, i32, i32]),
+        "kv_op_select_blocks": (i32, [vp, i64, i32, i32, i32, i32, i32, vp, vp, i32, i32, vp, i64, vp, i32, i32, i32, i32, vp, i64,
+                                      vp, vp, vp]),
+        "kv_op_paged_attention_selected": (i32, [vp, i64, i32, i32, i32, C.POINTER(CacheDesc), i32, vp, i64, i64, vp, i32,
+                                                 C.c_float, vp, i64, vp, i64, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -171,26 +180,38 @@ def _ptr(t) -> int:
     return 0 if t is None else (t.data_ptr() if hasattr(t, "data_ptr") else int(t))
 
 
+KV_ELEM_E2M1 = -2
+
+
+def _elem(elem_bytes) -> int:
+    """kv_cache_desc.elem_bytes of 2 (bf16), 1 (e4m3) or 0.5 (e2m1)."""
+    return KV_ELEM_E2M1 if elem_bytes == 0.5 else elem_bytes
+
+
 class PagedCache:
-    """A paged KV cache in device memory plus its descriptor: a torch tensor of bf16 bit patterns (elem_bytes 2, int16)
-    or of e4m3 pages with their scale bytes (elem_bytes 1, uint8).
+    """A paged KV cache in device memory plus its descriptor: a torch tensor of bf16 bit patterns (elem_bytes 2, int16),
+    of e4m3 pages with their scale bytes (elem_bytes 1, uint8) or of e2m1 pages with their scales (elem_bytes 0.5, uint8).
 
     layout "layer_major": [L][2][num_blocks][page]; "block_major": [num_blocks][L][2][page].  `data` gives the cache
     memory that is there already (contiguous, of exactly the pool's size) instead of allocating it.
     """
 
     def __init__(self, shape, num_blocks: int, layout: str = "layer_major", device="cuda", fill=None,
-                 elem_bytes: int = 2, data=None):
+                 elem_bytes: float = 2, data=None):
         import torch
         self.n_layers, self.n_kv_heads, self.head_dim = shape.n_layers, shape.n_kv_heads, shape.head_dim
         self.block_size, self.num_blocks, self.layout = shape.block_size, num_blocks, layout
         self.elem_bytes = elem_bytes
-        if elem_bytes not in (1, 2):
-            raise ValueError(f"elem_bytes {elem_bytes}: 2 (bf16) or 1 (e4m3)")
-        self.page_bytes = self.block_size * self.n_kv_heads * self.head_dim * elem_bytes
+        if elem_bytes not in (0.5, 1, 2):
+            raise ValueError(f"elem_bytes {elem_bytes}: 2 (bf16), 1 (e4m3) or 0.5 (e2m1)")
+        if elem_bytes == 0.5:
+            self.page_bytes = self.n_kv_heads * (-(-self.block_size * (self.head_dim // 2 + self.head_dim // 16 + 1) // 16) * 16)
+        else:
+            self.page_bytes = self.block_size * self.n_kv_heads * self.head_dim * elem_bytes
         if elem_bytes == 1:
             self.page_bytes += -(-self.block_size * self.n_kv_heads // 16) * 16
-        page_elems = self.page_bytes // elem_bytes
+        item = 2 if elem_bytes == 2 else 1
+        page_elems = self.page_bytes // item
         if layout == "layer_major":
             dims = (self.n_layers, 2, num_blocks, page_elems)
             strides = (2 * num_blocks * self.page_bytes, num_blocks * self.page_bytes, self.page_bytes)
@@ -201,18 +222,18 @@ class PagedCache:
             raise ValueError(layout)
         if data is None:
             self.data = torch.empty(dims, dtype=torch.int16 if elem_bytes == 2 else torch.uint8, device=device)
-        elif not data.is_contiguous() or data.numel() * data.element_size() != int(np.prod(dims)) * elem_bytes:
+        elif not data.is_contiguous() or data.numel() * data.element_size() != int(np.prod(dims)) * item:
             raise ValueError("data: a contiguous tensor of the pool's size is wanted")
         else:
             self.data = data.view(torch.int16 if elem_bytes == 2 else torch.uint8).view(dims)
         if fill is not None:
             self.data.fill_(fill)
         self.desc = CacheDesc(self.data.data_ptr(), strides[0], strides[1], strides[2], num_blocks, self.block_size,
-                              self.n_layers, self.n_kv_heads, self.head_dim, elem_bytes)
+                              self.n_layers, self.n_kv_heads, self.head_dim, _elem(elem_bytes))
         self._desc_ref = C.byref(self.desc)
 
     def pages(self, block_ids):
-        """int16 (bf16) or uint8 (e4m3) tensor [len(ids), L, 2, page] of the given blocks (torch indexing; test helper)."""
+        """int16 (bf16) or uint8 (e4m3, e2m1) tensor [len(ids), L, 2, page] of the given blocks (torch indexing; test helper)."""
         import torch
         idx = torch.as_tensor(np.asarray(block_ids, dtype=np.int64), device=self.data.device)
         if self.layout == "layer_major":
@@ -222,7 +243,7 @@ class PagedCache:
     def as_logical_numpy(self) -> np.ndarray:
         """uint16 array [L, 2, num_blocks, Bs, Hkv, d] of a bf16 cache on the host."""
         if self.elem_bytes != 2:
-            raise ValueError("as_logical_numpy: bf16 caches only (kv_op_cache_read decodes e4m3 pages)")
+            raise ValueError("as_logical_numpy: bf16 caches only (kv_op_cache_read decodes the others)")
         d = self.data if self.layout == "layer_major" else self.data.permute(1, 2, 0, 3)
         return d.contiguous().cpu().numpy().view(np.uint16).reshape(
             self.n_layers, 2, self.num_blocks, self.block_size, self.n_kv_heads, self.head_dim)
@@ -283,11 +304,11 @@ class Model:
 
 
 def kv_bytes_per_token(n_layers, n_kv_heads, head_dim, elem_bytes=2) -> int:
-    return load().kv_bytes_per_token(n_layers, n_kv_heads, head_dim, elem_bytes)
+    return load().kv_bytes_per_token(n_layers, n_kv_heads, head_dim, _elem(elem_bytes))
 
 
-def kv_cache_page_bytes(block_size: int, n_kv_heads: int, head_dim: int, elem_bytes: int) -> int:
-    r = load().kv_cache_page_bytes(block_size, n_kv_heads, head_dim, elem_bytes)
+def kv_cache_page_bytes(block_size: int, n_kv_heads: int, head_dim: int, elem_bytes: float) -> int:
+    r = load().kv_cache_page_bytes(block_size, n_kv_heads, head_dim, _elem(elem_bytes))
     if r < 0:
         raise KVError(int(r), "kv_cache_page_bytes")
     return int(r)
@@ -638,7 +659,7 @@ def _rows(name, cache, layer, k, v, slots):
 
 def kv_op_cache_write(cache: PagedCache, layer: int, k, v, slots, stream=None):
     """K and V rows [T, n_kv_heads, head_dim] (bf16 or fp32) into the cache's slots (int64 [T], block * block_size +
-    offset; -1 skips a token).  An e4m3 cache quantises them on the way."""
+    offset; -1 skips a token).  An e4m3 or e2m1 cache quantises them on the way."""
     name = "kv_op_cache_write"
     t, dtype, kt, kh, vt, vh = _rows(name, cache, layer, k, v, slots)
     index, stream = _on_device(name, stream, (cache.data, k, v, slots))
@@ -707,3 +728,176 @@ def kv_op_paged_attention_batched(q, cache: PagedCache, layer: int, block_tables
     _launch(name, index, (q.data_ptr(), qr if r > 1 else 0, dtype, r, hq, cache._desc_ref, layer, block_tables.data_ptr(),
                           row, context_lens.data_ptr(), max_ctx, d ** -0.5 if softmax_scale is None else softmax_scale,
                           scratch_ptr, scratch_bytes, out.data_ptr(), outr if r > 1 else 0, lse_ptr, stream))
+
+
+def kv_op_cache_append(rope: Rope, cache: PagedCache, layer: int, k, v, positions, slots, q=None, q_out=None, stream=None):
+    """kv_op_rope on k (and on q, into q_out) and kv_op_cache_write of the result in one launch: k and v [T, n_kv_heads, head_dim]
+    (left as they were), q and q_out [T, heads, head_dim] or None (q_out may be q), positions int32 [T], slots int64 [T]."""
+    name, torch = "kv_op_cache_append", _torch()
+    t, dtype, kt, kh, vt, vh = _rows(name, cache, layer, k, v, slots)
+    if positions.shape != (t,) or positions.dtype is not torch.int32 or not positions.is_contiguous():
+        _refuse(name, "positions is a contiguous int32 vector, one per token")
+    if (q is None) != (q_out is None):
+        _refuse(name, "q and q_out come together")
+    tensors = (cache.data, k, v, positions, slots)
+    hq = q_ptr = q_to = qt = qh = ot = oh = 0
+    if q is not None:
+        if q.dim() != 3 or q.shape[0] != t or q.shape[2] != cache.head_dim or q_out.shape != q.shape or \
+                q.dtype is not k.dtype or q_out.dtype is not k.dtype:
+            _refuse(name, "q and q_out are [tokens, heads, head_dim], of the type of k")
+        hq = q.shape[1]
+        (qt, qh, qd), (ot, oh, od) = q.stride(), q_out.stride()
+        if t and hq and (qd != 1 or od != 1):
+            _refuse(name, "head_dim has to be contiguous")
+        if hq > _INT32:
+            _int32(name, hq)
+        if t < 2:
+            qt = ot = 0
+        if hq < 2:
+            qh = oh = 0
+        tensors = (cache.data, k, v, positions, slots, q, q_out)
+        q_ptr, q_to = q.data_ptr(), q_out.data_ptr()
+    index, stream = _on_device(name, stream, tensors)
+    _launch(name, index, (rope.handle, cache._desc_ref, layer, q_ptr, qt, qh, hq, q_to, ot, oh, k.data_ptr(), kt, kh, v.data_ptr(), vt,
+                          vh, dtype, t, positions.data_ptr(), slots.data_ptr(), stream))
+
+
+class BlockBounds:
+    """What the keys of every block of a cache span, per layer and KV head: codes int8 [layers, blocks, n_kv_heads, 2, head_dim] and
+    scales uint8 [layers, blocks, n_kv_heads], written by kv_op_block_bounds.  codes and scales give memory that is there already."""
+
+    def __init__(self, cache: PagedCache, codes=None, scales=None):
+        torch = _torch()
+        self.n_layers, self.num_blocks, self.n_kv_heads = cache.n_layers, cache.num_blocks, cache.n_kv_heads
+        self.head_dim, self.block_size = cache.head_dim, cache.block_size
+        shape = (cache.n_layers, cache.num_blocks, cache.n_kv_heads)
+        if codes is None:
+            codes = torch.zeros(*shape, 2, cache.head_dim, dtype=torch.int8, device=cache.data.device)
+        if scales is None:
+            scales = torch.zeros(shape, dtype=torch.uint8, device=cache.data.device)
+        if codes.shape != (*shape, 2, cache.head_dim) or codes.dtype is not torch.int8 or not codes.is_contiguous():
+            _refuse("BlockBounds", "codes is contiguous int8 [layers, blocks, n_kv_heads, 2, head_dim]")
+        if scales.shape != shape or scales.dtype is not torch.uint8 or not scales.is_contiguous():
+            _refuse("BlockBounds", "scales is contiguous uint8 [layers, blocks, n_kv_heads]")
+        self.codes, self.scales = codes, scales
+
+    def _layer(self, name, layer):
+        """Addresses of a layer's codes and scales."""
+        if not 0 <= layer < self.n_layers:
+            raise KVError(-2, name)
+        blocks = self.num_blocks * self.n_kv_heads
+        return self.codes.data_ptr() + layer * blocks * 2 * self.head_dim, self.scales.data_ptr() + layer * blocks
+
+
+def kv_op_block_bounds(cache: PagedCache, layer: int, blocks, counts, bounds: BlockBounds, stream=None):
+    """Bounds of the blocks (int32 [n]) from the keys in their first counts (int32 [n]) slots."""
+    name, torch = "kv_op_block_bounds", _torch()
+    if blocks.dim() != 1 or blocks.dtype is not torch.int32 or not blocks.is_contiguous():
+        _refuse(name, "blocks is a contiguous int32 vector")
+    n = blocks.shape[0]
+    if counts.shape != (n,) or counts.dtype is not torch.int32 or not counts.is_contiguous():
+        _refuse(name, "counts is a contiguous int32 vector, one per block")
+    if (bounds.num_blocks, bounds.n_kv_heads, bounds.head_dim, bounds.n_layers) != \
+            (cache.num_blocks, cache.n_kv_heads, cache.head_dim, cache.n_layers):
+        _refuse(name, "bounds of another cache")
+    if n > _INT32:
+        _int32(name, n)
+    codes, scales = bounds._layer(name, layer)
+    index, stream = _on_device(name, stream, (cache.data, blocks, counts, bounds.codes, bounds.scales))
+    _launch(name, index, (cache._desc_ref, layer, blocks.data_ptr(), counts.data_ptr(), n, codes, scales, stream))
+
+
+def kv_select_blocks_scratch_bytes(n_req: int, cache, max_ctx: int) -> int:
+    """cache: the PagedCache or its BlockBounds."""
+    _int32("kv_select_blocks_scratch_bytes", n_req, max_ctx)
+    r = load().kv_select_blocks_scratch_bytes(n_req, cache.n_kv_heads, cache.block_size, max_ctx)
+    if r < 0:
+        raise KVError(int(r), "kv_select_blocks_scratch_bytes")
+    return int(r)
+
+
+def _table(name, what, table, r, rows):
+    """Strides of int32 [r, blocks] (rows None) or [r, rows, blocks]: (columns, of a request, of a row)."""
+    lead = (r,) if rows is None else (r, rows)
+    if table.dim() != len(lead) + 1 or tuple(table.shape[:-1]) != lead or table.dtype is not _torch().int32:
+        _refuse(name, f"{what} is int32 [requests, {'' if rows is None else 'n_kv_heads, '}blocks]")
+    columns, stride = table.shape[-1], table.stride()
+    if table.numel() and columns > 1 and stride[-1] != 1:
+        _refuse(name, f"rows of {what} have to be contiguous")
+    of_row = stride[-2] if rows is not None and rows > 1 else columns
+    of_req = stride[0] if r > 1 else max(columns, of_row * (1 if rows is None else rows))
+    if table.numel() and (of_row < columns or of_req < columns):
+        _refuse(name, f"rows of {what} must not overlap")
+    return columns, of_req, of_row
+
+
+def kv_op_select_blocks(q, bounds: BlockBounds, layer: int, block_tables, context_lens, max_ctx: int, kept, kept_lens, scratch,
+                        first: int = 1, last: int = 2, stream=None):
+    """Chooses kept.shape[2] blocks for each request and KV head: q [R, heads, head_dim] (bf16 or fp32, heads contiguous), block_tables
+    int32 [R, B], context_lens int32 [R] (clamped to max_ctx); writes kept int32 [R, n_kv_heads, keep] and kept_lens int32 [R].  The
+    first `first` and last `last` blocks of a context are always among them.  scratch: kv_select_blocks_scratch_bytes(R, ...) bytes."""
+    name, torch, shape = "kv_op_select_blocks", _torch(), q.shape
+    if len(shape) != 3 or shape[2] != bounds.head_dim:
+        _refuse(name, "q is [requests, heads, head_dim]")
+    r, hq, d = shape
+    qr, qh, qd = q.stride()
+    if r and (qd != 1 or (hq > 1 and qh != d)):
+        _refuse(name, "a request's heads have to be contiguous")
+    columns, row, _ = _table(name, "block_tables", block_tables, r, None)
+    for what, x in (("context_lens", context_lens), ("kept_lens", kept_lens)):
+        if x.shape != (r,) or x.dtype is not torch.int32 or not x.is_contiguous():
+            _refuse(name, f"{what} is a contiguous int32 vector, one per request")
+    if kept.dim() != 3 or tuple(kept.shape[:2]) != (r, bounds.n_kv_heads) or kept.dtype is not torch.int32 or not kept.is_contiguous():
+        _refuse(name, "kept is contiguous int32 [requests, n_kv_heads, keep]")
+    keep = kept.shape[2]
+    _int32(name, r, hq, max_ctx, first, last, keep)
+    if columns * bounds.block_size < max_ctx:
+        raise KVError(-8, name)
+    dtype = _dtype(name, q.dtype)
+    codes, scales = bounds._layer(name, layer)
+    tensors = [q, bounds.codes, bounds.scales, block_tables, context_lens, kept, kept_lens]
+    scratch_ptr = scratch_bytes = 0
+    if scratch is not None:
+        if not scratch.is_contiguous():
+            _refuse(name, "scratch has to be contiguous")
+        tensors.append(scratch)
+        scratch_ptr, scratch_bytes = scratch.data_ptr(), scratch.numel() * scratch.element_size()
+    index, stream = _on_device(name, stream, tensors)
+    _launch(name, index, (q.data_ptr(), qr if r > 1 else 0, dtype, r, hq, bounds.n_kv_heads, d, codes, scales, bounds.num_blocks,
+                          bounds.block_size, block_tables.data_ptr(), row, context_lens.data_ptr(), max_ctx, first, last, keep,
+                          scratch_ptr, scratch_bytes, kept.data_ptr(), kept_lens.data_ptr(), stream))
+
+
+def kv_op_paged_attention_selected(q, cache: PagedCache, layer: int, kept, kept_lens, out, scratch, lse=None, softmax_scale=None,
+                                   stream=None):
+    """kv_op_paged_attention_batched over the blocks that kv_op_select_blocks chose: kept int32 [R, n_kv_heads, keep], kept_lens
+    int32 [R]; scratch of kv_paged_attention_batched_scratch_bytes(R, heads, cache, keep * block_size) bytes."""
+    name, torch, shape = "kv_op_paged_attention_selected", _torch(), q.shape
+    if len(shape) != 3 or shape[2] != cache.head_dim or out.shape != shape or out.dtype is not q.dtype:
+        _refuse(name, "q and out are [requests, heads, head_dim] of one type")
+    r, hq, d = shape
+    (qr, qh, qd), (outr, outh, outd) = q.stride(), out.stride()
+    if r and (qd != 1 or outd != 1 or (hq > 1 and (qh != d or outh != d))):
+        _refuse(name, "a request's heads have to be contiguous")
+    columns, of_req, of_head = _table(name, "kept", kept, r, cache.n_kv_heads)
+    if kept_lens.shape != (r,) or kept_lens.dtype is not torch.int32 or not kept_lens.is_contiguous():
+        _refuse(name, "kept_lens is a contiguous int32 vector, one per request")
+    tensors = [cache.data, q, kept, kept_lens, out]
+    lse_ptr = scratch_ptr = scratch_bytes = 0
+    if lse is not None:
+        if lse.shape != (r, hq) or lse.dtype is not torch.float32 or not lse.is_contiguous():
+            _refuse(name, "lse is contiguous float32 [requests, heads]")
+        tensors.append(lse)
+        lse_ptr = lse.data_ptr()
+    if scratch is not None:
+        if not scratch.is_contiguous():
+            _refuse(name, "scratch has to be contiguous")
+        tensors.append(scratch)
+        scratch_ptr, scratch_bytes = scratch.data_ptr(), scratch.numel() * scratch.element_size()
+    dtype = _dtype(name, q.dtype)
+    longest = columns * cache.block_size
+    _int32(name, r, hq, longest, layer)
+    index, stream = _on_device(name, stream, tensors)
+    _launch(name, index, (q.data_ptr(), qr if r > 1 else 0, dtype, r, hq, cache._desc_ref, layer, kept.data_ptr(), of_req, of_head,
+                          kept_lens.data_ptr(), longest, d ** -0.5 if softmax_scale is None else softmax_scale, scratch_ptr, scratch_bytes,
+                          out.data_ptr(), outr if r > 1 else 0, lse_ptr, stream))

@@ -287,7 +287,7 @@ DecodeWs carve_decode(const kv_model_desc &d, void *base, int max_ctx, int /*blo
 }
 
 int check_cache(const kv_cache_desc *c) { return check_cache_desc(c); }
-// pack and unpack move whole pages as bytes: both page formats
+// pack and unpack move whole pages as bytes: every page format
 int check_cache_any(const kv_cache_desc *c) { return check_cache_desc(c, true); }
 
 int check_cache_vs_model(const kv_cache_desc *c, const kv_model_desc &d) {
@@ -422,7 +422,8 @@ const char *kv_last_cuda_error(void) { return g_cuda_error.c_str(); }
 
 int64_t kv_cache_page_bytes(int32_t block_size, int32_t n_kv_heads, int32_t head_dim, int32_t elem_bytes) {
   if (block_size <= 0 || n_kv_heads <= 0 || head_dim <= 0) return KV_ERR_ARG;
-  if (elem_bytes != 1 && elem_bytes != 2) return KV_ERR_SHAPE;
+  if (elem_bytes != 1 && elem_bytes != 2 && elem_bytes != KV_ELEM_E2M1) return KV_ERR_SHAPE;
+  if (elem_bytes == KV_ELEM_E2M1 && head_dim % 16 != 0) return KV_ERR_SHAPE;
   CacheView v = {};
   v.block_size = block_size;
   v.n_kv_heads = n_kv_heads;
@@ -432,7 +433,8 @@ int64_t kv_cache_page_bytes(int32_t block_size, int32_t n_kv_heads, int32_t head
 }
 
 int64_t kv_bytes_per_token(int32_t n_layers, int32_t n_kv_heads, int32_t head_dim, int32_t elem_bytes) {
-  return 2ll * n_layers * n_kv_heads * head_dim * elem_bytes;
+  const long long values = 2ll * n_layers * n_kv_heads * head_dim;
+  return elem_bytes == KV_ELEM_E2M1 ? values / 2 : values * elem_bytes;
 }
 
 int32_t kv_check_device_status(const void *workspace_dev, void *stream) {

@@ -1,4 +1,4 @@
-// K and V rows into the pages of a cache, and back, through a list of slots: bf16 pages and e4m3 pages.
+// K and V rows into the pages of a cache, and back, through a list of slots: bf16, e4m3 and e2m1 pages.
 //
 // e4m3 pages: one scale 2^e per (token, KV head) of K and of V, e the least integer with max |x| <= 448 * 2^e.  A power
 // of two instead of max / 448: x * 2^-e and code * 2^e are exact, so a stored value is x rounded once to four significant
@@ -15,24 +15,19 @@
 // 82 / 75 % of a copy's rate with the launch in it); bf16 to bf16 pages and back, 134 MB, 24.3 / 26.6 and 23.0 / 24.9 us (5.5 and 5.8
 // TB/s), fp32, 201 MB, 33.9 / 36.1 and 38.3 / 40.7 us.  64 tokens 1.9 to 2.5 us.  A piece of 8 to a lane and index arithmetic for
 // every row: 161 instructions a warp and row, 27 us.
-#include <float.h>
-
-#include "common.cuh"
+#include "cache_format.cuh"
 
 namespace kvr {
 namespace {
 
 constexpr int kRowThreads = 256;
 constexpr int kMaxTokens = 1 << 30;   // tokens are counted in 32 bits, a CTA's ahead
-constexpr int kMinExp = -110, kMaxExp = 119;
-// largest page pool for which slots fit 32 bits: the division by the block size is then a 32-bit one
-constexpr long long kSlots32 = 0x7fffffffll;
 
 struct RowsParams {
   CacheView cache;
-  int layer, block_shift;                         // block_shift: log2(block_size), -1 if it is no power of two
+  SlotMap map;
+  int layer;
   int n_tokens, heads;                            // heads of K, and of V, that a CTA takes
-  long long n_slots;
   const long long *slots;
   char *k, *v;                                    // rows
   long long k_ts, k_hs, v_ts, v_hs;               // strides, bytes
@@ -42,15 +37,17 @@ struct RowsParams {
 template <int D>
 struct Place {
   static constexpr int LPR = D / 16;              // lanes of a row
-  int sub, first, step;
+  int sub, first, step, kv, head;
   bool idle;
   unsigned group;                                 // the row's lanes
-  char *row, *values, *scale;                     // of token 0; of slot 0 of block 0
-  long long row_step, slot_bytes;
-  __device__ __forceinline__ Place(const RowsParams &p, int elem, int u, int bytes) {      // bytes: of a piece of the row
+  char *row;                                      // of token 0
+  long long row_step;
+  __device__ __forceinline__ Place(const RowsParams &p, int u, int bytes) {      // bytes: of a piece of the row
     const int per = 2 * p.heads * LPR, tokens = kRowThreads / per;      // threads of a token, tokens of a CTA at a time
     const int at = (int)threadIdx.x / per, in = (int)threadIdx.x - at * per;
-    const int line = in / LPR, kv = line >= p.heads, head = blockIdx.y * p.heads + line - kv * p.heads;
+    const int line = in / LPR;
+    kv = line >= p.heads;
+    head = blockIdx.y * p.heads + line - kv * p.heads;
     sub = in % LPR;
     idle = at >= tokens || head >= p.cache.n_kv_heads;
     step = tokens;
@@ -58,125 +55,14 @@ struct Place {
     group = (LPR == 32 ? 0xffffffffu : ((1u << LPR) - 1u)) << (threadIdx.x & 31 & ~(LPR - 1));
     row = (kv ? p.v + head * p.v_hs : p.k + head * p.k_hs) + sub * bytes;
     row_step = kv ? p.v_ts : p.k_ts;
-    slot_bytes = (long long)p.cache.n_kv_heads * D * elem;
-    char *page = p.cache.page(p.layer, kv, 0);
-    values = page + head * D * elem + sub * 8 * elem;
-    scale = page + p.cache.value_bytes() + head * p.cache.block_size;
-  }
-};
-// Block and offset of a slot; false if it lies outside the pool.
-__device__ __forceinline__ bool split_slot(const RowsParams &p, long long slot, int &block, int &offset) {
-  block = offset = 0;
-  if ((unsigned long long)slot >= (unsigned long long)p.n_slots) return false;
-  if (p.block_shift >= 0)
-    block = (int)(slot >> p.block_shift);
-  else if (p.n_slots <= kSlots32)
-    block = (int)((uint32_t)slot / (uint32_t)p.cache.block_size);
-  else
-    block = (int)(slot / p.cache.block_size);
-  offset = (int)(slot - (long long)block * p.cache.block_size);
-  return true;
-}
-
-// Two pieces of 8 values of a row: the raw registers are loaded first and unpacked later.
-template <typename T>
-struct Raw;
-template <>
-struct Raw<bf16> {
-  uint4 a[2];
-  __device__ __forceinline__ void load(const char *p, int apart) {
-    a[0] = *reinterpret_cast<const uint4 *>(p);
-    a[1] = *reinterpret_cast<const uint4 *>(p + apart);
-  }
-  __device__ __forceinline__ void unpack(int h, float (&f)[8]) const {
-    const uint32_t w[4] = {a[h].x, a[h].y, a[h].z, a[h].w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[2 * i] = __uint_as_float(w[i] << 16);
-      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  }
-  static __device__ __forceinline__ uint32_t max2(uint32_t x, uint32_t y) {
-    uint32_t r;
-    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
-    return r;
-  }
-  // The largest |x| over the row's lanes, as an fp32 pattern: above 0x7f7fffff if one is no finite number.
-  template <int LANES>
-  __device__ __forceinline__ uint32_t top(unsigned group) const {
-    const uint32_t s = 0x7fff7fffu;
-    uint32_t m = max2(max2(max2(a[0].x & s, a[0].y & s), max2(a[0].z & s, a[0].w & s)),
-                      max2(max2(a[1].x & s, a[1].y & s), max2(a[1].z & s, a[1].w & s)));
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) m = max2(m, __shfl_xor_sync(group, m, o));
-    return max(m & 0xffff0000u, m << 16);
-  }
-};
-template <>
-struct Raw<float> {
-  float4 a[2][2];
-  __device__ __forceinline__ void load(const char *p, int apart) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      a[h][0] = reinterpret_cast<const float4 *>(p + h * apart)[0];
-      a[h][1] = reinterpret_cast<const float4 *>(p + h * apart)[1];
-    }
-  }
-  __device__ __forceinline__ void unpack(int h, float (&f)[8]) const {
-    f[0] = a[h][0].x; f[1] = a[h][0].y; f[2] = a[h][0].z; f[3] = a[h][0].w;
-    f[4] = a[h][1].x; f[5] = a[h][1].y; f[6] = a[h][1].z; f[7] = a[h][1].w;
-  }
-  static __device__ __forceinline__ float larger(float x, float y) {      // of the magnitudes, NaN if one is NaN
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(x)), "f"(fabsf(y)));
-    return r;
-  }
-  template <int LANES>
-  __device__ __forceinline__ uint32_t top(unsigned group) const {
-    float m = 0.f;
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) m = larger(m, larger(larger(a[h][i].x, a[h][i].y), larger(a[h][i].z, a[h][i].w)));
-#pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) m = larger(m, __shfl_xor_sync(group, m, o));
-    return __float_as_uint(m) & 0x7fffffffu;
   }
 };
 
-__device__ __forceinline__ uint4 pack_bf16(const float (&f)[8]) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-    w[i] = *reinterpret_cast<const uint32_t *>(&h);
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ void store8(char *p, const float (&f)[8], bf16) { *reinterpret_cast<uint4 *>(p) = pack_bf16(f); }
-__device__ __forceinline__ void store8(char *p, const float (&f)[8], float) {
-  reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-  reinterpret_cast<float4 *>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
-}
-
-__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ float2 from_e4m3x2(uint16_t c) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(c));
-  float2 f;
-  asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, u;\n\t}"
-      : "=f"(f.x), "=f"(f.y) : "r"(h));
-  return f;
-}
-
-template <typename T, int D, bool E4M3, int U>      // U: tokens of a thread at a time
+template <typename T, int D, int FMT, int U>      // U: tokens of a thread at a time
 __global__ void __launch_bounds__(kRowThreads) cache_write_kernel(const __grid_constant__ RowsParams p) {
-  const Place<D> me(p, E4M3 ? 1 : 2, U, 8 * (int)sizeof(T));
+  const Place<D> me(p, U, 8 * (int)sizeof(T));
   if (me.idle) return;                                        // whole rows at a time: the shuffles are the row's own
+  const Pieces<D, FMT> to(p.cache, p.layer, me.kv, me.head, me.sub);
   for (int t0 = me.first; t0 < p.n_tokens; t0 += gridDim.x * me.step * U) {
     Raw<T> raw[U];
     long long slot[U];
@@ -190,56 +76,19 @@ __global__ void __launch_bounds__(kRowThreads) cache_write_kernel(const __grid_c
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       int block, offset;
-      const bool live = split_slot(p, slot[i], block, offset);
-      char *values = me.values + block * p.cache.block_stride + offset * me.slot_bytes;
-      float f[2][8];
-      raw[i].unpack(0, f[0]);
-      raw[i].unpack(1, f[1]);
-      if (!E4M3) {
-        if (live) {
-          *reinterpret_cast<uint4 *>(values) = pack_bf16(f[0]);
-          *reinterpret_cast<uint4 *>(values + D) = pack_bf16(f[1]);
-        }
-        continue;
-      }
-      uint32_t bits = raw[i].template top<Place<D>::LPR>(me.group);
-      if (bits > 0x7f7fffffu) {                                 // infinities and NaN do not set the scale and become NaN
-        float most = 0.f;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            if (!(fabsf(f[h][j]) <= FLT_MAX)) f[h][j] = __uint_as_float(0x7fc00000u);
-            most = fmaxf(most, fabsf(f[h][j]));                 // ignores NaN
-          }
-#pragma unroll
-        for (int o = Place<D>::LPR / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(me.group, most, o));
-        bits = __float_as_uint(most);
-      }
-      // |x| <= m * 2^x with 1 <= m < 2; 448 = 1.75 * 2^8, so e = x - 8, one more if m > 1.75
-      int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u);
-      e = min(max(e, kMinExp), kMaxExp);
-      const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-      uint2 c[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        c[h].x = e4m3x2(f[h][0] * inv, f[h][1] * inv) | (e4m3x2(f[h][2] * inv, f[h][3] * inv) << 16);
-        c[h].y = e4m3x2(f[h][4] * inv, f[h][5] * inv) | (e4m3x2(f[h][6] * inv, f[h][7] * inv) << 16);
-      }
-      if (live) {
-        *reinterpret_cast<uint2 *>(values) = c[0];
-        *reinterpret_cast<uint2 *>(values + D / 2) = c[1];
-        if (me.sub == 0) me.scale[block * p.cache.block_stride + offset] = (char)(e + 127);
-      }
+      const bool live = p.map.split(slot[i], block, offset);
+      put_row<T, D, FMT>(raw[i], to, block * p.cache.block_stride, offset, me.sub, me.group, live);
     }
   }
 }
 
-template <typename T, int D, bool E4M3, int U>
+template <typename T, int D, int FMT, int U>
 __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_constant__ RowsParams p) {
-  const Place<D> me(p, E4M3 ? 1 : 2, U, 8 * (int)sizeof(T));
+  const Place<D> me(p, U, 8 * (int)sizeof(T));
   if (me.idle) return;
-  uint4 raw[U][E4M3 ? 1 : 2];                                 // e4m3: both pieces in one
+  const Pieces<D, FMT> from(p.cache, p.layer, me.kv, me.head, me.sub);
+  constexpr int APART = Pieces<D, FMT>::apart;
+  uint4 raw[U][FMT == kBf16 ? 2 : 1];                         // e4m3, e2m1: both pieces in one
   uint32_t scale[U];
   long long slot[U];
   bool live[U];
@@ -251,15 +100,20 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
 #pragma unroll
   for (int i = 0; i < U; ++i) {
     int block, offset;
-    live[i] = split_slot(p, slot[i], block, offset);          // block 0, offset 0 if not: read, but not written anywhere
-    const char *values = me.values + block * p.cache.block_stride + offset * me.slot_bytes;
-    if (E4M3) {
-      const uint2 a = *reinterpret_cast<const uint2 *>(values), b = *reinterpret_cast<const uint2 *>(values + D / 2);
+    live[i] = p.map.split(slot[i], block, offset);            // block 0, offset 0 if not: read, but not written anywhere
+    const long long at = block * p.cache.block_stride;
+    const char *values = from.values + at + offset * from.slot_bytes;
+    if (FMT == kE4m3) {
+      const uint2 a = *reinterpret_cast<const uint2 *>(values), b = *reinterpret_cast<const uint2 *>(values + APART);
       raw[i][0] = make_uint4(a.x, a.y, b.x, b.y);
-      scale[i] = *reinterpret_cast<const uint8_t *>(me.scale + block * p.cache.block_stride + offset);
+      scale[i] = *reinterpret_cast<const uint8_t *>(from.scale + at + offset);
+    } else if (FMT == kE2m1) {
+      const uint8_t *g = reinterpret_cast<const uint8_t *>(from.groups + at + offset * (D / 16));
+      raw[i][0] = make_uint4(*reinterpret_cast<const uint32_t *>(values), *reinterpret_cast<const uint32_t *>(values + APART), g[0], g[D / 32]);
+      scale[i] = *reinterpret_cast<const uint8_t *>(from.scale + at + offset);
     } else {
       raw[i][0] = *reinterpret_cast<const uint4 *>(values);
-      raw[i][E4M3 ? 0 : 1] = *reinterpret_cast<const uint4 *>(values + D);
+      raw[i][FMT == kBf16] = *reinterpret_cast<const uint4 *>(values + APART);
     }
   }
 #pragma unroll
@@ -267,19 +121,34 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
     if (!live[i]) continue;
     char *row = me.row + (me.first + i * me.step) * me.row_step;
     float f[2][8];
-    if (E4M3) {
+    if (FMT == kE4m3) {
       const float s = __uint_as_float(scale[i] << 23);
       const uint32_t w[4] = {raw[i][0].x, raw[i][0].y, raw[i][0].z, raw[i][0].w};
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float2 c = from_e4m3x2((uint16_t)(w[j >> 1] >> ((j & 1) * 16)));
+        const float2 c = floats_of_half2(half2_of_e4m3x2(w[j >> 1] >> ((j & 1) * 16)));
         f[j >> 2][(2 * j) & 7] = c.x * s;
         f[j >> 2][(2 * j + 1) & 7] = c.y * s;
+      }
+    } else if (FMT == kE2m1) {
+      const float s = __uint_as_float(scale[i] << 23);
+      const uint32_t w[2] = {raw[i][0].x, raw[i][0].y}, g[2] = {raw[i][0].z, raw[i][0].w};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t both = half2_of_e4m3x2(g[h] * 0x101u);
+        uint32_t v[4];
+        halves_of_e2m1(w[h], v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 c = floats_of_half2(mul_half2(v[j], both));
+          f[h][2 * j] = c.x * s;
+          f[h][2 * j + 1] = c.y * s;
+        }
       }
     } else {
       Raw<bf16> b;
       b.a[0] = raw[i][0];
-      b.a[1] = raw[i][E4M3 ? 0 : 1];
+      b.a[1] = raw[i][FMT == kBf16];
       b.unpack(0, f[0]);
       b.unpack(1, f[1]);
     }
@@ -288,7 +157,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
   }
 }
 
-template <typename T, int D, bool E4M3, int U>
+template <typename T, int D, int FMT, int U>
 int launch_rows_u(const RowsParams &p, bool write, int sms, cudaStream_t st) {
   const int tokens = kRowThreads / (2 * p.heads * Place<D>::LPR) * U;
   dim3 grid((p.n_tokens + tokens - 1) / tokens, (p.cache.n_kv_heads + p.heads - 1) / p.heads);
@@ -298,9 +167,9 @@ int launch_rows_u(const RowsParams &p, bool write, int sms, cudaStream_t st) {
   const unsigned stay = (unsigned)(4 * sms / (int)grid.y > 1 ? 4 * sms / (int)grid.y : 1);
   if (write && grid.x > stay) grid.x = stay;
   if (write)
-    cache_write_kernel<T, D, E4M3, U><<<grid, kRowThreads, 0, st>>>(p);
+    cache_write_kernel<T, D, FMT, U><<<grid, kRowThreads, 0, st>>>(p);
   else
-    cache_read_kernel<T, D, E4M3, U><<<grid, kRowThreads, 0, st>>>(p);
+    cache_read_kernel<T, D, FMT, U><<<grid, kRowThreads, 0, st>>>(p);
   KV_COUNT_LAUNCH();
   KV_CUDA(cudaGetLastError());
   return KV_OK;
@@ -309,7 +178,7 @@ int launch_rows_u(const RowsParams &p, bool write, int sms, cudaStream_t st) {
 // Two tokens to a thread once that still gives every SM eight CTAs (16,384 tokens: write 20.7 us against 23.1 us with one,
 // read 18.8 us against 23.3 us; four are no better), one below that (few rows: the chain slot -> row ->
 // store is all there is, and more CTAs share it).
-template <typename T, int D, bool E4M3>
+template <typename T, int D, int FMT>
 int launch_rows(RowsParams &p, bool write, cudaStream_t st) {
   const int device = current_device();
   if (device < 0) return KV_ERR_CUDA;
@@ -317,8 +186,14 @@ int launch_rows(RowsParams &p, bool write, cudaStream_t st) {
   p.heads = p.cache.n_kv_heads < most ? p.cache.n_kv_heads : most;
   const long long threads = (long long)p.n_tokens * 2 * p.cache.n_kv_heads * Place<D>::LPR;
   const int sms = sm_count(device);
-  return threads >= 16ll * kRowThreads * sms ? launch_rows_u<T, D, E4M3, 2>(p, write, sms, st)
-                                             : launch_rows_u<T, D, E4M3, 1>(p, write, sms, st);
+  return threads >= 16ll * kRowThreads * sms ? launch_rows_u<T, D, FMT, 2>(p, write, sms, st)
+                                             : launch_rows_u<T, D, FMT, 1>(p, write, sms, st);
+}
+
+template <int FMT>
+int rows_format(RowsParams &p, int d, bool f32, bool write, cudaStream_t st) {
+  if (d == 128) return f32 ? launch_rows<float, 128, FMT>(p, write, st) : launch_rows<bf16, 128, FMT>(p, write, st);
+  return f32 ? launch_rows<float, 64, FMT>(p, write, st) : launch_rows<bf16, 64, FMT>(p, write, st);
 }
 
 // strides are in elements of dtype
@@ -343,11 +218,8 @@ int rows_call(const kv_cache_desc *cache, int layer, const void *k, int64_t k_ts
   }
   RowsParams p;
   p.cache = make_view(cache);
+  p.map = slot_map(cache);
   p.layer = layer;
-  p.n_slots = (long long)cache->num_blocks * cache->block_size;
-  p.block_shift = -1;
-  for (int b = 0; b < 31; ++b)
-    if ((1 << b) == cache->block_size) p.block_shift = b;
   p.n_tokens = n_tokens;
   p.slots = reinterpret_cast<const long long *>(slots);
   p.k = (char *)const_cast<void *>(k);
@@ -356,14 +228,13 @@ int rows_call(const kv_cache_desc *cache, int layer, const void *k, int64_t k_ts
   p.k_hs = k_hs * size;
   p.v_ts = v_ts * size;
   p.v_hs = v_hs * size;
+  const bool f32 = dtype == KV_DTYPE_F32;
   cudaStream_t st = (cudaStream_t)stream;
-  const bool e4m3 = cache->elem_bytes == 1, f32 = dtype == KV_DTYPE_F32;
-  if (d == 128) {
-    if (e4m3) return f32 ? launch_rows<float, 128, true>(p, write, st) : launch_rows<bf16, 128, true>(p, write, st);
-    return f32 ? launch_rows<float, 128, false>(p, write, st) : launch_rows<bf16, 128, false>(p, write, st);
+  switch (format_of(cache->elem_bytes)) {
+    case kBf16: return rows_format<kBf16>(p, d, f32, write, st);
+    case kE4m3: return rows_format<kE4m3>(p, d, f32, write, st);
+    default: return rows_format<kE2m1>(p, d, f32, write, st);
   }
-  if (e4m3) return f32 ? launch_rows<float, 64, true>(p, write, st) : launch_rows<bf16, 64, true>(p, write, st);
-  return f32 ? launch_rows<float, 64, false>(p, write, st) : launch_rows<bf16, 64, false>(p, write, st);
 }
 
 }  // namespace

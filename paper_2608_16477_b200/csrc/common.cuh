@@ -17,9 +17,15 @@ struct CacheView {
   char *base;
   long long layer_stride, kv_stride, block_stride;
   int block_size, n_kv_heads, head_dim, elem_bytes;
+  // of bf16 and e4m3 pages, whose values come first
   __host__ __device__ long long value_bytes() const { return (long long)block_size * n_kv_heads * head_dim * elem_bytes; }
+  // of a KV head in an e2m1 page: codes [slot][dim / 2], scales of 16 dims [slot][dim / 16], scale bytes [slot]
+  __host__ __device__ long long record_bytes() const {
+    return ((long long)block_size * (head_dim / 2 + head_dim / 16 + 1) + 15) / 16 * 16;
+  }
   // e4m3 pages (elem_bytes 1) carry one scale byte per (KV head, slot) behind the values, padded to 16 bytes
   __host__ __device__ long long page_bytes() const {
+    if (elem_bytes == KV_ELEM_E2M1) return n_kv_heads * record_bytes();
     return value_bytes() + (elem_bytes == 1 ? ((long long)block_size * n_kv_heads + 15) / 16 * 16 : 0);
   }
   __device__ __forceinline__ char *page(int layer, int kv, int block) const {
@@ -41,13 +47,14 @@ inline CacheView make_view(const kv_cache_desc *c) {
 }
 
 // Host-side validation of a cache descriptor, shared by every entry point that takes one.  Only the entry points that
-// know e4m3 pages pass allow_e4m3.
-inline int check_cache_desc(const kv_cache_desc *c, bool allow_e4m3 = false) {
+// know e4m3 and e2m1 pages pass allow_packed.
+inline int check_cache_desc(const kv_cache_desc *c, bool allow_packed = false) {
   if (c == nullptr || c->base_dev == nullptr) return KV_ERR_ARG;
   if (c->num_blocks <= 0 || c->block_size <= 0 || c->n_layers <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0)
     return KV_ERR_ARG;
-  if (c->elem_bytes != 2 && !(allow_e4m3 && c->elem_bytes == 1)) return KV_ERR_SHAPE;
-  if (c->elem_bytes == 1 && c->head_dim % 16 != 0) return KV_ERR_SHAPE;
+  const bool packed = c->elem_bytes == 1 || c->elem_bytes == KV_ELEM_E2M1;
+  if (c->elem_bytes != 2 && !(allow_packed && packed)) return KV_ERR_SHAPE;
+  if (packed && c->head_dim % 16 != 0) return KV_ERR_SHAPE;
   const long long page = make_view(c).page_bytes();
   if (page % 16 != 0) return KV_ERR_SHAPE;
   if (((uintptr_t)c->base_dev & 15) || (c->layer_stride & 15) || (c->kv_stride & 15) || (c->block_stride & 15))

@@ -6,8 +6,8 @@
 // compiled: up to 896 ids / 8 requests (under 4 KiB, the single-request calls of the migration path) and up
 // to 7,680 ids / 64 requests (under the 32 KiB limit of the launch interface, the batched calls); longer
 // lists are split over several launches.
-// A page (block_size * n_kv_heads * head_dim bf16, or as many e4m3 codes and their scale bytes) is contiguous on both sides;
-// it moves as bulk copies (cp.async.bulk) of 16 KiB, a little more for e4m3 pages, through a shared-memory ring.  HBM-bound: 2 * page bytes of traffic
+// A page (block_size * n_kv_heads * head_dim bf16, or as many e4m3 or e2m1 codes and their scales) is contiguous on both sides;
+// it moves as bulk copies (cp.async.bulk) of 16 KiB, a little more for e4m3 pages and less for e2m1 pages, through a shared-memory ring.  HBM-bound: 2 * page bytes of traffic
 // per page, nothing is re-read.
 #include <vector>
 
@@ -16,9 +16,9 @@
 namespace kvr {
 
 constexpr int kPieceBytes = 16384;    // bytes per bulk copy
-// An e4m3 page is a power of two of codes and a few scale bytes: cut at 16 KiB it would leave a scrap that takes a slot of
-// the ring of its own, so its pieces are equal parts of at most this.
-constexpr int kPieceBytesE4m3 = 18432;
+// An e4m3 or e2m1 page is a power of two of codes and a few scale bytes: cut at 16 KiB it would leave a scrap that takes a slot
+// of the ring of its own, so its pieces are equal parts of at most this.
+constexpr int kPieceBytesPacked = 18432;
 constexpr int kBufs = 8;              // shared-memory ring: 128 KiB per CTA, one CTA per SM (measured best: ~128 KiB in flight per SM)
 constexpr int kLag = 4;               // stores left in flight before a slot is refilled (kBufs - kLag loads in flight)
 constexpr int kCopyThreads = 32;
@@ -173,8 +173,8 @@ int copy_requests(const CacheView &cache, int n_layers, const CopyRequest *reqs,
     p.layout = wire_layout;
     p.page_bytes = (int)cache.page_bytes();
     p.piece_bytes = kPieceBytes;
-    if (cache.elem_bytes == 1) {
-      const int pieces = (p.page_bytes + kPieceBytesE4m3 - 1) / kPieceBytesE4m3;
+    if (cache.elem_bytes != 2) {
+      const int pieces = (p.page_bytes + kPieceBytesPacked - 1) / kPieceBytesPacked;
       p.piece_bytes = ((p.page_bytes + pieces - 1) / pieces + 127) / 128 * 128;
     }
     p.pieces_per_page = (p.page_bytes + p.piece_bytes - 1) / p.piece_bytes;
@@ -215,13 +215,13 @@ int copy_pages(CacheView cache, int n_layers, const CopyRequest *reqs, int n_req
   if (device < 0) return KV_ERR_CUDA;
   if (!attr_set[device]) {
     KV_CUDA(cudaFuncSetAttribute(copy_pages_kernel<true, SmallCopyParams>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kBufs * kPieceBytesE4m3));
+                                 kBufs * kPieceBytesPacked));
     KV_CUDA(cudaFuncSetAttribute(copy_pages_kernel<false, SmallCopyParams>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kBufs * kPieceBytesE4m3));
+                                 kBufs * kPieceBytesPacked));
     KV_CUDA(cudaFuncSetAttribute(copy_pages_kernel<true, LargeCopyParams>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kBufs * kPieceBytesE4m3));
+                                 kBufs * kPieceBytesPacked));
     KV_CUDA(cudaFuncSetAttribute(copy_pages_kernel<false, LargeCopyParams>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kBufs * kPieceBytesE4m3));
+                                 kBufs * kPieceBytesPacked));
     attr_set[device] = true;
   }
   const int sms = sm_count(device);

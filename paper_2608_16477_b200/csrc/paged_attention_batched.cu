@@ -39,9 +39,7 @@
 // e4m3 pages: codes go to fp16 fragments (exact) and the power-of-two scales stay outside: K's multiplies the score,
 // V's goes into the weight, w = 2^(t + e_v - M), with its own running maximum M of t + e_v, so that fp16 keeps the bits
 // of every weight that matters next to the largest CONTRIBUTION, however the rows' scales differ.
-#include <float.h>
-
-#include "common.cuh"
+#include "cache_format.cuh"
 
 namespace kvr {
 namespace {
@@ -53,18 +51,20 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kLookAhead = 3;        // stages between looking a page up and copying its rows
 constexpr int kNoRow = (int)0x80000000;
 template <int ELEM>
-constexpr float kLazy = ELEM == 1 ? 4.f : 8.f;      // a running maximum may be passed by 2^4 (2^8) before it is replaced
+constexpr float kLazy = ELEM == 2 ? 8.f : 4.f;      // a running maximum may be passed by 2^4 (2^8) before it is replaced
 constexpr float kWeightBits = 11.f;  // fp16 weights: 2^11 at the running maximum, so at most 2^15
 constexpr int kQueryBits = 12;       // ... and fp16 queries to less than 2^12
 
 // A stage is what a warp loads and consumes at a time: 32 keys, so that the softmax's and the loads' bookkeeping is paid
 // once for four 8-key fragments; 16 where 32 would leave the ring too few stages (bf16 rows of 128: 8 KB a stage either way).
+// ELEM, the page format: 2 bf16, 1 e4m3, 0 e2m1.
 template <int D, int ELEM>
 struct BaCfg {
-  static constexpr int row = D * ELEM;                                   // bytes of a K or V row
+  static constexpr int row = ELEM == 0 ? D / 2 : D * ELEM;               // bytes of a K or V row's values
   static constexpr int keys = row > 128 ? 16 : 32;
-  static constexpr int tile = keys * row;
-  static constexpr int stage = 2 * tile + (ELEM == 1 ? 256 : 0);         // K, V, a word with the scale byte of each row
+  static constexpr int codes = keys * row;
+  static constexpr int tile = codes + (ELEM == 0 ? keys * (D / 16) : 0); // e2m1: then the scales of 16 dims
+  static constexpr int stage = 2 * tile + (ELEM == 2 ? 0 : 256);         // K, V, a word with the scale byte of each row
   static constexpr int stages = stage > 6144 ? 3 : 5;
   static constexpr int ring = stages * stage;
   static constexpr int merge = (kBaWarps - 1) * kBaHeads * D * 4;        // outputs of warps 1-3 when they share a head
@@ -78,7 +78,7 @@ struct BaParams {
   const void *q;
   void *out;
   float *lse;
-  long long q_stride, out_stride, table_stride;
+  long long q_stride, out_stride, table_stride, head_stride;      // head_stride: from a KV head's table to the next, 0 if they share one
   const int *tables, *lens;
   int n_req, n_q_heads, group, passes, max_ctx;
   int parts;              // ranges; 0: one CTA per request (blockIdx.x), nothing is split
@@ -97,13 +97,16 @@ __device__ __forceinline__ float ex2(float x) {
 // of up to 18,433 tokens: 94.6 us against 99.1 us; no gain for bf16 rows).
 template <int ELEM>
 __device__ __forceinline__ void cp16(uint32_t dst, const char *src, bool valid) {
-  if (ELEM == 1)
+  if (ELEM != 2)
     asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
   else
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void cp4(uint32_t dst, const char *src, bool valid) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(valid ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void cp8(uint32_t dst, const char *src, bool valid) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(valid ? 8 : 0) : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -146,11 +149,15 @@ __device__ __forceinline__ uint32_t lds4(uint32_t a) {
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
   return v;
 }
-// two e4m3 codes -> two fp16 (exact)
-__device__ __forceinline__ uint32_t half2_of_e4m3(uint32_t two) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
-  return h;
+__device__ __forceinline__ uint32_t lds2(uint32_t a) {
+  uint16_t v;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds1(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
 }
 // x and y as the sum of N bf16 each (8 significant bits a part) or of N fp16 (11): what a part leaves goes to the next.
 template <int N>
@@ -183,13 +190,13 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   return r;
 }
 // The D / 4 values of a query head that a lane (c = lane % 4) turns into fragments, as they were loaded.  Pair i of
-// ELEM 2 is dims 8 i + 2 c, + 1; of ELEM 1 dims c D / 4 + 2 i, + 1.
+// ELEM 2 is dims 8 i + 2 c, + 1; of the others dims c D / 4 + 2 i, + 1.
 template <int D, int ELEM, typename T>
 struct RawQuery {
   static constexpr int W = sizeof(T) / 2;            // 32-bit words of a pair
   uint32_t w[D / 8 * W];
   __device__ __forceinline__ void load(const T *q, int c) {
-    if (ELEM == 1) {
+    if (ELEM != 2) {
       const uint4 *src = reinterpret_cast<const uint4 *>(q + c * (D / 4));
 #pragma unroll
       for (int i = 0; i < D / 8 * W / 4; ++i) {
@@ -227,7 +234,7 @@ __device__ __forceinline__ void store2(float *p, float a, float b) { *reinterpre
 __device__ __forceinline__ void store2(bf16 *p, float a, float b) {
   *reinterpret_cast<__nv_bfloat162 *>(p) = __floats2bfloat162_rn(a, b);
 }
-// The lane's share of the D values (times f) of head cq + i.  ELEM 2: dims 16 mt + lane / 4 + {0, 8}; ELEM 1: D / 8
+// The lane's share of the D values (times f) of head cq + i.  ELEM 2: dims 16 mt + lane / 4 + {0, 8}; the others: D / 8
 // consecutive ones.
 template <int D, int ELEM, typename P>
 __device__ __forceinline__ void store_head(P *row, const float (&oc)[D / 16][4], int i, int g, float f) {
@@ -258,10 +265,16 @@ __device__ __forceinline__ float quad_max(float v) {
 // loads of eight neighbouring lanes fall into different banks.
 template <int D, int ELEM>
 __device__ __forceinline__ uint32_t chunk_at(int r, int c) {
+  if (ELEM == 0) return (uint32_t)(r * (D / 2) + (D == 128 ? c ^ (r & 2) : c) * 16);
   if (ELEM == 1 && D == 64) return (uint32_t)((r >> 1) * 128 + ((((r & 1) * 4 + c) ^ (r & 6)) * 16));
   if (ELEM == 1) return (uint32_t)(r * 128 + ((c ^ (r & 7)) * 16));
   return (uint32_t)(r * (D * 2) + ((c & ~7) | ((c ^ r) & 7)) * 16);
 }
+
+// The key (of eight) that row x of a fragment holds.  e2m1 rows are 64 or 32 bytes, so that four of them, in natural order, would
+// share banks; any order will do, as long as K's rows and the weights agree.
+template <int ELEM>
+__device__ __forceinline__ int key_of(int x) { return ELEM == 0 ? x ^ (x >> 2) : x; }
 
 __device__ __forceinline__ int clamped_len(const BaParams &p, int r) {
   return min(max(__ldg(p.lens + r), 0), p.max_ctx);
@@ -291,7 +304,7 @@ __device__ __noinline__ bool infinite_key(const BaParams &p, int req, int kvh, i
   for (int s = 0; s < steps; ++s) {
     const int pos = first + s * tile + lane % KEYS;
     if (pos >= n) continue;
-    const int b = pos / p.cache.block_size, blk = __ldg(p.tables + req * p.table_stride + b);
+    const int b = pos / p.cache.block_size, blk = __ldg(p.tables + req * p.table_stride + kvh * p.head_stride + b);
     if ((unsigned)blk >= (unsigned)p.num_blocks) continue;
     const char *row = p.cache.page(p.layer, 0, blk) +
                       ((long long)(pos - b * p.cache.block_size) * p.cache.n_kv_heads + kvh) * row_bytes;
@@ -329,9 +342,9 @@ template <int D, int ELEM, typename T, int KW>      // KW: warps that share a KV
 __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(const __grid_constant__ BaParams p) {
   typedef BaCfg<D, ELEM> C;
   constexpr int KS = D / 16;                 // k-steps of S^T = K Q^T
-  constexpr int NT = D / 8;                  // dims of a lane's V fragments (ELEM 1)
+  constexpr int NT = D / 8;                  // dims of a lane's V fragments (ELEM 1, 0)
   constexpr int MO = D / 16;                 // 16-dim tiles of O^T
-  constexpr int QP = sizeof(T) == 2 ? 1 : (ELEM == 1 ? 2 : 3);          // parts of a query
+  constexpr int QP = sizeof(T) == 2 ? 1 : (ELEM == 2 ? 3 : 2);          // parts of a query
   constexpr int PP = sizeof(T) == 4 && ELEM == 2 ? 3 : 2;                // parts of a weight
   constexpr int CH = C::row / 16;            // 16-byte chunks of a row
   constexpr int RPI = 32 / CH;               // rows per copy instruction
@@ -406,6 +419,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
 
   // ---- loads.  Lane l looks up the page of row l % KEYS of a stage, kLookAhead stages before its copies are issued: a
   // table entry can be a microsecond away.
+  const int *tables = p.tables + kvh * p.head_stride;
   Cursor prod = cons;
   long long to_look = todo;
   int blks[kLookAhead] = {}, offs[kLookAhead] = {};   // of the next stages to be copied: block and slot of the lane's row (kNoRow: none)
@@ -418,7 +432,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
       if (pos < prod.n) {
         const int b = p.block_shift >= 0 ? pos >> p.block_shift : pos / p.cache.block_size;
         off = pos - b * p.cache.block_size;
-        blk = __ldg(p.tables + prod.r * p.table_stride + b);
+        blk = __ldg(tables + prod.r * p.table_stride + b);
       }
       off |= pos < prod.n ? 0 : kNoRow;
       --to_look;
@@ -427,10 +441,12 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
       off = kNoRow;
     }
   };
-  const long long row_stride = (long long)p.cache.n_kv_heads * C::row;
-  // the lane's chunk of row lane / CH, and the scale bytes, in block 0 of K
-  const char *base0 = p.cache.page(p.layer, 0, 0) + (long long)kvh * C::row + (lane / CH) * row_stride + (lane % CH) * 16;
-  const char *scale0 = p.cache.page(p.layer, 0, 0) + p.cache.value_bytes();
+  const long long row_stride = ELEM == 0 ? C::row : (long long)p.cache.n_kv_heads * C::row;
+  // the lane's chunk of row lane / CH, and the scale bytes, in block 0 of K (e2m1: both in the KV head's record)
+  const char *rec0 = p.cache.page(p.layer, 0, 0) + kvh * (ELEM == 0 ? p.cache.record_bytes() : (long long)C::row);
+  const char *base0 = rec0 + (lane / CH) * row_stride + (lane % CH) * 16;
+  const char *scale0 = ELEM == 0 ? rec0 + (long long)p.cache.block_size * (D / 2 + D / 16)
+                                 : p.cache.page(p.layer, 0, 0) + p.cache.value_bytes();
   unsigned poison = 0;                       // bit s: the stage in ring slot s has a row outside the pool
   int put = 0;                               // ring slot to fill next
   auto issue = [&]() {
@@ -471,9 +487,20 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
           cp16<ELEM>(v_s + dst, src + p.cache.kv_stride, ok);
         }
       }
-      if (ELEM == 1) {   // the words that hold the scale bytes of row l of K and of V
+      if (ELEM != 2) {   // the words that hold the scale bytes of row l of K and of V
         const bool ok = blk >= 0;
-        const int at = kvh * p.cache.block_size + (ok ? off : 0);
+        if (ELEM == 0) {      // ... and its scales of 16 dims
+          const char *src = rec0 + (ok ? blk * p.cache.block_stride : 0) + (long long)p.cache.block_size * (D / 2) + (ok ? off : 0) * (D / 16);
+          const uint32_t dst = k_s + C::codes + lane * (D / 16);
+          if (D == 128) {
+            cp8(dst, src, ok);
+            cp8(dst + C::tile, src + p.cache.kv_stride, ok);
+          } else {
+            cp4(dst, src, ok);
+            cp4(dst + C::tile, src + p.cache.kv_stride, ok);
+          }
+        }
+        const int at = (ELEM == 0 ? 0 : kvh * p.cache.block_size) + (ok ? off : 0);
         const char *src = scale0 + (ok ? blk * p.cache.block_stride : 0) + (at & ~3);
         cp4(k_s + 2 * C::tile + lane * 4, src, ok);
         cp4(k_s + 2 * C::tile + 128 + lane * 4, src + p.cache.kv_stride, ok);
@@ -491,6 +518,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
 #pragma unroll
   for (int i = 0; i < kLookAhead; ++i) look_up(blks[i], offs[i]);
   const int g = lane >> 2, c = lane & 3, cq = c * 2;   // the lane's query fragments are of head g, its results of cq, cq + 1
+  const int kg8 = key_of<ELEM>(g);                     // of eight keys, the one that row g of a fragment holds
   RawQuery<D, ELEM, T> raw;
   auto load_query = [&](int req) {
     raw.load(static_cast<const T *>(p.q) + req * p.q_stride + (long long)(head0 + min(g, nh - 1)) * D, c);
@@ -573,7 +601,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
       const uint32_t k_s = ring + get * C::stage, v_s = k_s + C::tile;
       const int key0 = (cons.tile * KW + kg) * KEYS;
       if (key0 < n) {
-        // ---- S^T = K Q^T: the lane ends with keys g + 8 j of heads cq, cq + 1
+        // ---- S^T = K Q^T: the lane ends with keys kg8 + 8 j of heads cq, cq + 1
         float t[2 * MK][2];
 #pragma unroll
         for (int mt = 0; mt < MK; ++mt) {
@@ -587,6 +615,41 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
 #pragma unroll
               for (int h = 0; h < QP; ++h) mma_bf16(sc[ks & 1], a, qf[h][ks][0], qf[h][ks][1]);
             }
+          } else if (ELEM == 0) {
+            // D / 4 consecutive codes of two keys, a word for two k-steps, and the scales of their groups
+            const uint32_t rx = k_s + C::codes + (mt * 16 + kg8) * (D / 16), ry = rx + 8 * (D / 16);
+            uint32_t xs[D / 32], ys[D / 32], sx[D / 64], sy[D / 64];
+            if (D == 128) {
+              const uint4 x = lds16(k_s + chunk_at<D, ELEM>(mt * 16 + kg8, c)), y = lds16(k_s + chunk_at<D, ELEM>(mt * 16 + kg8 + 8, c));
+              xs[0] = x.x; xs[1] = x.y; xs[D / 32 - 2] = x.z; xs[D / 32 - 1] = x.w;
+              ys[0] = y.x; ys[1] = y.y; ys[D / 32 - 2] = y.z; ys[D / 32 - 1] = y.w;
+              const uint32_t ex = half2_of_e4m3x2(lds2(rx + 2 * c)), ey = half2_of_e4m3x2(lds2(ry + 2 * c));
+              sx[0] = __byte_perm(ex, 0, 0x1010); sx[D / 64 - 1] = __byte_perm(ex, 0, 0x3232);
+              sy[0] = __byte_perm(ey, 0, 0x1010); sy[D / 64 - 1] = __byte_perm(ey, 0, 0x3232);
+            } else {
+              const uint2 x = lds8(k_s + (mt * 16 + kg8) * C::row + c * 8), y = lds8(k_s + (mt * 16 + kg8 + 8) * C::row + c * 8);
+              xs[0] = x.x; xs[1] = x.y;
+              ys[0] = y.x; ys[1] = y.y;
+              sx[0] = half2_of_e4m3x2(lds1(rx + c) * 0x101u);
+              sy[0] = half2_of_e4m3x2(lds1(ry + c) * 0x101u);
+            }
+#pragma unroll
+            for (int w = 0; w < D / 32; ++w) {
+              uint32_t vx[4], vy[4];
+              halves_of_e2m1(xs[w], vx);
+              halves_of_e2m1(ys[w], vy);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                vx[i] = mul_half2(vx[i], sx[w / 2]);
+                vy[i] = mul_half2(vy[i], sy[w / 2]);
+              }
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const uint32_t a[4] = {vx[2 * i], vy[2 * i], vx[2 * i + 1], vy[2 * i + 1]};
+#pragma unroll
+                for (int h = 0; h < QP; ++h) mma_f16(sc[i & 1], a, qf[h][2 * w + i][0], qf[h][2 * w + i][1]);
+              }
+            }
           } else {
 #pragma unroll
             for (int j = 0; j < KS / 4; ++j) {
@@ -595,8 +658,8 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
               const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                const uint32_t a[4] = {half2_of_e4m3(xs[i]), half2_of_e4m3(ys[i]), half2_of_e4m3(xs[i] >> 16),
-                                       half2_of_e4m3(ys[i] >> 16)};
+                const uint32_t a[4] = {half2_of_e4m3x2(xs[i]), half2_of_e4m3x2(ys[i]), half2_of_e4m3x2(xs[i] >> 16),
+                                       half2_of_e4m3x2(ys[i] >> 16)};
 #pragma unroll
                 for (int h = 0; h < QP; ++h) mma_f16(sc[i & 1], a, qf[h][4 * j + i][0], qf[h][4 * j + i][1]);
               }
@@ -610,16 +673,16 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
           for (int j = 0; j < 2 * MK; ++j) low = fminf(low, fminf(t[j][0], t[j][1]));
         }
         float ev[2 * MK];
-        if (ELEM == 1) {
+        if (ELEM != 2) {
           // lane l has the scale bytes of row l: K's goes to the exponent field of a float, V's to the low bits
           const int pos = min(key0 + my_row, n - 1);
           const int o = p.block_shift >= 0 ? pos & (p.cache.block_size - 1) : pos % p.cache.block_size;
-          const int shift = 8 * ((kvh * p.cache.block_size + o) & 3);
+          const int shift = 8 * (((ELEM == 0 ? 0 : kvh * p.cache.block_size) + o) & 3);
           const uint32_t ek = (lds4(k_s + 2 * C::tile + lane * 4) >> shift) & 255u;
           const uint32_t both = ek << 23 | ((lds4(k_s + 2 * C::tile + 128 + lane * 4) >> shift) & 255u);
 #pragma unroll
           for (int j = 0; j < 2 * MK; ++j) {
-            const uint32_t b = __shfl_sync(0xffffffffu, both, 8 * j + g);
+            const uint32_t b = __shfl_sync(0xffffffffu, both, 8 * j + kg8);
             t[j][0] *= __uint_as_float(b & 0x7f800000u);
             t[j][1] *= __uint_as_float(b & 0x7f800000u);
             ev[j] = __uint_as_float(0x4b000000u | (b & 255u)) - 8388735.f;      // 2^23 + byte, less 2^23 + 127
@@ -628,7 +691,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
         if (key0 + KEYS > n) {
 #pragma unroll
           for (int j = 0; j < 2 * MK; ++j)
-            if (key0 + 8 * j + g >= n) t[j][0] = t[j][1] = -INFINITY;
+            if (key0 + 8 * j + kg8 >= n) t[j][0] = t[j][1] = -INFINITY;
         }
         // ---- running maxima
         float top[2], wtop[2];
@@ -636,13 +699,13 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           top[i] = t[0][i];
-          wtop[i] = ELEM == 1 ? t[0][i] + ev[0] : 0.f;
+          wtop[i] = ELEM != 2 ? t[0][i] + ev[0] : 0.f;
 #pragma unroll
           for (int j = 1; j < 2 * MK; ++j) {
             top[i] = fmaxf(top[i], t[j][i]);
-            if (ELEM == 1) wtop[i] = fmaxf(wtop[i], t[j][i] + ev[j]);
+            if (ELEM != 2) wtop[i] = fmaxf(wtop[i], t[j][i] + ev[j]);
           }
-          raise |= top[i] > m[i] + kLazy<ELEM> || (ELEM == 1 && wtop[i] > mw[i] + kLazy<ELEM>);
+          raise |= top[i] > m[i] + kLazy<ELEM> || (ELEM != 2 && wtop[i] > mw[i] + kLazy<ELEM>);
         }
         if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
@@ -653,7 +716,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
             float corr = ex2(m[i] - sub);
             m[i] = m_new;
             m_sub[i] = sub;
-            if (ELEM == 1) {
+            if (ELEM != 2) {
               const float w_new = fmaxf(mw[i], column_max(wtop[i]));
               const float wsub = w_new == -INFINITY ? 0.f : w_new;
               corr = ex2(mw[i] - wsub);
@@ -695,6 +758,37 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
 #pragma unroll
               for (int h = 0; h < PP; ++h) mma_bf16(oc[mt], a, pf[h][2 * kk], pf[h][2 * kk + 1]);
             }
+          } else if (ELEM == 0) {
+            // As below, NT consecutive codes of four keys and the scale of their group: even and odd dims of two keys to a byte each
+            uint32_t v[4][NT / 8], sc[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int row = kk * 16 + key_of<ELEM>(cq + (i & 1)) + (i >> 1) * 8;
+              if (D == 128) {
+                const uint2 x = lds8(v_s + chunk_at<D, ELEM>(row, g >> 1) + (g & 1) * 8);
+                v[i][0] = x.x; v[i][NT / 8 - 1] = x.y;
+                sc[i] = lds1(v_s + C::codes + row * (D / 16) + g);
+              } else {
+                v[i][0] = lds4(v_s + row * C::row + g * 4);
+                sc[i] = lds1(v_s + C::codes + row * (D / 16) + (g >> 1));
+              }
+            }
+            const uint32_t s0 = half2_of_e4m3x2(sc[0] | sc[1] << 8), s1 = half2_of_e4m3x2(sc[2] | sc[3] << 8);
+#pragma unroll
+            for (int j = 0; j < NT / 8; ++j) {
+              constexpr uint32_t kLow = 0x0f0f0f0fu;
+              uint32_t even0[4], odd0[4], even1[4], odd1[4];
+              halves_of_e2m1((v[0][j] & kLow) | (v[1][j] << 4 & ~kLow), even0);
+              halves_of_e2m1((v[0][j] >> 4 & kLow) | (v[1][j] & ~kLow), odd0);
+              halves_of_e2m1((v[2][j] & kLow) | (v[3][j] << 4 & ~kLow), even1);
+              halves_of_e2m1((v[2][j] >> 4 & kLow) | (v[3][j] & ~kLow), odd1);
+#pragma unroll
+              for (int b = 0; b < 4; ++b) {
+                const uint32_t x[4] = {mul_half2(even0[b], s0), mul_half2(odd0[b], s0), mul_half2(even1[b], s1), mul_half2(odd1[b], s1)};
+#pragma unroll
+                for (int h = 0; h < PP; ++h) mma_f16(oc[4 * j + b], x, pf[h][2 * kk], pf[h][2 * kk + 1]);
+              }
+            }
           } else {
             // rows g and g + 8 of tile mt are dims g NT + 2 mt and + 1: the lane reads NT consecutive codes of four keys
             uint32_t v[4][NT / 4];
@@ -714,8 +808,8 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
               // bytes (key, key + 1) of dims 4 j, 4 j + 1 and of 4 j + 2, 4 j + 3
               const uint32_t a0 = __byte_perm(v[0][j], v[1][j], 0x5140), a1 = __byte_perm(v[0][j], v[1][j], 0x7362);
               const uint32_t b0 = __byte_perm(v[2][j], v[3][j], 0x5140), b1 = __byte_perm(v[2][j], v[3][j], 0x7362);
-              const uint32_t x[4] = {half2_of_e4m3(a0), half2_of_e4m3(a0 >> 16), half2_of_e4m3(b0), half2_of_e4m3(b0 >> 16)};
-              const uint32_t y[4] = {half2_of_e4m3(a1), half2_of_e4m3(a1 >> 16), half2_of_e4m3(b1), half2_of_e4m3(b1 >> 16)};
+              const uint32_t x[4] = {half2_of_e4m3x2(a0), half2_of_e4m3x2(a0 >> 16), half2_of_e4m3x2(b0), half2_of_e4m3x2(b0 >> 16)};
+              const uint32_t y[4] = {half2_of_e4m3x2(a1), half2_of_e4m3x2(a1 >> 16), half2_of_e4m3x2(b1), half2_of_e4m3x2(b1 >> 16)};
 #pragma unroll
               for (int h = 0; h < PP; ++h) {
                 mma_f16(oc[2 * j], x, pf[h][2 * kk], pf[h][2 * kk + 1]);
@@ -744,7 +838,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 4);
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 8);
       l[i] += __shfl_xor_sync(0xffffffffu, l[i], 16);
-      f[i] = ELEM == 1 && mw[i] != -INFINITY ? ex2(mw[i] - m[i] - kWeightBits) : 1.f;
+      f[i] = ELEM != 2 && mw[i] != -INFINITY ? ex2(mw[i] - m[i] - kWeightBits) : 1.f;
     }
     const bool whole = s_tile == 0 && steps == tiles_of(n, TILE);
     const long long rec_slot = s_tile == 0 ? 1 : 0;      // a range can begin and end inside a request: two records
@@ -948,7 +1042,7 @@ constexpr int kBaNeverSplit = 384;   // the least that this can be
 constexpr int kBaWholeWarp = 512;    // with a warp per KV head
 int ba_whole_ctx(int n_req, int kw, int elem_bytes) {
   if (kw == 1) return kBaWholeWarp;
-  return n_req >= 8 ? 768 : (elem_bytes == 1 ? 512 : kBaNeverSplit);
+  return n_req >= 8 ? 768 : (elem_bytes != 2 ? 512 : kBaNeverSplit);
 }
 constexpr int kBaShort = 1024;       // ... although up to half of the warps have no head
 // Positions and the tiles of 32 requests are counted in 32 bits.
@@ -1044,6 +1138,80 @@ int ba_type(const BaParams &p, const BaPlan &b, int dtype, int device, cudaStrea
   return dtype == KV_DTYPE_F32 ? ba_pick<D, ELEM, float>(p, b, device, st) : ba_pick<D, ELEM, bf16>(p, b, device, st);
 }
 
+template <int ELEM>
+int ba_dim(const BaParams &p, const BaPlan &b, int dtype, int device, cudaStream_t st) {
+  return p.cache.head_dim == 128 ? ba_type<128, ELEM>(p, b, dtype, device, st) : ba_type<64, ELEM>(p, b, dtype, device, st);
+}
+
+// head_stride: elements between the tables of a request's KV heads, 0 if they share one
+int ba_call(const void *q_dev, int64_t q_stride, int dtype, int n_req, int n_q_heads, const kv_cache_desc *cache, int layer,
+            const int32_t *block_tables_dev, int64_t table_stride, int64_t head_stride, const int32_t *context_lens_dev, int max_ctx,
+            float softmax_scale, void *scratch_dev, int64_t scratch_bytes, void *out_dev, int64_t out_stride, float *lse_out_dev,
+            void *stream) {
+  if (n_req < 0 || n_q_heads <= 0 || max_ctx <= 0 || (dtype != KV_DTYPE_BF16 && dtype != KV_DTYPE_F32)) return KV_ERR_ARG;
+  if (!(softmax_scale > 0.f) || softmax_scale > FLT_MAX / 2.f) return KV_ERR_ARG;      // times log2(e) it stays finite
+  if (max_ctx > kBaMaxCtx) return KV_ERR_SHAPE;
+  int rc = check_cache_desc(cache, true);
+  if (rc != KV_OK) return rc;
+  if (layer < 0 || layer >= cache->n_layers || n_q_heads % cache->n_kv_heads != 0 ||
+      (cache->head_dim != 64 && cache->head_dim != 128))
+    return KV_ERR_SHAPE;
+  if (n_req == 0) return KV_OK;
+  if (q_dev == nullptr || out_dev == nullptr || block_tables_dev == nullptr || context_lens_dev == nullptr) return KV_ERR_ARG;
+  const int size = dtype == KV_DTYPE_BF16 ? 2 : 4;
+  const long long width = (long long)n_q_heads * cache->head_dim;
+  if (((uintptr_t)q_dev & 15) || ((uintptr_t)out_dev & 15) || q_stride * size % 16 != 0 || out_stride * size % 16 != 0)
+    return KV_ERR_ARG;
+  if (((uintptr_t)block_tables_dev & 3) || ((uintptr_t)context_lens_dev & 3) || ((uintptr_t)lse_out_dev & 3)) return KV_ERR_ARG;
+  if (q_stride < 0 || table_stride < 0 || head_stride < 0 || (n_req > 1 && out_stride < width)) return KV_ERR_ARG;
+  if (q_dev == out_dev && n_req > 1 && q_stride != out_stride) return KV_ERR_ARG;      // one request's out would be another's query
+  const long long blocks = ((long long)max_ctx + cache->block_size - 1) / cache->block_size;
+  if (table_stride < blocks || (head_stride != 0 && head_stride < blocks)) return KV_ERR_TABLE_SHORT;
+  const int device = current_device();
+  BaParams p;
+  p.group = n_q_heads / cache->n_kv_heads;
+  p.passes = ba_passes(p.group);
+  const long long vheads = (long long)cache->n_kv_heads * p.passes;
+  if (vheads > 65535 || n_q_heads > 65535) return KV_ERR_SHAPE;      // second dimension of the grids
+  const BaPlan b = ba_plan(n_req, (int)vheads, max_ctx, cache->elem_bytes, sm_count(device));
+  const BaScratch s = ba_scratch(n_req, n_q_heads, cache->head_dim, b.parts);
+  if (!b.whole) {
+    if (scratch_dev == nullptr || ((uintptr_t)scratch_dev & 15) || scratch_bytes < s.bytes) return KV_ERR_WORKSPACE;
+  }
+  if (device < 0) return KV_ERR_CUDA;
+  p.cache = make_view(cache);
+  p.layer = layer;
+  p.num_blocks = cache->num_blocks;
+  p.block_shift = -1;
+  for (int i = 0; i < 31; ++i)
+    if ((1 << i) == cache->block_size) p.block_shift = i;
+  p.aligned16 = cache->block_size % 16 == 0;
+  p.q = q_dev;
+  p.out = out_dev;
+  p.lse = lse_out_dev;
+  p.q_stride = q_stride;
+  p.out_stride = out_stride;
+  p.table_stride = table_stride;
+  p.head_stride = head_stride;
+  p.tables = block_tables_dev;
+  p.lens = context_lens_dev;
+  p.n_req = n_req;
+  p.n_q_heads = n_q_heads;
+  p.max_ctx = max_ctx;
+  p.parts = b.whole ? 0 : b.parts;
+  p.scale = softmax_scale * kLog2e;
+  char *base = static_cast<char *>(scratch_dev);
+  p.tile_start = reinterpret_cast<long long *>(base);
+  p.ml = reinterpret_cast<float2 *>(base + s.ml);
+  p.o = reinterpret_cast<float *>(base + s.o);
+  cudaStream_t st = (cudaStream_t)stream;
+  switch (format_of(cache->elem_bytes)) {
+    case kBf16: return ba_dim<kBf16>(p, b, dtype, device, st);
+    case kE4m3: return ba_dim<kE4m3>(p, b, dtype, device, st);
+    default: return ba_dim<kE2m1>(p, b, dtype, device, st);
+  }
+}
+
 }  // namespace
 }  // namespace kvr
 
@@ -1075,66 +1243,18 @@ int32_t kv_op_paged_attention_batched(const void *q_dev, int64_t q_stride, int32
                                       const int32_t *context_lens_dev, int32_t max_ctx, float softmax_scale,
                                       void *scratch_dev, int64_t scratch_bytes, void *out_dev, int64_t out_stride,
                                       float *lse_out_dev, void *stream) {
-  using namespace kvr;
-  if (n_req < 0 || n_q_heads <= 0 || max_ctx <= 0 || (dtype != KV_DTYPE_BF16 && dtype != KV_DTYPE_F32)) return KV_ERR_ARG;
-  if (!(softmax_scale > 0.f) || softmax_scale > FLT_MAX / 2.f) return KV_ERR_ARG;      // times log2(e) it stays finite
-  if (max_ctx > kBaMaxCtx) return KV_ERR_SHAPE;
-  int rc = check_cache_desc(cache, true);
-  if (rc != KV_OK) return rc;
-  if (layer < 0 || layer >= cache->n_layers || n_q_heads % cache->n_kv_heads != 0 ||
-      (cache->head_dim != 64 && cache->head_dim != 128))
-    return KV_ERR_SHAPE;
-  if (n_req == 0) return KV_OK;
-  if (q_dev == nullptr || out_dev == nullptr || block_tables_dev == nullptr || context_lens_dev == nullptr) return KV_ERR_ARG;
-  const int size = dtype == KV_DTYPE_BF16 ? 2 : 4;
-  const long long width = (long long)n_q_heads * cache->head_dim;
-  if (((uintptr_t)q_dev & 15) || ((uintptr_t)out_dev & 15) || q_stride * size % 16 != 0 || out_stride * size % 16 != 0)
-    return KV_ERR_ARG;
-  if (((uintptr_t)block_tables_dev & 3) || ((uintptr_t)context_lens_dev & 3) || ((uintptr_t)lse_out_dev & 3)) return KV_ERR_ARG;
-  if (q_stride < 0 || table_stride < 0 || (n_req > 1 && out_stride < width)) return KV_ERR_ARG;
-  if (q_dev == out_dev && n_req > 1 && q_stride != out_stride) return KV_ERR_ARG;      // one request's out would be another's query
-  const long long blocks = ((long long)max_ctx + cache->block_size - 1) / cache->block_size;
-  if (table_stride < blocks) return KV_ERR_TABLE_SHORT;
-  const int device = current_device();
-  BaParams p;
-  p.group = n_q_heads / cache->n_kv_heads;
-  p.passes = ba_passes(p.group);
-  const long long vheads = (long long)cache->n_kv_heads * p.passes;
-  if (vheads > 65535 || n_q_heads > 65535) return KV_ERR_SHAPE;      // second dimension of the grids
-  const BaPlan b = ba_plan(n_req, (int)vheads, max_ctx, cache->elem_bytes, sm_count(device));
-  const BaScratch s = ba_scratch(n_req, n_q_heads, cache->head_dim, b.parts);
-  if (!b.whole) {
-    if (scratch_dev == nullptr || ((uintptr_t)scratch_dev & 15) || scratch_bytes < s.bytes) return KV_ERR_WORKSPACE;
-  }
-  if (device < 0) return KV_ERR_CUDA;
-  p.cache = make_view(cache);
-  p.layer = layer;
-  p.num_blocks = cache->num_blocks;
-  p.block_shift = -1;
-  for (int i = 0; i < 31; ++i)
-    if ((1 << i) == cache->block_size) p.block_shift = i;
-  p.aligned16 = cache->block_size % 16 == 0;
-  p.q = q_dev;
-  p.out = out_dev;
-  p.lse = lse_out_dev;
-  p.q_stride = q_stride;
-  p.out_stride = out_stride;
-  p.table_stride = table_stride;
-  p.tables = block_tables_dev;
-  p.lens = context_lens_dev;
-  p.n_req = n_req;
-  p.n_q_heads = n_q_heads;
-  p.max_ctx = max_ctx;
-  p.parts = b.whole ? 0 : b.parts;
-  p.scale = softmax_scale * kLog2e;
-  char *base = static_cast<char *>(scratch_dev);
-  p.tile_start = reinterpret_cast<long long *>(base);
-  p.ml = reinterpret_cast<float2 *>(base + s.ml);
-  p.o = reinterpret_cast<float *>(base + s.o);
-  cudaStream_t st = (cudaStream_t)stream;
-  if (cache->head_dim == 128)
-    return cache->elem_bytes == 2 ? ba_type<128, 2>(p, b, dtype, device, st) : ba_type<128, 1>(p, b, dtype, device, st);
-  return cache->elem_bytes == 2 ? ba_type<64, 2>(p, b, dtype, device, st) : ba_type<64, 1>(p, b, dtype, device, st);
+  return kvr::ba_call(q_dev, q_stride, dtype, n_req, n_q_heads, cache, layer, block_tables_dev, table_stride, 0, context_lens_dev, max_ctx,
+                      softmax_scale, scratch_dev, scratch_bytes, out_dev, out_stride, lse_out_dev, stream);
+}
+
+int32_t kv_op_paged_attention_selected(const void *q_dev, int64_t q_stride, int32_t dtype, int32_t n_req, int32_t n_q_heads,
+                                       const kv_cache_desc *cache, int32_t layer, const int32_t *kept_dev, int64_t kept_stride,
+                                       int64_t kept_head_stride, const int32_t *kept_lens_dev, int32_t max_len, float softmax_scale,
+                                       void *scratch_dev, int64_t scratch_bytes, void *out_dev, int64_t out_stride,
+                                       float *lse_out_dev, void *stream) {
+  if (kept_head_stride <= 0) return KV_ERR_ARG;
+  return kvr::ba_call(q_dev, q_stride, dtype, n_req, n_q_heads, cache, layer, kept_dev, kept_stride, kept_head_stride, kept_lens_dev, max_len,
+                      softmax_scale, scratch_dev, scratch_bytes, out_dev, out_stride, lse_out_dev, stream);
 }
 
 }  // extern "C"

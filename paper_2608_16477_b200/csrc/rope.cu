@@ -17,19 +17,12 @@
 #include <cmath>
 #include <new>
 
-#include "common.cuh"
-
-struct kv_rope {
-  kv_rope_desc d;
-  double theta[128];   // frequencies of the pairs
-  double turns[128];   // theta / (2 pi)
-};
+#include "rope.cuh"
 
 namespace kvr {
 namespace {
 
 constexpr int kRopeThreads = 128;
-constexpr int kRopeMaxPairs = 128;
 constexpr int kRopeMaxTokens = 2;   // tokens of a CTA (16,384 tokens of 72 heads: 97.7 us with two, 102 us with four)
 constexpr int kRopeAhead = 3;       // heads of a thread whose loads are in flight together
 
@@ -78,16 +71,12 @@ struct Vec<bf16> {
   }
 };
 
-// cosines and sines (times gain) of the CTA's tokens: cs[token][pair].  The product with gain is a rounding of its own, 2^-24
-// beside sincospi's ulp, and none where gain is 1: fp64 for it would be an operation more for each pair of every token.
+// cosines and sines (times gain) of the CTA's tokens: cs[token][pair]
 __device__ __forceinline__ void rope_table_of(const RopeParams &p, int t0, int nt, float2 (*cs)[kRopeMaxPairs]) {
   const int half = p.rotary >> 1;
   for (int i = threadIdx.x; i < nt * half; i += kRopeThreads) {
     const int t = i / half, j = i - t * half;
-    const double a = (double)p.positions[t0 + t] * p.turns[j];
-    float s, c;
-    sincospif(2.0f * (float)(a - rint(a)), &s, &c);
-    cs[t][j] = make_float2(c * p.gain, s * (p.gain * p.sign));
+    cs[t][j] = rope_turn(p.positions[t0 + t], p.turns[j], p.gain, p.sign);
   }
 }
 
@@ -146,12 +135,12 @@ __global__ void __launch_bounds__(kRopeThreads) rope_vec_kernel(const __grid_con
         const float2 w0 = w[i / 2], w1 = w[VE / 2 + i / 2];
         const float x0 = fa[i], y0 = fa[i + 1], x1 = fb[i], y1 = fb[i + 1];
         if (u * VE + i / 2 < half) {
-          fa[i] = x0 * w0.x - y0 * w0.y;
-          fa[i + 1] = y0 * w0.x + x0 * w0.y;
+          fa[i] = turned_first(x0, y0, w0);
+          fa[i + 1] = turned_second(x0, y0, w0);
         }
         if (u * VE + VE / 2 + i / 2 < half) {
-          fb[i] = x1 * w1.x - y1 * w1.y;
-          fb[i + 1] = y1 * w1.x + x1 * w1.y;
+          fb[i] = turned_first(x1, y1, w1);
+          fb[i + 1] = turned_second(x1, y1, w1);
         }
       }
     } else {
@@ -159,8 +148,8 @@ __global__ void __launch_bounds__(kRopeThreads) rope_vec_kernel(const __grid_con
       for (int i = 0; i < VE; ++i) {
         const float2 wi = w[i];
         const float xa = fa[i], xb = fb[i];
-        fa[i] = xa * wi.x - xb * wi.y;
-        fb[i] = xb * wi.x + xa * wi.y;
+        fa[i] = turned_first(xa, xb, wi);
+        fb[i] = turned_second(xa, xb, wi);
       }
     }
     *reinterpret_cast<uint4 *>(row + e0) = Vec<T>::pack(fa);
@@ -216,8 +205,8 @@ __global__ void __launch_bounds__(kRopeThreads) rope_row_kernel(const __grid_con
       for (int r = 0; r < n; ++r) {
         T *row = vals + r * p.head_dim;
         const float a = (float)row[j], b = (float)row[j + half];
-        row[j] = (T)(a * w.x - b * w.y);
-        row[j + half] = (T)(b * w.x + a * w.y);
+        row[j] = (T)turned_first(a, b, w);
+        row[j + half] = (T)turned_second(a, b, w);
       }
     }
     __syncwarp();
@@ -254,8 +243,8 @@ __global__ void __launch_bounds__(kRopeThreads) rope_any_kernel(const __grid_con
     const int ea = INTERLEAVED ? 2 * u : u, eb = INTERLEAVED ? 2 * u + 1 : u + half;
     const float2 w = cs[t][u];
     const float a = (float)src[ea], b = (float)src[eb];
-    dst[ea] = (T)(a * w.x - b * w.y);
-    dst[eb] = (T)(b * w.x + a * w.y);
+    dst[ea] = (T)turned_first(a, b, w);
+    dst[eb] = (T)turned_second(a, b, w);
   }
 }
 

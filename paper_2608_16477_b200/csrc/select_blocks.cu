@@ -1,0 +1,488 @@
+// Blocks of a paged cache that are worth attending to: what each block's keys span, and the choice of the blocks whose span
+// promises the largest scores.
+//
+// Bounds, per (block, KV head): for every dim the largest key value rounded up and the smallest rounded down, 8-bit whole numbers in
+// units of one power of two.  No key of the block has q . k above  sum_d max(q_d top_d, q_d low_d).
+//
+// Score of a block for a KV head: that bound summed over the group's query heads, which is u+ . top + u- . low with u+ (u-) the
+// sums of the positive (negative) parts of the heads' queries.  u is taken in 15 bits and a sign, so the score is a whole
+// number (at most 256 * 127 * 32767 < 2^31) times a power of two: it does not depend on the order of any sum, so neither does the
+// choice, and equal scores go to the lowest block.
+#include "cache_format.cuh"
+
+namespace kvr {
+namespace {
+
+constexpr int kInfinite = 255;          // scale byte of a block that no bound covers: always chosen
+constexpr int kMinBound = -60, kMaxBound = 60;      // exponents of a bound's unit
+constexpr int kSelMaxCtx = 1 << 26;
+
+// ---------------------------------------------------------------- bounds
+struct BoundsParams {
+  CacheView cache;
+  int layer, num_blocks, n;
+  const int *blocks, *counts;
+  int8_t *codes;        // [num_blocks][n_kv_heads][2][D]
+  uint8_t *scales;      // [num_blocks][n_kv_heads]
+};
+
+constexpr int kBoundThreads = 256;
+
+// A warp takes a (block, KV head), a lane D / 32 dims of every key.  HBM-bound: K's rows once.
+template <int D, int FMT>
+__global__ void __launch_bounds__(kBoundThreads) block_bounds_kernel(const __grid_constant__ BoundsParams p) {
+  constexpr int E = D / 32;
+  const int lane = threadIdx.x & 31;
+  const long long item = blockIdx.x * (long long)(kBoundThreads / 32) + (threadIdx.x >> 5);
+  const int heads = p.cache.n_kv_heads;
+  const long long i = item / heads;
+  const int head = (int)(item - i * heads);
+  if (i >= p.n) return;
+  const int block = __ldg(p.blocks + i), count = min(__ldg(p.counts + i), p.cache.block_size);
+  if ((unsigned)block >= (unsigned)p.num_blocks || count <= 0) return;
+  const char *page = p.cache.page(p.layer, 0, block);
+  const char *record = FMT == kE2m1 ? page + head * p.cache.record_bytes() : page + head * D * FMT;
+  const long long slot_bytes = FMT == kE2m1 ? D / 2 : (long long)heads * D * FMT;
+  const uint8_t *scale = reinterpret_cast<const uint8_t *>(FMT == kE2m1 ? record + (long long)p.cache.block_size * (D / 2 + D / 16)
+                                                                        : page + p.cache.value_bytes() + head * p.cache.block_size);
+  const uint8_t *groups = reinterpret_cast<const uint8_t *>(record + (long long)p.cache.block_size * (D / 2));
+  float top[E], low[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+    top[j] = -INFINITY;
+    low[j] = INFINITY;
+  }
+  bool fine = true;
+#pragma unroll 8
+  for (int s = 0; s < count; ++s) {
+    float f[E];
+    const char *row = record + s * slot_bytes;
+    if (FMT == kBf16) {
+#pragma unroll
+      for (int j = 0; j < E; j += 2) {
+        const uint32_t w = reinterpret_cast<const uint32_t *>(row)[lane * (E / 2) + j / 2];
+        f[j] = __uint_as_float(w << 16);
+        f[j + 1] = __uint_as_float(w & 0xffff0000u);
+      }
+    } else {
+      const float unit = __uint_as_float((uint32_t)scale[s] << 23);
+      uint32_t h[E / 2];
+      if (FMT == kE4m3) {
+        const uint32_t w = E == 4 ? reinterpret_cast<const uint32_t *>(row)[lane] : reinterpret_cast<const uint16_t *>(row)[lane];
+#pragma unroll
+        for (int j = 0; j < E / 2; ++j) h[j] = half2_of_e4m3x2(w >> (16 * j));
+      } else {
+        const uint32_t w = reinterpret_cast<const uint32_t *>(row)[lane * E / 8] >> (lane * E % 8 * 4);
+        const uint32_t s16 = half2_of_e4m3x2(groups[s * (D / 16) + lane * E / 16] * 0x101u);
+        uint32_t v[4];
+        halves_of_e2m1(w, v);
+#pragma unroll
+        for (int j = 0; j < E / 2; ++j) h[j] = mul_half2(v[j], s16);
+      }
+#pragma unroll
+      for (int j = 0; j < E / 2; ++j) {
+        const float2 x = floats_of_half2(h[j]);
+        f[2 * j] = x.x * unit;
+        f[2 * j + 1] = x.y * unit;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      fine &= fabsf(f[j]) <= 127.f * 0x1p60f;
+      top[j] = fmaxf(top[j], f[j]);
+      low[j] = fminf(low[j], f[j]);
+    }
+  }
+  float size = 0.f;
+#pragma unroll
+  for (int j = 0; j < E; ++j) size = fmaxf(size, fmaxf(fabsf(top[j]), fabsf(low[j])));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) size = fmaxf(size, __shfl_xor_sync(0xffffffffu, size, o));
+  fine = __all_sync(0xffffffffu, fine);
+  // size = m * 2^x with 1 <= m < 2; 127 = 1.984375 * 2^6
+  const uint32_t bits = __float_as_uint(size);
+  const int e = max((int)(bits >> 23) - 127 - 6 + ((bits & 0x7fffffu) > 0x7e0000u), kMinBound);
+  const float down = __uint_as_float((uint32_t)(127 - min(e, kMaxBound)) << 23);
+  uint32_t up = 0, lo = 0;
+#pragma unroll
+  for (int j = 0; j < E; ++j) {
+    up |= ((uint32_t)(int)ceilf(top[j] * down) & 255u) << (8 * j);
+    lo |= ((uint32_t)(int)floorf(low[j] * down) & 255u) << (8 * j);
+  }
+  if (!fine) up = lo = 0;
+  int8_t *to = p.codes + ((long long)block * heads + head) * (2 * D) + lane * E;
+  if (E == 4) {
+    *reinterpret_cast<uint32_t *>(to) = up;
+    *reinterpret_cast<uint32_t *>(to + D) = lo;
+  } else {
+    *reinterpret_cast<uint16_t *>(to) = (uint16_t)up;
+    *reinterpret_cast<uint16_t *>(to + D) = (uint16_t)lo;
+  }
+  if (lane == 0) p.scales[(long long)block * heads + head] = (uint8_t)(fine ? e + 127 : kInfinite);
+}
+
+template <int D, int FMT>
+int launch_bounds(const BoundsParams &p, cudaStream_t st) {
+  const long long warps = (long long)p.n * p.cache.n_kv_heads, ctas = (warps + kBoundThreads / 32 - 1) / (kBoundThreads / 32);
+  if (ctas > 0x7fffffffll) return KV_ERR_SHAPE;
+  block_bounds_kernel<D, FMT><<<(unsigned)ctas, kBoundThreads, 0, st>>>(p);
+  KV_COUNT_LAUNCH();
+  KV_CUDA(cudaGetLastError());
+  return KV_OK;
+}
+
+template <int FMT>
+int bounds_format(const BoundsParams &p, cudaStream_t st) {
+  return p.cache.head_dim == 128 ? launch_bounds<128, FMT>(p, st) : launch_bounds<64, FMT>(p, st);
+}
+
+// ---------------------------------------------------------------- scores
+struct SelectParams {
+  const void *q;
+  long long q_stride, table_stride;
+  int n_req, heads, group, num_blocks, block_size, max_ctx, max_blocks;
+  int first, last, keep;
+  const int8_t *codes;
+  const uint8_t *scales;
+  const int *tables, *lens;
+  uint32_t *keys;             // scratch: [n_req][heads][max_blocks], the scores in an order-preserving code
+  int *kept, *kept_lens;
+};
+
+__device__ __forceinline__ int blocks_of(const SelectParams &p, int r, int &len) {
+  len = min(max(__ldg(p.lens + r), 0), p.max_ctx);
+  return (len + p.block_size - 1) / p.block_size;
+}
+// fp32 -> a number whose order is the score's
+__device__ __forceinline__ uint32_t key_of_score(float s) {
+  const uint32_t b = __float_as_uint(s);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+constexpr uint32_t kAlways = 0xffffffffu;
+
+__device__ __forceinline__ int dp4_ss(uint32_t a, uint32_t b, int c) {
+  int r;
+  asm("dp4a.s32.s32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
+}
+__device__ __forceinline__ int dp4_su(uint32_t a, uint32_t b, int c) {
+  int r;
+  asm("dp4a.s32.u32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+  return r;
+}
+
+template <typename T>
+__device__ __forceinline__ double value_of(T x);
+template <>
+__device__ __forceinline__ double value_of<float>(float x) { return fabsf(x) <= FLT_MAX ? (double)x : 0.0; }
+template <>
+__device__ __forceinline__ double value_of<bf16>(bf16 x) { return value_of<float>(__bfloat162float(x)); }
+
+constexpr int kScoreThreads = 256;
+constexpr int kScoreBlocks = 32;      // of a warp at a time
+
+// The code of a KV head's queries into shared memory: hi[i] * 256 + lo[i] for value i of [u+ | u-].  The sums are fp64: with up to 2^29
+// between the heads' values they are exact.
+template <int D, typename T>
+__device__ __forceinline__ void query_code(const SelectParams &p, int req, int head, int8_t *hi, uint8_t *lo, double *warp_most) {
+  const int i = threadIdx.x, lane = i & 31, warp = i >> 5;
+  double u = 0.0;
+  if (i < 2 * D) {
+    const T *q = static_cast<const T *>(p.q) + req * p.q_stride + (long long)head * p.group * D + i % D;
+#pragma unroll 8
+    for (int h = 0; h < p.group; ++h) {
+      const double x = value_of<T>(q[(long long)h * D]);
+      u += i < D ? fmax(x, 0.0) : fmin(x, 0.0);
+    }
+  }
+  double most = fabs(u);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, o));
+  if (lane == 0) warp_most[warp] = most;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kScoreThreads / 32; ++w) most = fmax(most, warp_most[w]);
+  // most = m * 2^x with 1 <= m < 2; 32767 = (2 - 2^-14) * 2^14
+  const unsigned long long bits = (unsigned long long)__double_as_longlong(most);
+  int e = (int)(bits >> 52) - 1023 - 14 + ((bits & 0xfffffffffffffull) > 0xfffc000000000ull);
+  e = max(e, -100);
+  const int c = __double2int_rn(u * __longlong_as_double((long long)(1023 - e) << 52));
+  if (i < 2 * D) {
+    hi[i] = (int8_t)(c >> 8);
+    lo[i] = (uint8_t)c;
+  }
+  __syncthreads();
+}
+
+// A CTA takes one KV head of one request and `chunk` of its blocks, a warp 32 of them at a time: half of it (D = 64: a quarter) reads
+// a block's codes, 16 bytes to a lane, and the sums over the lanes are exchanged so that lane i ends with block i's.
+template <int D, typename T>
+__global__ void __launch_bounds__(kScoreThreads) block_score_kernel(const __grid_constant__ SelectParams p, int chunk) {
+  constexpr int LPB = D / 8;                  // lanes of a block
+  constexpr int N = LPB;                      // loads of a lane: kScoreBlocks / (32 / LPB)
+  __shared__ __align__(16) int8_t hi_s[2 * D];
+  __shared__ __align__(16) uint8_t lo_s[2 * D];
+  __shared__ double most_s[kScoreThreads / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int req = blockIdx.z, head = blockIdx.y;
+  int len;
+  const int n = blocks_of(p, req, len);
+  if (n <= p.keep) return;                    // all of them are chosen
+  const int from = p.first + blockIdx.x * chunk, to = min(from + chunk, n - p.last);
+  if (from >= to) return;
+  query_code<D, T>(p, req, head, hi_s, lo_s, most_s);
+  const int l = lane % LPB;                   // the lane has values 16 l ... of a block's codes
+  const uint4 hv = *reinterpret_cast<const uint4 *>(hi_s + 16 * l), lv = *reinterpret_cast<const uint4 *>(lo_s + 16 * l);
+  const uint32_t hi[4] = {hv.x, hv.y, hv.z, hv.w}, lo[4] = {lv.x, lv.y, lv.z, lv.w};
+  const int *table = p.tables + req * p.table_stride;
+  uint32_t *keys = p.keys + ((long long)req * p.heads + head) * p.max_blocks;
+  for (int b0 = from + warp * kScoreBlocks; b0 < to; b0 += kScoreThreads) {
+    const int b = b0 + lane;
+    const int phys = b < to ? __ldg(table + b) : -1;
+    const bool there = (unsigned)phys < (unsigned)p.num_blocks;
+    const long long entry = there ? (long long)phys * p.heads + head : 0;
+    const int scale = there ? (int)__ldg(p.scales + entry) : kInfinite;
+    uint4 x[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      // block g N + i for the g-th group of LPB lanes
+      const long long at = __shfl_sync(0xffffffffu, entry, (lane / LPB) * N + i);
+      x[i] = __ldg(reinterpret_cast<const uint4 *>(p.codes + at * (2 * D) + l * 16));
+    }
+    int sum[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+      int a = 0, c = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        a = dp4_ss(w[j], hi[j], a);
+        c = dp4_su(w[j], lo[j], c);
+      }
+      sum[i] = a * 256 + c;
+    }
+    // sums over the LPB lanes, lane l keeping block l's: half of the blocks handed over in each round
+#pragma unroll
+    for (int o = LPB / 2; o > 0; o >>= 1) {
+      const bool upper = l & o;
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) {
+        if (i >= o) break;
+        const int mine = upper ? sum[i + o] : sum[i], other = upper ? sum[i] : sum[i + o];
+        sum[i] = mine + __shfl_xor_sync(0xffffffffu, other, o);
+      }
+    }
+    const float score = (float)sum[0] * __uint_as_float((uint32_t)min(scale, 254) << 23);
+    if (b < to) keys[b] = scale == kInfinite ? kAlways : key_of_score(score);
+  }
+}
+
+// ---------------------------------------------------------------- choice
+constexpr int kPickThreads = 256;
+
+// One CTA per request and KV head: the key of rank `want` digit by digit (radix selection), then the blocks above it and the first of
+// its equals, in the order of their positions.
+__global__ void __launch_bounds__(kPickThreads) block_pick_kernel(const __grid_constant__ SelectParams p) {
+  __shared__ int hist[256];
+  __shared__ int sums[2][kPickThreads / 32];
+  __shared__ int digit_s, want_s;
+  const int req = blockIdx.x, head = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int len;
+  const int n = blocks_of(p, req, len), kept = min(n, p.keep);
+  const int *table = p.tables + req * p.table_stride;
+  int *out = p.kept + ((long long)req * p.heads + head) * p.keep;
+  if (head == 0 && tid == 0) p.kept_lens[req] = len - (n - kept) * p.block_size;
+  for (int i = kept + tid; i < p.keep; i += kPickThreads) out[i] = -1;
+  if (n <= p.keep) {
+    for (int i = tid; i < n; i += kPickThreads) out[i] = __ldg(table + i);
+    return;
+  }
+  const int from = p.first, to = n - p.last;
+  for (int i = tid; i < p.first; i += kPickThreads) out[i] = __ldg(table + i);
+  for (int i = tid; i < p.last; i += kPickThreads) out[p.keep - p.last + i] = __ldg(table + to + i);
+  int want = p.keep - p.first - p.last;      // how many of the middle ones
+  if (want == 0) return;
+  const uint32_t *keys = p.keys + ((long long)req * p.heads + head) * p.max_blocks;
+  uint32_t prefix = 0;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    hist[tid] = 0;
+    __syncthreads();
+    for (int b = from + tid; b < to; b += kPickThreads) {
+      const uint32_t k = keys[b];
+      if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1);
+    }
+    __syncthreads();
+    if (warp == 0) {
+      // lane l has digits 255 - 8 l ... 248 - 8 l: the running count from the top
+      int c[8], total = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        c[i] = hist[255 - 8 * lane - i];
+        total += c[i];
+      }
+      int above = total;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, above, o);
+        if (lane >= o) above += up;
+      }
+      above -= total;
+      if (above < want && want <= above + total) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (above < want && want <= above + c[i]) {
+            digit_s = 255 - 8 * lane - i;
+            want_s = want - above;
+          }
+          above += c[i];
+        }
+      }
+    }
+    __syncthreads();
+    prefix |= (uint32_t)digit_s << shift;
+    want = want_s;                            // of the keys that begin with prefix
+  }
+  // ---- keys above prefix, and the first `want` equal ones
+  int taken = p.first, equals = 0;            // so far
+  for (int b0 = from, turn = 0; b0 < to; b0 += kPickThreads, turn ^= 1) {
+    const int b = b0 + tid;
+    const uint32_t k = b < to ? keys[b] : 0;
+    const bool more = b < to && k > prefix, same = b < to && k == prefix;
+    const unsigned more_w = __ballot_sync(0xffffffffu, more), same_w = __ballot_sync(0xffffffffu, same);
+    if (lane == 0) sums[turn][warp] = __popc(more_w) | __popc(same_w) << 16;
+    __syncthreads();
+    int before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kPickThreads / 32; ++w) {
+      const int s = sums[turn][w];
+      before += w < warp ? s : 0;
+      all += s;
+    }
+    const unsigned below = (1u << lane) - 1u;
+    const int same_before = equals + (before >> 16) + __popc(same_w & below);
+    const int more_before = (before & 0xffff) + __popc(more_w & below);
+    if (more || (same && same_before < want))
+      out[taken - min(equals, want) + more_before + min(same_before, want)] = __ldg(table + b);
+    const int more_all = all & 0xffff, equals_new = equals + (all >> 16);
+    taken += more_all + min(equals_new, want) - min(equals, want);
+    equals = equals_new;
+  }
+}
+
+int select_max_blocks(int max_ctx, int block_size) { return (int)(((long long)max_ctx + block_size - 1) / block_size); }
+
+template <int D, typename T>
+int launch_select(const SelectParams &p, int sms, cudaStream_t st) {
+  const int middle = p.max_blocks - p.first - p.last;
+  if (p.max_blocks > p.keep) {
+    // a batch of blocks for every warp, or as many more as leave two CTAs for each SM
+    const long long lines = (long long)p.n_req * p.heads, batches = (middle + kScoreThreads - 1) / kScoreThreads;
+    const long long each = batches * lines / (2ll * sms);
+    const int chunk = (int)(each > 1 ? each < batches ? each : batches : 1) * kScoreThreads;
+    const dim3 grid((middle + chunk - 1) / chunk, p.heads, p.n_req);
+    block_score_kernel<D, T><<<grid, kScoreThreads, 0, st>>>(p, chunk);
+    KV_COUNT_LAUNCH();
+    KV_CUDA(cudaGetLastError());
+  }
+  block_pick_kernel<<<dim3(p.n_req, p.heads), kPickThreads, 0, st>>>(p);
+  KV_COUNT_LAUNCH();
+  KV_CUDA(cudaGetLastError());
+  return KV_OK;
+}
+
+}  // namespace
+}  // namespace kvr
+
+extern "C" {
+
+int32_t kv_op_block_bounds(const kv_cache_desc *cache, int32_t layer, const int32_t *blocks_dev, const int32_t *counts_dev, int32_t n,
+                           int8_t *bounds_dev, uint8_t *bound_scales_dev, void *stream) {
+  using namespace kvr;
+  if (n < 0) return KV_ERR_ARG;
+  int rc = check_cache_desc(cache, true);
+  if (rc != KV_OK) return rc;
+  if (cache->head_dim != 64 && cache->head_dim != 128) return KV_ERR_SHAPE;
+  if (layer < 0 || layer >= cache->n_layers) return KV_ERR_SHAPE;
+  if (n == 0) return KV_OK;
+  if (blocks_dev == nullptr || counts_dev == nullptr || bounds_dev == nullptr || bound_scales_dev == nullptr) return KV_ERR_ARG;
+  if (((uintptr_t)blocks_dev & 3) || ((uintptr_t)counts_dev & 3) || ((uintptr_t)bounds_dev & 15)) return KV_ERR_ARG;
+  BoundsParams p;
+  p.cache = make_view(cache);
+  p.layer = layer;
+  p.num_blocks = cache->num_blocks;
+  p.n = n;
+  p.blocks = blocks_dev;
+  p.counts = counts_dev;
+  p.codes = bounds_dev;
+  p.scales = bound_scales_dev;
+  cudaStream_t st = (cudaStream_t)stream;
+  switch (format_of(cache->elem_bytes)) {
+    case kBf16: return bounds_format<kBf16>(p, st);
+    case kE4m3: return bounds_format<kE4m3>(p, st);
+    default: return bounds_format<kE2m1>(p, st);
+  }
+}
+
+int64_t kv_select_blocks_scratch_bytes(int32_t n_req, int32_t n_kv_heads, int32_t block_size, int32_t max_ctx) {
+  using namespace kvr;
+  if (n_req < 0 || n_kv_heads <= 0 || block_size <= 0 || max_ctx <= 0) return KV_ERR_ARG;
+  if (max_ctx > kSelMaxCtx) return KV_ERR_SHAPE;
+  return ((long long)n_req * n_kv_heads * select_max_blocks(max_ctx, block_size) * 4 + 255) / 256 * 256;
+}
+
+int32_t kv_op_select_blocks(const void *q_dev, int64_t q_stride, int32_t dtype, int32_t n_req, int32_t n_q_heads, int32_t n_kv_heads,
+                            int32_t head_dim, const int8_t *bounds_dev, const uint8_t *bound_scales_dev, int32_t num_blocks,
+                            int32_t block_size, const int32_t *block_tables_dev, int64_t table_stride, const int32_t *context_lens_dev,
+                            int32_t max_ctx, int32_t first, int32_t last, int32_t keep, void *scratch_dev, int64_t scratch_bytes,
+                            int32_t *kept_dev, int32_t *kept_lens_dev, void *stream) {
+  using namespace kvr;
+  if (n_req < 0 || n_q_heads <= 0 || n_kv_heads <= 0 || num_blocks <= 0 || block_size <= 0 || max_ctx <= 0) return KV_ERR_ARG;
+  if (dtype != KV_DTYPE_BF16 && dtype != KV_DTYPE_F32) return KV_ERR_ARG;
+  // the last block may be partly filled: only there can a chosen context end
+  if (first < 0 || last < 1 || keep < 1 || (long long)first + last > keep) return KV_ERR_ARG;
+  if (n_q_heads % n_kv_heads != 0 || (head_dim != 64 && head_dim != 128)) return KV_ERR_SHAPE;
+  if (max_ctx > kSelMaxCtx || (long long)keep * block_size > kSelMaxCtx || n_req > 65535 || n_kv_heads > 65535) return KV_ERR_SHAPE;
+  if (n_req == 0) return KV_OK;
+  if (q_dev == nullptr || bounds_dev == nullptr || bound_scales_dev == nullptr || block_tables_dev == nullptr ||
+      context_lens_dev == nullptr || kept_dev == nullptr || kept_lens_dev == nullptr)
+    return KV_ERR_ARG;
+  const int size = dtype == KV_DTYPE_BF16 ? 2 : 4;
+  if (((uintptr_t)q_dev & 15) || q_stride < 0 || q_stride * size % 16 != 0 || table_stride < 0 || ((uintptr_t)bounds_dev & 15)) return KV_ERR_ARG;
+  for (const void *x : {(const void *)block_tables_dev, (const void *)context_lens_dev, (const void *)kept_dev, (const void *)kept_lens_dev})
+    if ((uintptr_t)x & 3) return KV_ERR_ARG;
+  const int max_blocks = select_max_blocks(max_ctx, block_size);
+  if (table_stride < max_blocks) return KV_ERR_TABLE_SHORT;
+  if (max_blocks > keep) {
+    const long long need = (long long)n_req * n_kv_heads * max_blocks * 4;
+    if (scratch_dev == nullptr || ((uintptr_t)scratch_dev & 15) || scratch_bytes < need) return KV_ERR_WORKSPACE;
+  }
+  const int device = current_device();
+  if (device < 0) return KV_ERR_CUDA;
+  SelectParams p;
+  p.q = q_dev;
+  p.q_stride = q_stride;
+  p.table_stride = table_stride;
+  p.n_req = n_req;
+  p.heads = n_kv_heads;
+  p.group = n_q_heads / n_kv_heads;
+  p.num_blocks = num_blocks;
+  p.block_size = block_size;
+  p.max_ctx = max_ctx;
+  p.max_blocks = max_blocks;
+  p.first = first;
+  p.last = last;
+  p.keep = keep;
+  p.codes = bounds_dev;
+  p.scales = bound_scales_dev;
+  p.tables = block_tables_dev;
+  p.lens = context_lens_dev;
+  p.keys = static_cast<uint32_t *>(scratch_dev);
+  p.kept = kept_dev;
+  p.kept_lens = kept_lens_dev;
+  const int sms = sm_count(device);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (head_dim == 128) return dtype == KV_DTYPE_F32 ? launch_select<128, float>(p, sms, st) : launch_select<128, bf16>(p, sms, st);
+  return dtype == KV_DTYPE_F32 ? launch_select<64, float>(p, sms, st) : launch_select<64, bf16>(p, sms, st);
+}
+
+}  // extern "C"
