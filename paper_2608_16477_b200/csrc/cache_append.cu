@@ -4,25 +4,26 @@
 // The same bits as the rotary operator on Q and K followed by the write of the rows (a turned key is rounded to the rows' type
 // before it is quantised), with K read once and written once, and one launch.  HBM-bound: q twice, k and v once, the pages once.
 //
-// head_dim / 16 lanes own a row, two pieces of 8 values each half a row apart, as in the write of rows; where the whole head turns in
-// halves both members of a pair are the lane's own.  Other pairs have their partner loaded once more (from L1, mostly).  A CTA takes
-// all rows of a few tokens, or 32 (64) rows of one where there are few tokens; its threads form each (token, pair)'s sine and cosine
-// once into shared memory while their first rows are on the way.
+// head_dim / 16 lanes own a row, two pieces of 8 values each, so placed that where pairs lie in halves a lane holds both members of
+// its own.  A CTA takes all rows of a few tokens, or 16 (32) rows of one where there are few tokens; its threads form each (token,
+// pair)'s sine and cosine once into shared memory while their first rows are on the way.  Small CTAs of few registers with one row to a
+// lane in flight, ten to an SM, were better than more rows in flight or CTAs that stay (16,384 tokens of 32 query and 8 KV heads of 128,
+// bf16 into e2m1 pages, 355 MB: 68 us against 73 to 104; 5.2 TB/s, 79 % of a copy's rate; the sines and cosines take 7 us of it, the
+// conversion to e2m1 most of the rest).  One token of 64 / 8 heads 2.4 us, 64 tokens 3.0 us.
 #include "cache_format.cuh"
 #include "rope.cuh"
 
 namespace kvr {
 namespace {
 
-constexpr int kAppendThreads = 256;
-constexpr int kAppendTokens = 8;      // most tokens of a CTA
-constexpr int kAppendAhead = 2;       // rows of a lane whose loads are in flight together
+constexpr int kAppendThreads = 128;
+constexpr int kAppendTokens = 4;      // most tokens of a CTA
 constexpr int kAppendMaxTokens = 1 << 30;
 
 struct AppendParams {
-  CacheView cache;
+  RowLayout layout;
   SlotMap map;
-  int layer, n_tokens, n_q, n_kv;
+  int n_tokens, n_q, n_kv;
   int rotary, interleaved, tokens_per_cta, rows_per_cta;
   float gain;
   const int *positions;
@@ -33,159 +34,148 @@ struct AppendParams {
   double turns[kRopeMaxPairs];
 };
 
-// One row that a group of lanes has in hand.
-template <typename T>
-struct Row {
-  Raw<T> raw;
-  int kind, head, token;      // 0 K, 1 V, 2 Q, 3 none
-  const char *src;            // the row
-  long long slot;
-};
+// How the pairs of a head lie to the lanes' pieces.  Halves whose members begin at multiples of 16 dims, the head's rest as well
+// (rotary_dim 32, 64, 96 or all of it): a lane's pieces are the two members of its pairs, or two pieces of the rest.  Interleaved pairs: a
+// piece holds its pairs.  Other halves: a lane loads the other members from global memory.
+enum { kHalves = 0, kInterleaved = 1, kAnyHalves = 2 };
 
-// Turns a lane's pieces; cs: the token's (cos, sin) by pair.
-template <typename T, int D>
-__device__ __forceinline__ void turn_any(const AppendParams &p, Raw<T> &raw, const char *src, int sub, unsigned group, const float2 *cs) {
-  const int half = p.rotary >> 1;
-  float f[2][8], other[2][8];
-  raw.unpack(0, f[0]);
-  raw.unpack(1, f[1]);
-  if (p.interleaved) {
+// Turns a lane's pieces, which begin at dims `first` and `first` + `apart`.  cs: the token's (cos, sin), by pair (kHalves: by place_of).
+template <typename T, int D, int MODE>
+__device__ __forceinline__ void turn(Raw<T> &raw, const char *row, int first, int apart, int sub, int rotary, unsigned group, const float2 *cs) {
+  const int half = rotary >> 1;
+  float f[2][8];
+  if (MODE == kHalves) {
+    if (first >= half) return;      // the rest of the head
+    raw.unpack(0, f[0]);
+    raw.unpack(1, f[1]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float4 w = *reinterpret_cast<const float4 *>(cs + (k * (D / 16) + sub) * 2);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float2 wi = i ? make_float2(w.z, w.w) : make_float2(w.x, w.y);
+        const float a = f[0][2 * k + i], b = f[1][2 * k + i];
+        f[0][2 * k + i] = turned_first(a, b, wi);
+        f[1][2 * k + i] = turned_second(a, b, wi);
+      }
+    }
+    raw.pack(0, f[0]);
+    raw.pack(1, f[1]);
+  } else if (MODE == kInterleaved) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int e0 = first + h * apart;
+      if (e0 >= rotary) continue;
+      raw.unpack(h, f[h]);
+#pragma unroll
+      for (int i = 0; i < 8; i += 4) {
+        const float4 w = *reinterpret_cast<const float4 *>(cs + (e0 + i) / 2);      // two pairs; past the last one: not used
+        const float a0 = f[h][i], b0 = f[h][i + 1], a1 = f[h][i + 2], b1 = f[h][i + 3];
+        if (e0 + i < rotary) {
+          f[h][i] = turned_first(a0, b0, make_float2(w.x, w.y));
+          f[h][i + 1] = turned_second(a0, b0, make_float2(w.x, w.y));
+        }
+        if (e0 + i + 2 < rotary) {
+          f[h][i + 2] = turned_first(a1, b1, make_float2(w.z, w.w));
+          f[h][i + 3] = turned_second(a1, b1, make_float2(w.z, w.w));
+        }
+      }
+      raw.pack(h, f[h]);
+    }
+  } else {
+    float other[2][8];
+    raw.unpack(0, f[0]);
+    raw.unpack(1, f[1]);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        const int pair = (h * (D / 2) + sub * 8 + i) >> 1;
-        if (pair < half) {
-          const float2 w = cs[pair];
-          const float a = f[h][i], b = f[h][i + 1];
-          f[h][i] = turned_first(a, b, w);
-          f[h][i + 1] = turned_second(a, b, w);
-        }
+      for (int i = 0; i < 8; ++i) {
+        const int e = first + h * apart + i;
+        other[h][i] = e < rotary ? (float)reinterpret_cast<const T *>(row)[e < half ? e + half : e - half] : 0.f;
       }
-  } else {
-    const T *row = reinterpret_cast<const T *>(src);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int e0 = h * (D / 2) + sub * 8;
-      if (half % 8 == 0) {
-        if (e0 < p.rotary) {
-          Raw<T> partner;
-          partner.load(src + (e0 < half ? e0 + half : e0 - half) * (int)sizeof(T), 0);
-          partner.unpack(0, other[h]);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int e = e0 + i;
-          other[h][i] = e < p.rotary ? (float)row[e < half ? e + half : e - half] : 0.f;
-        }
-      }
-    }
     __syncwarp(group);      // the row may be overwritten in place from here on
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int e = h * (D / 2) + sub * 8 + i;
+        const int e = first + h * apart + i;
         if (e < half)
           f[h][i] = turned_first(f[h][i], other[h][i], cs[e]);
-        else if (e < p.rotary)
+        else if (e < rotary)
           f[h][i] = turned_second(other[h][i], f[h][i], cs[e - half]);
       }
+    raw.pack(0, f[0]);
+    raw.pack(1, f[1]);
   }
-  raw.pack(0, f[0]);
-  raw.pack(1, f[1]);
 }
 
-// Place of pair j of a whole head turned in halves, so that the 16-byte loads of a row's lanes (pairs 8 sub, ... + 7) follow one another.
+// Place of pair j of a head turned in halves, so that the 16-byte loads of a row's lanes (pairs 8 sub, ... + 7) follow one another.
 template <int D>
 __device__ __forceinline__ int place_of(int j) {
   return ((((j & 7) >> 1) * (D / 16) + (j >> 3)) << 1) + (j & 1);
 }
 
-template <typename T, int D, int FMT, bool WHOLE>      // WHOLE: the whole head turns in halves
-__global__ void __launch_bounds__(kAppendThreads) cache_append_kernel(const __grid_constant__ AppendParams p) {
-  constexpr int LPR = D / 16, ROWS = kAppendThreads / LPR, PIECE = 8 * (int)sizeof(T);
+template <typename T, int D, int FMT, int MODE>
+__global__ void __launch_bounds__(kAppendThreads, sizeof(T) == 2 ? 10 : 8) cache_append_kernel(const __grid_constant__ AppendParams p) {
+  constexpr int LPR = D / 16, ROWS = kAppendThreads / LPR;
   __shared__ __align__(16) float2 cs[kAppendTokens][kRopeMaxPairs];
+  __shared__ long long block_s[kAppendTokens];      // of a token's slot: the block's place (-1: outside the pool), and the offset in it
+  __shared__ int offset_s[kAppendTokens];
   const int t0 = blockIdx.x * p.tokens_per_cta, nt = min(p.tokens_per_cta, p.n_tokens - t0);
   const int rows = p.n_q + 2 * p.n_kv, r0 = blockIdx.y * p.rows_per_cta, nr = min(p.rows_per_cta, rows - r0);
-  const int sub = threadIdx.x % LPR, items = nt * nr, half = p.rotary >> 1;
+  const int sub = threadIdx.x % LPR, half = p.rotary >> 1;
+  const int first = MODE != kHalves || sub < half / 8 ? sub * 8 : p.rotary + sub * 8 - half;      // dims of the lane's pieces
+  const int apart = MODE != kHalves ? D / 2 : sub < half / 8 ? half : (D - p.rotary) / 2;
   const unsigned group = ((1u << LPR) - 1u) << (threadIdx.x & 31 & ~(LPR - 1));
 
-  Row<T> r[kAppendAhead];
-  auto load = [&](int first) {
-#pragma unroll
-    for (int i = 0; i < kAppendAhead; ++i) {
-      const int it = first + i * ROWS;
-      r[i].kind = 3;
-      if (it >= items) continue;
-      const int t = it / nr, row = r0 + it - t * nr;
-      r[i].token = t;
-      r[i].slot = -1;
-      if (row < p.n_kv) {
-        r[i].kind = 0;
-        r[i].head = row;
-        r[i].src = p.k + (t0 + t) * p.k_ts + row * p.k_hs;
-      } else if (row < 2 * p.n_kv) {
-        r[i].kind = 1;
-        r[i].head = row - p.n_kv;
-        r[i].src = p.v + (t0 + t) * p.v_ts + r[i].head * p.v_hs;
-      } else {
-        r[i].kind = 2;
-        r[i].head = row - 2 * p.n_kv;
-        r[i].src = p.q + (t0 + t) * p.q_ts + r[i].head * p.q_hs;
-      }
-      if (r[i].kind < 2) r[i].slot = __ldg(p.slots + t0 + t);
-      r[i].raw.load(r[i].src + sub * PIECE, D / 2 * (int)sizeof(T));
+  // Row `at` of a token: K's heads come first, then V's, then the queries'.
+  int token = 0, at = threadIdx.x / LPR;
+  auto settle = [&]() {
+    while (at >= nr) {
+      at -= nr;
+      ++token;
     }
   };
-  load(threadIdx.x / LPR);      // under the trigonometry
+  settle();
+  Raw<T> x;
+  const char *src = nullptr;
+  auto load = [&]() {
+    const int row = r0 + at;
+    const long long t = t0 + token;
+    src = row < p.n_kv ? p.k + t * p.k_ts + row * p.k_hs
+                       : row < 2 * p.n_kv ? p.v + t * p.v_ts + (row - p.n_kv) * p.v_hs : p.q + t * p.q_ts + (row - 2 * p.n_kv) * p.q_hs;
+    x.load(src + first * (int)sizeof(T), apart * (int)sizeof(T));
+  };
+  if (token < nt) load();      // under the trigonometry
   for (int i = threadIdx.x; i < nt * half; i += kAppendThreads) {
     const int t = i / half, j = i - t * half;
-    cs[t][WHOLE ? place_of<D>(j) : j] = rope_turn(p.positions[t0 + t], p.turns[j], p.gain, 1.f);
+    cs[t][MODE == kHalves ? place_of<D>(j) : j] = rope_turn(p.positions[t0 + t], p.turns[j], p.gain, 1.f);
+  }
+  if (threadIdx.x < nt) {
+    int block, offset;
+    const bool live = p.map.split(p.slots[t0 + threadIdx.x], block, offset);
+    block_s[threadIdx.x] = live ? block * p.layout.block_stride : -1;
+    offset_s[threadIdx.x] = offset;
   }
   __syncthreads();
-  for (int first = threadIdx.x / LPR; first < items; first += kAppendAhead * ROWS) {
-    if (first >= ROWS) load(first);
-#pragma unroll
-    for (int i = 0; i < kAppendAhead; ++i) {
-      Row<T> &x = r[i];
-      if (x.kind == 3) continue;
-      if (x.kind != 1) {
-        if (WHOLE) {
-          float a[8], b[8];
-          x.raw.unpack(0, a);
-          x.raw.unpack(1, b);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float4 w = *reinterpret_cast<const float4 *>(&cs[x.token][(k * LPR + sub) * 2]);
-            const float2 w0 = make_float2(w.x, w.y), w1 = make_float2(w.z, w.w);
-            const float a0 = a[2 * k], b0 = b[2 * k], a1 = a[2 * k + 1], b1 = b[2 * k + 1];
-            a[2 * k] = turned_first(a0, b0, w0);
-            b[2 * k] = turned_second(a0, b0, w0);
-            a[2 * k + 1] = turned_first(a1, b1, w1);
-            b[2 * k + 1] = turned_second(a1, b1, w1);
-          }
-          x.raw.pack(0, a);
-          x.raw.pack(1, b);
-        } else {
-          turn_any<T, D>(p, x.raw, x.src, sub, group, cs[x.token]);
-        }
-      }
-      if (x.kind == 2) {
-        char *row = p.q_out + (t0 + x.token) * p.o_ts + x.head * p.o_hs + sub * PIECE;
-        float f[8];
-        x.raw.unpack(0, f);
-        store8(row, f, T());
-        x.raw.unpack(1, f);
-        store8(row + D / 2 * (int)sizeof(T), f, T());
-      } else {
-        int block, offset;
-        const bool live = p.map.split(x.slot, block, offset);
-        const Pieces<D, FMT> to(p.cache, p.layer, x.kind, x.head, sub);
-        put_row<T, D, FMT>(x.raw, to, block * p.cache.block_stride, offset, sub, group, live);
-      }
+  while (token < nt) {
+    const int row = r0 + at, kind = row < p.n_kv ? 0 : row < 2 * p.n_kv ? 1 : 2;      // K, V, Q
+    if (kind != 1) turn<T, D, MODE>(x, src, first, apart, sub, p.rotary, group, cs[token]);
+    if (kind == 2) {
+      char *to = p.q_out + (long long)(t0 + token) * p.o_ts + (row - 2 * p.n_kv) * p.o_hs + first * (int)sizeof(T);
+      float f[8];
+      x.unpack(0, f);
+      store8(to, f, T());
+      x.unpack(1, f);
+      store8(to + apart * (int)sizeof(T), f, T());
+    } else {
+      const long long block = block_s[token];
+      const Pieces<D, FMT> to(p.layout, kind, row - kind * p.n_kv, first);
+      put_row<T, D, FMT>(x, to, p.layout.slot_stride, apart, block, offset_s[token], sub, group, block >= 0);
     }
+    at += ROWS;
+    settle();
+    if (token < nt) load();
   }
 }
 
@@ -206,10 +196,12 @@ int launch_append(AppendParams &p, cudaStream_t st) {
       p.tokens_per_cta *= 2;
   const dim3 grid((p.n_tokens + p.tokens_per_cta - 1) / p.tokens_per_cta, (rows + p.rows_per_cta - 1) / p.rows_per_cta);
   if (grid.y > 65535) return KV_ERR_SHAPE;
-  if (p.rotary == D && !p.interleaved)
-    cache_append_kernel<T, D, FMT, true><<<grid, kAppendThreads, 0, st>>>(p);
+  if (p.interleaved)
+    cache_append_kernel<T, D, FMT, kInterleaved><<<grid, kAppendThreads, 0, st>>>(p);
+  else if (p.rotary % 32 == 0 && (D - p.rotary) % 32 == 0)
+    cache_append_kernel<T, D, FMT, kHalves><<<grid, kAppendThreads, 0, st>>>(p);
   else
-    cache_append_kernel<T, D, FMT, false><<<grid, kAppendThreads, 0, st>>>(p);
+    cache_append_kernel<T, D, FMT, kAnyHalves><<<grid, kAppendThreads, 0, st>>>(p);
   KV_COUNT_LAUNCH();
   KV_CUDA(cudaGetLastError());
   return KV_OK;
@@ -255,9 +247,8 @@ int32_t kv_op_cache_append(const kv_rope *rope, const kv_cache_desc *cache, int3
     if (q_dev == q_out_dev && (q_token_stride != q_out_token_stride || q_head_stride != q_out_head_stride)) return KV_ERR_ARG;
   }
   AppendParams p;
-  p.cache = make_view(cache);
+  p.layout = row_layout(make_view(cache), layer);
   p.map = slot_map(cache);
-  p.layer = layer;
   p.n_tokens = n_tokens;
   p.n_q = n_q_heads;
   p.n_kv = cache->n_kv_heads;

@@ -20,28 +20,47 @@ constexpr int kMaxExpE2m1 = 116;      // 6 * 448 * 2^e stays in fp32's range
 constexpr int kBf16 = 2, kE4m3 = 1, kE2m1 = 0;
 inline int format_of(int elem_bytes) { return elem_bytes == KV_ELEM_E2M1 ? kE2m1 : elem_bytes; }
 
-// Where a lane's pieces of a row lie: of slot 0 of block 0, for lane `sub` of head `head` of K or V.
+// Where the rows of a layer lie: slot 0 of block 0 of head 0 of K, and the ways from there (bytes).
+struct RowLayout {
+  char *values;
+  long long kv_stride, block_stride, head_stride, slot_stride;
+  long long groups, scale, scale_stride;          // from a head's values to its scales of 16 dims; from K's to the scale bytes of head 0, a head
+};
+inline RowLayout row_layout(const CacheView &c, int layer) {
+  RowLayout r;
+  r.values = c.base + layer * c.layer_stride;
+  r.kv_stride = c.kv_stride;
+  r.block_stride = c.block_stride;
+  const long long d = c.head_dim;
+  if (c.elem_bytes == KV_ELEM_E2M1) {
+    r.head_stride = r.scale_stride = c.record_bytes();
+    r.slot_stride = d / 2;
+    r.groups = c.block_size * (d / 2);
+    r.scale = c.block_size * (d / 2 + d / 16);
+  } else {
+    r.head_stride = d * c.elem_bytes;
+    r.slot_stride = c.n_kv_heads * d * c.elem_bytes;
+    r.groups = 0;
+    r.scale = c.value_bytes();
+    r.scale_stride = c.block_size;
+  }
+  return r;
+}
+// A lane's pieces of the rows of head `head` of K or V: the first begins at dim `first`, a multiple of 8, the other `apart` dims further on, a
+// multiple of 16.
 template <int D, int FMT>
 struct Pieces {
-  static constexpr int apart = FMT == kBf16 ? D : FMT == kE4m3 ? D / 2 : D / 4;      // bytes between the two
   char *values, *groups, *scale;
-  long long slot_bytes;
-  __device__ __forceinline__ Pieces(const CacheView &c, int layer, int kv, int head, int sub) {
-    char *page = c.page(layer, kv, 0);
-    if (FMT == kE2m1) {
-      char *record = page + head * c.record_bytes();
-      slot_bytes = D / 2;
-      values = record + sub * 4;
-      groups = record + (long long)c.block_size * (D / 2) + (sub >> 1);
-      scale = record + (long long)c.block_size * (D / 2 + D / 16);
-    } else {
-      slot_bytes = (long long)c.n_kv_heads * D * FMT;
-      values = page + head * D * FMT + sub * 8 * FMT;
-      groups = nullptr;
-      scale = page + c.value_bytes() + head * c.block_size;
-    }
+  __device__ __forceinline__ Pieces(const RowLayout &r, int kv, int head, int first) {
+    char *page = r.values + kv * r.kv_stride, *row = page + head * r.head_stride;
+    values = row + (FMT == kE2m1 ? first / 2 : first * FMT);
+    groups = row + r.groups + first / 16;
+    scale = page + r.scale + head * r.scale_stride;
   }
 };
+// bytes of so many dims of a row's values
+template <int FMT>
+__device__ __forceinline__ int value_bytes_of(int dims) { return FMT == kE2m1 ? dims / 2 : dims * FMT; }
 
 // Two pieces of 8 values of a row: the raw registers are loaded first and unpacked later.
 template <typename T>
@@ -136,12 +155,14 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
   return r;
 }
 
-// eight e2m1 codes (the first in the low nibble) -> four pairs of fp16, exact.  w comes of 32-bit loads: fed straight from an 8- or 16-bit
-// load, the unpacking into bytes came out wrong (nvcc 12.9.86).
+// eight e2m1 codes (the first in the low nibble) -> four pairs of fp16, exact.  One byte to a statement: each is then an operand of its
+// own conversion, while four out of one unpacking cost two instructions more (3.0 against 2.0 clocks of an SM).  w comes of 32-bit
+// loads: fed straight from an 8- or 16-bit load, the unpacking into bytes came out wrong (nvcc 12.9.86).
 __device__ __forceinline__ void halves_of_e2m1(uint32_t w, uint32_t (&h)[4]) {
-  asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
-      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+  asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\t}" : "=r"(h[0]) : "r"(w));
+  asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, b;\n\t}" : "=r"(h[1]) : "r"(w));
+  asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, c;\n\t}" : "=r"(h[2]) : "r"(w));
+  asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, d;\n\t}" : "=r"(h[3]) : "r"(w));
 }
 __device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
   uint32_t r;
@@ -176,13 +197,20 @@ __device__ __forceinline__ uint32_t e2m1_exact(float y, float s) {
   return (upper ? 4u : 0u) + (mid ? 2u : 0u) + (y >= b ? 1u : 0u);
 }
 
-// A lane's two pieces of a row into e2m1 codes and the scale codes of their groups; `bits`: the row's largest |x| (fp32 pattern),
-// `fine`: no infinity or NaN in the row.  All lanes of the row call it.  Returns the row's scale byte.
-// T = bf16: x has 8 bits and a border 7, so one that is not on a border is 2^-8 away from it, and the quotient times 1 + 2^-12
-// rounds as the comparisons decide, halves up.  fp32 values are compared.
-template <typename T, int LANES>
-__device__ __forceinline__ uint32_t e2m1_row(const float (&f)[2][8], uint32_t bits, bool fine, unsigned group, uint32_t (&codes)[2],
-                                             uint32_t (&scales)[2]) {
+// The scale of a group whose largest |x| is `top` in units of the row's 2^e: the least positive e4m3 number s with 6 s >= top.
+__device__ __forceinline__ uint32_t group_scale(float top, float &s) {
+  uint32_t code = e4m3x2(top * (1.f / 6.f), 0.f) & 255u;
+  if (6.f * floats_of_half2(half2_of_e4m3x2(code)).x < top) ++code;
+  code = min(max(code, 1u), 0x7eu);
+  s = floats_of_half2(half2_of_e4m3x2(code)).x;
+  return code;
+}
+
+// A lane's two pieces of a row into e2m1 codes and the scale codes of their groups, by the definition; the lanes of a group are
+// neighbours.  Infinities and NaN are left out of the maxima and make their group NaN.  All lanes of the row call it.  Returns the row's
+// scale byte.
+template <int LANES>
+__device__ __forceinline__ uint32_t e2m1_row(const float (&f)[2][8], unsigned group, uint32_t (&codes)[2], uint32_t (&scales)[2]) {
   float most[2] = {0.f, 0.f};
   bool whole[2] = {true, true};
 #pragma unroll
@@ -190,89 +218,139 @@ __device__ __forceinline__ uint32_t e2m1_row(const float (&f)[2][8], uint32_t bi
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float a = fabsf(f[h][j]);
-      if (fine) {
-        most[h] = fmaxf(most[h], a);
-      } else {
-        const bool ok = a <= FLT_MAX;
-        whole[h] &= ok;
-        most[h] = fmaxf(most[h], ok ? a : 0.f);
-      }
+      whole[h] &= a <= FLT_MAX;
+      most[h] = fmaxf(most[h], a <= FLT_MAX ? a : 0.f);
     }
-  if (!fine) {
-    float top = fmaxf(most[0], most[1]);
+  float top = fmaxf(most[0], most[1]);
 #pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(group, top, o));
-    bits = __float_as_uint(top);
-  }
+  for (int o = LANES / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(group, top, o));
   // |x| = m * 2^x with 1 <= m < 2; 6 * 448 = 1.3125 * 2^11
+  const uint32_t bits = __float_as_uint(top);
   int e = (int)(bits >> 23) - 127 - 11 + ((bits & 0x7fffffu) > 0x280000u);
   e = min(max(e, kMinExp), kMaxExpE2m1);
   const float down = __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     most[h] = fmaxf(most[h], __shfl_xor_sync(group, most[h], 1));
-    if (!fine) {      // the row's lanes all come here
-      const uint32_t other = __shfl_xor_sync(group, whole[h] ? 1u : 0u, 1);
-      whole[h] &= other != 0;
-    }
-    const float top = most[h] * down;
-    uint32_t code = e4m3x2(top * (1.f / 6.f), 0.f) & 255u;
-    float s = floats_of_half2(half2_of_e4m3x2(code)).x;
-    if (6.f * s < top) ++code;
-    code = min(max(code, 1u), 0x7eu);
-    s = floats_of_half2(half2_of_e4m3x2(code)).x;
-    if (sizeof(T) == 2) {
-      const float up = (1.f + 0x1p-12f) / s * down;
-      float y[8];
+    const uint32_t other = __shfl_xor_sync(group, whole[h] ? 1u : 0u, 1);
+    whole[h] &= other != 0;
+    float s;
+    scales[h] = group_scale(most[h] * down, s);
+    codes[h] = 0;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = f[h][j] * up;
-      codes[h] = e2m1x8(y);
-    } else {
-      codes[h] = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        codes[h] |= (e2m1_exact(fabsf(f[h][j]) * down, s) | (__float_as_uint(f[h][j]) >> 31) << 3) << (4 * j);
-    }
+    for (int j = 0; j < 8; ++j)
+      codes[h] |= (e2m1_exact(fabsf(f[h][j]) * down, s) | (__float_as_uint(f[h][j]) >> 31) << 3) << (4 * j);
     if (!whole[h]) {
       codes[h] = 0;
-      code = 0x7fu;      // NaN
+      scales[h] = 0x7fu;      // NaN
     }
-    scales[h] = code;
   }
   return (uint32_t)(e + 127);
 }
+// The same for finite bf16 rows.  x has 8 bits and a border 7, so one that is not on a border is 2^-8 away from it, and the quotient
+// times 1 + 2^-12 rounds as the comparisons decide, halves up.  `tops`: the largest |x| of the two groups (bf16 patterns), top: of the row.
+__device__ __forceinline__ uint32_t e2m1_row(const Raw<bf16> &raw, uint32_t tops, uint32_t top, uint32_t (&codes)[2], uint32_t (&scales)[2]) {
+  int e = (int)(top >> 7) - 127 - 11 + ((top & 0x7fu) > 0x28u);
+  e = min(max(e, kMinExp), kMaxExpE2m1);
+  const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float f[8], s;
+    raw.unpack(h, f);
+    scales[h] = group_scale(__uint_as_float(h ? tops & 0xffff0000u : tops << 16) * down, s);
+    const float up = __fdividef(1.f + 0x1p-12f, s) * down;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] *= up;
+    codes[h] = e2m1x8(f);
+  }
+  return (uint32_t)(e + 127);
+}
+// The largest |x| of the two groups that a lane's pieces belong to (bf16 patterns), and of the row.
+template <int LANES>
+__device__ __forceinline__ void group_tops(const Raw<bf16> &raw, unsigned group, uint32_t &tops, uint32_t &top) {
+  const uint32_t s = 0x7fff7fffu;
+  const uint32_t x = Raw<bf16>::max2(Raw<bf16>::max2(raw.a[0].x & s, raw.a[0].y & s), Raw<bf16>::max2(raw.a[0].z & s, raw.a[0].w & s));
+  const uint32_t y = Raw<bf16>::max2(Raw<bf16>::max2(raw.a[1].x & s, raw.a[1].y & s), Raw<bf16>::max2(raw.a[1].z & s, raw.a[1].w & s));
+  tops = Raw<bf16>::max2(__byte_perm(x, y, 0x5410), __byte_perm(x, y, 0x7632));
+  tops = Raw<bf16>::max2(tops, __shfl_xor_sync(group, tops, 1));
+  uint32_t m = tops;
+#pragma unroll
+  for (int o = LANES / 2; o > 1; o >>= 1) m = Raw<bf16>::max2(m, __shfl_xor_sync(group, m, o));
+  top = max(m & 0xffffu, m >> 16);
+}
+template <int LANES>
+__device__ __forceinline__ void group_tops(const Raw<float> &, unsigned, uint32_t &tops, uint32_t &top) { tops = top = 0xffffu; }
+__device__ __forceinline__ uint32_t e2m1_row(const Raw<float> &, uint32_t, uint32_t, uint32_t (&)[2], uint32_t (&)[2]) { return 0; }
 
-// One row, converted and stored by its lanes.  `to`: the pieces of slot 0 of block 0; at = block * block_stride, offset in the block.
+// Takes infinities and NaN out of a lane's pieces (zeros in their place); whole[h]: there was none among the 16 dims of piece h.
+__device__ __forceinline__ void take_out(Raw<bf16> &raw, unsigned group, bool (&whole)[2]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t w[4] = {raw.a[h].x, raw.a[h].y, raw.a[h].z, raw.a[h].w}, bad = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t lo = (w[i] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (w[i] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+      w[i] &= ~(lo | hi);
+      bad |= lo | hi;
+    }
+    raw.a[h] = make_uint4(w[0], w[1], w[2], w[3]);
+    whole[h] = (bad | __shfl_xor_sync(group, bad, 1)) == 0;
+  }
+}
+__device__ __forceinline__ void take_out(Raw<float> &, unsigned, bool (&)[2]) {}
+
+// One row, converted and stored by its lanes.  `to`: the lane's pieces in slot 0 of block 0; at = block * block_stride, offset in the block.
 template <typename T, int D, int FMT>
-__device__ __forceinline__ void put_row(const Raw<T> &raw, const Pieces<D, FMT> &to, long long at, int offset, int sub, unsigned group,
-                                        bool live) {
+__device__ __forceinline__ void put_row(const Raw<T> &raw, const Pieces<D, FMT> &to, long long slot_stride, int apart, long long at,
+                                        int offset, int sub, unsigned group, bool live) {
   constexpr int LANES = D / 16;
-  char *values = to.values + at + offset * to.slot_bytes;
+  char *values = to.values + at + offset * slot_stride, *second = values + value_bytes_of<FMT>(apart);
+  if (FMT == kE2m1) {
+    uint32_t codes[2], scales[2], tops, top, byte;
+    group_tops<LANES>(raw, group, tops, top);
+    if (sizeof(T) == 2) {
+      Raw<T> fine = raw;
+      bool whole[2] = {true, true};
+      if (top >= 0x7f80u) {      // the row's lanes all come here
+        take_out(fine, group, whole);
+        group_tops<LANES>(fine, group, tops, top);
+      }
+      byte = e2m1_row(fine, tops, top, codes, scales);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (!whole[h]) {
+          codes[h] = 0;
+          scales[h] = 0x7fu;      // NaN
+        }
+    } else {
+      float f[2][8];
+      raw.unpack(0, f[0]);
+      raw.unpack(1, f[1]);
+      byte = e2m1_row<LANES>(f, group, codes, scales);
+    }
+    if (live) {
+      *reinterpret_cast<uint32_t *>(values) = codes[0];
+      *reinterpret_cast<uint32_t *>(second) = codes[1];
+      if ((sub & 1) == 0) {
+        char *groups = to.groups + at + offset * (D / 16);
+        groups[0] = (char)scales[0];
+        groups[apart / 16] = (char)scales[1];
+      }
+      if (sub == 0) to.scale[at + offset] = (char)byte;
+    }
+    return;
+  }
   float f[2][8];
   raw.unpack(0, f[0]);
   raw.unpack(1, f[1]);
   if (FMT == kBf16) {
     if (live) {
       *reinterpret_cast<uint4 *>(values) = pack_bf16(f[0]);
-      *reinterpret_cast<uint4 *>(values + Pieces<D, FMT>::apart) = pack_bf16(f[1]);
+      *reinterpret_cast<uint4 *>(second) = pack_bf16(f[1]);
     }
     return;
   }
   uint32_t bits = raw.template top<LANES>(group);
-  if (FMT == kE2m1) {
-    uint32_t codes[2], scales[2];
-    const uint32_t byte = e2m1_row<T, LANES>(f, bits, bits <= 0x7f7fffffu, group, codes, scales);
-    if (live) {
-      *reinterpret_cast<uint32_t *>(values) = codes[0];
-      *reinterpret_cast<uint32_t *>(values + Pieces<D, FMT>::apart) = codes[1];
-      if ((sub & 1) == 0) {
-        to.groups[at + offset * (D / 16)] = (char)scales[0];
-        to.groups[at + offset * (D / 16) + D / 32] = (char)scales[1];
-      }
-      if (sub == 0) to.scale[at + offset] = (char)byte;
-    }
-    return;
-  }
   if (bits > 0x7f7fffffu) {                                 // infinities and NaN do not set the scale and become NaN
     float most = 0.f;
 #pragma unroll
@@ -298,7 +376,7 @@ __device__ __forceinline__ void put_row(const Raw<T> &raw, const Pieces<D, FMT> 
   }
   if (live) {
     *reinterpret_cast<uint2 *>(values) = c[0];
-    *reinterpret_cast<uint2 *>(values + Pieces<D, FMT>::apart) = c[1];
+    *reinterpret_cast<uint2 *>(second) = c[1];
     if (sub == 0) to.scale[at + offset] = (char)(e + 127);
   }
 }

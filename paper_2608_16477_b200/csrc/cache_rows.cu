@@ -24,9 +24,9 @@ constexpr int kRowThreads = 256;
 constexpr int kMaxTokens = 1 << 30;   // tokens are counted in 32 bits, a CTA's ahead
 
 struct RowsParams {
-  CacheView cache;
+  RowLayout layout;
   SlotMap map;
-  int layer;
+  int n_kv_heads;
   int n_tokens, heads;                            // heads of K, and of V, that a CTA takes
   const long long *slots;
   char *k, *v;                                    // rows
@@ -49,7 +49,7 @@ struct Place {
     kv = line >= p.heads;
     head = blockIdx.y * p.heads + line - kv * p.heads;
     sub = in % LPR;
-    idle = at >= tokens || head >= p.cache.n_kv_heads;
+    idle = at >= tokens || head >= p.n_kv_heads;
     step = tokens;
     first = blockIdx.x * tokens * u + at;
     group = (LPR == 32 ? 0xffffffffu : ((1u << LPR) - 1u)) << (threadIdx.x & 31 & ~(LPR - 1));
@@ -62,7 +62,7 @@ template <typename T, int D, int FMT, int U>      // U: tokens of a thread at a 
 __global__ void __launch_bounds__(kRowThreads) cache_write_kernel(const __grid_constant__ RowsParams p) {
   const Place<D> me(p, U, 8 * (int)sizeof(T));
   if (me.idle) return;                                        // whole rows at a time: the shuffles are the row's own
-  const Pieces<D, FMT> to(p.cache, p.layer, me.kv, me.head, me.sub);
+  const Pieces<D, FMT> to(p.layout, me.kv, me.head, me.sub * 8);
   for (int t0 = me.first; t0 < p.n_tokens; t0 += gridDim.x * me.step * U) {
     Raw<T> raw[U];
     long long slot[U];
@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_write_kernel(const __grid_c
     for (int i = 0; i < U; ++i) {
       int block, offset;
       const bool live = p.map.split(slot[i], block, offset);
-      put_row<T, D, FMT>(raw[i], to, block * p.cache.block_stride, offset, me.sub, me.group, live);
+      put_row<T, D, FMT>(raw[i], to, p.layout.slot_stride, D / 2, block * p.layout.block_stride, offset, me.sub, me.group, live);
     }
   }
 }
@@ -86,8 +86,8 @@ template <typename T, int D, int FMT, int U>
 __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_constant__ RowsParams p) {
   const Place<D> me(p, U, 8 * (int)sizeof(T));
   if (me.idle) return;
-  const Pieces<D, FMT> from(p.cache, p.layer, me.kv, me.head, me.sub);
-  constexpr int APART = Pieces<D, FMT>::apart;
+  const Pieces<D, FMT> from(p.layout, me.kv, me.head, me.sub * 8);
+  constexpr int APART = FMT == kE2m1 ? D / 4 : D / 2 * FMT;
   uint4 raw[U][FMT == kBf16 ? 2 : 1];                         // e4m3, e2m1: both pieces in one
   uint32_t scale[U];
   long long slot[U];
@@ -101,8 +101,8 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
   for (int i = 0; i < U; ++i) {
     int block, offset;
     live[i] = p.map.split(slot[i], block, offset);            // block 0, offset 0 if not: read, but not written anywhere
-    const long long at = block * p.cache.block_stride;
-    const char *values = from.values + at + offset * from.slot_bytes;
+    const long long at = block * p.layout.block_stride;
+    const char *values = from.values + at + offset * p.layout.slot_stride;
     if (FMT == kE4m3) {
       const uint2 a = *reinterpret_cast<const uint2 *>(values), b = *reinterpret_cast<const uint2 *>(values + APART);
       raw[i][0] = make_uint4(a.x, a.y, b.x, b.y);
@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
 template <typename T, int D, int FMT, int U>
 int launch_rows_u(const RowsParams &p, bool write, int sms, cudaStream_t st) {
   const int tokens = kRowThreads / (2 * p.heads * Place<D>::LPR) * U;
-  dim3 grid((p.n_tokens + tokens - 1) / tokens, (p.cache.n_kv_heads + p.heads - 1) / p.heads);
+  dim3 grid((p.n_tokens + tokens - 1) / tokens, (p.n_kv_heads + p.heads - 1) / p.heads);
   if (grid.y > 65535) return KV_ERR_SHAPE;
   // Writing stays in place with four CTAs per SM (16,384 tokens of 8 heads of 128: 18.4 us against 20.7 us with a CTA for
   // every two tokens); reading, whose loads wait for the slots, is better off with new CTAs (18.8 us against 19.2 us).
@@ -183,8 +183,8 @@ int launch_rows(RowsParams &p, bool write, cudaStream_t st) {
   const int device = current_device();
   if (device < 0) return KV_ERR_CUDA;
   const int most = kRowThreads / (2 * Place<D>::LPR);          // heads that fit a CTA with their K and V
-  p.heads = p.cache.n_kv_heads < most ? p.cache.n_kv_heads : most;
-  const long long threads = (long long)p.n_tokens * 2 * p.cache.n_kv_heads * Place<D>::LPR;
+  p.heads = p.n_kv_heads < most ? p.n_kv_heads : most;
+  const long long threads = (long long)p.n_tokens * 2 * p.n_kv_heads * Place<D>::LPR;
   const int sms = sm_count(device);
   return threads >= 16ll * kRowThreads * sms ? launch_rows_u<T, D, FMT, 2>(p, write, sms, st)
                                              : launch_rows_u<T, D, FMT, 1>(p, write, sms, st);
@@ -217,9 +217,9 @@ int rows_call(const kv_cache_desc *cache, int layer, const void *k, int64_t k_ts
       return KV_ERR_ARG;
   }
   RowsParams p;
-  p.cache = make_view(cache);
+  p.layout = row_layout(make_view(cache), layer);
   p.map = slot_map(cache);
-  p.layer = layer;
+  p.n_kv_heads = cache->n_kv_heads;
   p.n_tokens = n_tokens;
   p.slots = reinterpret_cast<const long long *>(slots);
   p.k = (char *)const_cast<void *>(k);

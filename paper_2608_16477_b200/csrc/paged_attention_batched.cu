@@ -57,15 +57,21 @@ constexpr int kQueryBits = 12;       // ... and fp16 queries to less than 2^12
 
 // A stage is what a warp loads and consumes at a time: 32 keys, so that the softmax's and the loads' bookkeeping is paid
 // once for four 8-key fragments; 16 where 32 would leave the ring too few stages (bf16 rows of 128: 8 KB a stage either way).
-// ELEM, the page format: 2 bf16, 1 e4m3, 0 e2m1.
-template <int D, int ELEM>
+// ELEM, the page format: 2 bf16, 1 e4m3, 0 e2m1, kUnits e2m1 in pages whose size is a multiple of 16: then 16 keys of a KV head and all
+// that belongs to them lie in three pieces of the head's record (one, in pages of 16), which are copied as they are.
+constexpr int kUnits = -1;
+// CTAs of an SM: e2m1 pages and bf16 queries three, whose registers and rings fit (many instructions for few bytes: the more warps
+// the better), two otherwise.
+constexpr int ba_ctas(bool e2m1, bool bf16_queries) { return e2m1 && bf16_queries ? 3 : 2; }
+template <int D, int ELEM, typename T>
 struct BaCfg {
-  static constexpr int row = ELEM == 0 ? D / 2 : D * ELEM;               // bytes of a K or V row's values
+  static constexpr int row = ELEM <= 0 ? D / 2 : D * ELEM;               // bytes of a K or V row's values
   static constexpr int keys = row > 128 ? 16 : 32;
   static constexpr int codes = keys * row;
-  static constexpr int tile = codes + (ELEM == 0 ? keys * (D / 16) : 0); // e2m1: then the scales of 16 dims
-  static constexpr int stage = 2 * tile + (ELEM == 2 ? 0 : 256);         // K, V, a word with the scale byte of each row
-  static constexpr int stages = stage > 6144 ? 3 : 5;
+  static constexpr int unit = 16 * (D / 2 + D / 16 + 1);                 // 16 keys of an e2m1 record: codes, scales of 16 dims, scale bytes
+  static constexpr int tile = ELEM == kUnits ? keys / 16 * unit : ELEM == 0 ? codes + keys * (D / 16) : codes;
+  static constexpr int stage = 2 * tile + (ELEM == 2 || ELEM == kUnits ? 0 : 256);      // K, V, a word with the scale byte of each row
+  static constexpr int stages = stage > 6144 || (ba_ctas(ELEM <= 0, sizeof(T) == 2) == 3 && D == 128) ? 3 : 5;
   static constexpr int ring = stages * stage;
   static constexpr int merge = (kBaWarps - 1) * kBaHeads * D * 4;        // outputs of warps 1-3 when they share a head
   static constexpr int smem(int kw) { return kBaWarps * ring + (kw > 1 ? merge : 0); }
@@ -102,6 +108,10 @@ __device__ __forceinline__ void cp16(uint32_t dst, const char *src, bool valid) 
   else
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
 }
+template <int ELEM>
+__device__ __forceinline__ void cp16(uint32_t dst, const char *src) {
+  asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cp4(uint32_t dst, const char *src, bool valid) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(valid ? 4 : 0) : "memory");
 }
@@ -113,14 +123,14 @@ template <int N>
 __device__ __forceinline__ void cp_wait_group() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
       "{%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
       "{%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -181,6 +191,55 @@ __device__ __forceinline__ void split_f16(float x, float y, uint32_t (&parts)[N]
         : "=f"(fx), "=f"(fy) : "r"(parts[i]));
     x -= fx;
     y -= fy;
+  }
+}
+// Two fp32 operations in one instruction: the scores of a lane's two heads.
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {      // NaN only if all are
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+template <int N>
+__device__ __forceinline__ float2 max_of(const float2 (&t)[N]) {
+  if (N == 2) return make_float2(fmaxf(t[0].x, t[1].x), fmaxf(t[0].y, t[1].y));
+  return make_float2(fmaxf(max3(t[0].x, t[1].x, t[2 % N].x), t[3 % N].x), fmaxf(max3(t[0].y, t[1].y, t[2 % N].y), t[3 % N].y));
+}
+// c += A B for the parts of B.  The matrix instruction truncates as it accumulates, some 2^-24 of the accumulator each time and always
+// towards zero: over the tiles of a long context that adds up to more than fp32 results should lose (1,000 keys of 16 requests: error
+// against 64 bits 1.3e-6, of the results' norm).  So fp32 calls start from zero and add what comes out, rounded.
+template <bool APART, bool BF16, int N, int M>
+__device__ __forceinline__ void add_product(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[N][M], int at) {
+  float own[4] = {};
+  float (&to)[4] = APART ? own : c;
+#pragma unroll
+  for (int h = 0; h < N; ++h) {
+    if (BF16)
+      mma_bf16(to, a, b[h][at], b[h][at + 1]);
+    else
+      mma_f16(to, a, b[h][at], b[h][at + 1]);
+  }
+  if (APART) {
+    const float2 x = add2(make_float2(c[0], c[1]), make_float2(own[0], own[1])), y = add2(make_float2(c[2], c[3]), make_float2(own[2], own[3]));
+    c[0] = x.x; c[1] = x.y; c[2] = y.x; c[3] = y.y;
   }
 }
 // 8x8 16-bit values, two of a row to a lane -> the same of the transposed block
@@ -265,7 +324,7 @@ __device__ __forceinline__ float quad_max(float v) {
 // loads of eight neighbouring lanes fall into different banks.
 template <int D, int ELEM>
 __device__ __forceinline__ uint32_t chunk_at(int r, int c) {
-  if (ELEM == 0) return (uint32_t)(r * (D / 2) + (D == 128 ? c ^ (r & 2) : c) * 16);
+  if (ELEM <= 0) return (uint32_t)(r * (D / 2) + (ELEM == 0 && D == 128 ? c ^ (r & 2) : c) * 16);
   if (ELEM == 1 && D == 64) return (uint32_t)((r >> 1) * 128 + ((((r & 1) * 4 + c) ^ (r & 6)) * 16));
   if (ELEM == 1) return (uint32_t)(r * 128 + ((c ^ (r & 7)) * 16));
   return (uint32_t)(r * (D * 2) + ((c & ~7) | ((c ^ r) & 7)) * 16);
@@ -274,7 +333,7 @@ __device__ __forceinline__ uint32_t chunk_at(int r, int c) {
 // The key (of eight) that row x of a fragment holds.  e2m1 rows are 64 or 32 bytes, so that four of them, in natural order, would
 // share banks; any order will do, as long as K's rows and the weights agree.
 template <int ELEM>
-__device__ __forceinline__ int key_of(int x) { return ELEM == 0 ? x ^ (x >> 2) : x; }
+__device__ __forceinline__ int key_of(int x) { return ELEM <= 0 ? x ^ (x >> 2) : x; }
 
 __device__ __forceinline__ int clamped_len(const BaParams &p, int r) {
   return min(max(__ldg(p.lens + r), 0), p.max_ctx);
@@ -339,13 +398,13 @@ struct Cursor {
 };
 
 template <int D, int ELEM, typename T, int KW>      // KW: warps that share a KV head
-__global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(const __grid_constant__ BaParams p) {
-  typedef BaCfg<D, ELEM> C;
+__global__ void __launch_bounds__(kBaThreads, ba_ctas(ELEM <= 0, sizeof(T) == 2)) paged_attention_batched_kernel(const __grid_constant__ BaParams p) {
+  typedef BaCfg<D, ELEM, T> C;
   constexpr int KS = D / 16;                 // k-steps of S^T = K Q^T
   constexpr int NT = D / 8;                  // dims of a lane's V fragments (ELEM 1, 0)
   constexpr int MO = D / 16;                 // 16-dim tiles of O^T
   constexpr int QP = sizeof(T) == 2 ? 1 : (ELEM == 2 ? 3 : 2);          // parts of a query
-  constexpr int PP = sizeof(T) == 4 && ELEM == 2 ? 3 : 2;                // parts of a weight
+  constexpr int PP = sizeof(T) == 2 && ELEM <= 0 ? 1 : sizeof(T) == 4 && ELEM == 2 ? 3 : 2;      // parts of a weight
   constexpr int CH = C::row / 16;            // 16-byte chunks of a row
   constexpr int RPI = 32 / CH;               // rows per copy instruction
   constexpr int KEYS = C::keys;
@@ -424,7 +483,38 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
   long long to_look = todo;
   int blks[kLookAhead] = {}, offs[kLookAhead] = {};   // of the next stages to be copied: block and slot of the lane's row (kNoRow: none)
   const int my_row = lane % KEYS;
+  // e2m1 units: the lanes' unit begins at `at` (lanes 0 to 15 the first of the stage, the others the second)
+  int at = (prod.tile * KW + kg) * KEYS + (lane & 16);
+  const int *table = tables + prod.r * p.table_stride;
+  auto look_up_unit = [&](int &blk, int &off) {
+    off = kNoRow;
+    if (to_look > 0) {
+      if (at < prod.n) {
+        int b;
+        if (p.block_shift >= 0) {
+          b = at >> p.block_shift;
+          off = at & (p.cache.block_size - 1);
+        } else {
+          b = at / p.cache.block_size;
+          off = at - b * p.cache.block_size;
+        }
+        blk = __ldg(table + b);
+      }
+      --to_look;
+      at += TILE;
+      const int r = prod.r;
+      prod.step(p, TILE);
+      if (prod.r != r) {
+        at = kg * KEYS + (lane & 16);
+        table = tables + prod.r * p.table_stride;
+      }
+    }
+  };
   auto look_up = [&](int &blk, int &off) {
+    if (ELEM == kUnits) {
+      look_up_unit(blk, off);
+      return;
+    }
     const int pos = (prod.tile * KW + kg) * KEYS + my_row;
     blk = -1;
     off = 0;
@@ -441,15 +531,57 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
       off = kNoRow;
     }
   };
-  const long long row_stride = ELEM == 0 ? C::row : (long long)p.cache.n_kv_heads * C::row;
+  const long long row_stride = ELEM <= 0 ? C::row : (long long)p.cache.n_kv_heads * C::row;
   // the lane's chunk of row lane / CH, and the scale bytes, in block 0 of K (e2m1: both in the KV head's record)
-  const char *rec0 = p.cache.page(p.layer, 0, 0) + kvh * (ELEM == 0 ? p.cache.record_bytes() : (long long)C::row);
+  const char *rec0 = p.cache.page(p.layer, 0, 0) + kvh * (ELEM <= 0 ? p.cache.record_bytes() : (long long)C::row);
   const char *base0 = rec0 + (lane / CH) * row_stride + (lane % CH) * 16;
-  const char *scale0 = ELEM == 0 ? rec0 + (long long)p.cache.block_size * (D / 2 + D / 16)
+  const char *scale0 = ELEM <= 0 ? rec0 + (long long)p.cache.block_size * (D / 2 + D / 16)
                                  : p.cache.page(p.layer, 0, 0) + p.cache.value_bytes();
   unsigned poison = 0;                       // bit s: the stage in ring slot s has a row outside the pool
   int put = 0;                               // ring slot to fill next
+  auto advance = [&]() {
+    put = put + 1 == C::stages ? 0 : put + 1;
+#pragma unroll
+    for (int i = 0; i + 1 < kLookAhead; ++i) {
+      blks[i] = blks[i + 1];
+      offs[i] = offs[i + 1];
+    }
+    look_up(blks[kLookAhead - 1], offs[kLookAhead - 1]);
+  };
+  // The unit of lanes 0 to 15 and that of the others, by all lanes: 16 rows of codes, then the piece of scales of 16 dims or of scale bytes that
+  // is the lane's.  What a context leaves of its last unit comes along (and is kept from the results below); a unit behind it does not.
+  constexpr int CODES = 16 * (D / 2) / 512, EXTRA = D / 16 + 1;      // copies of a lane; lanes that have a piece behind the codes
+  const long long extra0 = lane < D / 16 ? (long long)p.cache.block_size * (D / 2) + lane * 16 : (long long)p.cache.block_size * (D / 2 + D / 16);
+  const int extra_step = lane < D / 16 ? D / 16 : 1;
+  auto issue_units = [&]() {
+    const bool is = offs[0] >= 0, inside = is && (unsigned)blks[0] < (unsigned)p.num_blocks;
+    if (__any_sync(0xffffffffu, is != inside)) poison |= 1u << put;
+    const uint32_t dst0 = ring + put * C::stage + lane * 16;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int blk = __shfl_sync(0xffffffffu, inside ? blks[0] : -1, u * 16), off = __shfl_sync(0xffffffffu, offs[0], u * 16);
+      if (blk >= 0) {
+        const char *rec = rec0 + blk * p.cache.block_stride;
+        const char *codes = rec + off * (D / 2) + lane * 16, *extra = rec + extra0 + off * extra_step;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          const uint32_t dst = dst0 + u * C::unit + kv * C::tile;
+#pragma unroll
+          for (int i = 0; i < CODES; ++i) cp16<ELEM>(dst + i * 512, codes + i * 512);
+          if (lane < EXTRA) cp16<ELEM>(dst + CODES * 512, extra);
+          codes += p.cache.kv_stride;
+          extra += p.cache.kv_stride;
+        }
+      }
+    }
+    cp_commit();
+    advance();
+  };
   auto issue = [&]() {
+    if (ELEM == kUnits) {
+      issue_units();
+      return;
+    }
     const bool row_is = offs[0] >= 0;                                            // the lane's row is one of the context
     const int blk = row_is && (unsigned)blks[0] < (unsigned)p.num_blocks ? blks[0] : -1;      // -1: never followed
     const int off = row_is ? offs[0] : 0;
@@ -489,7 +621,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
       }
       if (ELEM != 2) {   // the words that hold the scale bytes of row l of K and of V
         const bool ok = blk >= 0;
-        if (ELEM == 0) {      // ... and its scales of 16 dims
+        if (ELEM <= 0) {      // ... and its scales of 16 dims
           const char *src = rec0 + (ok ? blk * p.cache.block_stride : 0) + (long long)p.cache.block_size * (D / 2) + (ok ? off : 0) * (D / 16);
           const uint32_t dst = k_s + C::codes + lane * (D / 16);
           if (D == 128) {
@@ -500,20 +632,14 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
             cp4(dst + C::tile, src + p.cache.kv_stride, ok);
           }
         }
-        const int at = (ELEM == 0 ? 0 : kvh * p.cache.block_size) + (ok ? off : 0);
+        const int at = (ELEM <= 0 ? 0 : kvh * p.cache.block_size) + (ok ? off : 0);
         const char *src = scale0 + (ok ? blk * p.cache.block_stride : 0) + (at & ~3);
         cp4(k_s + 2 * C::tile + lane * 4, src, ok);
         cp4(k_s + 2 * C::tile + 128 + lane * 4, src + p.cache.kv_stride, ok);
       }
     }
     cp_commit();
-    put = put + 1 == C::stages ? 0 : put + 1;
-#pragma unroll
-    for (int i = 0; i + 1 < kLookAhead; ++i) {
-      blks[i] = blks[i + 1];
-      offs[i] = offs[i + 1];
-    }
-    look_up(blks[kLookAhead - 1], offs[kLookAhead - 1]);
+    advance();
   };
 #pragma unroll
   for (int i = 0; i < kLookAhead; ++i) look_up(blks[i], offs[i]);
@@ -540,7 +666,7 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
     }
     done += steps;
     uint32_t qf[QP][KS][2];
-    float q_scale[2] = {p.scale, p.scale};
+    float2 q_scale = {p.scale, p.scale};
     {
       const float on = g < nh ? 1.f : 0.f;
       if (ELEM == 2) {
@@ -569,9 +695,10 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
         const int e = min(max((int)(__float_as_uint(most) >> 23) - 126, -100), 127);       // most < 2^e
         // NaN times everything where the largest is infinite
         const float up = __uint_as_float(most <= FLT_MAX ? (uint32_t)(127 + kQueryBits - e) << 23 : 0x7fc00000u);
-        const float down = p.scale * __uint_as_float((uint32_t)(127 - kQueryBits + e) << 23);
-        q_scale[0] = __shfl_sync(0xffffffffu, down, cq * 4);
-        q_scale[1] = __shfl_sync(0xffffffffu, down, cq * 4 + 4);
+        // (a scale of zero times the -inf of a key that is not there would be NaN)
+        const float down = fmaxf(p.scale * __uint_as_float((uint32_t)(127 - kQueryBits + e) << 23), FLT_MIN);
+        q_scale.x = __shfl_sync(0xffffffffu, down, cq * 4);
+        q_scale.y = __shfl_sync(0xffffffffu, down, cq * 4 + 4);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
@@ -585,9 +712,9 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
       }
     }
     // per head cq + i: running maxima of t and of t + e_v (ELEM 1; -inf: none yet, then 0 is subtracted), the lane's sum
-    float m[2] = {-INFINITY, -INFINITY}, mw[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-    float m_sub[2] = {0.f, 0.f}, w_sub[2] = {0.f, 0.f};
-    float low = INFINITY;      // ELEM 2: the lowest score
+    float2 m = {-INFINITY, -INFINITY}, mw = m, l = {};
+    float2 m_neg = {}, w_neg = {};      // what is added in the exponents
+    float low = INFINITY;      // ELEM 2: the lowest product
     float oc[MO][4];
 #pragma unroll
     for (int mt = 0; mt < MO; ++mt)
@@ -601,8 +728,30 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
       const uint32_t k_s = ring + get * C::stage, v_s = k_s + C::tile;
       const int key0 = (cons.tile * KW + kg) * KEYS;
       if (key0 < n) {
-        // ---- S^T = K Q^T: the lane ends with keys kg8 + 8 j of heads cq, cq + 1
-        float t[2 * MK][2];
+        // ---- S^T = K Q^T: the lane ends with keys kg8 + 8 j of heads cq, cq + 1.  t * q_scale is the score (log2 units); the product
+        // is only formed in the fma that takes a maximum away from it, so it is not rounded at its own size
+        uint32_t kx[MK][D / 32], ky[MK][D / 32], gx[MK], gy[MK];      // e2m1: codes and group scales of the lane's keys
+        if (ELEM <= 0) {
+#pragma unroll
+          for (int mt = 0; mt < MK; ++mt) {
+            const uint32_t rows = ELEM == kUnits ? k_s + mt * C::unit : k_s + mt * 16 * C::row;
+            const uint32_t rx = (ELEM == kUnits ? rows + 16 * C::row : k_s + C::codes + mt * 16 * (D / 16)) + kg8 * (D / 16), ry = rx + 8 * (D / 16);
+            if (D == 128) {
+              const uint4 x = lds16(rows + chunk_at<D, ELEM>(kg8, c)), y = lds16(rows + chunk_at<D, ELEM>(kg8 + 8, c));
+              kx[mt][0] = x.x; kx[mt][1] = x.y; kx[mt][D / 32 - 2] = x.z; kx[mt][D / 32 - 1] = x.w;
+              ky[mt][0] = y.x; ky[mt][1] = y.y; ky[mt][D / 32 - 2] = y.z; ky[mt][D / 32 - 1] = y.w;
+              gx[mt] = lds2(rx + 2 * c);
+              gy[mt] = lds2(ry + 2 * c);
+            } else {
+              const uint2 x = lds8(rows + kg8 * C::row + c * 8), y = lds8(rows + (kg8 + 8) * C::row + c * 8);
+              kx[mt][0] = x.x; kx[mt][1] = x.y;
+              ky[mt][0] = y.x; ky[mt][1] = y.y;
+              gx[mt] = lds1(rx + c) * 0x101u;
+              gy[mt] = lds1(ry + c) * 0x101u;
+            }
+          }
+        }
+        float2 t[2 * MK];
 #pragma unroll
         for (int mt = 0; mt < MK; ++mt) {
           float sc[2][4] = {};                        // two chains: even and odd k-steps
@@ -615,29 +764,21 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
 #pragma unroll
               for (int h = 0; h < QP; ++h) mma_bf16(sc[ks & 1], a, qf[h][ks][0], qf[h][ks][1]);
             }
-          } else if (ELEM == 0) {
+          } else if (ELEM <= 0) {
             // D / 4 consecutive codes of two keys, a word for two k-steps, and the scales of their groups
-            const uint32_t rx = k_s + C::codes + (mt * 16 + kg8) * (D / 16), ry = rx + 8 * (D / 16);
-            uint32_t xs[D / 32], ys[D / 32], sx[D / 64], sy[D / 64];
+            const uint32_t ex = half2_of_e4m3x2(gx[mt]), ey = half2_of_e4m3x2(gy[mt]);
+            uint32_t sx[D / 64], sy[D / 64];
+            sx[0] = D == 128 ? __byte_perm(ex, 0, 0x1010) : ex;
+            sy[0] = D == 128 ? __byte_perm(ey, 0, 0x1010) : ey;
             if (D == 128) {
-              const uint4 x = lds16(k_s + chunk_at<D, ELEM>(mt * 16 + kg8, c)), y = lds16(k_s + chunk_at<D, ELEM>(mt * 16 + kg8 + 8, c));
-              xs[0] = x.x; xs[1] = x.y; xs[D / 32 - 2] = x.z; xs[D / 32 - 1] = x.w;
-              ys[0] = y.x; ys[1] = y.y; ys[D / 32 - 2] = y.z; ys[D / 32 - 1] = y.w;
-              const uint32_t ex = half2_of_e4m3x2(lds2(rx + 2 * c)), ey = half2_of_e4m3x2(lds2(ry + 2 * c));
-              sx[0] = __byte_perm(ex, 0, 0x1010); sx[D / 64 - 1] = __byte_perm(ex, 0, 0x3232);
-              sy[0] = __byte_perm(ey, 0, 0x1010); sy[D / 64 - 1] = __byte_perm(ey, 0, 0x3232);
-            } else {
-              const uint2 x = lds8(k_s + (mt * 16 + kg8) * C::row + c * 8), y = lds8(k_s + (mt * 16 + kg8 + 8) * C::row + c * 8);
-              xs[0] = x.x; xs[1] = x.y;
-              ys[0] = y.x; ys[1] = y.y;
-              sx[0] = half2_of_e4m3x2(lds1(rx + c) * 0x101u);
-              sy[0] = half2_of_e4m3x2(lds1(ry + c) * 0x101u);
+              sx[D / 64 - 1] = __byte_perm(ex, 0, 0x3232);
+              sy[D / 64 - 1] = __byte_perm(ey, 0, 0x3232);
             }
 #pragma unroll
             for (int w = 0; w < D / 32; ++w) {
               uint32_t vx[4], vy[4];
-              halves_of_e2m1(xs[w], vx);
-              halves_of_e2m1(ys[w], vy);
+              halves_of_e2m1(kx[mt][w], vx);
+              halves_of_e2m1(ky[mt][w], vy);
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 vx[i] = mul_half2(vx[i], sx[w / 2]);
@@ -665,87 +806,124 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
               }
             }
           }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) t[2 * mt + (i >> 1)][i & 1] = (sc[0][i] + sc[1][i]) * q_scale[i & 1];
+          t[2 * mt] = add2(make_float2(sc[0][0], sc[0][1]), make_float2(sc[1][0], sc[1][1]));
+          t[2 * mt + 1] = add2(make_float2(sc[0][2], sc[0][3]), make_float2(sc[1][2], sc[1][3]));
         }
         if (ELEM == 2) {
 #pragma unroll
-          for (int j = 0; j < 2 * MK; ++j) low = fminf(low, fminf(t[j][0], t[j][1]));
+          for (int j = 0; j < 2 * MK; ++j) low = fminf(low, fminf(t[j].x, t[j].y));
         }
         float ev[2 * MK];
-        if (ELEM != 2) {
+        if (ELEM == kUnits) {
+#pragma unroll
+          for (int j = 0; j < 2 * MK; ++j) {
+            const uint32_t at = k_s + (j >> 1) * C::unit + 16 * (D / 2 + D / 16) + (j & 1) * 8 + kg8;
+            const float ek = __uint_as_float(lds1(at) << 23);
+            t[j] = mul2(t[j], make_float2(ek, ek));
+            ev[j] = __uint_as_float(0x4b000000u + lds1(at + C::tile)) - 8388735.f;      // 2^23 + byte, less 2^23 + 127
+          }
+        } else if (ELEM != 2) {
           // lane l has the scale bytes of row l: K's goes to the exponent field of a float, V's to the low bits
           const int pos = min(key0 + my_row, n - 1);
           const int o = p.block_shift >= 0 ? pos & (p.cache.block_size - 1) : pos % p.cache.block_size;
-          const int shift = 8 * (((ELEM == 0 ? 0 : kvh * p.cache.block_size) + o) & 3);
+          const int shift = 8 * (((ELEM <= 0 ? 0 : kvh * p.cache.block_size) + o) & 3);
           const uint32_t ek = (lds4(k_s + 2 * C::tile + lane * 4) >> shift) & 255u;
           const uint32_t both = ek << 23 | ((lds4(k_s + 2 * C::tile + 128 + lane * 4) >> shift) & 255u);
 #pragma unroll
           for (int j = 0; j < 2 * MK; ++j) {
             const uint32_t b = __shfl_sync(0xffffffffu, both, 8 * j + kg8);
-            t[j][0] *= __uint_as_float(b & 0x7f800000u);
-            t[j][1] *= __uint_as_float(b & 0x7f800000u);
+            const float ek = __uint_as_float(b & 0x7f800000u);
+            t[j] = mul2(t[j], make_float2(ek, ek));
             ev[j] = __uint_as_float(0x4b000000u | (b & 255u)) - 8388735.f;      // 2^23 + byte, less 2^23 + 127
           }
         }
         if (key0 + KEYS > n) {
 #pragma unroll
           for (int j = 0; j < 2 * MK; ++j)
-            if (key0 + 8 * j + kg8 >= n) t[j][0] = t[j][1] = -INFINITY;
+            if (key0 + 8 * j + kg8 >= n) t[j] = make_float2(-INFINITY, -INFINITY);
         }
         // ---- running maxima
-        float top[2], wtop[2];
-        bool raise = false;
+        const float2 top = max_of(t);
+        float2 wtop = {};
+        float over = fmaxf(fmaf(top.x, q_scale.x, -m.x), fmaf(top.y, q_scale.y, -m.y));      // NaN where both are -inf: no
+        if (ELEM != 2) {
+          float2 w[2 * MK];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          top[i] = t[0][i];
-          wtop[i] = ELEM != 2 ? t[0][i] + ev[0] : 0.f;
-#pragma unroll
-          for (int j = 1; j < 2 * MK; ++j) {
-            top[i] = fmaxf(top[i], t[j][i]);
-            if (ELEM != 2) wtop[i] = fmaxf(wtop[i], t[j][i] + ev[j]);
-          }
-          raise |= top[i] > m[i] + kLazy<ELEM> || (ELEM != 2 && wtop[i] > mw[i] + kLazy<ELEM>);
+          for (int j = 0; j < 2 * MK; ++j) w[j] = fma2(t[j], q_scale, make_float2(ev[j], ev[j]));
+          wtop = max_of(w);
+          over = max3(over, wtop.x - mw.x, wtop.y - mw.y);
         }
-        if (__any_sync(0xffffffffu, raise)) {
+        if (__any_sync(0xffffffffu, over > kLazy<ELEM>)) {
+          float corr[2];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const float m_new = fmaxf(m[i], column_max(top[i]));
+            float &m_i = i ? m.y : m.x, &w_i = i ? mw.y : mw.x;
+            const float m_new = fmaxf(m_i, column_max(i ? top.y * q_scale.y : top.x * q_scale.x));
             const float sub = m_new == -INFINITY ? 0.f : m_new;
-            l[i] *= ex2(m[i] - sub);
-            float corr = ex2(m[i] - sub);
-            m[i] = m_new;
-            m_sub[i] = sub;
+            corr[i] = ex2(m_i - sub);
+            (i ? l.y : l.x) *= corr[i];
+            m_i = m_new;
+            (i ? m_neg.y : m_neg.x) = -sub;
             if (ELEM != 2) {
-              const float w_new = fmaxf(mw[i], column_max(wtop[i]));
+              const float w_new = fmaxf(w_i, column_max(i ? wtop.y : wtop.x));
               const float wsub = w_new == -INFINITY ? 0.f : w_new;
-              corr = ex2(mw[i] - wsub);
-              mw[i] = w_new;
-              w_sub[i] = wsub - kWeightBits;
+              corr[i] = ex2(w_i - wsub);
+              w_i = w_new;
+              (i ? w_neg.y : w_neg.x) = kWeightBits - wsub;
             }
+          }
 #pragma unroll
-            for (int mt = 0; mt < MO; ++mt) {
-              oc[mt][i] *= corr;
-              oc[mt][2 + i] *= corr;
-            }
+          for (int mt = 0; mt < MO; ++mt) {
+            oc[mt][0] *= corr[0];
+            oc[mt][1] *= corr[1];
+            oc[mt][2] *= corr[0];
+            oc[mt][3] *= corr[1];
           }
         }
         // ---- weights, as B fragments of P^T (head g, two keys to a register)
         uint32_t pf[PP][2 * MK];
 #pragma unroll
         for (int j = 0; j < 2 * MK; ++j) {
-          const float p0 = ex2(t[j][0] - m_sub[0]), p1 = ex2(t[j][1] - m_sub[1]);
-          l[0] += p0;
-          l[1] += p1;
+          const float2 a = fma2(t[j], q_scale, m_neg);
+          const float p0 = ex2(a.x), p1 = ex2(a.y);
+          l = add2(l, make_float2(p0, p1));
           uint32_t parts[PP];
-          if (ELEM == 2)
+          if (ELEM == 2) {
             split_bf16(p0, p1, parts);
-          else
-            split_f16(ex2(t[j][0] + ev[j] - w_sub[0]), ex2(t[j][1] + ev[j] - w_sub[1]), parts);
+          } else {
+            const float2 w = fma2(t[j], q_scale, add2(make_float2(ev[j], ev[j]), w_neg));
+            split_f16(ex2(w.x), ex2(w.y), parts);
+          }
 #pragma unroll
           for (int h = 0; h < PP; ++h) pf[h][j] = transpose8(parts[h]);
         }
-        if ((poison >> get) & 1u) l[0] = l[1] = __uint_as_float(0x7fc00000u);   // a row outside the pool: the request is NaN
+        if (ELEM == kUnits ? poison != 0 && ((poison >> get) & 1u) : (poison >> get) & 1u) l.x = l.y = __uint_as_float(0x7fc00000u);   // a row outside the pool: the request is NaN
+        // the values' codes and scales, on their way through the softmax
+        uint32_t vc[MK][4][NT / 8], vg[MK][4];
+        if (ELEM <= 0) {
+#pragma unroll
+          for (int kk = 0; kk < MK; ++kk) {
+            const uint32_t rows = ELEM == kUnits ? v_s + kk * C::unit : v_s + kk * 16 * C::row;
+            const uint32_t groups = ELEM == kUnits ? rows + 16 * C::row : v_s + C::codes + kk * 16 * (D / 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int row = key_of<ELEM>(cq + (i & 1)) + (i >> 1) * 8;
+              if (D == 128) {
+                const uint2 x = lds8(rows + chunk_at<D, ELEM>(row, g >> 1) + (g & 1) * 8);
+                vc[kk][i][0] = x.x; vc[kk][i][NT / 8 - 1] = x.y;
+                vg[kk][i] = lds1(groups + row * (D / 16) + g);
+              } else {
+                vc[kk][i][0] = lds4(rows + row * C::row + g * 4);
+                vg[kk][i] = lds1(groups + row * (D / 16) + (g >> 1));
+              }
+            }
+            if (ELEM == kUnits && key0 + KEYS > n) {      // what stands behind a context may be anything, NaN too: its weights are zero
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (key0 + kk * 16 + key_of<ELEM>(cq + (i & 1)) + (i >> 1) * 8 >= n) vg[kk][i] = 0;
+            }
+          }
+        }
         // ---- O^T += V^T P^T
 #pragma unroll
         for (int kk = 0; kk < MK; ++kk) {
@@ -755,38 +933,23 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
             for (int mt = 0; mt < MO; ++mt) {
               uint32_t a[4];
               ldsm4_trans(v_s + chunk_at<D, ELEM>(row, mt * 2 + ((lane >> 3) & 1)), a);
-#pragma unroll
-              for (int h = 0; h < PP; ++h) mma_bf16(oc[mt], a, pf[h][2 * kk], pf[h][2 * kk + 1]);
+              add_product<sizeof(T) == 4, true>(oc[mt], a, pf, 2 * kk);
             }
-          } else if (ELEM == 0) {
+          } else if (ELEM <= 0) {
             // As below, NT consecutive codes of four keys and the scale of their group: even and odd dims of two keys to a byte each
-            uint32_t v[4][NT / 8], sc[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int row = kk * 16 + key_of<ELEM>(cq + (i & 1)) + (i >> 1) * 8;
-              if (D == 128) {
-                const uint2 x = lds8(v_s + chunk_at<D, ELEM>(row, g >> 1) + (g & 1) * 8);
-                v[i][0] = x.x; v[i][NT / 8 - 1] = x.y;
-                sc[i] = lds1(v_s + C::codes + row * (D / 16) + g);
-              } else {
-                v[i][0] = lds4(v_s + row * C::row + g * 4);
-                sc[i] = lds1(v_s + C::codes + row * (D / 16) + (g >> 1));
-              }
-            }
-            const uint32_t s0 = half2_of_e4m3x2(sc[0] | sc[1] << 8), s1 = half2_of_e4m3x2(sc[2] | sc[3] << 8);
+            const uint32_t s0 = half2_of_e4m3x2(vg[kk][0] | vg[kk][1] << 8), s1 = half2_of_e4m3x2(vg[kk][2] | vg[kk][3] << 8);
 #pragma unroll
             for (int j = 0; j < NT / 8; ++j) {
               constexpr uint32_t kLow = 0x0f0f0f0fu;
               uint32_t even0[4], odd0[4], even1[4], odd1[4];
-              halves_of_e2m1((v[0][j] & kLow) | (v[1][j] << 4 & ~kLow), even0);
-              halves_of_e2m1((v[0][j] >> 4 & kLow) | (v[1][j] & ~kLow), odd0);
-              halves_of_e2m1((v[2][j] & kLow) | (v[3][j] << 4 & ~kLow), even1);
-              halves_of_e2m1((v[2][j] >> 4 & kLow) | (v[3][j] & ~kLow), odd1);
+              halves_of_e2m1((vc[kk][0][j] & kLow) | (vc[kk][1][j] << 4 & ~kLow), even0);
+              halves_of_e2m1((vc[kk][0][j] >> 4 & kLow) | (vc[kk][1][j] & ~kLow), odd0);
+              halves_of_e2m1((vc[kk][2][j] & kLow) | (vc[kk][3][j] << 4 & ~kLow), even1);
+              halves_of_e2m1((vc[kk][2][j] >> 4 & kLow) | (vc[kk][3][j] & ~kLow), odd1);
 #pragma unroll
               for (int b = 0; b < 4; ++b) {
                 const uint32_t x[4] = {mul_half2(even0[b], s0), mul_half2(odd0[b], s0), mul_half2(even1[b], s1), mul_half2(odd1[b], s1)};
-#pragma unroll
-                for (int h = 0; h < PP; ++h) mma_f16(oc[4 * j + b], x, pf[h][2 * kk], pf[h][2 * kk + 1]);
+                add_product<sizeof(T) == 4, false>(oc[4 * j + b], x, pf, 2 * kk);
               }
             }
           } else {
@@ -810,15 +973,13 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
               const uint32_t b0 = __byte_perm(v[2][j], v[3][j], 0x5140), b1 = __byte_perm(v[2][j], v[3][j], 0x7362);
               const uint32_t x[4] = {half2_of_e4m3x2(a0), half2_of_e4m3x2(a0 >> 16), half2_of_e4m3x2(b0), half2_of_e4m3x2(b0 >> 16)};
               const uint32_t y[4] = {half2_of_e4m3x2(a1), half2_of_e4m3x2(a1 >> 16), half2_of_e4m3x2(b1), half2_of_e4m3x2(b1 >> 16)};
-#pragma unroll
-              for (int h = 0; h < PP; ++h) {
-                mma_f16(oc[2 * j], x, pf[h][2 * kk], pf[h][2 * kk + 1]);
-                mma_f16(oc[2 * j + 1], y, pf[h][2 * kk], pf[h][2 * kk + 1]);
-              }
+              add_product<false, false>(oc[2 * j], x, pf, 2 * kk);
+              add_product<false, false>(oc[2 * j + 1], y, pf, 2 * kk);
             }
           }
         }
       }
+      if (ELEM == kUnits) poison &= ~(1u << get);      // the slot's next stage says so itself
       get = get + 1 == C::stages ? 0 : get + 1;
       cons.step(p, TILE);
     }
@@ -829,16 +990,18 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
     // show.  (bf16 pages: e4m3 has no infinities.  Scores of +inf and NaN show by themselves.)
     if (ELEM == 2 && __any_sync(0xffffffffu, low == -INFINITY) &&
         infinite_key<KEYS>(p, req, kvh, (s_tile * KW + kg) * KEYS, TILE, steps, n))
-      l[0] = l[1] = __uint_as_float(0x7fc00000u);
+      l.x = l.y = __uint_as_float(0x7fc00000u);
 
     // ---- the request's share: sums over the lanes of a column, fp16 weights back to 2^(t - m)
     float f[2];
+    float ms[2] = {m.x, m.y}, ls[2] = {l.x, l.y};
+    const float mws[2] = {mw.x, mw.y};
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 4);
-      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 8);
-      l[i] += __shfl_xor_sync(0xffffffffu, l[i], 16);
-      f[i] = ELEM != 2 && mw[i] != -INFINITY ? ex2(mw[i] - m[i] - kWeightBits) : 1.f;
+      ls[i] += __shfl_xor_sync(0xffffffffu, ls[i], 4);
+      ls[i] += __shfl_xor_sync(0xffffffffu, ls[i], 8);
+      ls[i] += __shfl_xor_sync(0xffffffffu, ls[i], 16);
+      f[i] = ELEM != 2 && mws[i] != -INFINITY ? ex2(mws[i] - ms[i] - kWeightBits) : 1.f;
     }
     const bool whole = s_tile == 0 && steps == tiles_of(n, TILE);
     const long long rec_slot = s_tile == 0 ? 1 : 0;      // a range can begin and end inside a request: two records
@@ -848,13 +1011,13 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
         if (cq + i >= nh) break;
         const int h = head0 + cq + i;
         if (whole) {
-          store_head<D, ELEM>(static_cast<T *>(p.out) + req * p.out_stride + (long long)h * D, oc, i, g, n == 0 ? 0.f : f[i] / l[i]);
+          store_head<D, ELEM>(static_cast<T *>(p.out) + req * p.out_stride + (long long)h * D, oc, i, g, n == 0 ? 0.f : f[i] / ls[i]);
           if (p.lse != nullptr && g == 0)
-            p.lse[(long long)req * p.n_q_heads + h] = n == 0 ? -INFINITY : nan_of_inf((m[i] + log2f(l[i])) * (1.f / kLog2e));
+            p.lse[(long long)req * p.n_q_heads + h] = n == 0 ? -INFINITY : nan_of_inf((ms[i] + log2f(ls[i])) * (1.f / kLog2e));
         } else {
           const long long rec = ((long long)h * p.parts + part) * 2 + rec_slot;
           store_head<D, ELEM>(p.o + rec * D, oc, i, g, f[i]);
-          if (g == 0) p.ml[rec] = make_float2(m[i], l[i]);
+          if (g == 0) p.ml[rec] = make_float2(ms[i], ls[i]);
         }
       }
     };
@@ -866,8 +1029,8 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
       float4 *buf = reinterpret_cast<float4 *>(ba_smem + kBaWarps * C::ring);
       float2(*ml)[kBaHeads] = ml_s[seg & 1];
       if (g == 0) {
-        ml[warp][cq] = make_float2(m[0], l[0]);
-        ml[warp][cq + 1] = make_float2(m[1], l[1]);
+        ml[warp][cq] = make_float2(ms[0], ls[0]);
+        ml[warp][cq + 1] = make_float2(ms[1], ls[1]);
       }
       __syncthreads();
 #pragma unroll
@@ -875,14 +1038,14 @@ __global__ void __launch_bounds__(kBaThreads, 2) paged_attention_batched_kernel(
         float all = -INFINITY;
 #pragma unroll
         for (int w = 0; w < kBaWarps; ++w) all = fmaxf(all, ml[w][cq + i].x);
-        f[i] = m[i] == -INFINITY ? 0.f : f[i] * ex2(m[i] - all);
-        l[i] = 0.f;
+        f[i] = ms[i] == -INFINITY ? 0.f : f[i] * ex2(ms[i] - all);
+        ls[i] = 0.f;
 #pragma unroll
         for (int w = 0; w < kBaWarps; ++w) {
           const float2 x = ml[w][cq + i];
-          l[i] += x.x == -INFINITY ? x.y : x.y * ex2(x.x - all);
+          ls[i] += x.x == -INFINITY ? x.y : x.y * ex2(x.x - all);
         }
-        m[i] = all;
+        ms[i] = all;
 #pragma unroll
         for (int mt = 0; mt < MO; ++mt) {
           oc[mt][i] *= f[i];
@@ -1053,7 +1216,7 @@ struct BaPlan {
   bool whole;               // they are not: a CTA per request
 };
 
-BaPlan ba_plan(int n_req, int vheads, int max_ctx, int elem_bytes, int sms) {
+BaPlan ba_plan(int n_req, int vheads, int max_ctx, int elem_bytes, int dtype, int sms) {
   BaPlan b;
   // A warp per KV head once the batch has a (request, head) for every other warp of the machine; four warps per head below
   // that.  Measured, a warp / four warps: 128 requests of up to 577 tokens 28.8 / 34.2 us, 256 of up to 500 39.4 / 48.3,
@@ -1075,7 +1238,7 @@ BaPlan ba_plan(int n_req, int vheads, int max_ctx, int elem_bytes, int sms) {
   b.whole = max_ctx <= ba_whole_ctx(n_req, b.kw, elem_bytes);
   // no more parts than 16-key tiles (the shortest there are) could give work to
   const long long tiles = (long long)n_req * ((max_ctx + b.kw * 16 - 1) / (b.kw * 16) + 1);
-  long long parts = 2ll * sms / b.columns;         // two CTAs per SM
+  long long parts = (long long)ba_ctas(elem_bytes == KV_ELEM_E2M1, dtype == KV_DTYPE_BF16) * sms / b.columns;
   parts = parts < 1 ? 1 : parts;
   b.parts = (int)(parts < tiles ? parts : tiles);
   return b;
@@ -1101,11 +1264,11 @@ int ba_launch(const BaParams &p, const BaPlan &b, int device, cudaStream_t st) {
   static bool attr_set[kMaxDevices] = {};
   auto kernel = paged_attention_batched_kernel<D, ELEM, T, KW>;
   if (!attr_set[device]) {
-    KV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BaCfg<D, ELEM>::smem(KW)));
+    KV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BaCfg<D, ELEM, T>::smem(KW)));
     attr_set[device] = true;
   }
   const dim3 grid(b.whole ? p.n_req : b.parts, b.columns);
-  kernel<<<grid, kBaThreads, BaCfg<D, ELEM>::smem(KW), st>>>(p);
+  kernel<<<grid, kBaThreads, BaCfg<D, ELEM, T>::smem(KW), st>>>(p);
   KV_COUNT_LAUNCH();
   KV_CUDA(cudaGetLastError());
   if (b.whole) return KV_OK;
@@ -1122,8 +1285,8 @@ int ba_launch(const BaParams &p, const BaPlan &b, int device, cudaStream_t st) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  KV_CUDA(wph == 4 ? cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<D, T, 4>, p, KW * BaCfg<D, ELEM>::keys)
-                   : cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<D, T, 1>, p, KW * BaCfg<D, ELEM>::keys));
+  KV_CUDA(wph == 4 ? cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<D, T, 4>, p, KW * BaCfg<D, ELEM, T>::keys)
+                   : cudaLaunchKernelEx(&cfg, paged_attention_join_kernel<D, T, 1>, p, KW * BaCfg<D, ELEM, T>::keys));
   KV_COUNT_LAUNCH();
   return KV_OK;
 }
@@ -1173,7 +1336,7 @@ int ba_call(const void *q_dev, int64_t q_stride, int dtype, int n_req, int n_q_h
   p.passes = ba_passes(p.group);
   const long long vheads = (long long)cache->n_kv_heads * p.passes;
   if (vheads > 65535 || n_q_heads > 65535) return KV_ERR_SHAPE;      // second dimension of the grids
-  const BaPlan b = ba_plan(n_req, (int)vheads, max_ctx, cache->elem_bytes, sm_count(device));
+  const BaPlan b = ba_plan(n_req, (int)vheads, max_ctx, cache->elem_bytes, dtype, sm_count(device));
   const BaScratch s = ba_scratch(n_req, n_q_heads, cache->head_dim, b.parts);
   if (!b.whole) {
     if (scratch_dev == nullptr || ((uintptr_t)scratch_dev & 15) || scratch_bytes < s.bytes) return KV_ERR_WORKSPACE;
@@ -1199,7 +1362,7 @@ int ba_call(const void *q_dev, int64_t q_stride, int dtype, int n_req, int n_q_h
   p.n_q_heads = n_q_heads;
   p.max_ctx = max_ctx;
   p.parts = b.whole ? 0 : b.parts;
-  p.scale = softmax_scale * kLog2e;
+  p.scale = fmaxf(softmax_scale * kLog2e, FLT_MIN);
   char *base = static_cast<char *>(scratch_dev);
   p.tile_start = reinterpret_cast<long long *>(base);
   p.ml = reinterpret_cast<float2 *>(base + s.ml);
@@ -1208,7 +1371,7 @@ int ba_call(const void *q_dev, int64_t q_stride, int dtype, int n_req, int n_q_h
   switch (format_of(cache->elem_bytes)) {
     case kBf16: return ba_dim<kBf16>(p, b, dtype, device, st);
     case kE4m3: return ba_dim<kE4m3>(p, b, dtype, device, st);
-    default: return ba_dim<kE2m1>(p, b, dtype, device, st);
+    default: return p.aligned16 ? ba_dim<kUnits>(p, b, dtype, device, st) : ba_dim<kE2m1>(p, b, dtype, device, st);
   }
 }
 
@@ -1229,9 +1392,9 @@ int64_t kv_paged_attention_batched_scratch_bytes(int32_t n_req, int32_t n_q_head
   // change to it, longer contexts also from it.
   if (max_ctx <= kBaNeverSplit || n_req == 0) return 256;
   const int sms = sm_count(current_device());
-  int parts = ba_plan(n_req, vheads, max_ctx, 2, sms).parts;
+  int parts = ba_plan(n_req, vheads, max_ctx, KV_ELEM_E2M1, KV_DTYPE_BF16, sms).parts;
   if (max_ctx > kBaShort) {
-    const int short_parts = ba_plan(n_req, vheads, kBaShort, 2, sms).parts;
+    const int short_parts = ba_plan(n_req, vheads, kBaShort, KV_ELEM_E2M1, KV_DTYPE_BF16, sms).parts;
     parts = parts > short_parts ? parts : short_parts;
   }
   return ba_scratch(n_req, n_q_heads, head_dim, parts).bytes;
