@@ -8,6 +8,8 @@
 // sums of the positive (negative) parts of the heads' queries.  u is taken in 15 bits and a sign, so the score is a whole
 // number (at most 256 * 127 * 32767 < 2^31) times a power of two: it does not depend on the order of any sum, so neither does the
 // choice, and equal scores go to the lowest block.
+#include <cooperative_groups.h>
+
 #include "cache_format.cuh"
 
 namespace kvr {
@@ -214,41 +216,40 @@ __device__ __forceinline__ void query_code(const SelectParams &p, int req, int h
   __syncthreads();
 }
 
-// A CTA takes one KV head of one request and `chunk` of its blocks, a warp 32 of them at a time: half of it (D = 64: a quarter) reads
-// a block's codes, 16 bytes to a lane, and the sums over the lanes are exchanged so that lane i ends with block i's.
-template <int D, typename T>
-__global__ void __launch_bounds__(kScoreThreads) block_score_kernel(const __grid_constant__ SelectParams p, int chunk) {
+// The scores of blocks [from, to) of a request for a KV head, in an order-preserving code; emit(block, key).  The CTA's warps take 32
+// blocks at a time: half a warp (D = 64: a quarter) reads a block's codes, 16 bytes to a lane, and the sums over the lanes are exchanged so
+// that lane i ends with block i's.  The first blocks are on their way while the query's code is formed.
+template <int D, typename T, typename Emit>
+__device__ __forceinline__ void score_blocks(const SelectParams &p, int req, int head, int from, int to, Emit emit) {
   constexpr int LPB = D / 8;                  // lanes of a block
   constexpr int N = LPB;                      // loads of a lane: kScoreBlocks / (32 / LPB)
   __shared__ __align__(16) int8_t hi_s[2 * D];
   __shared__ __align__(16) uint8_t lo_s[2 * D];
   __shared__ double most_s[kScoreThreads / 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int req = blockIdx.z, head = blockIdx.y;
-  int len;
-  const int n = blocks_of(p, req, len);
-  if (n <= p.keep) return;                    // all of them are chosen
-  const int from = p.first + blockIdx.x * chunk, to = min(from + chunk, n - p.last);
-  if (from >= to) return;
-  query_code<D, T>(p, req, head, hi_s, lo_s, most_s);
   const int l = lane % LPB;                   // the lane has values 16 l ... of a block's codes
-  const uint4 hv = *reinterpret_cast<const uint4 *>(hi_s + 16 * l), lv = *reinterpret_cast<const uint4 *>(lo_s + 16 * l);
-  const uint32_t hi[4] = {hv.x, hv.y, hv.z, hv.w}, lo[4] = {lv.x, lv.y, lv.z, lv.w};
   const int *table = p.tables + req * p.table_stride;
-  uint32_t *keys = p.keys + ((long long)req * p.heads + head) * p.max_blocks;
-  for (int b0 = from + warp * kScoreBlocks; b0 < to; b0 += kScoreThreads) {
+  uint4 x[N];
+  int scale = kInfinite;
+  auto load = [&](int b0) {
     const int b = b0 + lane;
     const int phys = b < to ? __ldg(table + b) : -1;
     const bool there = (unsigned)phys < (unsigned)p.num_blocks;
     const long long entry = there ? (long long)phys * p.heads + head : 0;
-    const int scale = there ? (int)__ldg(p.scales + entry) : kInfinite;
-    uint4 x[N];
+    scale = there ? (int)__ldg(p.scales + entry) : kInfinite;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       // block g N + i for the g-th group of LPB lanes
       const long long at = __shfl_sync(0xffffffffu, entry, (lane / LPB) * N + i);
       x[i] = __ldg(reinterpret_cast<const uint4 *>(p.codes + at * (2 * D) + l * 16));
     }
+  };
+  int b0 = from + warp * kScoreBlocks;
+  if (b0 < to) load(b0);
+  query_code<D, T>(p, req, head, hi_s, lo_s, most_s);
+  const uint4 hv = *reinterpret_cast<const uint4 *>(hi_s + 16 * l), lv = *reinterpret_cast<const uint4 *>(lo_s + 16 * l);
+  const uint32_t hi[4] = {hv.x, hv.y, hv.z, hv.w}, lo[4] = {lv.x, lv.y, lv.z, lv.w};
+  while (b0 < to) {
     int sum[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -261,6 +262,9 @@ __global__ void __launch_bounds__(kScoreThreads) block_score_kernel(const __grid
       }
       sum[i] = a * 256 + c;
     }
+    const int b = b0 + lane, unit = scale;
+    b0 += kScoreThreads;
+    if (b0 < to) load(b0);                    // under the exchange
     // sums over the LPB lanes, lane l keeping block l's: half of the blocks handed over in each round
 #pragma unroll
     for (int o = LPB / 2; o > 0; o >>= 1) {
@@ -272,111 +276,256 @@ __global__ void __launch_bounds__(kScoreThreads) block_score_kernel(const __grid
         sum[i] = mine + __shfl_xor_sync(0xffffffffu, other, o);
       }
     }
-    const float score = (float)sum[0] * __uint_as_float((uint32_t)min(scale, 254) << 23);
-    if (b < to) keys[b] = scale == kInfinite ? kAlways : key_of_score(score);
+    const float score = (float)sum[0] * __uint_as_float((uint32_t)min(unit, 254) << 23);
+    if (b < to) emit(b, unit == kInfinite ? kAlways : key_of_score(score));
   }
 }
 
 // ---------------------------------------------------------------- choice
-constexpr int kPickThreads = 256;
-
-// One CTA per request and KV head: the key of rank `want` digit by digit (radix selection), then the blocks above it and the first of
-// its equals, in the order of their positions.
-__global__ void __launch_bounds__(kPickThreads) block_pick_kernel(const __grid_constant__ SelectParams p) {
-  __shared__ int hist[256];
-  __shared__ int sums[2][kPickThreads / 32];
-  __shared__ int digit_s, want_s;
-  const int req = blockIdx.x, head = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  int len;
-  const int n = blocks_of(p, req, len), kept = min(n, p.keep);
+// What a context leaves for the choice: the middle blocks [from, to), of which `want` are taken; false if there is nothing to choose.  The
+// blocks at the ends, or all of a short context, are written here, by the whole CTA.
+__device__ __forceinline__ bool write_ends(const SelectParams &p, int req, int head, int n, int len, int *out, int &from, int &to, int &want) {
+  const int tid = threadIdx.x, kept = min(n, p.keep);
   const int *table = p.tables + req * p.table_stride;
-  int *out = p.kept + ((long long)req * p.heads + head) * p.keep;
   if (head == 0 && tid == 0) p.kept_lens[req] = len - (n - kept) * p.block_size;
-  for (int i = kept + tid; i < p.keep; i += kPickThreads) out[i] = -1;
+  for (int i = kept + tid; i < p.keep; i += kScoreThreads) out[i] = -1;
   if (n <= p.keep) {
-    for (int i = tid; i < n; i += kPickThreads) out[i] = __ldg(table + i);
-    return;
+    for (int i = tid; i < n; i += kScoreThreads) out[i] = __ldg(table + i);
+    return false;
   }
-  const int from = p.first, to = n - p.last;
-  for (int i = tid; i < p.first; i += kPickThreads) out[i] = __ldg(table + i);
-  for (int i = tid; i < p.last; i += kPickThreads) out[p.keep - p.last + i] = __ldg(table + to + i);
-  int want = p.keep - p.first - p.last;      // how many of the middle ones
-  if (want == 0) return;
-  const uint32_t *keys = p.keys + ((long long)req * p.heads + head) * p.max_blocks;
-  uint32_t prefix = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    hist[tid] = 0;
+  from = p.first;
+  to = n - p.last;
+  want = p.keep - p.first - p.last;
+  for (int i = tid; i < p.first; i += kScoreThreads) out[i] = __ldg(table + i);
+  for (int i = tid; i < p.last; i += kScoreThreads) out[p.keep - p.last + i] = __ldg(table + to + i);
+  return want > 0;
+}
+
+// The `want` largest of keys(0 .. m) by one CTA, the first of equal ones, written in their order: out[i] = table[index].  0 < want <= m, and
+// no key is 0.
+// The key of that rank is found two bits at a time, from the first in which keys differ: three counts of larger keys in each round.
+// It ends as soon as a count is `want`, which for distinct keys is long before the last bit.  Up to kOwn keys for each thread
+// stay in registers; more are read again in each round.
+constexpr int kOwn = 8;
+template <typename Keys>
+__device__ __forceinline__ void pick(const Keys &keys, int m, int want, const int *table, int *out) {
+  constexpr int W = kScoreThreads / 32;
+  __shared__ uint32_t most_s[W], least_s[W];
+  __shared__ int count_s[2][3][W];
+  __shared__ uint32_t sums[kOwn * W];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const bool few = m <= kOwn * kScoreThreads;
+  uint32_t own[kOwn];
+#pragma unroll
+  for (int r = 0; r < kOwn; ++r) own[r] = tid + r * kScoreThreads < m ? keys(tid + r * kScoreThreads) : 0;
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int r = 0; r < kOwn; ++r) f(own[r]);
+    if (!few)
+      for (int i = tid + kOwn * kScoreThreads; i < m; i += kScoreThreads) f(keys(i));
+  };
+  uint32_t most = 0, least = 0xffffffffu;
+  each([&](uint32_t k) {
+    most = max(most, k);
+    least = min(least, k - 1u);               // 0 is none
+  });
+  most = __reduce_max_sync(0xffffffffu, most);
+  least = __reduce_min_sync(0xffffffffu, least);
+  if (lane == 0) {
+    most_s[warp] = most;
+    least_s[warp] = least;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    most = max(most, most_s[w]);
+    least = min(least, least_s[w]);
+  }
+  ++least;
+  // the largest bar with at least `want` keys that reach it, its bits from the top one in which keys differ
+  int bits = most == least ? 0 : 32 - __clz(most ^ least), reach = m;
+  bits += bits & 1;
+  uint32_t bar = bits >= 32 ? 0u : most & ~((1u << bits) - 1u);
+  for (int turn = 0; bits > 0 && reach != want; turn ^= 1) {
+    bits -= 2;
+    const uint32_t b1 = bar + (1u << bits), b2 = bar + (2u << bits), b3 = bar + (3u << bits);
+    int c1 = 0, c2 = 0, c3 = 0;               // keys that reach them
+    each([&](uint32_t k) {
+      c1 += k >= b1;
+      c2 += k >= b2;
+      c3 += k >= b3;
+    });
+    c1 = __reduce_add_sync(0xffffffffu, c1);
+    c2 = __reduce_add_sync(0xffffffffu, c2);
+    c3 = __reduce_add_sync(0xffffffffu, c3);
+    if (lane < 3) count_s[turn][lane][warp] = lane == 0 ? c1 : lane == 1 ? c2 : c3;
     __syncthreads();
-    for (int b = from + tid; b < to; b += kPickThreads) {
-      const uint32_t k = keys[b];
-      if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1);
+    c1 = c2 = c3 = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      c1 += count_s[turn][0][w];
+      c2 += count_s[turn][1][w];
+      c3 += count_s[turn][2][w];
+    }
+    if (c3 >= want) {
+      bar = b3;
+      reach = c3;
+    } else if (c2 >= want) {
+      bar = b2;
+      reach = c2;
+    } else if (c1 >= want) {
+      bar = b1;
+      reach = c1;
+    }
+  }
+  // ---- keys above the bar, and of those on it what is wanting (all, if the search ended early)
+  const bool all = reach == want;
+  int ties = 0;
+  if (!all) {                                 // the bar is a key, and has equals
+    uint32_t above = 0;
+    each([&](uint32_t k) { above += k > bar; });
+    above = __reduce_add_sync(0xffffffffu, above);
+    __syncthreads();
+    if (lane == 0) count_s[0][0][warp] = (int)above;
+    __syncthreads();
+    ties = want;
+#pragma unroll
+    for (int w = 0; w < W; ++w) ties -= count_s[0][0][w];
+  }
+  // ---- their places: rounds of kOwn keys a thread, the counts of all warps and all keys of a round scanned by one warp
+  int taken = 0, equals = 0;                  // so far
+  const unsigned below = (1u << lane) - 1u;
+  for (int i0 = 0; i0 < m; i0 += kOwn * kScoreThreads) {
+    unsigned more_w[kOwn], same_w[kOwn];
+#pragma unroll
+    for (int r = 0; r < kOwn; ++r) {
+      const int i = i0 + r * kScoreThreads + tid;
+      const uint32_t k = i0 == 0 ? own[r] : i < m ? keys(i) : 0;
+      more_w[r] = __ballot_sync(0xffffffffu, all ? k >= bar && k > 0 : k > bar);
+      same_w[r] = __ballot_sync(0xffffffffu, !all && k == bar);
+      if (lane == r) sums[r * W + warp] = __popc(more_w[r]) | __popc(same_w[r]) << 16;
     }
     __syncthreads();
     if (warp == 0) {
-      // lane l has digits 255 - 8 l ... 248 - 8 l: the running count from the top
-      int c[8], total = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        c[i] = hist[255 - 8 * lane - i];
-        total += c[i];
-      }
-      int above = total;
+      const uint2 two = reinterpret_cast<const uint2 *>(sums)[lane];
+      uint32_t scan = two.x + two.y;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const int up = __shfl_up_sync(0xffffffffu, above, o);
-        if (lane >= o) above += up;
+        const uint32_t up = __shfl_up_sync(0xffffffffu, scan, o);
+        if (lane >= o) scan += up;
       }
-      above -= total;
-      if (above < want && want <= above + total) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (above < want && want <= above + c[i]) {
-            digit_s = 255 - 8 * lane - i;
-            want_s = want - above;
-          }
-          above += c[i];
-        }
-      }
+      reinterpret_cast<uint2 *>(sums)[lane] = make_uint2(scan - two.y, scan);      // inclusive
     }
     __syncthreads();
-    prefix |= (uint32_t)digit_s << shift;
-    want = want_s;                            // of the keys that begin with prefix
-  }
-  // ---- keys above prefix, and the first `want` equal ones
-  int taken = p.first, equals = 0;            // so far
-  for (int b0 = from, turn = 0; b0 < to; b0 += kPickThreads, turn ^= 1) {
-    const int b = b0 + tid;
-    const uint32_t k = b < to ? keys[b] : 0;
-    const bool more = b < to && k > prefix, same = b < to && k == prefix;
-    const unsigned more_w = __ballot_sync(0xffffffffu, more), same_w = __ballot_sync(0xffffffffu, same);
-    if (lane == 0) sums[turn][warp] = __popc(more_w) | __popc(same_w) << 16;
-    __syncthreads();
-    int before = 0, all = 0;
 #pragma unroll
-    for (int w = 0; w < kPickThreads / 32; ++w) {
-      const int s = sums[turn][w];
-      before += w < warp ? s : 0;
-      all += s;
+    for (int r = 0; r < kOwn; ++r) {
+      const int i = i0 + r * kScoreThreads + tid;
+      const uint32_t before = r * W + warp > 0 ? sums[r * W + warp - 1] : 0;
+      const int same_before = equals + (int)(before >> 16) + __popc(same_w[r] & below);
+      const int more_before = (int)(before & 0xffffu) + __popc(more_w[r] & below);
+      const bool take = (more_w[r] >> lane & 1u) || ((same_w[r] >> lane & 1u) && same_before < ties);
+      if (take) out[taken + more_before + min(same_before, ties) - min(equals, ties)] = __ldg(table + i);
     }
-    const unsigned below = (1u << lane) - 1u;
-    const int same_before = equals + (before >> 16) + __popc(same_w & below);
-    const int more_before = (before & 0xffff) + __popc(more_w & below);
-    if (more || (same && same_before < want))
-      out[taken - min(equals, want) + more_before + min(same_before, want)] = __ldg(table + b);
-    const int more_all = all & 0xffff, equals_new = equals + (all >> 16);
-    taken += more_all + min(equals_new, want) - min(equals, want);
+    const uint32_t total = sums[kOwn * W - 1];
+    const int equals_new = equals + (int)(total >> 16);
+    taken += (int)(total & 0xffffu) + min(equals_new, ties) - min(equals, ties);
     equals = equals_new;
+    if (taken >= want) break;
+    __syncthreads();
   }
+}
+
+// Up to kClusterBlocks blocks: a cluster of CTAs shares the blocks of a (request, KV head), hands the keys to its first CTA's shared memory, and
+// that one chooses.  One launch, and no keys in global memory.
+constexpr int kClusterBlocks = 16384;
+template <int D, typename T>
+__global__ void __launch_bounds__(kScoreThreads) select_cluster_kernel(const __grid_constant__ SelectParams p) {
+  extern __shared__ uint32_t keys_s[];
+  namespace cg = cooperative_groups;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int req = blockIdx.z, head = blockIdx.y, rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
+  int len, from = 0, to = 0, want = 0;
+  const int n = blocks_of(p, req, len);
+  if (n <= p.keep || p.keep == p.first + p.last) {      // nothing to choose: the same for the whole cluster
+    if (rank == 0) write_ends(p, req, head, n, len, p.kept + ((long long)req * p.heads + head) * p.keep, from, to, want);
+    return;
+  }
+  if (ctas > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  from = p.first;
+  to = n - p.last;
+  // whole rounds of the warps to a CTA
+  const int each = ((to - from + ctas - 1) / ctas + kScoreBlocks - 1) / kScoreBlocks * kScoreBlocks;
+  const int mine = from + rank * each;
+  uint32_t *keys = ctas > 1 ? cluster.map_shared_rank(keys_s, 0) : keys_s;
+  if (ctas > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // the first CTA is there
+  if (mine < to)
+    score_blocks<D, T>(p, req, head, mine, min(mine + each, to), [&](int b, uint32_t key) { keys[b - from] = key; });
+  if (ctas > 1)
+    cluster.sync();
+  else
+    __syncthreads();
+  if (rank > 0) return;
+  int *out = p.kept + ((long long)req * p.heads + head) * p.keep;
+  write_ends(p, req, head, n, len, out, from, to, want);
+  pick([&](int i) { return keys_s[i]; }, to - from, want, p.tables + req * p.table_stride + from, out + p.first);
+}
+
+// More blocks than that: the keys go through global memory, and a CTA for each (request, KV head) chooses.
+template <int D, typename T>
+__global__ void __launch_bounds__(kScoreThreads) block_score_kernel(const __grid_constant__ SelectParams p, int chunk) {
+  const int req = blockIdx.z, head = blockIdx.y;
+  int len;
+  const int n = blocks_of(p, req, len);
+  if (n <= p.keep) return;                    // all of them are chosen
+  const int from = p.first + blockIdx.x * chunk, to = min(from + chunk, n - p.last);
+  if (from >= to) return;
+  uint32_t *keys = p.keys + ((long long)req * p.heads + head) * p.max_blocks;
+  score_blocks<D, T>(p, req, head, from, to, [&](int b, uint32_t key) { keys[b] = key; });
+}
+__global__ void __launch_bounds__(kScoreThreads) block_pick_kernel(const __grid_constant__ SelectParams p) {
+  const int req = blockIdx.x, head = blockIdx.y;
+  int len, from, to, want;
+  const int n = blocks_of(p, req, len);
+  int *out = p.kept + ((long long)req * p.heads + head) * p.keep;
+  if (!write_ends(p, req, head, n, len, out, from, to, want)) return;
+  const uint32_t *keys = p.keys + ((long long)req * p.heads + head) * p.max_blocks + from;
+  pick([&](int i) { return keys[i]; }, to - from, want, p.tables + req * p.table_stride + from, out + p.first);
 }
 
 int select_max_blocks(int max_ctx, int block_size) { return (int)(((long long)max_ctx + block_size - 1) / block_size); }
 
 template <int D, typename T>
-int launch_select(const SelectParams &p, int sms, cudaStream_t st) {
-  const int middle = p.max_blocks - p.first - p.last;
+int launch_select(const SelectParams &p, int device, cudaStream_t st) {
+  const int middle = p.max_blocks - p.first - p.last, sms = sm_count(device);
+  const long long lines = (long long)p.n_req * p.heads;
+  if (p.max_blocks <= kClusterBlocks) {
+    auto kernel = select_cluster_kernel<D, T>;
+    static bool attr_set[kMaxDevices] = {};
+    if (!attr_set[device]) {
+      KV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kClusterBlocks * 4));
+      attr_set[device] = true;
+    }
+    // as many CTAs as run at once (two to an SM), of at least four warps' blocks each
+    int ctas = 1;
+    while (ctas < 8 && lines * ctas * 2 <= 2ll * sms && middle > ctas * 4 * kScoreBlocks) ctas *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas, p.heads, p.n_req);
+    cfg.blockDim = dim3(kScoreThreads);
+    cfg.dynamicSmemBytes = p.max_blocks > p.keep ? (size_t)p.max_blocks * 4 : 0;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    KV_CUDA(cudaLaunchKernelEx(&cfg, kernel, p));
+    KV_COUNT_LAUNCH();
+    return KV_OK;
+  }
   if (p.max_blocks > p.keep) {
     // a batch of blocks for every warp, or as many more as leave two CTAs for each SM
-    const long long lines = (long long)p.n_req * p.heads, batches = (middle + kScoreThreads - 1) / kScoreThreads;
+    const long long batches = (middle + kScoreThreads - 1) / kScoreThreads;
     const long long each = batches * lines / (2ll * sms);
     const int chunk = (int)(each > 1 ? each < batches ? each : batches : 1) * kScoreThreads;
     const dim3 grid((middle + chunk - 1) / chunk, p.heads, p.n_req);
@@ -384,7 +533,7 @@ int launch_select(const SelectParams &p, int sms, cudaStream_t st) {
     KV_COUNT_LAUNCH();
     KV_CUDA(cudaGetLastError());
   }
-  block_pick_kernel<<<dim3(p.n_req, p.heads), kPickThreads, 0, st>>>(p);
+  block_pick_kernel<<<dim3(p.n_req, p.heads), kScoreThreads, 0, st>>>(p);
   KV_COUNT_LAUNCH();
   KV_CUDA(cudaGetLastError());
   return KV_OK;
@@ -479,10 +628,9 @@ int32_t kv_op_select_blocks(const void *q_dev, int64_t q_stride, int32_t dtype, 
   p.keys = static_cast<uint32_t *>(scratch_dev);
   p.kept = kept_dev;
   p.kept_lens = kept_lens_dev;
-  const int sms = sm_count(device);
   cudaStream_t st = (cudaStream_t)stream;
-  if (head_dim == 128) return dtype == KV_DTYPE_F32 ? launch_select<128, float>(p, sms, st) : launch_select<128, bf16>(p, sms, st);
-  return dtype == KV_DTYPE_F32 ? launch_select<64, float>(p, sms, st) : launch_select<64, bf16>(p, sms, st);
+  if (head_dim == 128) return dtype == KV_DTYPE_F32 ? launch_select<128, float>(p, device, st) : launch_select<128, bf16>(p, device, st);
+  return dtype == KV_DTYPE_F32 ? launch_select<64, float>(p, device, st) : launch_select<64, bf16>(p, device, st);
 }
 
 }  // extern "C"
