@@ -1203,9 +1203,14 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(cons
 // queries: 25.7 / 30.0).
 constexpr int kBaNeverSplit = 384;   // the least that this can be
 constexpr int kBaWholeWarp = 512;    // with a warp per KV head
-int ba_whole_ctx(int n_req, int kw, int elem_bytes) {
+// e2m1 pages: a CTA works longer on a context of the same bytes, and there is as much to gain from the heads that run beside it.
+// Measured, split / whole, heads of 128: 16 requests over 2 heads of up to 512 tokens 8.6 / 8.2 us, of 768 9.0 / 10.3; over 4 heads 768 9.6 /
+// 10.3; over 8 heads 768 12.8 / 10.0, 1,024 13.3 / 12.8, 1,536 14.6 / 16.1; 32 over 8 heads, all of 1,024, 21.5 / 16.7; fp32 queries, 64 over 8
+// heads of 1,024 29.1 / 31.8.
+int ba_whole_ctx(int n_req, long long heads, int kw, int elem_bytes, int slots) {
   if (kw == 1) return kBaWholeWarp;
-  return n_req >= 8 ? 768 : (elem_bytes != 2 ? 512 : kBaNeverSplit);
+  if (elem_bytes == KV_ELEM_E2M1) return heads < 64 ? 512 : heads < 128 || 4 * heads > 5ll * slots ? 768 : 1024;
+  return n_req >= 8 ? 768 : (elem_bytes == 1 ? 512 : kBaNeverSplit);
 }
 constexpr int kBaShort = 1024;       // ... although up to half of the warps have no head
 // Positions and the tiles of 32 requests are counted in 32 bits.
@@ -1235,7 +1240,7 @@ BaPlan ba_plan(int n_req, int vheads, int max_ctx, int elem_bytes, int dtype, in
   b.kw = single ? 1 : kBaWarps;
   const int per_cta = kBaWarps / b.kw;
   b.columns = (vheads + per_cta - 1) / per_cta;
-  b.whole = max_ctx <= ba_whole_ctx(n_req, b.kw, elem_bytes);
+  b.whole = max_ctx <= ba_whole_ctx(n_req, heads, b.kw, elem_bytes, ba_ctas(elem_bytes == KV_ELEM_E2M1, dtype == KV_DTYPE_BF16) * sms);
   // no more parts than 16-key tiles (the shortest there are) could give work to
   const long long tiles = (long long)n_req * ((max_ctx + b.kw * 16 - 1) / (b.kw * 16) + 1);
   long long parts = (long long)ba_ctas(elem_bytes == KV_ELEM_E2M1, dtype == KV_DTYPE_BF16) * sms / b.columns;

@@ -21,8 +21,8 @@ constexpr int kSelMaxCtx = 1 << 26;
 
 // ---------------------------------------------------------------- bounds
 struct BoundsParams {
-  CacheView cache;
-  int layer, num_blocks, n;
+  RowLayout layout;
+  int block_size, n_kv_heads, num_blocks, n;
   const int *blocks, *counts;
   int8_t *codes;        // [num_blocks][n_kv_heads][2][D]
   uint8_t *scales;      // [num_blocks][n_kv_heads]
@@ -30,102 +30,140 @@ struct BoundsParams {
 
 constexpr int kBoundThreads = 256;
 
-// A warp takes a (block, KV head), a lane D / 32 dims of every key.  HBM-bound: K's rows once.
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {      // NaN if one is
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t min_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// A warp takes a (block, KV head), a lane eight dims of every second key (D = 64: fourth), with the loads of 16 (32) keys in flight.
+// Bound by HBM over bf16 pages, whose keys are compared two at a time as they are, and by instructions over the others, whose values bf16
+// holds exactly.
 template <int D, int FMT>
 __global__ void __launch_bounds__(kBoundThreads) block_bounds_kernel(const __grid_constant__ BoundsParams p) {
-  constexpr int E = D / 32;
-  const int lane = threadIdx.x & 31;
+  constexpr int LANES = D / 8, ROWS = 32 / LANES, AHEAD = 8;      // lanes of a key; keys of a load, loads in flight
+  const int lane = threadIdx.x & 31, sub = lane % LANES, mine = lane / LANES;
   const long long item = blockIdx.x * (long long)(kBoundThreads / 32) + (threadIdx.x >> 5);
-  const int heads = p.cache.n_kv_heads;
+  const int heads = p.n_kv_heads;
   const long long i = item / heads;
   const int head = (int)(item - i * heads);
   if (i >= p.n) return;
-  const int block = __ldg(p.blocks + i), count = min(__ldg(p.counts + i), p.cache.block_size);
+  const int block = __ldg(p.blocks + i), count = min(__ldg(p.counts + i), p.block_size);
   if ((unsigned)block >= (unsigned)p.num_blocks || count <= 0) return;
-  const char *page = p.cache.page(p.layer, 0, block);
-  const char *record = FMT == kE2m1 ? page + head * p.cache.record_bytes() : page + head * D * FMT;
-  const long long slot_bytes = FMT == kE2m1 ? D / 2 : (long long)heads * D * FMT;
-  const uint8_t *scale = reinterpret_cast<const uint8_t *>(FMT == kE2m1 ? record + (long long)p.cache.block_size * (D / 2 + D / 16)
-                                                                        : page + p.cache.value_bytes() + head * p.cache.block_size);
-  const uint8_t *groups = reinterpret_cast<const uint8_t *>(record + (long long)p.cache.block_size * (D / 2));
-  float top[E], low[E];
+  const Pieces<D, FMT> at(p.layout, 0, head, sub * 8);
+  const long long from = block * p.layout.block_stride;
+  const char *keys = at.values + from;
+  const uint8_t *groups = reinterpret_cast<const uint8_t *>(at.groups + from), *scale = reinterpret_cast<const uint8_t *>(at.scale + from);
+  uint32_t top2[4], low2[4];
 #pragma unroll
-  for (int j = 0; j < E; ++j) {
-    top[j] = -INFINITY;
-    low[j] = INFINITY;
+  for (int j = 0; j < 4; ++j) {
+    top2[j] = 0xff80ff80u;      // -inf, -inf
+    low2[j] = 0x7f807f80u;
   }
-  bool fine = true;
-#pragma unroll 8
-  for (int s = 0; s < count; ++s) {
-    float f[E];
-    const char *row = record + s * slot_bytes;
-    if (FMT == kBf16) {
+  const long long step = ROWS * p.layout.slot_stride;
+  const char *row = keys + mine * p.layout.slot_stride;
+  for (int s0 = 0; s0 < count; s0 += AHEAD * ROWS) {
+    uint4 raw[AHEAD];
+    uint32_t units = 0, group[AHEAD];
+    // the scale bytes of up to 32 keys, one to a lane
+    if (FMT != kBf16) units = scale[min(s0 + lane, count - 1)];
 #pragma unroll
-      for (int j = 0; j < E; j += 2) {
-        const uint32_t w = reinterpret_cast<const uint32_t *>(row)[lane * (E / 2) + j / 2];
-        f[j] = __uint_as_float(w << 16);
-        f[j + 1] = __uint_as_float(w & 0xffff0000u);
-      }
-    } else {
-      const float unit = __uint_as_float((uint32_t)scale[s] << 23);
-      uint32_t h[E / 2];
-      if (FMT == kE4m3) {
-        const uint32_t w = E == 4 ? reinterpret_cast<const uint32_t *>(row)[lane] : reinterpret_cast<const uint16_t *>(row)[lane];
-#pragma unroll
-        for (int j = 0; j < E / 2; ++j) h[j] = half2_of_e4m3x2(w >> (16 * j));
+    for (int a = 0; a < AHEAD; ++a) {
+      const int s = min(s0 + a * ROWS + mine, count - 1);
+      const char *from = s0 + a * ROWS + mine < count ? row : keys + (count - 1) * p.layout.slot_stride;      // behind the last key: the last again
+      row += step;
+      if (FMT == kBf16) {
+        raw[a] = *reinterpret_cast<const uint4 *>(from);
+      } else if (FMT == kE4m3) {
+        const uint2 x = *reinterpret_cast<const uint2 *>(from);
+        raw[a].x = x.x;
+        raw[a].y = x.y;
       } else {
-        const uint32_t w = reinterpret_cast<const uint32_t *>(row)[lane * E / 8] >> (lane * E % 8 * 4);
-        const uint32_t s16 = half2_of_e4m3x2(groups[s * (D / 16) + lane * E / 16] * 0x101u);
-        uint32_t v[4];
-        halves_of_e2m1(w, v);
-#pragma unroll
-        for (int j = 0; j < E / 2; ++j) h[j] = mul_half2(v[j], s16);
-      }
-#pragma unroll
-      for (int j = 0; j < E / 2; ++j) {
-        const float2 x = floats_of_half2(h[j]);
-        f[2 * j] = x.x * unit;
-        f[2 * j + 1] = x.y * unit;
+        raw[a].x = *reinterpret_cast<const uint32_t *>(from);
+        group[a] = groups[s * (D / 16)];
       }
     }
 #pragma unroll
-    for (int j = 0; j < E; ++j) {
-      fine &= fabsf(f[j]) <= 127.f * 0x1p60f;
-      top[j] = fmaxf(top[j], f[j]);
-      low[j] = fminf(low[j], f[j]);
+    for (int a = 0; a < AHEAD; ++a) {
+      uint32_t w[4] = {raw[a].x, raw[a].y, raw[a].z, raw[a].w};
+      if (FMT != kBf16) {                               // exact in bf16: at most six bits
+        uint32_t h[4];
+        if (FMT == kE4m3) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) h[j] = half2_of_e4m3x2((j < 2 ? raw[a].x : raw[a].y) >> (16 * (j & 1)));
+        } else {
+          halves_of_e2m1(raw[a].x, h);
+          const uint32_t s16 = half2_of_e4m3x2(group[a] * 0x101u);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) h[j] = mul_half2(h[j], s16);
+        }
+        const float u = __uint_as_float(__shfl_sync(0xffffffffu, units, a * ROWS + mine) << 23);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 x = floats_of_half2(h[j]);
+          const __nv_bfloat162 y = __floats2bfloat162_rn(x.x * u, x.y * u);
+          w[j] = *reinterpret_cast<const uint32_t *>(&y);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        top2[j] = max_bf16x2(top2[j], w[j]);
+        low2[j] = min_bf16x2(low2[j], w[j]);
+      }
     }
   }
-  float size = 0.f;
+  // over the keys of the other lanes, and the largest size over the dims: NaN if there is one, infinite if there is an infinity
+  uint32_t size2 = 0;
 #pragma unroll
-  for (int j = 0; j < E; ++j) size = fmaxf(size, fmaxf(fabsf(top[j]), fabsf(low[j])));
+  for (int j = 0; j < 4; ++j) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) size = fmaxf(size, __shfl_xor_sync(0xffffffffu, size, o));
-  fine = __all_sync(0xffffffffu, fine);
+    for (int o = LANES; o < 32; o <<= 1) {
+      top2[j] = max_bf16x2(top2[j], __shfl_xor_sync(0xffffffffu, top2[j], o));
+      low2[j] = min_bf16x2(low2[j], __shfl_xor_sync(0xffffffffu, low2[j], o));
+    }
+    size2 = max_bf16x2(size2, max_bf16x2(top2[j] & 0x7fff7fffu, low2[j] & 0x7fff7fffu));
+  }
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) size2 = max_bf16x2(size2, __shfl_xor_sync(0xffffffffu, size2, o));
+  size2 = max_bf16x2(size2, size2 >> 16 | size2 << 16);
+  const uint32_t bits = size2 << 16;
+  const bool fine = __uint_as_float(bits) <= 127.f * 0x1p60f;
   // size = m * 2^x with 1 <= m < 2; 127 = 1.984375 * 2^6
-  const uint32_t bits = __float_as_uint(size);
   const int e = max((int)(bits >> 23) - 127 - 6 + ((bits & 0x7fffffu) > 0x7e0000u), kMinBound);
   const float down = __uint_as_float((uint32_t)(127 - min(e, kMaxBound)) << 23);
-  uint32_t up = 0, lo = 0;
+  uint32_t up[2] = {}, lo[2] = {};
+  if (fine) {
+    // 1.5 * 2^23 added, rounded up or down: the whole number is in the lowest byte
+    constexpr float kWhole = 12582912.f;
+    uint32_t u8[8], l8[8];
 #pragma unroll
-  for (int j = 0; j < E; ++j) {
-    up |= ((uint32_t)(int)ceilf(top[j] * down) & 255u) << (8 * j);
-    lo |= ((uint32_t)(int)floorf(low[j] * down) & 255u) << (8 * j);
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t t = j & 1 ? top2[j / 2] & 0xffff0000u : top2[j / 2] << 16, l = j & 1 ? low2[j / 2] & 0xffff0000u : low2[j / 2] << 16;
+      u8[j] = __float_as_uint(__fmaf_ru(__uint_as_float(t), down, kWhole));
+      l8[j] = __float_as_uint(__fmaf_rd(__uint_as_float(l), down, kWhole));
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      up[h] = __byte_perm(__byte_perm(u8[4 * h], u8[4 * h + 1], 0x40), __byte_perm(u8[4 * h + 2], u8[4 * h + 3], 0x40), 0x5410);
+      lo[h] = __byte_perm(__byte_perm(l8[4 * h], l8[4 * h + 1], 0x40), __byte_perm(l8[4 * h + 2], l8[4 * h + 3], 0x40), 0x5410);
+    }
   }
-  if (!fine) up = lo = 0;
-  int8_t *to = p.codes + ((long long)block * heads + head) * (2 * D) + lane * E;
-  if (E == 4) {
-    *reinterpret_cast<uint32_t *>(to) = up;
-    *reinterpret_cast<uint32_t *>(to + D) = lo;
-  } else {
-    *reinterpret_cast<uint16_t *>(to) = (uint16_t)up;
-    *reinterpret_cast<uint16_t *>(to + D) = (uint16_t)lo;
+  if (mine == 0) {
+    int8_t *to = p.codes + ((long long)block * heads + head) * (2 * D) + sub * 8;
+    *reinterpret_cast<uint2 *>(to) = make_uint2(up[0], up[1]);
+    *reinterpret_cast<uint2 *>(to + D) = make_uint2(lo[0], lo[1]);
   }
   if (lane == 0) p.scales[(long long)block * heads + head] = (uint8_t)(fine ? e + 127 : kInfinite);
 }
 
 template <int D, int FMT>
 int launch_bounds(const BoundsParams &p, cudaStream_t st) {
-  const long long warps = (long long)p.n * p.cache.n_kv_heads, ctas = (warps + kBoundThreads / 32 - 1) / (kBoundThreads / 32);
+  const long long warps = (long long)p.n * p.n_kv_heads, ctas = (warps + kBoundThreads / 32 - 1) / (kBoundThreads / 32);
   if (ctas > 0x7fffffffll) return KV_ERR_SHAPE;
   block_bounds_kernel<D, FMT><<<(unsigned)ctas, kBoundThreads, 0, st>>>(p);
   KV_COUNT_LAUNCH();
@@ -134,8 +172,8 @@ int launch_bounds(const BoundsParams &p, cudaStream_t st) {
 }
 
 template <int FMT>
-int bounds_format(const BoundsParams &p, cudaStream_t st) {
-  return p.cache.head_dim == 128 ? launch_bounds<128, FMT>(p, st) : launch_bounds<64, FMT>(p, st);
+int bounds_format(const BoundsParams &p, int d, cudaStream_t st) {
+  return d == 128 ? launch_bounds<128, FMT>(p, st) : launch_bounds<64, FMT>(p, st);
 }
 
 // ---------------------------------------------------------------- scores
@@ -556,8 +594,9 @@ int32_t kv_op_block_bounds(const kv_cache_desc *cache, int32_t layer, const int3
   if (blocks_dev == nullptr || counts_dev == nullptr || bounds_dev == nullptr || bound_scales_dev == nullptr) return KV_ERR_ARG;
   if (((uintptr_t)blocks_dev & 3) || ((uintptr_t)counts_dev & 3) || ((uintptr_t)bounds_dev & 15)) return KV_ERR_ARG;
   BoundsParams p;
-  p.cache = make_view(cache);
-  p.layer = layer;
+  p.layout = row_layout(make_view(cache), layer);
+  p.block_size = cache->block_size;
+  p.n_kv_heads = cache->n_kv_heads;
   p.num_blocks = cache->num_blocks;
   p.n = n;
   p.blocks = blocks_dev;
@@ -566,9 +605,9 @@ int32_t kv_op_block_bounds(const kv_cache_desc *cache, int32_t layer, const int3
   p.scales = bound_scales_dev;
   cudaStream_t st = (cudaStream_t)stream;
   switch (format_of(cache->elem_bytes)) {
-    case kBf16: return bounds_format<kBf16>(p, st);
-    case kE4m3: return bounds_format<kE4m3>(p, st);
-    default: return bounds_format<kE2m1>(p, st);
+    case kBf16: return bounds_format<kBf16>(p, cache->head_dim, st);
+    case kE4m3: return bounds_format<kE4m3>(p, cache->head_dim, st);
+    default: return bounds_format<kE2m1>(p, cache->head_dim, st);
   }
 }
 
