@@ -386,3 +386,43 @@ def test_two_selections_at_once(kv, torch):
     torch.cuda.synchronize()
     for x, (kept, out) in zip((a, b), want):
         assert torch.equal(x.kept, kept) and torch.equal(x.b.out, out)
+
+
+@pytest.mark.parametrize("ctx", [15 * 16 + 1, 700 * 16, 2051 * 16, 2600 * 16 + 3])
+@pytest.mark.parametrize("kind", ["apart", "equal", "one far", "few values", "infinite"])
+def test_scores_of_every_distribution(kv, torch, kind, ctx):
+    """Scores that spread, that are one value, that lie close together but for one, that take few values, with many that no bound covers:
+    each asks for another way to the block of the last rank.  Bounds are given, not formed: any bytes are bounds."""
+    heads, d, block, keep = 2, 64, 16, 12
+    n = -(-ctx // block)
+    rng = np.random.default_rng(n)
+    codes = rng.integers(-127, 128, (n, heads, 2, d)).astype(np.int8)
+    scales = np.full((n, heads), 127 - 7, np.uint8)
+    if kind == "equal":
+        codes[:] = codes[:1]
+    elif kind == "one far":
+        codes[:] = codes[:1] // 8
+        codes[:, :, 0, 0] = rng.integers(-3, 4, (n, heads))
+        scales[:] = 40
+        scales[n // 2] = 140
+    elif kind == "few values":
+        codes[:] = codes[rng.integers(0, 5, n)]
+    elif kind == "infinite":
+        scales[rng.integers(0, n, n // 3)] = 255
+    cache = kv.PagedCache(_shape(heads, d, block, 1), n, elem_bytes=2)
+    bounds = kv.BlockBounds(cache)
+    bounds.codes[0].copy_(torch.from_numpy(codes.reshape(bounds.codes[0].shape)))
+    bounds.scales[0].copy_(torch.from_numpy(scales.reshape(bounds.scales[0].shape)))
+    q = torch.from_numpy(rng.standard_normal((1, 2 * heads, d)).astype(np.float32)).cuda()
+    table = torch.from_numpy(rng.permutation(n).astype(np.int32)[None]).cuda()
+    lens = torch.tensor([ctx], dtype=torch.int32, device="cuda")
+    kept = torch.empty(1, heads, keep, dtype=torch.int32, device="cuda")
+    kept_lens = torch.empty(1, dtype=torch.int32, device="cuda")
+    scratch = torch.empty(max(kv.kv_select_blocks_scratch_bytes(1, cache, ctx), 16), dtype=torch.uint8, device="cuda")
+    kv.kv_op_select_blocks(q, bounds, 0, table, lens, ctx, kept, kept_lens, scratch)
+    torch.cuda.synchronize()
+    for h in range(heads):
+        at = table[0].cpu().numpy()
+        blocks, length = P.select(_np(q)[0, 2 * h:2 * h + 2], codes[:, h], scales[:, h], at, ctx, block, keep, 1, 2)
+        assert kept_lens.tolist() == [length]
+        assert np.array_equal(kept[0, h].cpu().numpy(), at[blocks])
