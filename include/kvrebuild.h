@@ -391,13 +391,13 @@ int32_t kv_op_cache_append(const kv_rope *rope, const kv_cache_desc *cache, int3
  * with max_ctx <= table_stride * block_size and at most 2^26; table entries behind a request's last block are not read.
  * A block id outside the pool inside a context is not followed: that request's out and lse are NaN.  Infinities and NaN turn
  * into NaN what they enter, and nothing else: in a query, its head's out and lse; in a cached key inside a context, the out and
- * lse of that request's heads that read its KV head; in a cached value, its dim (e2m1: the 16 dims of its scale) of those outs.  What
- * lies behind a context
- * enters no result.  Where finite numbers leave fp32: a score below its range weighs nothing, a score or a weighted sum of
+ * lse of that request's heads that read its KV head; in a cached value, its dim (e2m1: the 16 dims of its scale) of those outs.
+ * What lies behind a context enters no result.  Where finite numbers leave fp32: a score below its range weighs nothing, a score or a weighted sum of
  * values beyond it gives NaN, and a context whose scores are all below it gives NaN in out and lse.
  * Sums, softmax and accumulators are fp32.  The operands of the matrix instructions are sums of 16-bit parts: in fp32 calls queries
- * and weights to 2^-24 over bf16 pages and to 2^-22 over e4m3 and e2m1 pages, in bf16 calls queries as they are and weights to 2^-16
- * (2^-22); over e4m3 and e2m1 pages nothing finer than 2^-36 of a query's largest value or of a request's largest contribution.
+ * and weights to 2^-24 over bf16 pages and to 2^-22 over e4m3 and e2m1 pages; in bf16 calls queries as they are, weights to 2^-16 over
+ * bf16, 2^-22 over e4m3 and 2^-11 (an eighth of the result's own rounding) over e2m1 pages, lse from the whole weights in each.  Over
+ * e4m3 and e2m1 pages nothing is finer than 2^-36 of a query's largest value or of a request's largest contribution.
  * out may be q itself with the same strides (KV_ERR_ARG with others).
  * scratch_dev: kv_paged_attention_batched_scratch_bytes() bytes (what is enough for n_req and max_ctx is enough for fewer
  * requests and a smaller max_ctx), 16-byte aligned, contents need not survive between calls; calls that may overlap on the
@@ -446,7 +446,8 @@ int32_t kv_op_select_blocks(const void *q_dev, int64_t q_stride, int32_t dtype, 
 
 /* kv_op_paged_attention_batched with a block table for every KV head: KV head h of request r reads kept_dev[r * kept_stride + h *
  * kept_head_stride ..] (strides in elements, at least the blocks of max_len).  Everything else, the scratch included, is as there, with
- * max_len in the place of max_ctx and the one length kept_lens_dev[r] for all heads of a request. */
+ * max_len in the place of max_ctx and the one length kept_lens_dev[r] for all heads of a request; an id outside the pool makes NaN of
+ * the heads that read the KV head whose table holds it. */
 int32_t kv_op_paged_attention_selected(const void *q_dev, int64_t q_stride, int32_t dtype, int32_t n_req, int32_t n_q_heads,
                                        const kv_cache_desc *cache, int32_t layer, const int32_t *kept_dev, int64_t kept_stride,
                                        int64_t kept_head_stride, const int32_t *kept_lens_dev, int32_t max_len, float softmax_scale,

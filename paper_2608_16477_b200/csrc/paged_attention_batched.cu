@@ -26,7 +26,7 @@
 // hold 8 useful columns of at least 16 as well, but wants its operands through shared-memory descriptors, and e4m3 rows
 // would have to be converted and written back there first.)  Groups of more than 8 heads are taken 8 at a time, each time with
 // a copy of K and V from L2 (16 requests of up to 8,192, 64 / 128 / 256 query heads: 36 / 55 / 99 us, over bf16 pages 56 / 67 / 115).
-// fp32 operands go in as sums of 16-bit parts that are multiplied one after the other.  Over e4m3 pages q and the weights p
+// fp32 operands go in as sums of 16-bit parts that are multiplied one after the other.  Over e4m3 and e2m1 pages q and the weights p
 // are two fp16: off by 2^-22 of themselves, and by up to 2^-36 of the query's largest value or of the request's largest contribution
 // so far, where fp16 ends (a bf16 query is one part: exact down to 2^-28 of its largest value).
 // Over bf16 pages they are three bf16 in fp32 calls (2^-24); in bf16 calls q is one part, exact, and p two (2^-16, a 256th of
@@ -1263,6 +1263,10 @@ BaScratch ba_scratch(int n_req, int n_q_heads, int head_dim, int parts) {
   s.bytes = s.o + up(recs * head_dim * 4);
   return s;
 }
+// Ranges that scratch has room for: those of e2m1 pages and bf16 queries, of which there are the most.  One size for every format.
+int ba_scratch_parts(int n_req, int vheads, int max_ctx, int sms) {
+  return ba_plan(n_req, vheads, max_ctx, KV_ELEM_E2M1, KV_DTYPE_BF16, sms).parts;
+}
 
 template <int D, int ELEM, typename T, int KW>
 int ba_launch(const BaParams &p, const BaPlan &b, int device, cudaStream_t st) {
@@ -1342,7 +1346,7 @@ int ba_call(const void *q_dev, int64_t q_stride, int dtype, int n_req, int n_q_h
   const long long vheads = (long long)cache->n_kv_heads * p.passes;
   if (vheads > 65535 || n_q_heads > 65535) return KV_ERR_SHAPE;      // second dimension of the grids
   const BaPlan b = ba_plan(n_req, (int)vheads, max_ctx, cache->elem_bytes, dtype, sm_count(device));
-  const BaScratch s = ba_scratch(n_req, n_q_heads, cache->head_dim, b.parts);
+  const BaScratch s = ba_scratch(n_req, n_q_heads, cache->head_dim, ba_scratch_parts(n_req, (int)vheads, max_ctx, sm_count(device)));
   if (!b.whole) {
     if (scratch_dev == nullptr || ((uintptr_t)scratch_dev & 15) || scratch_bytes < s.bytes) return KV_ERR_WORKSPACE;
   }
@@ -1397,9 +1401,9 @@ int64_t kv_paged_attention_batched_scratch_bytes(int32_t n_req, int32_t n_q_head
   // change to it, longer contexts also from it.
   if (max_ctx <= kBaNeverSplit || n_req == 0) return 256;
   const int sms = sm_count(current_device());
-  int parts = ba_plan(n_req, vheads, max_ctx, KV_ELEM_E2M1, KV_DTYPE_BF16, sms).parts;
+  int parts = ba_scratch_parts(n_req, vheads, max_ctx, sms);
   if (max_ctx > kBaShort) {
-    const int short_parts = ba_plan(n_req, vheads, kBaShort, KV_ELEM_E2M1, KV_DTYPE_BF16, sms).parts;
+    const int short_parts = ba_scratch_parts(n_req, vheads, kBaShort, sms);
     parts = parts > short_parts ? parts : short_parts;
   }
   return ba_scratch(n_req, n_q_heads, head_dim, parts).bytes;

@@ -252,6 +252,34 @@ def test_attention(kv, torch, case):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_attention_equal_weights_that_round_alike(kv, torch, d, dtype):
+    """All keys of a request are one key, so all its weights are one number, and its rounding does not average out: 2^-11 of the result in
+    bf16 calls (one fp16 part), 2^-22 in fp32 calls.  lse takes the weights whole.  Counted with it: the maximum's and the exponential's
+    rounding (2^-13 of the largest score, 2^-14 as in Batch.check) touch all weights alike here and cancel but for 2^-22, a rounding of
+    each fp32 sum (2^-23 a tile), and the result's own rounding."""
+    lens = [1, 2, 3, 15, 16, 17, 40, 63, 200, 511] * 3
+    b = Batch(kv, torch, lens, 2, 4, d, 16, 0.5, getattr(torch, dtype))
+    table = b.table.cpu().numpy()
+    for r, n in enumerate(lens):
+        pos = np.arange(n)
+        slots = torch.from_numpy(table[r, pos // 16].astype(np.int64) * 16 + pos % 16).cuda()
+        keys = torch.from_numpy(np.repeat(b.k[r][:1], n, 0).astype(np.float32)).cuda()
+        rows = torch.from_numpy(b.v[r][:n].astype(np.float32)).cuda()
+        kv.kv_op_cache_write(b.cache, b.layer, keys, rows, slots)
+        kv.kv_op_cache_read(b.cache, b.layer, slots, keys, rows)
+        b.k[r], b.v[r] = _np(keys), _np(rows)
+    b.run(kv)
+    out, half = _np(b.out), _half_step(torch, b.q.dtype)
+    weight = 2.0 ** -11 if dtype == "bfloat16" else 2.0 ** -22
+    for r, n in enumerate(lens):
+        o, ls, size, most = S.attend(_np(b.q)[r], b.k[r][:n], b.v[r][:n], d ** -0.5)
+        share = weight * 1.01 + (n / 16 + 64) * 2.0 ** -22
+        assert (np.abs(out[r] - o) <= size * share + half * np.abs(o) * 1.01).all(), (r, n)
+    b.check(torch)
+
+
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("block", [1, 3, 8, 16, 17, 48, 64])
 def test_attention_pages_of_every_size(kv, torch, d, block):
     b = Batch(kv, torch, LENGTHS + [700], 3, 4, d, block, 0.5, torch.float32, layout="block_major", layers=2)
