@@ -742,10 +742,11 @@ def kv_op_cache_append(rope: Rope, cache: PagedCache, layer: int, k, v, position
     tensors = (cache.data, k, v, positions, slots)
     hq = q_ptr = q_to = qt = qh = ot = oh = 0
     if q is not None:
-        if q.dim() != 3 or q.shape[0] != t or q.shape[2] != cache.head_dim or q_out.shape != q.shape or \
-                q.dtype is not k.dtype or q_out.dtype is not k.dtype:
+        shape, kind = q.shape, k.dtype
+        if len(shape) != 3 or shape[0] != t or shape[2] != cache.head_dim or q_out.shape != shape or q.dtype is not kind or \
+                q_out.dtype is not kind:
             _refuse(name, "q and q_out are [tokens, heads, head_dim], of the type of k")
-        hq = q.shape[1]
+        hq = shape[1]
         (qt, qh, qd), (ot, oh, od) = q.stride(), q_out.stride()
         if t and hq and (qd != 1 or od != 1):
             _refuse(name, "head_dim has to be contiguous")
@@ -816,19 +817,10 @@ def kv_select_blocks_scratch_bytes(n_req: int, cache, max_ctx: int) -> int:
     return int(r)
 
 
-def _table(name, what, table, r, rows):
-    """Strides of int32 [r, blocks] (rows None) or [r, rows, blocks]: (columns, of a request, of a row)."""
-    lead = (r,) if rows is None else (r, rows)
-    if table.dim() != len(lead) + 1 or tuple(table.shape[:-1]) != lead or table.dtype is not _torch().int32:
-        _refuse(name, f"{what} is int32 [requests, {'' if rows is None else 'n_kv_heads, '}blocks]")
-    columns, stride = table.shape[-1], table.stride()
-    if table.numel() and columns > 1 and stride[-1] != 1:
-        _refuse(name, f"rows of {what} have to be contiguous")
-    of_row = stride[-2] if rows is not None and rows > 1 else columns
-    of_req = stride[0] if r > 1 else max(columns, of_row * (1 if rows is None else rows))
-    if table.numel() and (of_row < columns or of_req < columns):
-        _refuse(name, f"rows of {what} must not overlap")
-    return columns, of_req, of_row
+def _vector(name, what, x, n, torch):
+    """x is a contiguous int32 vector of n."""
+    if x.shape != (n,) or x.dtype is not torch.int32 or not x.is_contiguous():
+        _refuse(name, f"{what} is a contiguous int32 vector, one per request")
 
 
 def kv_op_select_blocks(q, bounds: BlockBounds, layer: int, block_tables, context_lens, max_ctx: int, kept, kept_lens, scratch,
@@ -843,29 +835,35 @@ def kv_op_select_blocks(q, bounds: BlockBounds, layer: int, block_tables, contex
     qr, qh, qd = q.stride()
     if r and (qd != 1 or (hq > 1 and qh != d)):
         _refuse(name, "a request's heads have to be contiguous")
-    columns, row, _ = _table(name, "block_tables", block_tables, r, None)
-    for what, x in (("context_lens", context_lens), ("kept_lens", kept_lens)):
-        if x.shape != (r,) or x.dtype is not torch.int32 or not x.is_contiguous():
-            _refuse(name, f"{what} is a contiguous int32 vector, one per request")
-    if kept.dim() != 3 or tuple(kept.shape[:2]) != (r, bounds.n_kv_heads) or kept.dtype is not torch.int32 or not kept.is_contiguous():
+    if len(block_tables.shape) != 2 or block_tables.shape[0] != r or block_tables.dtype is not torch.int32:
+        _refuse(name, "block_tables is int32 [requests, blocks]")
+    columns, (row, step) = block_tables.shape[1], block_tables.stride()
+    if r < 2:
+        qr, row = 0, columns                        # one row may have any row stride: what counts is its length
+    if (r and columns > 1 and step != 1) or row < columns:
+        _refuse(name, "rows of block_tables have to be contiguous, and not to overlap")
+    _vector(name, "context_lens", context_lens, r, torch)
+    _vector(name, "kept_lens", kept_lens, r, torch)
+    heads, keep = bounds.n_kv_heads, kept.shape[-1]
+    if kept.shape != (r, heads, keep) or kept.dtype is not torch.int32 or not kept.is_contiguous():
         _refuse(name, "kept is contiguous int32 [requests, n_kv_heads, keep]")
-    keep = kept.shape[2]
-    _int32(name, r, hq, max_ctx, first, last, keep)
+    if r > _INT32 or hq > _INT32 or max_ctx > _INT32 or keep > _INT32 or not 0 <= first <= _INT32 or not 0 <= last <= _INT32 or max_ctx < 0:
+        _int32(name, r, hq, max_ctx, first, last, keep)
     if columns * bounds.block_size < max_ctx:
         raise KVError(-8, name)
     dtype = _dtype(name, q.dtype)
     codes, scales = bounds._layer(name, layer)
-    tensors = [q, bounds.codes, bounds.scales, block_tables, context_lens, kept, kept_lens]
     scratch_ptr = scratch_bytes = 0
+    tensors = [q, bounds.codes, bounds.scales, block_tables, context_lens, kept, kept_lens]
     if scratch is not None:
         if not scratch.is_contiguous():
             _refuse(name, "scratch has to be contiguous")
         tensors.append(scratch)
-        scratch_ptr, scratch_bytes = scratch.data_ptr(), scratch.numel() * scratch.element_size()
+        scratch_ptr, scratch_bytes = scratch.data_ptr(), scratch.nbytes
     index, stream = _on_device(name, stream, tensors)
-    _launch(name, index, (q.data_ptr(), qr if r > 1 else 0, dtype, r, hq, bounds.n_kv_heads, d, codes, scales, bounds.num_blocks,
-                          bounds.block_size, block_tables.data_ptr(), row, context_lens.data_ptr(), max_ctx, first, last, keep,
-                          scratch_ptr, scratch_bytes, kept.data_ptr(), kept_lens.data_ptr(), stream))
+    _launch(name, index, (q.data_ptr(), qr, dtype, r, hq, heads, d, codes, scales, bounds.num_blocks, bounds.block_size,
+                          block_tables.data_ptr(), row, context_lens.data_ptr(), max_ctx, first, last, keep, scratch_ptr, scratch_bytes,
+                          kept.data_ptr(), kept_lens.data_ptr(), stream))
 
 
 def kv_op_paged_attention_selected(q, cache: PagedCache, layer: int, kept, kept_lens, out, scratch, lse=None, softmax_scale=None,
@@ -879,9 +877,17 @@ def kv_op_paged_attention_selected(q, cache: PagedCache, layer: int, kept, kept_
     (qr, qh, qd), (outr, outh, outd) = q.stride(), out.stride()
     if r and (qd != 1 or outd != 1 or (hq > 1 and (qh != d or outh != d))):
         _refuse(name, "a request's heads have to be contiguous")
-    columns, of_req, of_head = _table(name, "kept", kept, r, cache.n_kv_heads)
-    if kept_lens.shape != (r,) or kept_lens.dtype is not torch.int32 or not kept_lens.is_contiguous():
-        _refuse(name, "kept_lens is a contiguous int32 vector, one per request")
+    heads, columns = cache.n_kv_heads, kept.shape[-1]
+    if kept.shape != (r, heads, columns) or kept.dtype is not torch.int32:
+        _refuse(name, "kept is int32 [requests, n_kv_heads, blocks]")
+    of_req, of_head, step = kept.stride()
+    if heads < 2:
+        of_head = columns
+    if r < 2:
+        of_req = max(columns, of_head * heads)
+    if (r and columns > 1 and step != 1) or of_head < columns or of_req < columns:
+        _refuse(name, "rows of kept have to be contiguous, and not to overlap")
+    _vector(name, "kept_lens", kept_lens, r, torch)
     tensors = [cache.data, q, kept, kept_lens, out]
     lse_ptr = scratch_ptr = scratch_bytes = 0
     if lse is not None:
@@ -893,10 +899,11 @@ def kv_op_paged_attention_selected(q, cache: PagedCache, layer: int, kept, kept_
         if not scratch.is_contiguous():
             _refuse(name, "scratch has to be contiguous")
         tensors.append(scratch)
-        scratch_ptr, scratch_bytes = scratch.data_ptr(), scratch.numel() * scratch.element_size()
+        scratch_ptr, scratch_bytes = scratch.data_ptr(), scratch.nbytes
     dtype = _dtype(name, q.dtype)
     longest = columns * cache.block_size
-    _int32(name, r, hq, longest, layer)
+    if r > _INT32 or hq > _INT32 or longest > _INT32 or not 0 <= layer <= _INT32:
+        _int32(name, r, hq, longest, layer)
     index, stream = _on_device(name, stream, tensors)
     _launch(name, index, (q.data_ptr(), qr if r > 1 else 0, dtype, r, hq, cache._desc_ref, layer, kept.data_ptr(), of_req, of_head,
                           kept_lens.data_ptr(), longest, d ** -0.5 if softmax_scale is None else softmax_scale, scratch_ptr, scratch_bytes,
