@@ -70,14 +70,15 @@ __device__ __forceinline__ void turn(Raw<T> &raw, const char *row, int first, in
 #pragma unroll
       for (int i = 0; i < 8; i += 4) {
         const float4 w = *reinterpret_cast<const float4 *>(cs + (e0 + i) / 2);      // two pairs; past the last one: not used
+        const bool front = (e0 + i) * (int)sizeof(T) % 32 < 16;
         const float a0 = f[h][i], b0 = f[h][i + 1], a1 = f[h][i + 2], b1 = f[h][i + 3];
         if (e0 + i < rotary) {
           f[h][i] = turned_first(a0, b0, make_float2(w.x, w.y));
-          f[h][i + 1] = turned_second(a0, b0, make_float2(w.x, w.y));
+          f[h][i + 1] = front ? turned_neighbour(a0, b0, make_float2(w.x, w.y)) : turned_second(a0, b0, make_float2(w.x, w.y));
         }
         if (e0 + i + 2 < rotary) {
           f[h][i + 2] = turned_first(a1, b1, make_float2(w.z, w.w));
-          f[h][i + 3] = turned_second(a1, b1, make_float2(w.z, w.w));
+          f[h][i + 3] = front ? turned_neighbour(a1, b1, make_float2(w.z, w.w)) : turned_second(a1, b1, make_float2(w.z, w.w));
         }
       }
       raw.pack(h, f[h]);

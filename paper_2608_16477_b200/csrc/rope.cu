@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_vec_kernel(const __grid_con
         const float x0 = fa[i], y0 = fa[i + 1], x1 = fb[i], y1 = fb[i + 1];
         if (u * VE + i / 2 < half) {
           fa[i] = turned_first(x0, y0, w0);
-          fa[i + 1] = turned_second(x0, y0, w0);
+          fa[i + 1] = turned_neighbour(x0, y0, w0);
         }
         if (u * VE + VE / 2 + i / 2 < half) {
           fb[i] = turned_first(x1, y1, w1);

@@ -27,6 +27,9 @@ __device__ __forceinline__ float2 rope_turn(int position, double turns, float ga
 // head have to leave the same bits.
 __device__ __forceinline__ float turned_first(float a, float b, float2 w) { return fmaf(a, w.x, -(b * w.y)); }
 __device__ __forceinline__ float turned_second(float a, float b, float2 w) { return fmaf(a, w.y, b * w.x); }
+// The same of interleaved pairs in the first 16 of 32 bytes of a head, where vectors are turned: the bits that these kernels have always
+// left (the two differ by an ulp at most).
+__device__ __forceinline__ float turned_neighbour(float a, float b, float2 w) { return fmaf(b, w.x, a * w.y); }
 
 }  // namespace
 }  // namespace kvr
