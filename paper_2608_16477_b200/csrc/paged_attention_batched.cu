@@ -55,7 +55,7 @@ namespace kvr {
 namespace {
 
 constexpr int kBaWarps = 4;
-constexpr int kBaThreads = kBaWarps * 32;
+constexpr int kBaWide = 8;           // warps that share a KV head where whole contexts are so few that each has an SM to itself
 constexpr int kBaHeads = 8;          // query heads of a pass
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kLookAhead = 3;        // stages between looking a page up and copying its rows
@@ -73,6 +73,7 @@ constexpr int kUnits = -1;
 // CTAs of an SM: e2m1 pages and bf16 queries three, whose registers and rings fit (many instructions for few bytes: the more warps
 // the better), two otherwise.
 constexpr int ba_ctas(bool e2m1, bool bf16_queries) { return e2m1 && bf16_queries ? 3 : 2; }
+__host__ __device__ constexpr int ba_warps(int kw) { return kw > kBaWarps ? kw : kBaWarps; }
 template <int D, int ELEM, typename T>
 struct BaCfg {
   static constexpr int row = ELEM <= 0 ? D / 2 : D * ELEM;               // bytes of a K or V row's values
@@ -83,8 +84,9 @@ struct BaCfg {
   static constexpr int stage = 2 * tile + (ELEM == 2 || ELEM == kUnits ? 0 : 256);      // K, V, a word with the scale byte of each row
   static constexpr int stages = stage > 6144 || (ba_ctas(ELEM <= 0, sizeof(T) == 2) == 3 && D == 128) ? 3 : 5;
   static constexpr int ring = stages * stage;
-  static constexpr int merge = (kBaWarps - 1) * kBaHeads * D * 4;        // outputs of warps 1-3 when they share a head
-  static constexpr int smem(int kw) { return kBaWarps * ring + (kw > 1 ? merge : 0); }
+  // outputs of warps 1-3 when they share a head; those of a wide CTA, which has one request, take the rings' place
+  static constexpr int merge(int kw) { return kw == 1 ? 0 : (kw - 1) * kBaHeads * D * 4; }
+  static constexpr int smem(int kw) { return kw <= kBaWarps ? kBaWarps * ring + merge(kw) : kw * ring > merge(kw) ? kw * ring : merge(kw); }
 };
 
 struct BaParams {
@@ -408,8 +410,11 @@ struct Cursor {
 };
 
 template <int D, int ELEM, typename T, int KW>      // KW: warps that share a KV head
-__global__ void __launch_bounds__(kBaThreads, ba_ctas(ELEM <= 0, sizeof(T) == 2)) paged_attention_batched_kernel(const __grid_constant__ BaParams p) {
+__global__ void __launch_bounds__(ba_warps(KW) * 32, KW == kBaWide ? 1 : ba_ctas(ELEM <= 0, sizeof(T) == 2))
+    paged_attention_batched_kernel(const __grid_constant__ BaParams p) {
   typedef BaCfg<D, ELEM, T> C;
+  constexpr bool WIDE = KW > kBaWarps;       // whole contexts only
+  constexpr int WARPS = ba_warps(KW);
   constexpr int KS = D / 16;                 // k-steps of S^T = K Q^T
   constexpr int NT = D / 8;                  // dims of a lane's V fragments (ELEM 1, 0)
   constexpr int MO = D / 16;                 // 16-dim tiles of O^T
@@ -421,10 +426,10 @@ __global__ void __launch_bounds__(kBaThreads, ba_ctas(ELEM <= 0, sizeof(T) == 2)
   constexpr int MK = KEYS / 16;              // 16-key tiles of S^T
   constexpr int TILE = KW * KEYS;            // keys of a tile of the split
   extern __shared__ __align__(128) unsigned char ba_smem[];
-  __shared__ float2 ml_s[2][kBaWarps][kBaHeads];
+  __shared__ float2 ml_s[2][WARPS][kBaHeads];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int kg = warp % KW;                                        // which of the tile's stages
-  const int vh = blockIdx.y * (kBaWarps / KW) + warp / KW;         // (KV head, pass over its query heads)
+  const int vh = blockIdx.y * (WARPS / KW) + warp / KW;         // (KV head, pass over its query heads)
   if (KW == 1 && vh >= p.cache.n_kv_heads * p.passes) return;
   const int kvh = vh / p.passes, pass = vh % p.passes;
   const int head0 = kvh * p.group + pass * kBaHeads, nh = min(kBaHeads, p.group - pass * kBaHeads);
@@ -434,7 +439,7 @@ __global__ void __launch_bounds__(kBaThreads, ba_ctas(ELEM <= 0, sizeof(T) == 2)
   Cursor cons;
   long long todo, total = 0, first_tile = 0;
   const int part = blockIdx.x;
-  if (p.parts == 0) {
+  if (WIDE || p.parts == 0) {
     cons.open(p, blockIdx.x, TILE);
     todo = cons.n_tiles;
   } else {
@@ -670,7 +675,7 @@ __global__ void __launch_bounds__(kBaThreads, ba_ctas(ELEM <= 0, sizeof(T) == 2)
     const int req = cons.r, n = cons.n, s_tile = cons.tile;
     const int steps = (int)min((long long)(cons.n_tiles - s_tile), todo);
     // for the joining kernel: where the request's tiles start
-    if (p.parts > 0 && s_tile == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+    if (!WIDE && p.parts > 0 && s_tile == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
       p.tile_start[req] = first_tile + done;
       if (req == 0) p.tile_start[p.n_req] = total;
     }
@@ -1013,7 +1018,7 @@ __global__ void __launch_bounds__(kBaThreads, ba_ctas(ELEM <= 0, sizeof(T) == 2)
       ls[i] += __shfl_xor_sync(0xffffffffu, ls[i], 16);
       f[i] = ELEM != 2 && mws[i] != -INFINITY ? ex2(mws[i] - ms[i] - kWeightBits) : 1.f;
     }
-    const bool whole = s_tile == 0 && steps == tiles_of(n, TILE);
+    const bool whole = WIDE || s_tile == 0 && steps == tiles_of(n, TILE);
     const long long rec_slot = s_tile == 0 ? 1 : 0;      // a range can begin and end inside a request: two records
     auto finish = [&]() {
 #pragma unroll
@@ -1034,9 +1039,10 @@ __global__ void __launch_bounds__(kBaThreads, ba_ctas(ELEM <= 0, sizeof(T) == 2)
     if (KW == 1) {
       finish();
     } else {
-      // the CTA's four warps share the head: brought to the common maximum, warps 1-3 hand theirs to warp 0, lane by lane.
+      // the CTA's warps share the head: brought to the common maximum, the others hand theirs to warp 0, lane by lane.
       // (ml_s takes turns: warp 0 may still read it while the others write the next request's.)
-      float4 *buf = reinterpret_cast<float4 *>(ba_smem + kBaWarps * C::ring);
+      float4 *buf = reinterpret_cast<float4 *>(ba_smem + (WIDE ? 0 : kBaWarps * C::ring));
+      if (WIDE) cp_wait_group<0>();
       float2(*ml)[kBaHeads] = ml_s[seg & 1];
       if (g == 0) {
         ml[warp][cq] = make_float2(ms[0], ls[0]);
@@ -1047,11 +1053,11 @@ __global__ void __launch_bounds__(kBaThreads, ba_ctas(ELEM <= 0, sizeof(T) == 2)
       for (int i = 0; i < 2; ++i) {
         float all = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kBaWarps; ++w) all = fmaxf(all, ml[w][cq + i].x);
+        for (int w = 0; w < WARPS; ++w) all = fmaxf(all, ml[w][cq + i].x);
         f[i] = ms[i] == -INFINITY ? 0.f : f[i] * ex2(ms[i] - all);
         ls[i] = 0.f;
 #pragma unroll
-        for (int w = 0; w < kBaWarps; ++w) {
+        for (int w = 0; w < WARPS; ++w) {
           const float2 x = ml[w][cq + i];
           ls[i] += x.x == -INFINITY ? x.y : x.y * ex2(x.x - all);
         }
@@ -1071,7 +1077,7 @@ __global__ void __launch_bounds__(kBaThreads, ba_ctas(ELEM <= 0, sizeof(T) == 2)
       __syncthreads();
       if (warp == 0) {
 #pragma unroll
-        for (int w = 0; w < kBaWarps - 1; ++w)
+        for (int w = 0; w < WARPS - 1; ++w)
 #pragma unroll
           for (int mt = 0; mt < MO; ++mt) {
             const float4 x = buf[(w * MO + mt) * 32 + lane];
@@ -1207,19 +1213,25 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(cons
 
 // Short contexts are not split: one launch, a CTA per request and KV head or four.  Splitting costs a second kernel and the
 // search for the range (3 to 5 us), not splitting leaves the longest request to one CTA.  Measured (8 KV heads of 128, 64
-// query heads, uniform lengths; split against whole): one request of 400 tokens 7.6 / 7.3 us (8-bit), 7.6 / 8.2 (bf16), of
-// 1,000 7.8 / 10.7; 8 of up to 577 10.3 / 8.3 and 11.5 / 10.0, of 1,000 10.7 / 10.8 and 12.0 / 13.7; 32 of up to 577 13.1 /
-// 9.7, of 1,000 15.7 / 13.8; with a warp per KV head 128 of up to 400 23.7 / 20.7 and of up to 577 27.0 / 25.9 (fp32
-// queries: 25.7 / 30.0).
+// query heads, uniform lengths; split against whole): 32 of up to 577 13.1 / 9.7 us, of 1,000 15.7 / 13.8; with a warp per KV head 128 of up to
+// 400 23.7 / 20.7 and of up to 577 27.0 / 25.9 (fp32 queries: 25.7 / 30.0).
 constexpr int kBaNeverSplit = 384;   // the least that this can be
 constexpr int kBaWholeWarp = 512;    // with a warp per KV head
-// e2m1 pages: a CTA works longer on a context of the same bytes, and there is as much to gain from the heads that run beside it.
-// Measured, split / whole, heads of 128: 16 requests over 2 heads of up to 512 tokens 8.6 / 8.2 us, of 768 9.0 / 10.3; over 4 heads 768 9.6 /
-// 10.3; over 8 heads 768 12.8 / 10.0, 1,024 13.3 / 12.8, 1,536 14.6 / 16.1; 32 over 8 heads, all of 1,024, 21.5 / 16.7; fp32 queries, 64 over 8
-// heads of 1,024 29.1 / 31.8.
-int ba_whole_ctx(int n_req, long long heads, int kw, int elem_bytes, int slots) {
+// Where every (request, head) has an SM to itself, its CTA has eight warps: contexts last longer whole.  Measured, split / four warps /
+// eight, 32 query and 8 KV heads of 128, bf16 queries over bf16 pages, fp32 over bf16, bf16 over e4m3, bf16 over e2m1: one request of 384 tokens
+// 7.2 / 8.1 / 7.4, 7.9 / 9.9 / 8.3, 7.5 / 7.7 / 6.7, 8.0 / 7.3 / 7.1 us; of 512 7.2 / 9.2 / 8.1, 7.7 / 11.7 / 9.5, 7.8 / 8.5 / 7.2, 8.2 / 8.5 /
+// 7.6; four of 512 9.3 / 9.2 / 8.2, 10.0 / 11.8 / 9.6, 8.3 / 8.5 / 7.3, 8.8 / 8.7 / 7.6, ragged of up to 768 8.0 / 11.5 / 9.6, 8.7 / 15.0 / 11.4,
+// 8.1 / 10.2 / 8.6, 8.8 / 10.2 / 9.1; eight of 1,024 12.6 / 14.2 / 11.4, 14.1 / 18.7 / 13.9, 11.5 / 12.6 / 10.2, 13.0 / 12.8 / 10.9; 16 ragged of up to
+// 1,024 12.3 / 14.0 / 11.3, 13.9 / 18.7 / 13.9, 12.3 / 12.2 / 9.7, 12.8 / 12.1 / 10.5, of up to 1,536 13.7 / 18.9 / 14.5, 15.4 / 25.4 / 18.0, 12.8 /
+// 16.2 / 12.6, 13.1 / 16.1 / 13.6.  Up to 128 tokens four warps are as good (eight of 128 over e4m3 pages, fp32, 5.1 / 5.7).
+constexpr int kBaWideCtx = 128;
+// Beyond that, e2m1 pages: a CTA works longer on a context of the same bytes, and there is as much to gain from the heads that run beside it.
+// Split / whole, 32 requests over 8 heads, all of 1,024, 21.5 / 16.7 us; fp32 queries, 64 over 8 heads of 1,024 29.1 / 31.8.  (Six warps to
+// a CTA for up to two heads an SM: 3 to 7 % faster from 768 tokens on, 5 % slower at 256.)
+int ba_whole_ctx(int n_req, long long heads, int kw, int elem_bytes, int slots, int sms) {
   if (kw == 1) return kBaWholeWarp;
-  if (elem_bytes == KV_ELEM_E2M1) return heads < 64 ? 512 : heads < 128 || 4 * heads > 5ll * slots ? 768 : 1024;
+  if (heads <= sms) return heads >= 64 ? 1024 : heads >= 32 || elem_bytes != 2 ? 512 : kBaNeverSplit;
+  if (elem_bytes == KV_ELEM_E2M1) return 4 * heads > 5ll * slots ? 768 : 1024;
   return n_req >= 8 ? 768 : (elem_bytes == 1 ? 512 : kBaNeverSplit);
 }
 constexpr int kBaShort = 1024;       // ... although up to half of the warps have no head
@@ -1229,6 +1241,7 @@ constexpr int kBaMaxCtx = 1 << 26;
 struct BaPlan {
   int kw, parts, columns;   // warps per KV head, ranges if contexts are split, CTAs over the KV heads
   bool whole;               // they are not: a CTA per request
+  bool wide;                // ... of eight warps
 };
 
 BaPlan ba_plan(int n_req, int vheads, int max_ctx, int elem_bytes, int dtype, int sms) {
@@ -1250,10 +1263,12 @@ BaPlan ba_plan(int n_req, int vheads, int max_ctx, int elem_bytes, int dtype, in
   b.kw = single ? 1 : kBaWarps;
   const int per_cta = kBaWarps / b.kw;
   b.columns = (vheads + per_cta - 1) / per_cta;
-  b.whole = max_ctx <= ba_whole_ctx(n_req, heads, b.kw, elem_bytes, ba_ctas(elem_bytes == KV_ELEM_E2M1, dtype == KV_DTYPE_BF16) * sms);
+  const int ctas = ba_ctas(elem_bytes == KV_ELEM_E2M1, dtype == KV_DTYPE_BF16);
+  b.whole = max_ctx <= ba_whole_ctx(n_req, heads, b.kw, elem_bytes, ctas * sms, sms);
+  b.wide = b.whole && b.kw == kBaWarps && heads <= sms && max_ctx > kBaWideCtx;
   // no more parts than 16-key tiles (the shortest there are) could give work to
   const long long tiles = (long long)n_req * ((max_ctx + b.kw * 16 - 1) / (b.kw * 16) + 1);
-  long long parts = (long long)ba_ctas(elem_bytes == KV_ELEM_E2M1, dtype == KV_DTYPE_BF16) * sms / b.columns;
+  long long parts = (long long)ctas * sms / b.columns;
   parts = parts < 1 ? 1 : parts;
   b.parts = (int)(parts < tiles ? parts : tiles);
   return b;
@@ -1287,10 +1302,10 @@ int ba_launch(const BaParams &p, const BaPlan &b, int device, cudaStream_t st) {
     attr_set[device] = true;
   }
   const dim3 grid(b.whole ? p.n_req : b.parts, b.columns);
-  kernel<<<grid, kBaThreads, BaCfg<D, ELEM, T>::smem(KW), st>>>(p);
+  kernel<<<grid, ba_warps(KW) * 32, BaCfg<D, ELEM, T>::smem(KW), st>>>(p);
   KV_COUNT_LAUNCH();
   KV_CUDA(cudaGetLastError());
-  if (b.whole) return KV_OK;
+  if (KW > kBaWarps || b.whole) return KV_OK;
   // Four warps per head up to eight heads an SM, one beyond that.  Measured, the whole call, four / one, 64 heads: one request of
   // 18,433 tokens 16.0 / 21.2 us, 4 of up to 4,608 10.7 / 12.8, 16 23.8 / 24.0, 32 39.8 / 38.1, 128 of up to 577 48.6 / 28.4 (nearly
   // every block has nothing, or two records, to join).
@@ -1312,6 +1327,7 @@ int ba_launch(const BaParams &p, const BaPlan &b, int device, cudaStream_t st) {
 
 template <int D, int ELEM, typename T>
 int ba_pick(const BaParams &p, const BaPlan &b, int device, cudaStream_t st) {
+  if (b.wide) return ba_launch<D, ELEM, T, kBaWide>(p, b, device, st);
   return b.kw == 1 ? ba_launch<D, ELEM, T, 1>(p, b, device, st) : ba_launch<D, ELEM, T, kBaWarps>(p, b, device, st);
 }
 

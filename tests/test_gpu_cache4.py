@@ -287,6 +287,22 @@ def test_attention_pages_of_every_size(kv, torch, d, block):
     b.check(torch)
 
 
+@pytest.mark.parametrize("elem", [0.5, 1, 2])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("d,block", [(128, 16), (64, 7)])
+def test_attention_of_few_whole_contexts(kv, torch, elem, dtype, d, block):
+    """Heads enough for an SM each and contexts short enough to stay whole, of every length around the eight warps' rows; and one more
+    than that, which is split."""
+    lens = [1024, 0, 1, 127, 128, 129, 255, 256, 257, 512, 900, 1023, 16]
+    for longest in (1024, 1025):
+        b = Batch(kv, torch, [longest] + lens, 8, 3, d, block, elem, getattr(torch, dtype))
+        b.run(kv)
+        b.check(torch)
+        first = b.out.clone()
+        b.run(kv)
+        assert torch.equal(first, b.out)
+
+
 @pytest.mark.parametrize("many", [False, True])
 def test_attention_rows_of_very_different_sizes(kv, torch, many):
     """Scales of K and V rows spread over 2^-12 .. 2^4, and values 2^20 times larger where the scores are lowest: a weight near zero on a
