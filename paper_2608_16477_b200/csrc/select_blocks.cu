@@ -10,8 +10,8 @@
 // choice, and equal scores go to the lowest block.
 //
 // Measured in a graph, 8 KV heads of 128 (floor: the bytes at a copy's rate).  Bounds of 4,096 blocks of 16: bf16 pages 24 us (21.7), e4m3
-// 25.8, e2m1 27; of 64 blocks 2.7.  Selection, 64 query heads: one request of 1,153 blocks 7.9 us (0.4), 16 of up to 512 9.8 (1.4), 32
-// of up to 1,153 17.8 (4.8), of which finding the score of the last rank and writing the list take 3 us.
+// 25.8, e2m1 27; of 64 blocks 2.7.  Selection, 64 query heads: one request of 1,153 blocks 7.7 us (0.4), 16 of up to 512 9.4 (1.4), 32
+// of up to 1,153 15.4 (4.8), of which finding the score of the last rank and writing the list take 3 us.
 #include <cooperative_groups.h>
 
 #include "cache_format.cuh"
@@ -223,7 +223,7 @@ template <>
 __device__ __forceinline__ double value_of<bf16>(bf16 x) { return value_of<float>(__bfloat162float(x)); }
 
 constexpr int kScoreThreads = 256;
-constexpr int kScoreBlocks = 32;      // of a warp at a time
+constexpr int kScoreBlocks = 32;      // of a warp: a CTA's share is a multiple
 
 // The code of a KV head's queries into shared memory: hi[i] * 256 + lo[i] for value i of [u+ | u-].  The sums are fp64: with up to 2^29
 // between the heads' values they are exact.
@@ -258,46 +258,66 @@ __device__ __forceinline__ void query_code(const SelectParams &p, int req, int h
   __syncthreads();
 }
 
-// The scores of blocks [from, to) of a request for a KV head, in an order-preserving code; emit(block, key, id).  The CTA's warps take 32
-// blocks at a time: half a warp (D = 64: a quarter) reads a block's codes, 16 bytes to a lane, and the sums over the lanes are exchanged so
-// that lane i ends with block i's.  The first blocks are on their way while the query's code is formed.
+// The scores of blocks [from, to) of a request for a KV head, in an order-preserving code; emit(block, key, id).  A warp takes a stage of
+// 16 blocks (D = 64: 32) at a time: half a warp (a quarter) copies a block's codes, 16 bytes to a lane, and the sums over its lanes are
+// exchanged so that lanes end with one block's each.  The copies of two stages, 8 KB a warp, are in flight in a ring of shared memory from
+// which each lane reads what it copied itself (32 requests of up to 1,153 blocks, the whole selection 15.4 us; three stages 16.2; 8 KB in
+// registers, with nothing in flight under the products, 17.8).  Table entries are looked up a stage before they are needed, and the first
+// copies are on their way while the query's code is formed.
+constexpr int kScoreStages = 2, kStageBytes = 4096;
+constexpr int kRingBytes = kScoreThreads / 32 * kScoreStages * kStageBytes;
 template <int D, typename T, typename Emit>
-__device__ __forceinline__ void score_blocks(const SelectParams &p, int req, int head, int from, int to, Emit emit) {
+__device__ __forceinline__ void score_blocks(const SelectParams &p, int req, int head, int from, int to, unsigned char *ring, Emit emit) {
   constexpr int LPB = D / 8;                  // lanes of a block
-  constexpr int N = LPB;                      // loads of a lane: kScoreBlocks / (32 / LPB)
+  constexpr int N = 8;                        // blocks of those lanes in a stage
+  constexpr int BLOCKS = N * (32 / LPB);      // of a stage
+  constexpr int SHARE = LPB / N;              // lanes that end with the same block
   __shared__ __align__(16) int8_t hi_s[2 * D];
   __shared__ __align__(16) uint8_t lo_s[2 * D];
   __shared__ double most_s[kScoreThreads / 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int l = lane % LPB;                   // the lane has values 16 l ... of a block's codes
+  const int mine = lane / LPB * N + l / SHARE;      // the block of a stage that the lane looks up and ends with
   const int *table = p.tables + req * p.table_stride;
-  uint4 x[N];
-  int scale = kInfinite, phys = -1, next = -1;      // of the lane's block in this batch, and of that in the next one
-  auto look_up = [&](int b0) { next = b0 + lane < to ? __ldg(table + b0 + lane) : -1; };
-  auto load = [&](int b0) {
-    phys = next;
-    look_up(b0 + kScoreThreads);
-    const bool there = (unsigned)phys < (unsigned)p.num_blocks;
-    const long long entry = there ? (long long)phys * p.heads + head : 0;
-    scale = there ? (int)__ldg(p.scales + entry) : kInfinite;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      // block g N + i for the g-th group of LPB lanes
-      const long long at = __shfl_sync(0xffffffffu, entry, (lane / LPB) * N + i);
-      x[i] = __ldg(reinterpret_cast<const uint4 *>(p.codes + at * (2 * D) + l * 16));
-    }
+  const uint32_t mem = (uint32_t)__cvta_generic_to_shared(ring) + warp * (kScoreStages * kStageBytes) + lane * 16;
+  int look = from + warp * BLOCKS + mine, put = 0;
+  int next = -1, ids[kScoreStages], units[kScoreStages];      // ids and scale bytes of the stages in flight, the oldest first
+  auto look_up = [&]() {
+    next = look < to ? __ldg(table + look) : -1;
+    look += kScoreThreads / 32 * BLOCKS;
   };
-  int b0 = from + warp * kScoreBlocks;
-  look_up(b0);
-  if (b0 < to) load(b0);
+  auto issue = [&](int &id, int &unit) {
+    id = next;
+    const bool there = (unsigned)id < (unsigned)p.num_blocks;
+    const bool any = look - kScoreThreads / 32 * BLOCKS - mine < to;      // the stage has blocks
+    look_up();
+    if (any) {
+      const long long entry = there ? (long long)id * p.heads + head : 0;
+      unit = there ? (int)__ldg(p.scales + entry) : kInfinite;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const long long at = __shfl_sync(0xffffffffu, entry, lane / LPB * LPB + i * SHARE);
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(mem + put * kStageBytes + i * 512), "l"(p.codes + at * (2 * D) + l * 16)
+                     : "memory");
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    put = put + 1 == kScoreStages ? 0 : put + 1;
+  };
+  look_up();
+#pragma unroll
+  for (int i = 0; i < kScoreStages; ++i) issue(ids[i], units[i]);
   query_code<D, T>(p, req, head, hi_s, lo_s, most_s);
   const uint4 hv = *reinterpret_cast<const uint4 *>(hi_s + 16 * l), lv = *reinterpret_cast<const uint4 *>(lo_s + 16 * l);
   const uint32_t hi[4] = {hv.x, hv.y, hv.z, hv.w}, lo[4] = {lv.x, lv.y, lv.z, lv.w};
-  while (b0 < to) {
+  for (int b0 = from + warp * BLOCKS; b0 < to; b0 += kScoreThreads / 32 * BLOCKS) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kScoreStages - 1) : "memory");
     int sum[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+      uint32_t w[4];
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(mem + put * kStageBytes + i * 512) : "memory");
       int a = 0, c = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -306,22 +326,32 @@ __device__ __forceinline__ void score_blocks(const SelectParams &p, int req, int
       }
       sum[i] = a * 256 + c;
     }
-    const int b = b0 + lane, unit = scale, id = phys;
-    b0 += kScoreThreads;
-    if (b0 < to) load(b0);                    // under the exchange
-    // sums over the LPB lanes, lane l keeping block l's: half of the blocks handed over in each round
+    const int b = b0 + mine, id = ids[0], unit = units[0];
+#pragma unroll
+    for (int i = 0; i + 1 < kScoreStages; ++i) {
+      ids[i] = ids[i + 1];
+      units[i] = units[i + 1];
+    }
+    issue(ids[kScoreStages - 1], units[kScoreStages - 1]);      // into the stage just read
+    // sums over the LPB lanes: half of the blocks handed over in each round, until one is left
 #pragma unroll
     for (int o = LPB / 2; o > 0; o >>= 1) {
+      constexpr int first = LPB / 2;
+      const int left = N * o / first / 2;     // blocks after this round
       const bool upper = l & o;
+      if (left == 0) {
+        sum[0] += __shfl_xor_sync(0xffffffffu, sum[0], o);
+        continue;
+      }
 #pragma unroll
       for (int i = 0; i < N / 2; ++i) {
-        if (i >= o) break;
-        const int mine = upper ? sum[i + o] : sum[i], other = upper ? sum[i] : sum[i + o];
-        sum[i] = mine + __shfl_xor_sync(0xffffffffu, other, o);
+        if (i >= left) break;
+        const int keep = upper ? sum[i + left] : sum[i], give = upper ? sum[i] : sum[i + left];
+        sum[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
       }
     }
     const float score = (float)sum[0] * __uint_as_float((uint32_t)min(unit, 254) << 23);
-    if (b < to) emit(b, unit == kInfinite ? kAlways : key_of_score(score), id);
+    if (l % SHARE == 0 && b < to) emit(b, unit == kInfinite ? kAlways : key_of_score(score), id);
   }
 }
 
@@ -564,12 +594,13 @@ __device__ __forceinline__ void pick(const Keys &keys, int m, int want, const Id
 }
 
 // Up to kClusterBlocks blocks: a cluster of CTAs shares the blocks of a (request, KV head), hands the keys and the blocks' ids to its first CTA's
-// shared memory, and that one chooses.  One launch, and no keys in global memory (32 requests of up to 1,153 blocks, against a kernel for the
-// scores and one for the choice: 19.9 / 29.8 us).
-constexpr int kClusterBlocks = 16384;
+// shared memory, and that one chooses.  One launch, and no keys in global memory (32 requests of up to 1,153 blocks, before the ring, against a kernel
+// for the scores and one for the choice: 19.9 / 29.8 us).
+constexpr int kClusterBlocks = 16384;      // 128 KB of keys and ids, and the ring
 template <int D, typename T>
 __global__ void __launch_bounds__(kScoreThreads) select_cluster_kernel(const __grid_constant__ SelectParams p) {
-  extern __shared__ uint32_t keys_s[];
+  extern __shared__ __align__(16) unsigned char select_smem[];
+  uint32_t *keys_s = reinterpret_cast<uint32_t *>(select_smem + kRingBytes);
   namespace cg = cooperative_groups;
   cg::cluster_group cluster = cg::this_cluster();
   const int req = blockIdx.z, head = blockIdx.y, rank = (int)cluster.block_rank(), ctas = (int)cluster.num_blocks();
@@ -590,7 +621,7 @@ __global__ void __launch_bounds__(kScoreThreads) select_cluster_kernel(const __g
   int *ids = reinterpret_cast<int *>(keys + p.max_blocks);
   if (ctas > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");      // the first CTA is there
   if (mine < to)
-    score_blocks<D, T>(p, req, head, mine, min(mine + each, to), [&](int b, uint32_t key, int id) {
+    score_blocks<D, T>(p, req, head, mine, min(mine + each, to), select_smem, [&](int b, uint32_t key, int id) {
       keys[b - from] = key;
       ids[b - from] = id;
     });
@@ -614,7 +645,8 @@ __global__ void __launch_bounds__(kScoreThreads) block_score_kernel(const __grid
   const int from = p.first + blockIdx.x * chunk, to = min(from + chunk, n - p.last);
   if (from >= to) return;
   uint32_t *keys = p.keys + ((long long)req * p.heads + head) * p.max_blocks;
-  score_blocks<D, T>(p, req, head, from, to, [&](int b, uint32_t key, int) { keys[b] = key; });
+  extern __shared__ __align__(16) unsigned char select_smem[];
+  score_blocks<D, T>(p, req, head, from, to, select_smem, [&](int b, uint32_t key, int) { keys[b] = key; });
 }
 __global__ void __launch_bounds__(kScoreThreads) block_pick_kernel(const __grid_constant__ SelectParams p) {
   const int req = blockIdx.x, head = blockIdx.y;
@@ -637,17 +669,17 @@ int launch_select(const SelectParams &p, int device, cudaStream_t st) {
     auto kernel = select_cluster_kernel<D, T>;
     static bool attr_set[kMaxDevices] = {};
     if (!attr_set[device]) {
-      KV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kClusterBlocks * 8));
+      KV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes + kClusterBlocks * 8));
       attr_set[device] = true;
     }
     // As many CTAs as run at once (two to an SM), of at least four warps' blocks each.  Twice as many CTAs, 16 requests of up to 512
-    // blocks 11.4 -> 15.0 us, 32 of up to 1,153 20.1 -> 23.1; four times, 15.0 and 28.5.
+    // blocks 9.4 -> 11.3 us, 32 of up to 1,153 15.4 -> 19.7.
     int ctas = 1;
     while (ctas < 8 && lines * ctas * 2 <= 2ll * sms && middle > ctas * 4 * kScoreBlocks) ctas *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ctas, p.heads, p.n_req);
     cfg.blockDim = dim3(kScoreThreads);
-    cfg.dynamicSmemBytes = p.max_blocks > p.keep ? (size_t)p.max_blocks * 8 : 0;
+    cfg.dynamicSmemBytes = p.max_blocks > p.keep ? (size_t)(kRingBytes + p.max_blocks * 8) : 0;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -665,7 +697,12 @@ int launch_select(const SelectParams &p, int device, cudaStream_t st) {
     const long long each = batches * lines / (2ll * sms);
     const int chunk = (int)(each > 1 ? each < batches ? each : batches : 1) * kScoreThreads;
     const dim3 grid((middle + chunk - 1) / chunk, p.heads, p.n_req);
-    block_score_kernel<D, T><<<grid, kScoreThreads, 0, st>>>(p, chunk);
+    static bool score_set[kMaxDevices] = {};
+    if (!score_set[device]) {
+      KV_CUDA(cudaFuncSetAttribute(block_score_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes));
+      score_set[device] = true;
+    }
+    block_score_kernel<D, T><<<grid, kScoreThreads, kRingBytes, st>>>(p, chunk);
     KV_COUNT_LAUNCH();
     KV_CUDA(cudaGetLastError());
   }
