@@ -1266,9 +1266,13 @@ BaPlan ba_plan(int n_req, int vheads, int max_ctx, int elem_bytes, int dtype, in
   const int ctas = ba_ctas(elem_bytes == KV_ELEM_E2M1, dtype == KV_DTYPE_BF16);
   b.whole = max_ctx <= ba_whole_ctx(n_req, heads, b.kw, elem_bytes, ctas * sms, sms);
   b.wide = b.whole && b.kw == kBaWarps && heads <= sms && max_ctx > kBaWideCtx;
+  // As many ranges as CTAs run at once.  Three to an SM leave a head of few requests more records than the joining kernel's four warps have in flight
+  // (e2m1 pages, bf16 queries, 8 heads, three / two: one request of 18,433 tokens 17.4 / 14.1 us, of 60,000 30.6 / 27.8; four of 9,000
+  // ragged 14.7 / 14.1, all alike 21.0 / 19.3; eight of 6,000 16.9 / 17.7 and 23.3 / 24.8).
+  const int at_once = (heads < 64 && ctas > 2 ? 2 : ctas) * sms;
   // no more parts than 16-key tiles (the shortest there are) could give work to
   const long long tiles = (long long)n_req * ((max_ctx + b.kw * 16 - 1) / (b.kw * 16) + 1);
-  long long parts = (long long)ctas * sms / b.columns;
+  long long parts = at_once / b.columns;
   parts = parts < 1 ? 1 : parts;
   b.parts = (int)(parts < tiles ? parts : tiles);
   return b;
