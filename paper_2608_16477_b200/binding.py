@@ -791,7 +791,7 @@ class BlockBounds:
 
 
 def kv_op_block_bounds(cache: PagedCache, layer: int, blocks, counts, bounds: BlockBounds, stream=None):
-    """Bounds of the blocks (int32 [n]) from the keys in their first counts (int32 [n]) slots."""
+    """Bounds of the blocks (int32 [n], each once) from the keys in their first counts (int32 [n]) slots; a block of -1 is left out."""
     name, torch = "kv_op_block_bounds", _torch()
     if blocks.dim() != 1 or blocks.dtype is not torch.int32 or not blocks.is_contiguous():
         _refuse(name, "blocks is a contiguous int32 vector")

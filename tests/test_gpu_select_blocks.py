@@ -388,8 +388,9 @@ def test_two_selections_at_once(kv, torch):
         assert torch.equal(x.kept, kept) and torch.equal(x.b.out, out)
 
 
-@pytest.mark.parametrize("ctx", [15 * 16 + 1, 700 * 16, 2051 * 16, 2600 * 16 + 3])
-@pytest.mark.parametrize("kind", ["apart", "equal", "one far", "few values", "infinite"])
+@pytest.mark.parametrize("kind,ctx", [(kind, ctx) for kind in ("apart", "equal", "one far", "few values", "infinite")
+                                      for ctx in (15 * 16 + 1, 700 * 16, 2051 * 16, 2600 * 16 + 3)] +
+                         [(kind, blocks * 16) for kind in ("apart", "few values") for blocks in (16384, 16385)])
 def test_scores_of_every_distribution(kv, torch, kind, ctx):
     """Scores that spread, that are one value, that lie close together but for one, that take few values, with many that no bound covers:
     each asks for another way to the block of the last rank.  Bounds are given, not formed: any bytes are bounds."""
