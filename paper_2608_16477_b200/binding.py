@@ -844,7 +844,7 @@ def kv_op_select_blocks(q, bounds: BlockBounds, layer: int, block_tables, contex
         _refuse(name, "rows of block_tables have to be contiguous, and not to overlap")
     _vector(name, "context_lens", context_lens, r, torch)
     _vector(name, "kept_lens", kept_lens, r, torch)
-    heads, keep = bounds.n_kv_heads, kept.shape[-1]
+    heads, keep = bounds.n_kv_heads, kept.shape[-1] if kept.dim() else 0
     if kept.shape != (r, heads, keep) or kept.dtype is not torch.int32 or not kept.is_contiguous():
         _refuse(name, "kept is contiguous int32 [requests, n_kv_heads, keep]")
     if r > _INT32 or hq > _INT32 or max_ctx > _INT32 or keep > _INT32 or not 0 <= first <= _INT32 or not 0 <= last <= _INT32 or max_ctx < 0:
@@ -877,7 +877,7 @@ def kv_op_paged_attention_selected(q, cache: PagedCache, layer: int, kept, kept_
     (qr, qh, qd), (outr, outh, outd) = q.stride(), out.stride()
     if r and (qd != 1 or outd != 1 or (hq > 1 and (qh != d or outh != d))):
         _refuse(name, "a request's heads have to be contiguous")
-    heads, columns = cache.n_kv_heads, kept.shape[-1]
+    heads, columns = cache.n_kv_heads, kept.shape[-1] if kept.dim() else 0
     if kept.shape != (r, heads, columns) or kept.dtype is not torch.int32:
         _refuse(name, "kept is int32 [requests, n_kv_heads, blocks]")
     of_req, of_head, step = kept.stride()

@@ -338,12 +338,12 @@ def test_binding_refuses_what_does_not_fit(kv):
         return lambda: kv.kv_op_select_blocks(q, bounds, 0, tab, lens, ctx, kept, kept_lens, None)
     bad += [select(q=q[0]), select(q=q[..., :32]), select(q=q.half()), select(q=q[:, ::2]), select(tab=tab.long()), select(tab=tab[:1]),
             select(tab=tab.t()), select(tab=torch.zeros(4, dtype=torch.int32).expand(2, 4)), select(lens=lens[:1]), select(lens=lens.long()),
-            select(kept=kept[:1]), select(kept=kept[:, :1]), select(kept=kept.long()), select(kept=kept[..., :2]), select(kept_lens=kept_lens.long()),
+            select(kept=kept[:1]), select(kept=kept[0]), select(kept=kept[0, 0, 0]), select(kept=kept[:, :1]), select(kept=kept.long()), select(kept=kept[..., :2]), select(kept_lens=kept_lens.long()),
             select()]
 
     def attend(q=q, kept=kept, lens=kept_lens, out=q, lse=None):
         return lambda: kv.kv_op_paged_attention_selected(q, cache, 0, kept, lens, out, None, lse=lse)
-    bad += [attend(q=q[..., :32]), attend(out=q[:1]), attend(out=q.bfloat16()), attend(q=q[:, ::2], out=q[:, ::2]), attend(kept=kept[:, 0]),
+    bad += [attend(q=q[..., :32]), attend(out=q[:1]), attend(out=q.bfloat16()), attend(q=q[:, ::2], out=q[:, ::2]), attend(kept=kept[:, 0]), attend(kept=kept[0, 0, 0]),
             attend(kept=kept[:, :1]), attend(kept=kept.long()), attend(kept=kept.transpose(1, 2)), attend(kept=kept[:, :1].expand(2, 2, 3)),
             attend(lens=kept_lens[:1]), attend(lens=kept_lens.long()), attend(lse=torch.zeros(2, 3)), attend(lse=torch.zeros(2, 4).double()),
             attend()]
