@@ -180,7 +180,7 @@ __device__ __forceinline__ uint32_t half2_of_e4m3x2(uint32_t two) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
   return h;
 }
-// eight values -> codes, nearest, halves already moved off the borders (below)
+// eight values -> codes, nearest; whoever calls it has moved halves off the borders, or looks at them again
 __device__ __forceinline__ uint32_t e2m1x8(const float (&f)[8]) {
   uint32_t r;
   asm("{\n\t.reg .b8 a, b, c, d;\n\tcvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
@@ -206,7 +206,7 @@ __device__ __forceinline__ uint32_t group_scale(float top, float &s) {
   return code;
 }
 
-// A lane's two pieces of a row into e2m1 codes and the scale codes of their groups, by the definition; the lanes of a group are
+// A lane's two pieces of a row into e2m1 codes and the scale codes of their groups, as defined; the lanes of a group are
 // neighbours.  Infinities and NaN are left out of the maxima and make their group NaN.  All lanes of the row call it.  Returns the row's
 // scale byte.
 template <int LANES>
@@ -236,10 +236,21 @@ __device__ __forceinline__ uint32_t e2m1_row(const float (&f)[2][8], unsigned gr
     whole[h] &= other != 0;
     float s;
     scales[h] = group_scale(most[h] * down, s);
-    codes[h] = 0;
+    // Quotients that are off by less than 2^-21, moved down and up by 2^-19: where all eight round alike, that is the answer.
+    const float inv = __fdividef(1.f, s) * down, less = inv * (1.f - 0x1p-19f), greater = inv * (1.f + 0x1p-19f);
+    float a[8], b[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      codes[h] |= (e2m1_exact(fabsf(f[h][j]) * down, s) | (__float_as_uint(f[h][j]) >> 31) << 3) << (4 * j);
+    for (int j = 0; j < 8; ++j) {
+      a[j] = f[h][j] * less;
+      b[j] = f[h][j] * greater;
+    }
+    codes[h] = e2m1x8(a);
+    if (codes[h] != e2m1x8(b)) {              // on a border, or next to it
+      codes[h] = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        codes[h] |= (e2m1_exact(fabsf(f[h][j]) * down, s) | (__float_as_uint(f[h][j]) >> 31) << 3) << (4 * j);
+    }
     if (!whole[h]) {
       codes[h] = 0;
       scales[h] = 0x7fu;      // NaN

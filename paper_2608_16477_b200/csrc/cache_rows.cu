@@ -15,8 +15,8 @@
 // 82 / 75 % of a copy's rate with the launch in it); bf16 to bf16 pages and back, 134 MB, 24.3 / 26.6 and 23.0 / 24.9 us (5.5 and 5.8
 // TB/s), fp32, 201 MB, 33.9 / 36.1 and 38.3 / 40.7 us.  64 tokens 1.9 to 2.5 us.  A piece of 8 to a lane and index arithmetic for
 // every row: 161 instructions a warp and row, 27 us.
-// e2m1 pages (16,384 tokens of 8 heads of 128; floor): from bf16 20.3 us (13.1), into bf16 19.0 (13.1), from fp32 49 (23.4): bound by the
-// instructions of the conversion.
+// e2m1 pages (16,384 tokens of 8 heads of 128; floor): from bf16 20.3 us (13.1), into bf16 19.0 (13.1), from fp32 37 (23.4; 49 with
+// three comparisons for every value): bound by the instructions of the conversion.
 #include "cache_format.cuh"
 
 namespace kvr {
