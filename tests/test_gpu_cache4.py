@@ -156,6 +156,29 @@ def test_many_rows_and_every_code(kv, torch):
         assert ((x - y).unflatten(-1, (-1, 16)).abs() <= top * (1.125 / 6) + 2.0 ** -20).all()
 
 
+@pytest.mark.parametrize("power", [-110, -3, 0, 100])
+def test_values_next_to_the_borders_of_codes(kv, torch, power):
+    """fp32 rows of values on a border between two codes, and a few units in the last place to either side of it, for scales of every
+    significand: the code is the definition's."""
+    rng = np.random.default_rng(200 + power)
+    t, d, borders = 150, 64, np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0])
+    scales = S.e4m3_values()[rng.integers(60, 127, (t, d // 16))]
+    scales[:, 0] = 448.0                                              # the row's largest value is 6 * 448 * 2^power
+    x = np.float32(np.repeat(scales, 16, 1) * borders[rng.integers(0, 7, (t, d))])
+    steps = rng.choice([0, 0, 1, 2, 3, 7, 20, 60], (t, d)) * rng.choice([-1, 1], (t, d))
+    x = (x.view(np.int32) + steps.astype(np.int32)).view(np.float32)
+    x[:, ::16] = np.float32(6 * scales)                               # sets the group's scale
+    x = np.ldexp(x * rng.choice([-1, 1], (t, d)).astype(np.float32), power).astype(np.float32)
+    cache = kv.PagedCache(_shape(1, d, 16), 10, elem_bytes=0.5, fill=0)
+    rows, slots = torch.from_numpy(x[:, None]).cuda(), torch.arange(t, device="cuda")
+    kv.kv_op_cache_write(cache, 0, rows, rows, slots)
+    back, other = torch.empty_like(rows), torch.empty_like(rows)
+    kv.kv_op_cache_read(cache, 0, slots, back, other)
+    for i in range(t):
+        assert np.array_equal(P.stored(x[i]), _np(back)[i, 0]), i
+    assert torch.equal(back, other)
+
+
 # ------------------------------------------------------------------ appending
 APPEND = [  # tokens, q heads, kv heads, dim, rotary, layout, block, type
     (1, 8, 2, 128, 128, "half", 16, "bfloat16"), (1, 64, 8, 128, 128, "half", 16, "bfloat16"),
