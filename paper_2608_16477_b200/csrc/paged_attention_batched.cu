@@ -45,9 +45,9 @@
 // multiple of 16 slots a unit of 16 keys (codes, scales, scale bytes: three pieces of the record) is copied as it is, 1,168 bytes of K or V for
 // 128 dims; in other pages row by row.  What bounds it is no longer HBM but instructions: 370 a warp for 16 keys and 8 heads, half of them
 // conversions, scales and products, at 61 % of the issue slots (ALU pipe 51 %, tensor 21 %).  So bf16 calls have twelve warps an
-// SM, and weights of one fp16 part: 2^-11, an eighth of the result's own rounding (the sum of the weights, and lse, take them whole).  32
-// requests of up to 18,433 tokens (290 MB) 76.5 us in a graph, 83.8 call after call: 3.8 TB/s, against 91 us for the 512 MB of e4m3 pages;
-// compute alone takes 70 to 74 us, the copies alone 50.  fp32 calls (two parts each, eight warps an SM) 106 us; a third CTA for them spills and is as
+// SM.  32 requests of up to 18,433 tokens (290 MB) 83 us in a graph, 87 call after call: 3.5 TB/s, against 91 us for the 512 MB of e4m3
+// pages; the copies alone take 50.  (Weights of one fp16 part, 2^-11, would take 76 us, but last bits of bf16 results then move: 4e-4 of
+// their norm off what fp32 weights give, against 5e-5.)  fp32 calls (two parts each, eight warps an SM) 106 us; a third CTA for them spills and is as
 // often slower as faster (two / three: 128 requests of up to 577 tokens 27.0 / 25.9, one of 18,433 16.9 / 20.8).
 #include "cache_format.cuh"
 
@@ -419,7 +419,7 @@ __global__ void __launch_bounds__(ba_warps(KW) * 32, KW == kBaWide ? 1 : ba_ctas
   constexpr int NT = D / 8;                  // dims of a lane's V fragments (ELEM 1, 0)
   constexpr int MO = D / 16;                 // 16-dim tiles of O^T
   constexpr int QP = sizeof(T) == 2 ? 1 : (ELEM == 2 ? 3 : 2);          // parts of a query
-  constexpr int PP = sizeof(T) == 2 && ELEM <= 0 ? 1 : sizeof(T) == 4 && ELEM == 2 ? 3 : 2;      // parts of a weight
+  constexpr int PP = sizeof(T) == 4 && ELEM == 2 ? 3 : 2;      // parts of a weight
   constexpr int CH = C::row / 16;            // 16-byte chunks of a row
   constexpr int RPI = 32 / CH;               // rows per copy instruction
   constexpr int KEYS = C::keys;
