@@ -396,7 +396,8 @@ int32_t kv_op_cache_append(const kv_rope *rope, const kv_cache_desc *cache, int3
  * values beyond it gives NaN, and a context whose scores are all below it gives NaN in out and lse.
  * Sums, softmax and accumulators are fp32.  The operands of the matrix instructions are sums of 16-bit parts: in fp32 calls queries
  * and weights to 2^-24 over bf16 pages and to 2^-22 over e4m3 and e2m1 pages; in bf16 calls queries as they are, weights to 2^-16 over
- * bf16 and 2^-22 over e4m3 and e2m1 pages, lse from the whole weights in each.  Over e4m3 and e2m1 pages nothing is finer than 2^-36 of a query's largest value or of a request's largest contribution.
+ * bf16 and 2^-22 over e4m3 and e2m1 pages, lse from the whole weights in each.  Over e4m3 and e2m1 pages nothing is finer than
+ * 2^-36 of a query's largest value or of a request's largest contribution.
  * out may be q itself with the same strides (KV_ERR_ARG with others).
  * scratch_dev: kv_paged_attention_batched_scratch_bytes() bytes (what is enough for n_req and max_ctx is enough for fewer
  * requests and a smaller max_ctx), 16-byte aligned, contents need not survive between calls; calls that may overlap on the

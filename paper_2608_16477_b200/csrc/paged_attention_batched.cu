@@ -37,7 +37,7 @@
 // goes to small fp16 weights), so most stages need no reduction over the lanes and no rescaling.
 //
 // e4m3 pages: codes go to fp16 fragments (exact) and the power-of-two scales stay outside: K's multiplies the score,
-// V's goes into the weight, w = 2^(t + e_v - M), with its own running maximum M of t + e_v, so that fp16 keeps the bits
+// V's goes into the weight, w = 2^(t - m + e_v - M), with a running maximum M of t - m + e_v of its own, so that fp16 keeps the bits
 // of every weight that matters next to the largest CONTRIBUTION, however the rows' scales differ.
 //
 // e2m1 pages: the same, and the scale of 16 dims is multiplied into the fp16 fragment (code times e4m3 number: six bits, exact).  The
@@ -216,13 +216,6 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   float2 r;
   asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
       : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return r;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 r;
-  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
-      "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
-      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
   return r;
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {      // NaN only if all are
@@ -681,7 +674,8 @@ __global__ void __launch_bounds__(ba_warps(KW) * 32, KW == kBaWide ? 1 : ba_ctas
     }
     done += steps;
     uint32_t qf[QP][KS][2];
-    float2 q_scale = {p.scale, p.scale};
+    // What makes scores (log2 units) of the products: q_pre, a power of two, ahead of the key's 2^e, and q_scale behind it.
+    float2 q_pre = {1.f, 1.f}, q_scale = {p.scale, p.scale};
     {
       const float on = g < nh ? 1.f : 0.f;
       if (ELEM == 2) {
@@ -710,10 +704,17 @@ __global__ void __launch_bounds__(ba_warps(KW) * 32, KW == kBaWide ? 1 : ba_ctas
         const int e = min(max((int)(__float_as_uint(most) >> 23) - 126, -100), 127);       // most < 2^e
         // NaN times everything where the largest is infinite
         const float up = __uint_as_float(most <= FLT_MAX ? (uint32_t)(127 + kQueryBits - e) << 23 : 0x7fc00000u);
-        // (a scale of zero times the -inf of a key that is not there would be NaN)
-        const float down = fmaxf(p.scale * __uint_as_float((uint32_t)(127 - kQueryBits + e) << 23), FLT_MIN);
-        q_scale.x = __shfl_sync(0xffffffffu, down, cq * 4);
-        q_scale.y = __shfl_sync(0xffffffffu, down, cq * 4 + 4);
+        // Products, below 2^31, are in units of 2^(e - kQueryBits); with the power of two of p.scale, 2^whole.  All of it goes to q_pre
+        // within 2^-100 .. 2^96, so that nothing on the way leaves fp32 where the score does not: product * q_pre stays below 2^127, and what is
+        // left for q_scale is 1 to 2 there, more above (the score is then the largest of all), less below (where scores are 0).
+        const uint32_t bits = __float_as_uint(p.scale);
+        const int whole = e - kQueryBits + (int)(bits >> 23) - 127;
+        const int rest = min(max(whole - min(max(whole, -100), 96), -126), 126);      // no zero: times the -inf of a key that is not there it would be NaN
+        const float pre = __uint_as_float((uint32_t)(127 + whole - rest) << 23), post = __uint_as_float((bits & 0x7fffffu) | (uint32_t)(127 + rest) << 23);
+        q_pre.x = __shfl_sync(0xffffffffu, pre, cq * 4);
+        q_pre.y = __shfl_sync(0xffffffffu, pre, cq * 4 + 4);
+        q_scale.x = __shfl_sync(0xffffffffu, post, cq * 4);
+        q_scale.y = __shfl_sync(0xffffffffu, post, cq * 4 + 4);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
 #pragma unroll
@@ -726,9 +727,10 @@ __global__ void __launch_bounds__(ba_warps(KW) * 32, KW == kBaWide ? 1 : ba_ctas
         }
       }
     }
-    // per head cq + i: running maxima of t and of t + e_v (ELEM 1; -inf: none yet, then 0 is subtracted), the lane's sum
+    // per head cq + i: running maxima, m of the scores in units of q_scale and mw of score + e_v (not ELEM 2) in log2 units from m on (-inf:
+    // none yet, then 0 is subtracted), the lane's sum
     float2 m = {-INFINITY, -INFINITY}, mw = m, l = {};
-    float2 m_neg = {}, w_neg = {};      // what is added in the exponents
+    float2 m_neg = {}, w_neg = {};      // what is added to scores, and in the exponents of the weights
     float low = INFINITY;      // ELEM 2: the lowest product
     float oc[MO][4];
 #pragma unroll
@@ -743,8 +745,8 @@ __global__ void __launch_bounds__(ba_warps(KW) * 32, KW == kBaWide ? 1 : ba_ctas
       const uint32_t k_s = ring + get * C::stage, v_s = k_s + C::tile;
       const int key0 = (cons.tile * KW + kg) * KEYS;
       if (key0 < n) {
-        // ---- S^T = K Q^T: the lane ends with keys kg8 + 8 j of heads cq, cq + 1.  t * q_scale is the score (log2 units); the product
-        // is only formed in the fma that takes a maximum away from it, so it is not rounded at its own size
+        // ---- S^T = K Q^T: the lane ends with keys kg8 + 8 j of heads cq, cq + 1.  t * q_scale is the score (log2 units); the maximum is
+        // taken off t, and the difference multiplied, so a score is not rounded at its own size, and the largest comes out as 0 whatever its size
         uint32_t kx[MK][D / 32], ky[MK][D / 32], gx[MK], gy[MK];      // e2m1: codes and group scales of the lane's keys
         if (ELEM <= 0) {
 #pragma unroll
@@ -823,6 +825,10 @@ __global__ void __launch_bounds__(ba_warps(KW) * 32, KW == kBaWide ? 1 : ba_ctas
           }
           t[2 * mt] = add2(make_float2(sc[0][0], sc[0][1]), make_float2(sc[1][0], sc[1][1]));
           t[2 * mt + 1] = add2(make_float2(sc[0][2], sc[0][3]), make_float2(sc[1][2], sc[1][3]));
+          if (ELEM != 2) {
+            t[2 * mt] = mul2(t[2 * mt], q_pre);
+            t[2 * mt + 1] = mul2(t[2 * mt + 1], q_pre);
+          }
         }
         if (ELEM == 2) {
 #pragma unroll
@@ -857,15 +863,20 @@ __global__ void __launch_bounds__(ba_warps(KW) * 32, KW == kBaWide ? 1 : ba_ctas
           for (int j = 0; j < 2 * MK; ++j)
             if (key0 + 8 * j + kg8 >= n) t[j] = make_float2(-INFINITY, -INFINITY);
         }
-        // ---- running maxima
+        // ---- running maxima, and the exponents of the weights: t off m, and e_v more
         const float2 top = max_of(t);
-        float2 wtop = {};
-        float over = fmaxf(fmaf(top.x, q_scale.x, -m.x), fmaf(top.y, q_scale.y, -m.y));      // NaN where both are -inf: no
-        if (ELEM != 2) {
-          float2 w[2 * MK];
+        float2 x[2 * MK], w[2 * MK];
+        auto off_maximum = [&]() {
 #pragma unroll
-          for (int j = 0; j < 2 * MK; ++j) w[j] = fma2(t[j], q_scale, make_float2(ev[j], ev[j]));
-          wtop = max_of(w);
+          for (int j = 0; j < 2 * MK; ++j) {
+            x[j] = mul2(add2(t[j], m_neg), q_scale);
+            if (ELEM != 2) w[j] = add2(x[j], make_float2(ev[j], ev[j]));
+          }
+        };
+        off_maximum();
+        float over = fmaxf((top.x - m.x) * q_scale.x, (top.y - m.y) * q_scale.y);      // NaN where both are -inf: no
+        if (ELEM != 2) {
+          const float2 wtop = max_of(w);
           over = max3(over, wtop.x - mw.x, wtop.y - mw.y);
         }
         if (__any_sync(0xffffffffu, over > kLazy<ELEM>)) {
@@ -873,13 +884,21 @@ __global__ void __launch_bounds__(ba_warps(KW) * 32, KW == kBaWide ? 1 : ba_ctas
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             float &m_i = i ? m.y : m.x, &w_i = i ? mw.y : mw.x;
-            const float m_new = fmaxf(m_i, column_max(i ? top.y * q_scale.y : top.x * q_scale.x));
+            const float m_new = fmaxf(m_i, column_max(i ? top.y : top.x));
             const float sub = m_new == -INFINITY ? 0.f : m_new;
-            corr[i] = ex2(m_i - sub);
+            const float down = (m_i - sub) * (i ? q_scale.y : q_scale.x);
+            corr[i] = ex2(down);
             (i ? l.y : l.x) *= corr[i];
             m_i = m_new;
+            w_i += down;
             (i ? m_neg.y : m_neg.x) = -sub;
-            if (ELEM != 2) {
+          }
+          off_maximum();
+          if (ELEM != 2) {
+            const float2 wtop = max_of(w);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              float &w_i = i ? mw.y : mw.x;
               const float w_new = fmaxf(w_i, column_max(i ? wtop.y : wtop.x));
               const float wsub = w_new == -INFINITY ? 0.f : w_new;
               corr[i] = ex2(w_i - wsub);
@@ -899,15 +918,14 @@ __global__ void __launch_bounds__(ba_warps(KW) * 32, KW == kBaWide ? 1 : ba_ctas
         uint32_t pf[PP][2 * MK];
 #pragma unroll
         for (int j = 0; j < 2 * MK; ++j) {
-          const float2 a = fma2(t[j], q_scale, m_neg);
-          const float p0 = ex2(a.x), p1 = ex2(a.y);
+          const float p0 = ex2(x[j].x), p1 = ex2(x[j].y);
           l = add2(l, make_float2(p0, p1));
           uint32_t parts[PP];
           if (ELEM == 2) {
             split_bf16(p0, p1, parts);
           } else {
-            const float2 w = fma2(t[j], q_scale, add2(make_float2(ev[j], ev[j]), w_neg));
-            split_f16(ex2(w.x), ex2(w.y), parts);
+            const float2 u = add2(w[j], w_neg);
+            split_f16(ex2(u.x), ex2(u.y), parts);
           }
 #pragma unroll
           for (int h = 0; h < PP; ++h) pf[h][j] = transpose8(parts[h]);
@@ -1009,14 +1027,16 @@ __global__ void __launch_bounds__(ba_warps(KW) * 32, KW == kBaWide ? 1 : ba_ctas
 
     // ---- the request's share: sums over the lanes of a column, fp16 weights back to 2^(t - m)
     float f[2];
-    float ms[2] = {m.x, m.y}, ls[2] = {l.x, l.y};
+    float ms[2] = {m.x * q_scale.x, m.y * q_scale.y}, ls[2] = {l.x, l.y};
     const float mws[2] = {mw.x, mw.y};
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       ls[i] += __shfl_xor_sync(0xffffffffu, ls[i], 4);
       ls[i] += __shfl_xor_sync(0xffffffffu, ls[i], 8);
       ls[i] += __shfl_xor_sync(0xffffffffu, ls[i], 16);
-      f[i] = ELEM != 2 && mws[i] != -INFINITY ? ex2(mws[i] - ms[i] - kWeightBits) : 1.f;
+      // a largest score below fp32's range leaves no weight, one beyond it NaN
+      ls[i] = ms[i] == -INFINITY ? ls[i] * 0.f : fmaf(ms[i], 0.f, ls[i]);
+      f[i] = ELEM != 2 && mws[i] != -INFINITY ? ex2(mws[i] - kWeightBits) : 1.f;
     }
     const bool whole = WIDE || s_tile == 0 && steps == tiles_of(n, TILE);
     const long long rec_slot = s_tile == 0 ? 1 : 0;      // a range can begin and end inside a request: two records
