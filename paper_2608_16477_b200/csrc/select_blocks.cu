@@ -142,14 +142,14 @@ __global__ void __launch_bounds__(kBoundThreads) block_bounds_kernel(const __gri
   const float down = __uint_as_float((uint32_t)(127 - min(e, kMaxBound)) << 23);
   uint32_t up[2] = {}, lo[2] = {};
   if (fine) {
-    // 1.5 * 2^23 added, rounded up or down: the whole number is in the lowest byte
+    // 1.5 * 2^23 added, rounded up or down: the whole number is in the lowest byte.  (The ieee forms: the others take subnormal keys for 0.)
     constexpr float kWhole = 12582912.f;
     uint32_t u8[8], l8[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const uint32_t t = j & 1 ? top2[j / 2] & 0xffff0000u : top2[j / 2] << 16, l = j & 1 ? low2[j / 2] & 0xffff0000u : low2[j / 2] << 16;
-      u8[j] = __float_as_uint(__fmaf_ru(__uint_as_float(t), down, kWhole));
-      l8[j] = __float_as_uint(__fmaf_rd(__uint_as_float(l), down, kWhole));
+      u8[j] = __float_as_uint(__fmaf_ieee_ru(__uint_as_float(t), down, kWhole));
+      l8[j] = __float_as_uint(__fmaf_ieee_rd(__uint_as_float(l), down, kWhole));
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
