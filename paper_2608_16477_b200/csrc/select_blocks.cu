@@ -469,7 +469,7 @@ __device__ __forceinline__ void pick(const Keys &keys, int m, int want, const Id
   constexpr int W = kScoreThreads / 32;
   __shared__ uint32_t most_s[W], least_s[W];
   __shared__ int count_s[2][3][W];
-  __shared__ uint32_t sums[kOwn * W];
+  __shared__ __align__(8) uint32_t sums[kOwn * W];      // also read two at a time
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool few = m <= kOwn * kScoreThreads;
   uint32_t own[kOwn];
