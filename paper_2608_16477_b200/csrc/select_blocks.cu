@@ -597,6 +597,7 @@ __device__ __forceinline__ void pick(const Keys &keys, int m, int want, const Id
 // shared memory, and that one chooses.  One launch, and no keys in global memory (32 requests of up to 1,153 blocks, before the ring, against a kernel
 // for the scores and one for the choice: 19.9 / 29.8 us).
 constexpr int kClusterBlocks = 16384;      // 128 KB of keys and ids, and the ring
+constexpr int kSmBytes = 228 * 1024, kSelectStatic = 4608;      // shared memory of an SM; of a CTA beside that: its static arrays, and 1 KB that is reserved
 template <int D, typename T>
 __global__ void __launch_bounds__(kScoreThreads) select_cluster_kernel(const __grid_constant__ SelectParams p) {
   extern __shared__ __align__(16) unsigned char select_smem[];
@@ -672,10 +673,13 @@ int launch_select(const SelectParams &p, int device, cudaStream_t st) {
       KV_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes + kClusterBlocks * 8));
       attr_set[device] = true;
     }
-    // As many CTAs as run at once (two to an SM), of at least four warps' blocks each.  Twice as many CTAs, 16 requests of up to 512
-    // blocks 9.4 -> 11.3 us, 32 of up to 1,153 15.4 -> 19.7.
+    // As many CTAs as run at once, of at least four warps' blocks each.  Two to an SM: twice as many CTAs, 16 requests of up to 512
+    // blocks 9.4 -> 11.3 us, 32 of up to 1,153 15.4 -> 19.7.  One, where keys and ids of more than some 5,800 blocks leave no room for a second:
+    // with CTAs for two, 4 / 8 / 16 requests of 8,192 blocks 33.8 / 43.8 / 62.6 -> 43.5 / 59.1 / 79.7 us, all of 16,384 51 / 74 / 111 -> 66 / 97 /
+    // 136; ragged ones 10 % slower to 10 % faster.
+    const int per_sm = 2 * (kRingBytes + p.max_blocks * 8 + kSelectStatic) <= kSmBytes ? 2 : 1;
     int ctas = 1;
-    while (ctas < 8 && lines * ctas * 2 <= 2ll * sms && middle > ctas * 4 * kScoreBlocks) ctas *= 2;
+    while (ctas < 8 && lines * ctas * 2 <= (long long)per_sm * sms && middle > ctas * 4 * kScoreBlocks) ctas *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ctas, p.heads, p.n_req);
     cfg.blockDim = dim3(kScoreThreads);
