@@ -1312,7 +1312,8 @@ BaScratch ba_scratch(int n_req, int n_q_heads, int head_dim, int parts) {
   s.bytes = s.o + up(recs * head_dim * 4);
   return s;
 }
-// Ranges that scratch has room for: those of e2m1 pages and bf16 queries, of which there are the most.  One size for every format.
+// Ranges that the size function counts: those of e2m1 pages and bf16 queries, of which there are the most.  One size for every format; calls
+// over the others do with less where their own ranges are fewer.
 int ba_scratch_parts(int n_req, int vheads, int max_ctx, int sms) {
   return ba_plan(n_req, vheads, max_ctx, KV_ELEM_E2M1, KV_DTYPE_BF16, sms).parts;
 }
@@ -1396,7 +1397,7 @@ int ba_call(const void *q_dev, int64_t q_stride, int dtype, int n_req, int n_q_h
   const long long vheads = (long long)cache->n_kv_heads * p.passes;
   if (vheads > 65535 || n_q_heads > 65535) return KV_ERR_SHAPE;      // second dimension of the grids
   const BaPlan b = ba_plan(n_req, (int)vheads, max_ctx, cache->elem_bytes, dtype, sm_count(device));
-  const BaScratch s = ba_scratch(n_req, n_q_heads, cache->head_dim, ba_scratch_parts(n_req, (int)vheads, max_ctx, sm_count(device)));
+  const BaScratch s = ba_scratch(n_req, n_q_heads, cache->head_dim, b.parts);      // this call's own ranges: no more than the size function counts
   if (!b.whole) {
     if (scratch_dev == nullptr || ((uintptr_t)scratch_dev & 15) || scratch_bytes < s.bytes) return KV_ERR_WORKSPACE;
   }
