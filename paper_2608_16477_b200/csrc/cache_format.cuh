@@ -343,7 +343,7 @@ __device__ __forceinline__ void put_row(const Raw<T> &raw, const Pieces<D, FMT> 
       *reinterpret_cast<uint32_t *>(values) = codes[0];
       *reinterpret_cast<uint32_t *>(second) = codes[1];
       if ((sub & 1) == 0) {
-        char *groups = to.groups + at + offset * (D / 16);
+        char *groups = to.groups + at + (long long)offset * (D / 16);
         groups[0] = (char)scales[0];
         groups[apart / 16] = (char)scales[1];
       }

@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(kRowThreads) cache_read_kernel(const __grid_co
       raw[i][0] = make_uint4(a.x, a.y, b.x, b.y);
       scale[i] = *reinterpret_cast<const uint8_t *>(from.scale + at + offset);
     } else if (FMT == kE2m1) {
-      const uint8_t *g = reinterpret_cast<const uint8_t *>(from.groups + at + offset * (D / 16));
+      const uint8_t *g = reinterpret_cast<const uint8_t *>(from.groups + at + (long long)offset * (D / 16));
       raw[i][0] = make_uint4(*reinterpret_cast<const uint32_t *>(values), *reinterpret_cast<const uint32_t *>(values + APART), g[0], g[D / 32]);
       scale[i] = *reinterpret_cast<const uint8_t *>(from.scale + at + offset);
     } else {

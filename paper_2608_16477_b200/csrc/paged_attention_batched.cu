@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(ba_warps(KW) * 32, KW == kBaWide ? 1 : ba_ctas
       const int blk = __shfl_sync(0xffffffffu, inside ? blks[0] : -1, u * 16), off = __shfl_sync(0xffffffffu, offs[0], u * 16);
       if (blk >= 0) {
         const char *rec = rec0 + blk * p.cache.block_stride;
-        const char *codes = rec + off * (D / 2) + lane * 16, *extra = rec + extra0 + off * extra_step;
+        const char *codes = rec + (long long)off * (D / 2) + lane * 16, *extra = rec + extra0 + off * extra_step;
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
           const uint32_t dst = dst0 + u * C::unit + kv * C::tile;

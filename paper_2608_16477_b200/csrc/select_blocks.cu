@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kBoundThreads) block_bounds_kernel(const __gri
         raw[a].y = x.y;
       } else {
         raw[a].x = *reinterpret_cast<const uint32_t *>(from);
-        group[a] = groups[s * (D / 16)];
+        group[a] = groups[(long long)s * (D / 16)];
       }
     }
 #pragma unroll
