@@ -229,8 +229,10 @@ __device__ __forceinline__ float2 max_of(const float2 (&t)[N]) {
   return make_float2(fmaxf(max3(t[0].x, t[1].x, t[2 % N].x), t[3 % N].x), fmaxf(max3(t[0].y, t[1].y, t[2 % N].y), t[3 % N].y));
 }
 // c += A B for the parts of B.  The matrix instruction truncates as it accumulates, some 2^-24 of the accumulator each time and always
-// towards zero: over the tiles of a long context that adds up to more than fp32 results should lose (1,000 keys of 16 requests: error
-// against 64 bits 1.3e-6, of the results' norm).  So fp32 calls start from zero and add what comes out, rounded.
+// towards zero: over the tiles of a long context that adds up to more than fp32 results should lose.  So fp32 calls over bf16 and e2m1
+// pages start from zero and add what comes out, rounded (APART; of the results' norm, 1,024 keys of 128 requests 1.2e-7, 16,384 3.5e-7, which accumulated
+// inside would be 3e-5 to 5e-5).  Over e4m3 pages they accumulate inside, as bf16 calls do, whose own rounding is far larger: 1,024
+// keys of 128 requests 9e-7, 16,384 of one request 1e-7, of 16 3e-6, of 128 4e-5; apart, these calls would take 2 to 9 % longer.
 template <bool APART, bool BF16, int N, int M>
 __device__ __forceinline__ void add_product(float (&c)[4], const uint32_t (&a)[4], const uint32_t (&b)[N][M], int at) {
   float own[4] = {};

@@ -6,6 +6,12 @@ a weight by 2^-36 of the request's largest contribution (a stored value is up to
 that only where another row's is larger: twice the largest value times the largest weight).  The running maximum of the contributions may
 be replaced twice (scores within 2 T < 8, values within a binade): a factor, 2^-22 and a rounding, each time.  The result's own rounding is
 counted as what it is, half a unit in the last place of the result.
+
+Sums over long contexts, fp32 calls: a warp adds the products of 16 keys at a time, N = n / 16 additions of positive numbers or fewer, each
+rounded to nearest.  Such roundings have no sign in common, so over the results of a whole batch they add up as a random walk does: with a
+sum that grows evenly, 2^-24 sqrt(N) / 3 of its size (a uniform error of half a unit, 1 / sqrt 3; steps that grow, another 1 / sqrt 3), and
+the sums of the weights likewise.  Allowed, of the norm of the results: three times 2^-24 sqrt(N) and 2^-22 for the exponential.  Accumulated inside the matrix
+instruction, which truncates, N additions of three or two parts lose N 2^-24 / 2 and more of the sum, all in one direction: several times that.
 """
 import numpy as np
 import pytest
@@ -92,3 +98,24 @@ def test_attention_one_weight_at_a_time(kv, torch, dtype, dim, block, place, top
             assert (err <= tol).all(), (r, h, n, (err / tol).max(), share)
             lse_want = np.log(p.sum())
             assert abs(got_lse[r, h] - lse_want) <= sums + 2.0 ** -21 + 2.0 ** -22 * abs(lse_want), (r, h, got_lse[r, h], lse_want)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("elem", [0.5, 2])
+def test_sums_over_a_long_context_do_not_drift(kv, torch, elem, dim):
+    n, requests, heads, block = 16384, 128, 8, 16
+    rng = np.random.default_rng(dim)
+    cache = kv.PagedCache(_shape(heads, dim, block), n // block, elem_bytes=elem)
+    rows = [torch.from_numpy(x.astype(np.float32)).cuda() for x in (rng.uniform(-1, 1, (n, heads, dim)), rng.uniform(0.5, 3, (n, heads, dim)))]
+    slots = torch.arange(n, device="cuda")
+    kv.kv_op_cache_write(cache, 0, rows[0], rows[1], slots)
+    kv.kv_op_cache_read(cache, 0, slots, rows[0], rows[1])
+    q = torch.from_numpy(rng.uniform(-0.5, 0.5, (requests, heads, dim)).astype(np.float32)).cuda()
+    out = torch.empty_like(q)
+    table = torch.arange(n // block, dtype=torch.int32, device="cuda").expand(requests, -1).contiguous()      # one context, attended to by all
+    scratch = torch.empty(kv.kv_paged_attention_batched_scratch_bytes(requests, heads, cache, n), dtype=torch.uint8, device="cuda")
+    kv.kv_op_paged_attention_batched(q, cache, 0, table, torch.full((requests,), n, dtype=torch.int32, device="cuda"), n, out, scratch)
+    k, v, q = (x.double() for x in (*rows, q))
+    p = torch.softmax(torch.einsum("rhd,nhd->rhn", q, k) * dim ** -0.5, -1)
+    want = torch.einsum("rhn,nhd->rhd", p, v)
+    assert float((out.double() - want).norm() / want.norm()) <= 3 * 2.0 ** -24 * (n / 16) ** 0.5 + 2.0 ** -22
