@@ -199,7 +199,8 @@ int32_t kv_prefill_prefix_batched(kv_model *m, const kv_cache_desc *cache, int32
 
 /* Source-side suffix block extraction (Section 5: physical block ids from the block manager ->
  * per-layer KV tensors -> bytes).  wire[i] <- all pages of block block_ids_host[i], i in logical
- * order.  Bytes are copied verbatim.  Duplicate ids are allowed. */
+ * order.  Bytes are copied verbatim.  Duplicate ids are allowed.  A page (here and in every call that moves pages) has
+ * at most 2^31 - 2^16 bytes. */
 int32_t kv_pack_blocks(const kv_cache_desc *src, const int32_t *block_ids_host, int32_t n_blocks,
                        void *wire_dev, int64_t wire_bytes, int32_t wire_layout, void *stream);
 

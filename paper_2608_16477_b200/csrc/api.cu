@@ -287,8 +287,11 @@ DecodeWs carve_decode(const kv_model_desc &d, void *base, int max_ctx, int /*blo
 }
 
 int check_cache(const kv_cache_desc *c) { return check_cache_desc(c); }
-// pack and unpack move whole pages as bytes: every page format
-int check_cache_any(const kv_cache_desc *c) { return check_cache_desc(c, true); }
+// pack and unpack move whole pages as bytes: every page format, a page's bytes (and a piece more) counted in 32 bits
+int check_cache_any(const kv_cache_desc *c) {
+  const int rc = check_cache_desc(c, true);
+  return rc == KV_OK && make_view(c).page_bytes() > 0x7fff0000ll ? KV_ERR_SHAPE : rc;
+}
 
 int check_cache_vs_model(const kv_cache_desc *c, const kv_model_desc &d) {
   int rc = check_cache(c);
