@@ -420,8 +420,8 @@ int32_t kv_op_paged_attention_batched(const void *q_dev, int64_t q_stride, int32
  * KV head, e is the least integer with max |k| <= 127 * 2^e, at least -60; bounds_dev[block][head][0][dim] (int8, [num_blocks][n_kv_heads]
  * [2][head_dim], 16-byte aligned) is the largest key value of the dim in units of 2^e rounded up, [1] the smallest rounded down, and
  * bound_scales_dev[block][head] = e + 127.  Keys that are not finite or larger than 127 * 2^60 make codes of 0 and the scale byte 255:
- * such a block is always chosen.  A block outside the pool, or a count below 1, is left out: nothing is written.  The listed blocks are
- * distinct; what the bounds of a block hold that is listed twice with different counts is undefined (other blocks' are not affected). */
+ * such a block is always chosen.  A block outside the pool, or a count below 1, is left out: nothing is written.  Blocks of at most 2^30
+ * slots.  The listed blocks are distinct; what the bounds of a block hold that is listed twice with different counts is undefined (other blocks' are not affected). */
 int32_t kv_op_block_bounds(const kv_cache_desc *cache, int32_t layer, const int32_t *blocks_dev, const int32_t *counts_dev, int32_t n,
                            int8_t *bounds_dev, uint8_t *bound_scales_dev, void *stream);
 

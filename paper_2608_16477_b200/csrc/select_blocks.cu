@@ -729,6 +729,7 @@ int32_t kv_op_block_bounds(const kv_cache_desc *cache, int32_t layer, const int3
   if (rc != KV_OK) return rc;
   if (cache->head_dim != 64 && cache->head_dim != 128) return KV_ERR_SHAPE;
   if (layer < 0 || layer >= cache->n_layers) return KV_ERR_SHAPE;
+  if (cache->block_size > 1 << 30) return KV_ERR_SHAPE;      // keys are counted in 32 bits, those of a load ahead
   if (n == 0) return KV_OK;
   if (blocks_dev == nullptr || counts_dev == nullptr || bounds_dev == nullptr || bound_scales_dev == nullptr) return KV_ERR_ARG;
   if (((uintptr_t)blocks_dev & 3) || ((uintptr_t)counts_dev & 3) || ((uintptr_t)bounds_dev & 15)) return KV_ERR_ARG;

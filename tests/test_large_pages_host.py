@@ -1,7 +1,6 @@
 """Pages and blocks larger than the kernels count are refused, without a GPU (fake addresses are never dereferenced)."""
 import ctypes as C
 
-import numpy as np
 import pytest
 
 from oracle import kv_oracle as O
@@ -27,3 +26,13 @@ def test_pages_of_two_gigabytes_are_not_moved(kv, no_gpu, elem):
     fits = 0x7fff0000 // row // 16 * 16
     assert calls(fits) == {CLOSED}
     assert calls(fits + 16) == calls((1 << 31) // row + 16) == calls((1 << 32) // row // 16 * 16 + 16) == {O.ERR_SHAPE}
+
+
+@pytest.mark.parametrize("elem", [E2M1, 1, 2])
+def test_bounds_count_keys_in_32_bits(kv, no_gpu, elem):
+    lib = kv.load()
+
+    def call(block_size):
+        return lib.kv_op_block_bounds(C.byref(_desc(elem, block_size=block_size, n_kv_heads=1)), 0, _at(1), _at(2), 3, _at(3), _at(4), 0)
+    assert call(1 << 30) == CLOSED
+    assert call((1 << 30) + 1) == call((1 << 31) - 16) == call((1 << 31) - 1) == O.ERR_SHAPE
