@@ -15,8 +15,9 @@
 // 82 / 75 % of a copy's rate with the launch in it); bf16 to bf16 pages and back, 134 MB, 24.3 / 26.6 and 23.0 / 24.9 us (5.5 and 5.8
 // TB/s), fp32, 201 MB, 33.9 / 36.1 and 38.3 / 40.7 us.  64 tokens 1.9 to 2.5 us.  A piece of 8 to a lane and index arithmetic for
 // every row: 161 instructions a warp and row, 27 us.
-// e2m1 pages (16,384 tokens of 8 heads of 128; floor): from bf16 20.3 us (13.1), into bf16 19.0 (13.1), from fp32 37 (23.4; 49 with
-// three comparisons for every value): bound by the instructions of the conversion.
+// e2m1 pages (16,384 tokens of 8 heads of 128; floor): from bf16 20.4 us (13.1), into bf16 19.2 (13.1), from fp32 37.1 (23.4; 49 with
+// three comparisons for every value), into fp32 39.0 (23.4).  Writing from bf16 and reading into bf16 are busy with conversions (issue slots 68 and 75 %,
+// ALU pipe 62 and 58 %); fp32 rows wait for their loads (issue slots 53 %), or for the path to memory (30 %).
 #include "cache_format.cuh"
 
 namespace kvr {

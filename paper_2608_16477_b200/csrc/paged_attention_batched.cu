@@ -43,12 +43,12 @@
 // e2m1 pages: the same, and the scale of 16 dims is multiplied into the fp16 fragment (code times e4m3 number: six bits, exact).  The
 // codes of two keys of V are paired as nibbles, before they are converted, so the fragments of V^T need no exchange after it.  In pages of a
 // multiple of 16 slots a unit of 16 keys (codes, scales, scale bytes: three pieces of the record) is copied as it is, 1,168 bytes of K or V for
-// 128 dims; in other pages row by row.  What bounds it is no longer HBM but instructions: 370 a warp for 16 keys and 8 heads, half of them
-// conversions, scales and products, at 61 % of the issue slots (ALU pipe 51 %, tensor 21 %).  So bf16 calls have twelve warps an
+// 128 dims; in other pages row by row.  What bounds it is no longer HBM but instructions: 397 a warp for 16 keys and 8 heads, half of them
+// conversions, scales and products, at 59 % of the issue slots (ALU pipe 46 %, tensor 29 %).  So bf16 calls have twelve warps an
 // SM.  32 requests of up to 18,433 tokens (290 MB) 83 us in a graph, 87 call after call: 3.5 TB/s, against 91 us for the 512 MB of e4m3
 // pages; the copies alone take 50.  (Weights of one fp16 part, 2^-11, would take 76 us, but last bits of bf16 results then move: 4e-4 of
-// their norm off what fp32 weights give, against 5e-5.)  fp32 calls (two parts each, eight warps an SM) 106 us; a third CTA for them spills and is as
-// often slower as faster (two / three: 128 requests of up to 577 tokens 27.0 / 25.9, one of 18,433 16.9 / 20.8).
+// their norm off what fp32 weights give, against 5e-5.)  fp32 calls (two parts each, eight warps an SM) 102 us; a third CTA for them spills and is as
+// often slower as faster (two / three: 128 requests of up to 577 tokens 28.8 / 28.2, 64 of 1,024 39.2 / 43.0).
 #include "cache_format.cuh"
 
 namespace kvr {
@@ -1241,14 +1241,14 @@ constexpr int kBaNeverSplit = 384;   // the least that this can be
 constexpr int kBaWholeWarp = 512;    // with a warp per KV head
 // Where every (request, head) has an SM to itself, its CTA has eight warps: contexts last longer whole.  Measured, split / four warps /
 // eight, 32 query and 8 KV heads of 128, bf16 queries over bf16 pages, fp32 over bf16, bf16 over e4m3, bf16 over e2m1: one request of 384 tokens
-// 7.2 / 8.1 / 7.4, 7.9 / 9.9 / 8.3, 7.5 / 7.7 / 6.7, 8.0 / 7.3 / 7.1 us; of 512 7.2 / 9.2 / 8.1, 7.7 / 11.7 / 9.5, 7.8 / 8.5 / 7.2, 8.2 / 8.5 /
-// 7.6; four of 512 9.3 / 9.2 / 8.2, 10.0 / 11.8 / 9.6, 8.3 / 8.5 / 7.3, 8.8 / 8.7 / 7.6, ragged of up to 768 8.0 / 11.5 / 9.6, 8.7 / 15.0 / 11.4,
-// 8.1 / 10.2 / 8.6, 8.8 / 10.2 / 9.1; eight of 1,024 12.6 / 14.2 / 11.4, 14.1 / 18.7 / 13.9, 11.5 / 12.6 / 10.2, 13.0 / 12.8 / 10.9; 16 ragged of up to
-// 1,024 12.3 / 14.0 / 11.3, 13.9 / 18.7 / 13.9, 12.3 / 12.2 / 9.7, 12.8 / 12.1 / 10.5, of up to 1,536 13.7 / 18.9 / 14.5, 15.4 / 25.4 / 18.0, 12.8 /
-// 16.2 / 12.6, 13.1 / 16.1 / 13.6.  Up to 128 tokens four warps are as good (eight of 128 over e4m3 pages, fp32, 5.1 / 5.7).
+// 7.2 / 8.1 / 7.4, 7.9 / 9.9 / 8.3, 7.5 / 7.7 / 6.7, 7.6 / 7.3 / 6.9 us; of 512 7.2 / 9.2 / 8.1, 7.7 / 11.7 / 9.5, 7.8 / 8.5 / 7.2, 8.2 / 8.5 /
+// 7.6; four of 512 9.3 / 9.2 / 8.2, 10.0 / 11.8 / 9.6, 8.3 / 8.5 / 7.3, 8.9 / 8.7 / 7.7, ragged of up to 768 8.0 / 11.5 / 9.6, 8.7 / 15.0 / 11.4,
+// 8.1 / 10.2 / 8.6, 8.7 / 10.6 / 9.2; eight of 1,024 12.6 / 14.2 / 11.4, 14.1 / 18.7 / 13.9, 11.5 / 12.6 / 10.2, 13.3 / 13.2 / 11.0; 16 ragged of up to
+// 1,024 12.3 / 14.0 / 11.3, 13.9 / 18.7 / 13.9, 12.3 / 12.2 / 9.7, 13.5 / 13.1 / 11.1, of up to 1,536 13.7 / 18.9 / 14.5, 15.4 / 25.4 / 18.0, 12.8 /
+// 16.2 / 12.6, 15.2 / 17.2 / 14.0.  Up to 128 tokens four warps are as good (eight of 128 over e4m3 pages, fp32, 5.1 / 5.7).
 constexpr int kBaWideCtx = 128;
 // Beyond that, e2m1 pages: a CTA works longer on a context of the same bytes, and there is as much to gain from the heads that run beside it.
-// Split / whole, 32 requests over 8 heads, all of 1,024, 21.5 / 16.7 us; fp32 queries, 64 over 8 heads of 1,024 29.1 / 31.8.  (Six warps to
+// Split / whole, 32 requests over 8 heads, all of 1,024, 22.6 / 18.4 us; fp32 queries, 64 over 8 heads of 1,024 29.1 / 31.8.  (Six warps to
 // a CTA for up to two heads an SM: 3 to 7 % faster from 768 tokens on, 5 % slower at 256.)
 int ba_whole_ctx(int n_req, long long heads, int kw, int elem_bytes, int slots, int sms) {
   if (kw == 1) return kBaWholeWarp;
@@ -1289,8 +1289,8 @@ BaPlan ba_plan(int n_req, int vheads, int max_ctx, int elem_bytes, int dtype, in
   b.whole = max_ctx <= ba_whole_ctx(n_req, heads, b.kw, elem_bytes, ctas * sms, sms);
   b.wide = b.whole && b.kw == kBaWarps && heads <= sms && max_ctx > kBaWideCtx;
   // As many ranges as CTAs run at once.  Three to an SM leave a head of few requests more records than the joining kernel's four warps have in flight
-  // (e2m1 pages, bf16 queries, 8 heads, three / two: one request of 18,433 tokens 17.4 / 14.1 us, of 60,000 30.6 / 27.8; four of 9,000
-  // ragged 14.7 / 14.1, all alike 21.0 / 19.3; eight of 6,000 16.9 / 17.7 and 23.3 / 24.8).
+  // (e2m1 pages, bf16 queries, 8 heads, three / two: one request of 18,433 tokens 17.7 / 14.1 us, of 60,000 31.8 / 29.2; four of 9,000
+  // ragged 15.9 / 15.7, all alike 23.4 / 21.4; eight of 6,000 17.5 / 18.2 and 26.1 / 27.9).
   const int at_once = (heads < 64 && ctas > 2 ? 2 : ctas) * sms;
   // no more parts than 16-key tiles (the shortest there are) could give work to
   const long long tiles = (long long)n_req * ((max_ctx + b.kw * 16 - 1) / (b.kw * 16) + 1);

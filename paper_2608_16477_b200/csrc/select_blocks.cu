@@ -9,8 +9,8 @@
 // number (at most 256 * 127 * 32767 < 2^31) times a power of two: it does not depend on the order of any sum, so neither does the
 // choice, and equal scores go to the lowest block.
 //
-// Measured in a graph, 8 KV heads of 128 (floor: the bytes at a copy's rate).  Bounds of 4,096 blocks of 16: bf16 pages 24 us (21.7), e4m3
-// 25.8, e2m1 27; of 64 blocks 2.7.  Selection, 64 query heads: one request of 1,153 blocks 7.7 us (0.4), 16 of up to 512 9.4 (1.4), 32
+// Measured in a graph, 8 KV heads of 128 (floor: the bytes at a copy's rate).  Bounds of 4,096 blocks of 16: bf16 pages 25 us (21.7), e4m3
+// 26.1 (11.6), e2m1 27.2 (7.1: issue slots 78 %, ALU pipe 71 %); of 64 blocks 2.7.  Selection, 64 query heads: one request of 1,153 blocks 7.8 us (0.4), 16 of up to 512 9.5 (1.4), 32
 // of up to 1,153 15.4 (4.8), of which finding the score of the last rank and writing the list take 3 us.
 #include <cooperative_groups.h>
 
