@@ -24,6 +24,7 @@ def torch():
 def test_rows_at_the_end_of_a_huge_page(kv, torch):
     """Scales of 16 dims lie 8 bytes a slot apart: from slot 2^28 on their places pass 31 bits."""
     block, d = (1 << 28) + 64, 128
+    torch.cuda.empty_cache()
     if torch.cuda.mem_get_info()[0] < 50 << 30:
         pytest.skip("memory for one page of K and one of V")
     cache = kv.PagedCache(_shape(1, d, block), 1, elem_bytes=0.5)
@@ -52,6 +53,7 @@ def test_attention_at_the_end_of_a_huge_page(kv, torch, dtype):
     is that of all others together; the bound is that of the batched attention's tests, with the sums of equal weights counted exactly."""
     n, d, group = (1 << 25) + 100, 128, 4
     block = n + 12
+    torch.cuda.empty_cache()
     if torch.cuda.mem_get_info()[0] < 8 << 30:
         pytest.skip("memory for one page of K and one of V")
     cache = kv.PagedCache(_shape(1, d, block), 1, elem_bytes=0.5, fill=0)
