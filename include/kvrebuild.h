@@ -393,8 +393,9 @@ int32_t kv_op_cache_append(const kv_rope *rope, const kv_cache_desc *cache, int3
  * A block id outside the pool inside a context is not followed: that request's out and lse are NaN.  Infinities and NaN turn
  * into NaN what they enter, and nothing else: in a query, its head's out and lse; in a cached key inside a context, the out and
  * lse of that request's heads that read its KV head; in a cached value, its dim (e2m1: the 16 dims of its scale) of those outs.
- * What lies behind a context enters no result.  Where finite numbers leave fp32: a score below its range weighs nothing, a score or a weighted sum of
- * values beyond it gives NaN, and a context whose scores are all below it gives NaN in out and lse.
+ * What lies behind a context enters no result.  Where finite numbers leave fp32: a score below its range weighs nothing, a score or
+ * a weighted sum of values beyond it gives NaN, and a context whose scores are all below it gives NaN in out and lse.  (A score counts
+ * times log2(e) here; over bf16 pages q . k as well, ahead of softmax_scale.)
  * Sums, softmax and accumulators are fp32.  The operands of the matrix instructions are sums of 16-bit parts: in fp32 calls queries
  * and weights to 2^-24 over bf16 pages and to 2^-22 over e4m3 and e2m1 pages; in bf16 calls queries as they are, weights to 2^-16 over
  * bf16 and 2^-22 over e4m3 and e2m1 pages, lse from the whole weights in each.  Over e4m3 and e2m1 pages nothing is finer than
